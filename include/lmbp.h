@@ -16,6 +16,9 @@
  *   msrms_linear_act_fwd           MS-RMSNorm, the merged linear layer and ReGELU2 /
  *                                  ReSiLU2 forward, fused (the norm in the GEMM)
  *   msrms_linear_swiglu_fwd        MS-RMSNorm and the LLaMA MLP's input side, fused
+ *   q8_rows / q8_values            rows in 8 bits with one scale each, and back
+ *   msrms_q8_fwd / msrms_q8_bwd    MS-RMSNorm with the residual's addition, output in 8 bits
+ *   linear_q8_fwd / linear_q8_bwd  a frozen linear layer of 8-bit rows and 8-bit weights
  *
  * Conventions shared by every call
  * --------------------------------
@@ -290,6 +293,79 @@ lmbp_status linear_act_bwd(lmbp_act act, lmbp_dtype dt, int64_t m, int64_t n, in
                            const void *dy, const uint32_t *codes, const void *x, void *dz,
                            void *dw, void *db, void *workspace, int64_t workspace_bytes,
                            void *stream);
+
+/* ------------------------------------------------------------------------
+ * Rows in 8 bits, one fp32 scale per row. Of a row t:
+ *
+ *   a = max(max |t|, 2^-100),  scale = a / 127,  q = t r rounded half to even
+ *
+ * with r = 127 / a rounded to fp32 and the product t r not rounded before q. The row stands
+ * for q scale; q lies in -127 .. 127. A row that holds an infinity or a NaN gets scale NaN
+ * and q = 0, so that what is formed from it is NaN.
+ *
+ *   q8_rows   : x [rows x cols] of dtype -> q [rows x cols], scale [rows].
+ *   q8_values : v = q scale, one rounding to dtype. Any q (also -128) and scale.
+ * Nothing overlaps. scale: 4-byte aligned.
+ * ------------------------------------------------------------------------ */
+lmbp_status q8_rows(lmbp_dtype dt, int64_t rows, int64_t cols, const void *x, int8_t *q,
+                    float *scale, void *stream);
+lmbp_status q8_values(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t *q,
+                      const float *scale, void *v, void *stream);
+
+/* ------------------------------------------------------------------------
+ * MS-RMSNorm (Appendix G Alg. 3) with the residual's addition in front and its output in 8
+ * bits: the tensor that the norm and the next (merged) linear layer both keep takes one
+ * byte per element. Per row:
+ *
+ * Forward:  s = x + res, rounded to dtype (s = x without res),
+ *           rstd = 1 / sqrt(p^-1 |s|^2 + eps),  z = s rstd  as q scale:
+ *           q the 8-bit row of s (as q8_rows), scale = a rstd / 127.
+ * Backward: with z = q scale,  dx = rstd (dz - z mean(z dz)) + ds.
+ *           dx is the gradient of x and of res alike; ds is the gradient that reaches s
+ *           past the norm.
+ *
+ *   x, res, s : rows x cols of dtype. res and s both NULL or both given; s == x and
+ *               s == res are allowed, x == res too.
+ *   q         : rows x cols; scale, rstd: rows fp32 values.
+ *   eps       : finite, > 0.
+ *   dz, ds, dx: rows x cols of dtype; ds NULL for none. dx == dz and dx == ds are allowed.
+ * No other overlap. The rounding to 8 bits is passed over by the backward, which is the
+ * gradient of the norm at the z that was kept.
+ * ------------------------------------------------------------------------ */
+lmbp_status msrms_q8_fwd(lmbp_dtype dt, int64_t rows, int64_t cols, float eps, const void *x,
+                         const void *res, void *s, int8_t *q, float *scale, float *rstd,
+                         void *stream);
+lmbp_status msrms_q8_bwd(lmbp_dtype dt, int64_t rows, int64_t cols, const void *dz,
+                         const int8_t *q, const float *scale, const float *rstd, const void *ds,
+                         void *dx, void *stream);
+
+/* ------------------------------------------------------------------------
+ * A linear layer whose frozen weight is kept in 8 bits, one scale per output channel (as
+ * q8_rows gives for w [n x k]), on rows in 8 bits:
+ *
+ *   y  = (sum_k q[m, k] w[n, k]) (scale[m] w_scale[n]) + bias[n]
+ *   dx = (sum_n p[m, n] w[n, k]) p_scale[m],   p, p_scale the 8-bit rows of dy w_scale
+ *
+ * The sums are exact (whole numbers in 32 bits), everything behind them is fp32 with one
+ * rounding to dtype.
+ *
+ *   dt     : type of y, bias, dy, dx.
+ *   m,n,k  : any sizes >= 0 below 2^31; the length of the sums (k forward, n backward) at
+ *            most 131071. k = 0 gives y = bias (0 without), n = 0 gives dx = 0.
+ *   q [m x k], w [n x k]: any values; scale [m], w_scale [n]; bias [n] or NULL; y, dy [m x n];
+ *            dx [m x k].
+ *   workspace : lmbp_linear_q8_bwd_bytes(m, n, k) bytes, 16-byte aligned. Its contents do
+ *            not matter before or after.
+ * q and w with k a multiple of 16 on 16-byte aligned pointers take the fast path, anything
+ * else a slower one with the same results. No output overlaps another buffer.
+ * ------------------------------------------------------------------------ */
+lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t *q,
+                          const float *scale, const int8_t *w, const float *w_scale,
+                          const void *bias, void *y, void *stream);
+size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k);
+lmbp_status linear_q8_bwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const void *dy,
+                          const int8_t *w, const float *w_scale, void *dx, void *workspace,
+                          int64_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
  * Test utilities (host only, no launch): the kernel form that a size takes on the calling

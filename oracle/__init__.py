@@ -21,6 +21,8 @@ What it computes, each function citing the passage it follows:
   ReGELU2 / ReSiLU2 (the fused forward of the MLP's first projection), and the gated
   form (two projections feeding ReSiLU2 inside SwiGLU); both also with MS-RMSNorm in
   front (the norm's output feeding the merged layer, Sec. 5.2 eq. norm_linear).
+* ``q8``: rows in 8 bits, MS-RMSNorm with the residual's addition and its output in 8 bits,
+  and linear layers of 8-bit rows and weights, forward and input gradient.
 * ``dtypes``: decoding of fp32 / bf16 storage to fp64 and correct round-to-nearest-even
   encoding of fp64 results back to storage.
 
@@ -41,6 +43,7 @@ from .norms import msln_fwd, msln_bwd, msrms_fwd, msrms_bwd
 from . import variants
 from .linear import (linear, linear_act_fwd, linear_swiglu_fwd, msrms_linear_act_fwd,
                      msrms_linear_swiglu_fwd)
+from . import q8
 
 __all__ = [
     "decode", "encode", "round_to_dtype", "DTYPES",
@@ -51,4 +54,5 @@ __all__ = [
     "reswiglu2_fwd", "reswiglu2_bwd",
     "msln_fwd", "msln_bwd", "msrms_fwd", "msrms_bwd", "variants",
     "linear", "linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd", "msrms_linear_swiglu_fwd",
+    "q8",
 ]

@@ -7,7 +7,9 @@ pass (Sec. 4.2); ReSiLU2 also comes fused with the SwiGLU product of the LLaMA
 MLP, and both come fused into the epilogue of the preceding linear layer's matrix
 product (bf16 MFMA). MS-LN / MS-RMSNorm, with the affine merged into the next
 linear layer, save only their output and one fp32 statistic per row (Sec. 5.2);
-MS-RMSNorm also comes fused into that linear layer's matrix product.
+MS-RMSNorm also comes fused into that linear layer's matrix product, and with its output
+in 8 bits (the residual's addition in front), which linear layers of frozen 8-bit weights
+take as it is.
 
 The kernels live in liblmbp.so (C ABI in include/lmbp.h); ``binding`` marshals
 torch tensors into it. The library is loaded on first use.
@@ -21,6 +23,8 @@ from .binding import (  # noqa: F401
     lib,
     linear_act_bwd,
     linear_act_fwd,
+    linear_q8_bwd,
+    linear_q8_fwd,
     linear_swiglu_fwd,
     linear_weight_grad,
     msln_bwd,
@@ -29,6 +33,10 @@ from .binding import (  # noqa: F401
     msrms_fwd,
     msrms_linear_act_fwd,
     msrms_linear_swiglu_fwd,
+    msrms_q8_bwd,
+    msrms_q8_fwd,
+    q8_rows,
+    q8_values,
     regelu2_bwd,
     regelu2_fwd,
     resilu2_bwd,

@@ -33,6 +33,7 @@ NORM_OPS = ("msln_fwd", "msln_bwd", "msrms_fwd", "msrms_bwd")
 GLU_OPS = ("reswiglu2_fwd", "reswiglu2_bwd")
 STEP_OPS = ("stepact_fwd", "stepact_bwd")
 LINEAR_OPS = ("linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd", "msrms_linear_swiglu_fwd")
+Q8_OPS = ("q8_rows", "q8_values", "msrms_q8_fwd", "msrms_q8_bwd", "linear_q8_fwd", "linear_q8_bwd")
 ACT_GELU, ACT_SILU = 0, 1
 
 
@@ -108,6 +109,15 @@ def lib():
     L.linear_weight_grad.restype = i32
     L.linear_act_bwd.argtypes = [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     L.linear_act_bwd.restype = i32
+    L.q8_rows.argtypes = L.q8_values.argtypes = [i32, i64, i64, vp, vp, vp, vp]
+    L.msrms_q8_fwd.argtypes = [i32, i64, i64, f32, vp, vp, vp, vp, vp, vp, vp]
+    L.msrms_q8_bwd.argtypes = [i32, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.linear_q8_fwd.argtypes = [i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.lmbp_linear_q8_bwd_bytes.argtypes = [i64, i64, i64]
+    L.lmbp_linear_q8_bwd_bytes.restype = ctypes.c_size_t
+    L.linear_q8_bwd.argtypes = [i32, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp]
+    for name in Q8_OPS:
+        getattr(L, name).restype = i32
     L.lmbp_copy.argtypes = [vp, vp, i64, vp]
     L.lmbp_copy.restype = i32
     _bind_fast(L)
@@ -719,3 +729,144 @@ def msrms_linear_swiglu_fwd(x, w_gate, w_up, eps, h=None, s=None, u=None, codes=
             BF16, m, n, k, float(eps), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(h), _ptr(s), _ptr(u),
             _ptr(codes), _ptr(g) if g is not None else None, _ptr(z), _ptr(rstd), _stream(x, stream)))
     return (h, s, u, codes, z, rstd, g) if g is not None else (h, s, u, codes, z, rstd)
+
+
+def _q8_rows_cols(t):
+    if t.dim() == 0:
+        raise ValueError("rows in 8 bits need at least one dimension")
+    return math.prod(t.shape[:-1]), t.shape[-1]   # rows of no columns are the library's to refuse
+
+
+def _q8_in(q, ref, what, shape=None):
+    """An int8 tensor on the same device as ``ref`` (of the given shape)."""
+    _on(q, ref, what)
+    if q.dtype != torch.int8 or (shape is not None and q.shape != shape):
+        raise ValueError(f"{what} must be an int8 tensor" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    return q
+
+
+def _per_row(t, ref, count, what):
+    _on(t, ref, what)
+    if t.dtype != torch.float32 or t.numel() != count:
+        raise ValueError(f"{what} must be a float32 tensor of {count} elements")
+    return t
+
+
+def _opt(t):
+    return _ptr(t) if t is not None else None
+
+
+def q8_rows(x, stream=None):
+    """Rows (the last dimension) in 8 bits: returns (q, scale), q int8 of x's shape and one
+    fp32 scale per row; x is q * scale up to half a scale. Also for a weight [n, k]: one
+    scale per output channel."""
+    _dev(x, "x")
+    dt = _dtype_code(x)
+    rows, cols = _q8_rows_cols(x)
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    with _device_of(x):   # launches go to the tensors' GPU
+        _check("q8_rows", lib().q8_rows(dt, rows, cols, _ptr(x), _ptr(q), _ptr(scale), _stream(x, stream)))
+    return q, scale
+
+
+def q8_values(q, scale, dtype=torch.bfloat16, stream=None):
+    """The values that rows in 8 bits stand for: q * scale in ``dtype``."""
+    _q8_in(q, q, "q")
+    rows, cols = _q8_rows_cols(q)
+    _per_row(scale, q, rows, "scale")
+    v = torch.empty(q.shape, dtype=dtype, device=q.device)
+    with _device_of(q):   # launches go to the tensors' GPU
+        _check("q8_values", lib().q8_values(_dtype_code(v), rows, cols, _ptr(q), _ptr(scale), _ptr(v),
+                                            _stream(q, stream)))
+    return v
+
+
+def msrms_q8_fwd(x, eps, res=None, s=None, stream=None):
+    """MS-RMSNorm over the last dimension with its output in 8 bits: returns (q, scale, rstd),
+    z = q * scale. With a residual, of s = x + res (rounded to x's type): returns (q, scale,
+    rstd, s); s may be given, x and res themselves included (the sum in place)."""
+    _dev(x, "x")
+    dt = _dtype_code(x)
+    rows, cols = _q8_rows_cols(x)
+    if res is not None:
+        if _same(res, x, "res").shape != x.shape:
+            raise ValueError("res must have the shape of x")
+        s = _like(x, s, "s")
+    elif s is not None:
+        raise ValueError("s is the sum of x and res: it needs res")
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    with _device_of(x):   # launches go to the tensors' GPU
+        _check("msrms_q8_fwd", lib().msrms_q8_fwd(dt, rows, cols, float(eps), _ptr(x), _opt(res), _opt(s), _ptr(q),
+                                                  _ptr(scale), _ptr(rstd), _stream(x, stream)))
+    return (q, scale, rstd) if res is None else (q, scale, rstd, s)
+
+
+def msrms_q8_bwd(dz, q, scale, rstd, ds=None, dx=None, stream=None):
+    """MS-RMSNorm backward from the output kept in 8 bits: dx = rstd (dz - z mean(z dz)) + ds,
+    z = q * scale. dx is the gradient of x and of the residual alike; ds (None: none) the
+    gradient that reaches their sum past the norm. dx may be dz or ds."""
+    _dev(dz, "dz")
+    dt = _dtype_code(dz)
+    rows, cols = _q8_rows_cols(dz)
+    _q8_in(q, dz, "q", dz.shape)
+    _per_row(scale, dz, rows, "scale")
+    _per_row(rstd, dz, rows, "rstd")
+    if ds is not None and _same(ds, dz, "ds").shape != dz.shape:
+        raise ValueError("ds must have the shape of dz")
+    dx = _like(dz, dx, "dx")
+    with _device_of(dz):   # launches go to the tensors' GPU
+        _check("msrms_q8_bwd", lib().msrms_q8_bwd(dt, rows, cols, _ptr(dz), _ptr(q), _ptr(scale), _ptr(rstd), _opt(ds),
+                                                  _ptr(dx), _stream(dz, stream)))
+    return dx
+
+
+def _q8_weight(w, w_scale, ref):
+    _q8_in(w, ref, "w")
+    if w.dim() != 2:
+        raise ValueError("w must be [n, k]")
+    _per_row(w_scale, ref, w.shape[0], "w_scale")
+    return w.shape
+
+
+def linear_q8_fwd(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=None):
+    """Linear layer of 8-bit rows q [..., k] (one scale per row) and an 8-bit weight w [n, k]
+    (one scale per output channel): y = (q w^T) scale w_scale + bias in ``dtype``, the sums
+    exact. bias [n] of that dtype or None."""
+    _q8_in(q, q, "q")
+    n, k = _q8_weight(w, w_scale, q)
+    if q.dim() == 0 or q.shape[-1] != k:
+        raise ValueError("q must be [..., k] and w [n, k]")
+    m = math.prod(q.shape[:-1])
+    _per_row(scale, q, m, "scale")
+    if bias is not None:
+        _on(bias, q, "bias")
+        if bias.dtype != dtype or bias.numel() != n:
+            raise ValueError(f"bias must be a {dtype} tensor of n elements")
+    y = torch.empty((*q.shape[:-1], n), dtype=dtype, device=q.device)
+    with _device_of(q):   # launches go to the tensors' GPU
+        _check("linear_q8_fwd", lib().linear_q8_fwd(_dtype_code(y), m, n, k, _ptr(q), _ptr(scale), _ptr(w), _ptr(w_scale),
+                                                    _opt(bias), _ptr(y), _stream(q, stream)))
+    return y
+
+
+def linear_q8_bwd(dy, w, w_scale, stream=None):
+    """Input gradient of linear_q8_fwd: dx = (dy w_scale) w, the rows of dy w_scale [..., n]
+    brought to 8 bits first (one scale per row), dx [..., k] of dy's type."""
+    _dev(dy, "dy")
+    dt = _dtype_code(dy)
+    n, k = _q8_weight(w, w_scale, dy)
+    if dy.dim() == 0 or dy.shape[-1] != n:
+        raise ValueError("dy must be [..., n] and w [n, k]")
+    m = math.prod(dy.shape[:-1])
+    L = lib()
+    with _device_of(dy):   # launches go to the tensors' GPU
+        nbytes = L.lmbp_linear_q8_bwd_bytes(m, n, k)
+        handle = _stream(dy, stream)
+        work = _workspace(nbytes, dy, stream)
+        dx = torch.empty((*dy.shape[:-1], k), dtype=dy.dtype, device=dy.device)
+        _check("linear_q8_bwd", L.linear_q8_bwd(dt, m, n, k, _ptr(dy), _ptr(w), _ptr(w_scale), _ptr(dx), _ptr(work),
+                                                nbytes, handle))
+    return dx

@@ -433,6 +433,128 @@ lmbp_status msrms_linear_swiglu_fwd_impl(lmbp_dtype dt, int64_t m, int64_t n, in
                                                   rstd, static_cast<hipStream_t>(stream)));
 }
 
+// A matrix of rows x cols elements of the storage type (or bytes), its sizes already checked.
+bool bad_matrix(int64_t rows, int64_t cols) {
+  return rows < 0 || cols < 0 || (rows > 0 && cols > 0 && uint64_t(rows) > (uint64_t(1) << 60) / uint64_t(cols));
+}
+
+lmbp_status q8_rows_impl(lmbp_dtype dt, int64_t rows, int64_t cols, const void* x, int8_t* q, float* scale,
+                         void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  if (bad_matrix(rows, cols)) return LMBP_EINVAL;
+  if (rows == 0) return LMBP_OK;
+  if (cols == 0 || !x || !q || !scale) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt);
+  if (!aligned(x, eb) || !aligned(scale, 4)) return LMBP_EINVAL;
+  const uint64_t count = uint64_t(rows) * uint64_t(cols);
+  const Span sx = span(x, count * eb), sq = span(q, count), ss = span(scale, uint64_t(rows) * 4);
+  if (overlaps(sx, sq) || overlaps(sx, ss) || overlaps(sq, ss)) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_q8_rows(dt == LMBP_BF16, rows, cols, cols, x, nullptr, q, scale,
+                                       static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status q8_values_impl(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t* q, const float* scale, void* v,
+                           void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  if (bad_matrix(rows, cols)) return LMBP_EINVAL;
+  if (rows == 0) return LMBP_OK;
+  if (cols == 0 || !q || !scale || !v) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt);
+  if (!aligned(v, eb) || !aligned(scale, 4)) return LMBP_EINVAL;
+  const uint64_t count = uint64_t(rows) * uint64_t(cols);
+  const Span sv = span(v, count * eb);
+  if (overlaps(sv, span(q, count)) || overlaps(sv, span(scale, uint64_t(rows) * 4))) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_q8_values(dt == LMBP_BF16, rows, cols, q, scale, v, static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status msrms_q8_fwd_impl(lmbp_dtype dt, int64_t rows, int64_t cols, float eps, const void* x, const void* res,
+                              void* s, int8_t* q, float* scale, float* rstd, void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  if (bad_matrix(rows, cols)) return LMBP_EINVAL;
+  if (rows == 0) return LMBP_OK;
+  if (cols == 0) return LMBP_EINVAL;
+  if (!(std::isfinite(eps) && eps > 0.0f)) return LMBP_EINVAL;
+  if (!x || !q || !scale || !rstd || (res == nullptr) != (s == nullptr)) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt);
+  if (!aligned(x, eb) || (res && (!aligned(res, eb) || !aligned(s, eb))) || !aligned(scale, 4) || !aligned(rstd, 4))
+    return LMBP_EINVAL;
+  const uint64_t count = uint64_t(rows) * uint64_t(cols);
+  const Span sx = span(x, count * eb), sr = span(res, res ? count * eb : 0), ss = span(s, s ? count * eb : 0);
+  const Span outs[3] = {span(q, count), span(scale, uint64_t(rows) * 4), span(rstd, uint64_t(rows) * 4)};
+  if (bad_pair(ss, sx, true) || bad_pair(ss, sr, true)) return LMBP_EOVERLAP;
+  for (int i = 0; i < 3; ++i) {
+    if (overlaps(outs[i], sx) || overlaps(outs[i], sr) || overlaps(outs[i], ss)) return LMBP_EOVERLAP;
+    for (int j = i + 1; j < 3; ++j)
+      if (overlaps(outs[i], outs[j])) return LMBP_EOVERLAP;
+  }
+  return from_hip(lmbp::launch_msrms_q8_fwd(dt == LMBP_BF16, rows, cols, eps, x, res, s, q, scale, rstd,
+                                            static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status msrms_q8_bwd_impl(lmbp_dtype dt, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
+                              const float* scale, const float* rstd, const void* ds, void* dx, void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  if (bad_matrix(rows, cols)) return LMBP_EINVAL;
+  if (rows == 0) return LMBP_OK;
+  if (cols == 0 || !dz || !q || !scale || !rstd || !dx) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt);
+  if (!aligned(dz, eb) || !aligned(dx, eb) || (ds && !aligned(ds, eb)) || !aligned(scale, 4) || !aligned(rstd, 4))
+    return LMBP_EINVAL;
+  const uint64_t count = uint64_t(rows) * uint64_t(cols);
+  const Span sd = span(dx, count * eb);
+  if (bad_pair(sd, span(dz, count * eb), true) || bad_pair(sd, span(ds, ds ? count * eb : 0), true) ||
+      overlaps(sd, span(q, count)) || overlaps(sd, span(scale, uint64_t(rows) * 4)) ||
+      overlaps(sd, span(rstd, uint64_t(rows) * 4)))
+    return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_msrms_q8_bwd(dt == LMBP_BF16, rows, cols, dz, q, scale, rstd, ds, dx,
+                                            static_cast<hipStream_t>(stream)));
+}
+
+bool bad_layer(int64_t m, int64_t n, int64_t k) {
+  const int64_t lim = int64_t(1) << 31;
+  return m < 0 || n < 0 || k < 0 || m >= lim || n >= lim || k >= lim;
+}
+
+lmbp_status linear_q8_fwd_impl(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t* q, const float* scale,
+                               const int8_t* w, const float* w_scale, const void* bias, void* y, void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  if (bad_layer(m, n, k) || k > lmbp::kQ8MaxDepth || bad_matrix(m, n)) return LMBP_EINVAL;
+  if (m == 0 || n == 0) return LMBP_OK;
+  if (!y || !scale || !w_scale || (k > 0 && (!q || !w))) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt);
+  if (!aligned(y, eb) || !aligned(scale, 4) || !aligned(w_scale, 4) || (bias && !aligned(bias, eb))) return LMBP_EINVAL;
+  const Span sy = span(y, uint64_t(m) * uint64_t(n) * eb);
+  const Span ins[5] = {span(q, q ? uint64_t(m) * uint64_t(k) : 0), span(w, w ? uint64_t(n) * uint64_t(k) : 0),
+                       span(scale, uint64_t(m) * 4), span(w_scale, uint64_t(n) * 4),
+                       span(bias, bias ? uint64_t(n) * eb : 0)};
+  for (const Span& in : ins)
+    if (overlaps(sy, in)) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_linear_q8_fwd(dt == LMBP_BF16, m, n, k, q, scale, w, w_scale, bias, y,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status linear_q8_bwd_impl(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const void* dy, const int8_t* w,
+                               const float* w_scale, void* dx, void* workspace, int64_t workspace_bytes,
+                               void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  if (bad_layer(m, n, k) || n > lmbp::kQ8MaxDepth || bad_matrix(m, k)) return LMBP_EINVAL;
+  if (m == 0 || k == 0) return LMBP_OK;
+  if (!dx || (n > 0 && (!dy || !w || !w_scale))) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt);
+  if (!aligned(dx, eb) || (n > 0 && (!aligned(dy, eb) || !aligned(w_scale, 4)))) return LMBP_EINVAL;
+  const uint64_t need = lmbp_linear_q8_bwd_bytes(m, n, k);
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || uint64_t(workspace_bytes) < need)
+    return LMBP_EINVAL;
+  const Span sd = span(dx, uint64_t(m) * uint64_t(k) * eb), sp = span(workspace, need);
+  const Span ins[3] = {span(dy, n > 0 ? uint64_t(m) * uint64_t(n) * eb : 0),
+                       span(w, n > 0 ? uint64_t(n) * uint64_t(k) : 0), span(w_scale, uint64_t(n) * 4)};
+  if (overlaps(sd, sp)) return LMBP_EOVERLAP;
+  for (const Span& in : ins)
+    if (overlaps(sd, in) || overlaps(sp, in)) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_linear_q8_bwd(dt == LMBP_BF16, m, n, k, dy, w, w_scale, dx, workspace,
+                                             static_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -560,6 +682,34 @@ lmbp_status msrms_linear_swiglu_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t
                                     void* u, uint32_t* codes, void* g, void* z, float* rstd, void* stream) {
   return msrms_linear_swiglu_fwd_impl(dt, m, n, k, eps, x, w_gate, w_up, h, s, u, codes, g, z, rstd,
                                       stream);
+}
+
+lmbp_status q8_rows(lmbp_dtype dt, int64_t rows, int64_t cols, const void* x, int8_t* q, float* scale, void* stream) {
+  return q8_rows_impl(dt, rows, cols, x, q, scale, stream);
+}
+lmbp_status q8_values(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t* q, const float* scale, void* v,
+                      void* stream) {
+  return q8_values_impl(dt, rows, cols, q, scale, v, stream);
+}
+lmbp_status msrms_q8_fwd(lmbp_dtype dt, int64_t rows, int64_t cols, float eps, const void* x, const void* res, void* s,
+                         int8_t* q, float* scale, float* rstd, void* stream) {
+  return msrms_q8_fwd_impl(dt, rows, cols, eps, x, res, s, q, scale, rstd, stream);
+}
+lmbp_status msrms_q8_bwd(lmbp_dtype dt, int64_t rows, int64_t cols, const void* dz, const int8_t* q, const float* scale,
+                         const float* rstd, const void* ds, void* dx, void* stream) {
+  return msrms_q8_bwd_impl(dt, rows, cols, dz, q, scale, rstd, ds, dx, stream);
+}
+lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t* q, const float* scale,
+                          const int8_t* w, const float* w_scale, const void* bias, void* y, void* stream) {
+  return linear_q8_fwd_impl(dt, m, n, k, q, scale, w, w_scale, bias, y, stream);
+}
+size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k) {
+  if (m <= 0 || k <= 0 || bad_layer(m, n, k) || n > lmbp::kQ8MaxDepth) return 0;
+  return lmbp::linear_q8_bwd_workspace(m, n);
+}
+lmbp_status linear_q8_bwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const void* dy, const int8_t* w,
+                          const float* w_scale, void* dx, void* workspace, int64_t workspace_bytes, void* stream) {
+  return linear_q8_bwd_impl(dt, m, n, k, dy, w, w_scale, dx, workspace, workspace_bytes, stream);
 }
 
 lmbp_status lmbp_copy(const void* src, void* dst, int64_t bytes, void* stream) {

@@ -14,6 +14,12 @@
 * ``LinearReSwiGLU2``: the LLaMA MLP's gate and up projections with SwiGLU, forward fused
   in one kernel (g never stored); backward through the SwiGLU activation backward and
   the linear layers' products.
+* ``LinearQ8``: a linear layer whose frozen weight is kept in 8 bits (one scale per output
+  channel); its input's rows are brought to 8 bits and the product runs on whole numbers.
+  Keeps nothing of its input.
+* ``MSRMSNormLinearQ8``: residual addition, MS-RMSNorm with its output in 8 bits, and the
+  ``LinearQ8`` layers that consume it. Keeps one byte per element of the norm's output and
+  two fp32 values per row, for the norm and all its layers together.
 * ``merge_norm_into_linears``: folds a norm's affine (alpha, beta) into the linear layers
   that consume its output, W~ = W diag(alpha), b~ = W beta + b (Sec. 5.2), and returns
   the parameter-free MS norm to use in its place.
@@ -234,6 +240,141 @@ class MSRMSNorm(nn.Module):
 
     def forward(self, x):
         return _MSNorm.apply(x, self.eps, False)
+
+    def extra_repr(self):
+        return f"eps={self.eps}"
+
+
+class _LinearQ8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, scale, bias):
+        x2 = _flat(x).reshape(-1, x.shape[-1])
+        q, q_scale = binding.q8_rows(x2)
+        ctx.has_bias = bias is not None
+        ctx.bias_dtype = bias.dtype if bias is not None else None
+        ctx.save_for_backward(weight, scale)
+        return _product_q8(q, q_scale, weight, scale, bias, x.dtype).reshape(*x.shape[:-1], weight.shape[0])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        weight, scale = ctx.saved_tensors
+        dx = binding.linear_q8_bwd(_flat(dy), weight, scale) if ctx.needs_input_grad[0] else None
+        return dx, None, None, _bias_grad(dy, ctx.bias_dtype) if ctx.needs_input_grad[3] else None
+
+
+def _product_q8(q, q_scale, weight, scale, bias, dtype):
+    if bias is not None:
+        bias = _flat(bias if bias.dtype == dtype else bias.to(dtype))
+    return binding.linear_q8_fwd(q, q_scale, weight, scale, bias, dtype)
+
+
+def _bias_grad(dy, dtype):
+    return dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32).to(dtype)
+
+
+class LinearQ8(nn.Module):
+    """Linear layer with a frozen 8-bit weight: ``weight`` int8 [n, k] and ``scale`` fp32 [n]
+    (buffers; w = weight * scale), ``bias`` [n] or None (a parameter, frozen unless its
+    ``requires_grad`` is set). The input's rows are brought to 8 bits, and so are the rows of
+    the output's gradient in the backward; nothing of the input is kept."""
+
+    def __init__(self, weight, scale, bias=None):
+        super().__init__()
+        if weight.dtype != torch.int8 or weight.dim() != 2:
+            raise ValueError("weight must be an int8 tensor [n, k]")
+        if scale.dtype != torch.float32 or scale.shape != weight.shape[:1]:
+            raise ValueError("scale must be a float32 tensor [n]")
+        if bias is not None and bias.shape != weight.shape[:1]:
+            raise ValueError("bias must have n elements")
+        self.register_buffer("weight", weight.contiguous())
+        self.register_buffer("scale", scale.contiguous())
+        self.bias = None if bias is None else nn.Parameter(bias.detach().clone(), requires_grad=False)
+
+    @classmethod
+    @torch.no_grad()
+    def from_linear(cls, linear):
+        """The 8-bit form of a linear layer on the GPU (after merging a norm's affine, if any)."""
+        weight, scale = binding.q8_rows(_flat(linear.weight.detach()))
+        return cls(weight, scale, linear.bias)
+
+    @property
+    def in_features(self):
+        return self.weight.shape[1]
+
+    @property
+    def out_features(self):
+        return self.weight.shape[0]
+
+    def _apply(self, fn, recurse=True):
+        scale = self.scale
+        super()._apply(fn, recurse)
+        if self.scale.dtype != torch.float32:   # a change of the model's type is not meant for the scales
+            self.scale = scale.to(self.scale.device)
+        return self
+
+    def values(self, dtype=torch.bfloat16):
+        """The weight that the layer computes with, in ``dtype``."""
+        return binding.q8_values(self.weight, self.scale, dtype)
+
+    def forward(self, x):
+        return _LinearQ8.apply(x, self.weight, self.scale, self.bias)
+
+    def extra_repr(self):
+        return f"in_features={self.in_features}, out_features={self.out_features}, bias={self.bias is not None}"
+
+
+class _NormLinearQ8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, res, eps, *layers):
+        out = binding.msrms_q8_fwd(_flat(x), eps, None if res is None else _flat(res))
+        q, q_scale, rstd = out[:3]
+        ctx.set_materialize_grads(False)
+        ctx.bias_dtypes = [b.dtype if b is not None else None for b in layers[2::3]]
+        ctx.save_for_backward(q, q_scale, rstd, *(t for i, t in enumerate(layers) if i % 3 != 2))
+        ys = [_product_q8(q, q_scale, w, sc, b, x.dtype) for w, sc, b in zip(*(layers[i::3] for i in range(3)))]
+        return (*ys, *out[3:])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, *grads):
+        q, q_scale, rstd, *weights = ctx.saved_tensors
+        count = len(ctx.bias_dtypes)
+        ds = grads[count] if len(grads) > count else None
+        need_x, need_res = ctx.needs_input_grad[:2]
+        dx = None
+        if need_x or need_res:
+            dz = None
+            for dy, w, sc in zip(grads, weights[::2], weights[1::2]):
+                if dy is not None:
+                    part = binding.linear_q8_bwd(_flat(dy), w, sc)
+                    dz = part if dz is None else dz.add_(part)
+            if dz is None:
+                dx = ds
+            else:
+                dx = binding.msrms_q8_bwd(dz, q, q_scale, rstd, None if ds is None else _flat(ds), dx=dz)
+        db = [_bias_grad(grads[i], t) if ctx.needs_input_grad[5 + 3 * i] and grads[i] is not None else None
+              for i, t in enumerate(ctx.bias_dtypes)]
+        return (dx if need_x else None, dx if need_res else None, None,
+                *(g for b in db for g in (None, None, b)))
+
+
+class MSRMSNormLinearQ8(nn.Module):
+    """Residual addition, RMSNorm without weight (Alg. 3; its affine merged into the layers)
+    and the ``LinearQ8`` layers behind it. ``forward(x, res)`` returns the layers' outputs and
+    s = x + res; ``forward(x)`` the outputs alone (one tensor for a single layer)."""
+
+    def __init__(self, layers, eps=1e-5):
+        super().__init__()
+        self.layers = nn.ModuleList(layers)
+        if not self.layers or not all(isinstance(m, LinearQ8) for m in self.layers):
+            raise TypeError("layers must be LinearQ8 modules")
+        self.eps = float(eps)
+
+    def forward(self, x, res=None):
+        flat = [t for m in self.layers for t in (m.weight, m.scale, m.bias)]
+        out = _NormLinearQ8.apply(x, res, self.eps, *flat)
+        return out[0] if len(out) == 1 else out
 
     def extra_repr(self):
         return f"eps={self.eps}"
