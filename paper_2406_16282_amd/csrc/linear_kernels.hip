@@ -70,6 +70,7 @@
 #include "act_codes.hpp"
 #include "act_math.hpp"
 #include "lmbp_launch.hpp"
+#include "tile_device.hpp"
 
 #include <algorithm>
 #include <atomic>
@@ -80,11 +81,7 @@ namespace lin {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int kGroupM = 8;
-constexpr uint32_t kBufferGDword3 = 0x00020000;  // raw 32-bit buffer, gfx9 family
-constexpr uint32_t kOutOfRange = 0x80000000u;    // beyond any resource's range: reads 0
 constexpr int kBK = 64;                          // K step: an LDS row is 128 bytes
 
 // MINW: waves per SIMD that the registers are budgeted for (blocks per CU follow from it).
@@ -110,69 +107,6 @@ using BigTile = Tile<256, 256, 2, 4, 2>;      // one block of 8 waves per CU
 using MidTile = Tile<128, 256, 1, 4, 2, 3>;   // two blocks of 4 waves
 using SmallTile = Tile<128, 128, 4, 2, 4>;    // two blocks of 8 waves
 using LowTile = Tile<64, 128, 2, 2, 3>;       // three blocks of 4 waves
-
-// The grid of tiles: sizes, tiles per XCD, and floor(2^32 / tiles_n).
-struct TileMap {
-  uint32_t tiles_m, tiles_n, tiles, per_xcd, inv_n;
-};
-
-// The target builtins below are wrapped in device functions: used directly in the body of
-// a kernel template, they make the host-side instantiation fail silently and the launch
-// stub is never emitted.
-
-// A raw buffer resource over `bytes` bytes at `base` (reads beyond return zeros).
-__device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int64_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, int(bytes), kBufferGDword3);
-}
-// 16 or 4 bytes per lane from the buffer into LDS at `dst` + lane * 16 or 4 (dst wave-uniform).
-// CPOL: cache policy bits of the instruction (nt = 2).
-template <int CPOL = 0>
-__device__ inline void load_lds16(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t offset) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)dst, 16, offset, 0, 0, CPOL);
-}
-__device__ inline void load_lds4(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t offset) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)dst, 4, offset, 0, 0, 0);
-}
-
-// Scheduling groups for MF MFMAs, with VM buffer loads and then DS LDS reads spread over
-// the first half of them (so the reads have landed before the next wait).
-template <int MF, int VM, int DS, int I = 0>
-__device__ inline void spread() {
-  if constexpr (I < MF) {
-    constexpr int W = MF / 2 < 1 ? 1 : MF / 2;
-    constexpr int T = VM + DS;
-    constexpr int lo = I < W ? T * I / W : T, hi = I < W ? T * (I + 1) / W : T;
-    constexpr int vm = (hi < VM ? hi : VM) - (lo < VM ? lo : VM);
-    constexpr int ds = (hi - lo) - vm;
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                  // one MFMA
-    if constexpr (vm > 0) __builtin_amdgcn_sched_group_barrier(0x020, vm, 0);  // buffer loads
-    if constexpr (ds > 0) __builtin_amdgcn_sched_group_barrier(0x100, ds, 0);  // LDS reads
-    spread<MF, VM, DS, I + 1>();
-  }
-}
-
-// Tile coordinates of the t-th tile (see the file comment). tiles_n is divided by with a
-// host-made reciprocal (floor(2^32 / tiles_n), at most one short of the quotient for
-// t < 2^30) instead of an integer division.
-__device__ inline void tile_of(uint32_t t, const TileMap& m, uint32_t& tm, uint32_t& tn) {
-  const uint32_t id = (t < m.per_xcd * kXcds) ? (t % kXcds) * m.per_xcd + t / kXcds : t;
-  const uint32_t id8 = id / kGroupM;
-  uint32_t group = __umulhi(id8, m.inv_n);
-  uint32_t in = id8 - group * m.tiles_n;
-  while (in >= m.tiles_n) {
-    in -= m.tiles_n;
-    ++group;
-  }
-  const uint32_t first_m = group * kGroupM, r = in * kGroupM + id % kGroupM;
-  const uint32_t left = m.tiles_m - first_m;
-  if (left >= uint32_t(kGroupM)) {
-    tm = first_m + r % kGroupM;
-    tn = r / kGroupM;
-  } else {   // the last, smaller group of row tiles
-    tm = first_m + r % left;
-    tn = r / left;
-  }
-}
 
 // Arguments of the kernel (by value). Plain form: y = act(z), z = x w^T + bias.
 // Gated form (GLU): g = x w^T and u = x w2^T (no bias), y = h = act(g) * u, s = act(g),
