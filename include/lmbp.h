@@ -328,44 +328,49 @@ lmbp_status q8_values(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t *q
  *               s == res are allowed, x == res too.
  *   q         : rows x cols; scale, rstd: rows fp32 values.
  *   eps       : finite, > 0.
- *   dz, ds, dx: rows x cols of dtype; ds NULL for none. dx == dz and dx == ds are allowed.
+ *   dz, ds, dx: rows x cols, dz of dt_dz, ds (NULL for none) and dx of dtype: the same, or dz
+ *               fp32 with dtype bf16 (a sum over several layers is worth keeping in fp32;
+ *               LMBP_EDTYPE the other way round). dx == dz, if of one type, and dx == ds are
+ *               allowed.
  * No other overlap. The rounding to 8 bits is passed over by the backward, which is the
  * gradient of the norm at the z that was kept.
  * ------------------------------------------------------------------------ */
 lmbp_status msrms_q8_fwd(lmbp_dtype dt, int64_t rows, int64_t cols, float eps, const void *x,
                          const void *res, void *s, int8_t *q, float *scale, float *rstd,
                          void *stream);
-lmbp_status msrms_q8_bwd(lmbp_dtype dt, int64_t rows, int64_t cols, const void *dz,
-                         const int8_t *q, const float *scale, const float *rstd, const void *ds,
-                         void *dx, void *stream);
+lmbp_status msrms_q8_bwd(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t cols,
+                         const void *dz, const int8_t *q, const float *scale, const float *rstd,
+                         const void *ds, void *dx, void *stream);
 
 /* ------------------------------------------------------------------------
  * A linear layer whose frozen weight is kept in 8 bits, one scale per output channel (as
  * q8_rows gives for w [n x k]), on rows in 8 bits:
  *
  *   y  = (sum_k q[m, k] w[n, k]) (scale[m] w_scale[n]) + bias[n]
- *   dx = (sum_n p[m, n] w[n, k]) p_scale[m],   p, p_scale the 8-bit rows of dy w_scale
+ *   dx = (sum_n p[m, n] w[n, k]) p_scale[m] + add,   p, p_scale the 8-bit rows of dy w_scale
  *
  * The sums are exact (whole numbers in 32 bits), everything behind them is fp32 with one
  * rounding to dtype.
  *
- *   dt     : type of y, bias, dy, dx.
+ *   dt     : type of y and bias, or of dy; dt_dx: type of add and dx.
  *   m,n,k  : any sizes >= 0 below 2^31; the length of the sums (k forward, n backward) at
  *            most 131071. k = 0 gives y = bias (0 without), n = 0 gives dx = 0.
  *   q [m x k], w [n x k]: any values; scale [m], w_scale [n]; bias [n] or NULL; y, dy [m x n];
- *            dx [m x k].
+ *            add, dx [m x k], add NULL for none; dx == add is allowed (the sum of several
+ *            layers' gradients).
  *   workspace : lmbp_linear_q8_bwd_bytes(m, n, k) bytes, 16-byte aligned. Its contents do
  *            not matter before or after.
  * q and w with k a multiple of 16 on 16-byte aligned pointers take the fast path, anything
- * else a slower one with the same results. No output overlaps another buffer.
+ * else a slower one with the same results. No other output overlaps another buffer.
  * ------------------------------------------------------------------------ */
 lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t *q,
                           const float *scale, const int8_t *w, const float *w_scale,
                           const void *bias, void *y, void *stream);
 size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k);
-lmbp_status linear_q8_bwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const void *dy,
-                          const int8_t *w, const float *w_scale, void *dx, void *workspace,
-                          int64_t workspace_bytes, void *stream);
+lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n, int64_t k,
+                          const void *dy, const int8_t *w, const float *w_scale,
+                          const void *add, void *dx, void *workspace, int64_t workspace_bytes,
+                          void *stream);
 
 /* ------------------------------------------------------------------------
  * Test utilities (host only, no launch): the kernel form that a size takes on the calling

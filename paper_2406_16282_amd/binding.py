@@ -111,11 +111,11 @@ def lib():
     L.linear_act_bwd.restype = i32
     L.q8_rows.argtypes = L.q8_values.argtypes = [i32, i64, i64, vp, vp, vp, vp]
     L.msrms_q8_fwd.argtypes = [i32, i64, i64, f32, vp, vp, vp, vp, vp, vp, vp]
-    L.msrms_q8_bwd.argtypes = [i32, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.msrms_q8_bwd.argtypes = [i32, i32, i64, i64, vp, vp, vp, vp, vp, vp, vp]
     L.linear_q8_fwd.argtypes = [i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
     L.lmbp_linear_q8_bwd_bytes.argtypes = [i64, i64, i64]
     L.lmbp_linear_q8_bwd_bytes.restype = ctypes.c_size_t
-    L.linear_q8_bwd.argtypes = [i32, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp]
+    L.linear_q8_bwd.argtypes = [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     for name in Q8_OPS:
         getattr(L, name).restype = i32
     L.lmbp_copy.argtypes = [vp, vp, i64, vp]
@@ -752,6 +752,16 @@ def _per_row(t, ref, count, what):
     return t
 
 
+def _typed_out(ref, out, shape, dtype, what):
+    """An output of that shape and type on ``ref``'s device, allocated unless given."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=ref.device)
+    _on(out, ref, what)
+    if out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)}")
+    return out
+
+
 def _opt(t):
     return _ptr(t) if t is not None else None
 
@@ -804,22 +814,26 @@ def msrms_q8_fwd(x, eps, res=None, s=None, stream=None):
     return (q, scale, rstd) if res is None else (q, scale, rstd, s)
 
 
-def msrms_q8_bwd(dz, q, scale, rstd, ds=None, dx=None, stream=None):
+def msrms_q8_bwd(dz, q, scale, rstd, ds=None, dx=None, dtype=None, stream=None):
     """MS-RMSNorm backward from the output kept in 8 bits: dx = rstd (dz - z mean(z dz)) + ds,
     z = q * scale. dx is the gradient of x and of the residual alike; ds (None: none) the
-    gradient that reaches their sum past the norm. dx may be dz or ds."""
+    gradient that reaches their sum past the norm. dx has the type of ds, else ``dtype``, else
+    that of dz; dz may be fp32 where they are bf16. dx may be given, dz (of one type) or ds
+    included."""
     _dev(dz, "dz")
-    dt = _dtype_code(dz)
+    dt_dz = _dtype_code(dz)
+    dtype = ds.dtype if isinstance(ds, torch.Tensor) else dtype or dz.dtype
     rows, cols = _q8_rows_cols(dz)
     _q8_in(q, dz, "q", dz.shape)
     _per_row(scale, dz, rows, "scale")
     _per_row(rstd, dz, rows, "rstd")
-    if ds is not None and _same(ds, dz, "ds").shape != dz.shape:
+    if ds is not None and _on(ds, dz, "ds").shape != dz.shape:
         raise ValueError("ds must have the shape of dz")
-    dx = _like(dz, dx, "dx")
+    dx = _typed_out(dz, dx, dz.shape, dtype, "dx")
+    dt = _dtype_code(dx)
     with _device_of(dz):   # launches go to the tensors' GPU
-        _check("msrms_q8_bwd", lib().msrms_q8_bwd(dt, rows, cols, _ptr(dz), _ptr(q), _ptr(scale), _ptr(rstd), _opt(ds),
-                                                  _ptr(dx), _stream(dz, stream)))
+        _check("msrms_q8_bwd", lib().msrms_q8_bwd(dt_dz, dt, rows, cols, _ptr(dz), _ptr(q), _ptr(scale), _ptr(rstd),
+                                                  _opt(ds), _ptr(dx), _stream(dz, stream)))
     return dx
 
 
@@ -852,21 +866,29 @@ def linear_q8_fwd(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=
     return y
 
 
-def linear_q8_bwd(dy, w, w_scale, stream=None):
-    """Input gradient of linear_q8_fwd: dx = (dy w_scale) w, the rows of dy w_scale [..., n]
-    brought to 8 bits first (one scale per row), dx [..., k] of dy's type."""
+def linear_q8_bwd(dy, w, w_scale, add=None, dx=None, dtype=None, stream=None):
+    """Input gradient of linear_q8_fwd: dx = (dy w_scale) w + add, the rows of dy w_scale [..., n]
+    brought to 8 bits first (one scale per row). dx [..., k] has the type of ``add`` (None: none),
+    else ``dtype``, else that of dy; it may be given, ``add`` itself included (the sum of several
+    layers' gradients)."""
     _dev(dy, "dy")
     dt = _dtype_code(dy)
     n, k = _q8_weight(w, w_scale, dy)
     if dy.dim() == 0 or dy.shape[-1] != n:
         raise ValueError("dy must be [..., n] and w [n, k]")
     m = math.prod(dy.shape[:-1])
+    shape = torch.Size((*dy.shape[:-1], k))
+    if add is not None:
+        dtype = _on(add, dy, "add").dtype
+        if add.shape != shape:
+            raise ValueError("add must be [..., k]")
+    dx = _typed_out(dy, dx, shape, dtype or dy.dtype, "dx")
+    dt_dx = _dtype_code(dx)
     L = lib()
     with _device_of(dy):   # launches go to the tensors' GPU
         nbytes = L.lmbp_linear_q8_bwd_bytes(m, n, k)
         handle = _stream(dy, stream)
         work = _workspace(nbytes, dy, stream)
-        dx = torch.empty((*dy.shape[:-1], k), dtype=dy.dtype, device=dy.device)
-        _check("linear_q8_bwd", L.linear_q8_bwd(dt, m, n, k, _ptr(dy), _ptr(w), _ptr(w_scale), _ptr(dx), _ptr(work),
-                                                nbytes, handle))
+        _check("linear_q8_bwd", L.linear_q8_bwd(dt, dt_dx, m, n, k, _ptr(dy), _ptr(w), _ptr(w_scale), _opt(add), _ptr(dx),
+                                                _ptr(work), nbytes, handle))
     return dx

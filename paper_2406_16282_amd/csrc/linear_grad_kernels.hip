@@ -32,6 +32,7 @@
 #include "act_codes.hpp"
 #include "lmbp_device.hpp"
 #include "lmbp_launch.hpp"
+#include "tile_device.hpp"
 
 #include <algorithm>
 #include <atomic>
@@ -43,7 +44,9 @@ namespace lgrad {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
+using lin::lds_addr;
+using lin::load_lds16_asm;
+using lin::rsrc_words;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int kRowsPerSlot = 32;
@@ -68,21 +71,6 @@ using BigTile = Tile<256, 256, 2, 4, 2>;      // one block of 8 waves per CU
 using MidTile = Tile<128, 256, 1, 4, 2, 3>;   // two blocks of 4 waves
 using SmallTile = Tile<128, 128, 2, 2, 2>;    // two blocks of 4 waves
 
-__device__ inline u32x4 rsrc(uint64_t base, uint32_t bytes) {
-  return u32x4{uint32_t(base), uint32_t(base >> 32) & 0xffffu, bytes, 0x00020000u};
-}
-// 16 bytes per lane into LDS at `dst` + lane * 16 (see the file comment). The wait states
-// cover a resource whose registers a VALU operation has just written (5, with the move).
-// The compiler reserves m0 for itself and warns that it cannot keep a value there across
-// the asm; the clobber is to say just that, so that it never counts on one.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ inline void load_lds16(const u32x4& r, uint32_t dst, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(dst), "v"(offset), "s"(r) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-__device__ inline uint32_t lds_addr(const uint16_t* p) { return uint32_t(uintptr_t((lds_void*)p)); }
 __device__ inline s16x4 read_tr(const uint16_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
 }
@@ -176,8 +164,8 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void grad_weight_kernel(
     }
   };
   auto load = [&](uint32_t S, int q) {
-    if (q < kLA) load_lds16(rsrc(pa, na), S + (wave + kWaves * q) * 1024, ld_a[q < kLA ? q : 0]);
-    else load_lds16(rsrc(pb, nb), S + BM * kRowsPerSlot * 2 + (wave + kWaves * (q - kLA)) * 1024, ld_b[q < kLA ? 0 : q - kLA]);
+    if (q < kLA) load_lds16_asm(rsrc_words(pa, na), S + (wave + kWaves * q) * 1024, ld_a[q < kLA ? q : 0]);
+    else load_lds16_asm(rsrc_words(pb, nb), S + BM * kRowsPerSlot * 2 + (wave + kWaves * (q - kLA)) * 1024, ld_b[q < kLA ? 0 : q - kLA]);
   };
   auto advance = [&]() {
     pa += uint64_t(kRowsPerSlot) * N * 2;

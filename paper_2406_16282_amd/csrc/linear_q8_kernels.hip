@@ -1,125 +1,483 @@
-// Linear layers of 8-bit rows and 8-bit weights, for gfx950.
+// Linear layers of 8-bit rows and 8-bit weights, forward, for gfx950.
 //
-//   linear_q8_fwd : y = (sum_k q[m, k] w[n, k]) scale[m] w_scale[n] + bias[n]
-//   linear_q8_bwd : dx = (sum_n p[m, n] w[n, k]) p_scale[m], p and p_scale the rows of
-//                   dy[m, n] w_scale[n] in 8 bits
+//   y = (sum_k q[m, k] w[n, k]) scale[m] w_scale[n] + bias[n]
 //
 // The sums are whole numbers in 32 bits and exact for up to kQ8MaxDepth products (128 * 128 *
 // kQ8MaxDepth < 2^31); one conversion to fp32, one product of the scales, one fused
 // multiply-add with the bias, one rounding to the output's type.
-#include "lmbp_device.hpp"
-#include "lmbp_launch.hpp"
+#include "linear_q8_device.hpp"
+
+#include <algorithm>
+#include <cstdlib>
 
 namespace lmbp {
 namespace lq8 {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4_at1 __attribute__((ext_vector_type(4), aligned(1)));
+constexpr int kBK = 128;   // K step in bytes: an LDS row
 
-struct Args {
-  const int8_t* a;        // [M x K], rows a_pitch bytes apart
-  const int8_t* b;        // forward: [N x K]; backward (TR): [K x N]
-  const float* a_scale;   // per row, or null where there is nothing to add up (K = 0)
-  const float* b_scale;   // per column of the result, or null
-  const void* bias;       // per column, of the result's type, or null
-  void* y;                // [M x N]
-  int64_t M, N, K, a_pitch;
+// MINW: waves per SIMD that the registers are budgeted for (blocks per CU follow from it).
+template <int BM_, int BN_, int WM_, int WN_, int MINW_, int RING_ = 4>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kMinWaves = MINW_;
+  static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
+  static constexpr int HM = BM / WM / 2, HN = BN / WN / 2;   // half of a wave's rows, columns
+  static constexpr int TMH = HM / 16, TNH = HN / 16;         // MFMA tiles per half
+  static constexpr int TM = 2 * TMH, TN = 2 * TNH;
+  static constexpr int kSlot = (BM + BN) / 2 * kBK;          // one ring slot: half of A and of B
+  static constexpr int kRing = RING_;
+  static constexpr int kBlocksPerCu = kMinWaves * 4 / kWaves;
+  static constexpr int kLA = BM / 16 / kWaves, kLB = BN / 16 / kWaves;   // 1 KiB loads per wave
+  static constexpr int kSide = 4 * (BM + BN) * 4;            // the scales of four tiles
+  static constexpr int kLdsBytes = kRing * kSlot + kSide;
+  static_assert(HN % 32 == 0 && HM % 16 == 0, "wave tile");
+  static_assert(kLA >= 1 && kLB >= 1 && (BM / 16) % kWaves == 0 && (BN / 16) % kWaves == 0, "loads");
+  static_assert(kLdsBytes * kBlocksPerCu <= 160 * 1024, "LDS per CU");
 };
 
-// 16 bytes of a row from byte k0 on, zeros from byte `end` on; any alignment.
-__device__ inline u32x4 row_piece(const int8_t* row, int64_t k0, int64_t end) {
-  if (k0 + 16 <= end) return *reinterpret_cast<const u32x4_at1*>(row + k0);
-  u32x4 v = {0u, 0u, 0u, 0u};
-  for (int i = 0; i < 16 && k0 + i < end; ++i) v[i / 4] |= uint32_t(uint8_t(row[k0 + i])) << (8 * (i % 4));
-  return v;
+// 16 consecutive results of a row from column `col` on; those from N on are not stored.
+template <class OUT>
+__device__ inline void store16(const Args& a, int64_t row, int64_t col, const float (&f)[16]) {
+  const int64_t base = row * a.N + col;
+  if (a.vec) {
+#pragma unroll
+    for (int p = 0; p < 16 / OUT::kPerVec; ++p) {
+      float v[OUT::kPerVec];
+#pragma unroll
+      for (int e = 0; e < OUT::kPerVec; ++e) v[e] = f[p * OUT::kPerVec + e];
+      if (col + p * OUT::kPerVec < a.N)
+        *reinterpret_cast<u32x4*>(static_cast<char*>(a.y) + (base + p * OUT::kPerVec) * OUT::kBytes) = OUT::pack(v);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (col + e < a.N) OUT::store1(a.y, base + e, f[e]);
+  }
 }
 
-// Any sizes and alignments: a block of 4 waves takes 64 x 64 results, 64 products at a time,
-// both operands staged through registers into LDS with the products contiguous.
-template <class OUT, bool TR>
-__global__ __launch_bounds__(256) void product_any(Args a) {
-  constexpr int kStep = 64, kRow = kStep + 16;
-  __shared__ __attribute__((aligned(16))) int8_t la[64 * kRow], lb[64 * kRow];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_in_block();
-  const int64_t tiles_n = (a.N + 63) / 64;
-  const int64_t m0 = int64_t(blockIdx.x) / tiles_n * 64, n0 = int64_t(blockIdx.x) % tiles_n * 64;
-  i32x4 acc[4];
+template <class C, class OUT>
+__global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tile(Args a) {
+  constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, TMH = C::TMH, TNH = C::TNH;
+  constexpr int HM = C::HM, HN = C::HN, kWaves = C::kWaves;
+  constexpr int kLA = C::kLA, kLB = C::kLB, kL = kLA + kLB, kSlot = C::kSlot, kRing = C::kRing;
+  const int64_t M = a.M, N = a.N;
+  const uint32_t K = uint32_t(a.K);
+  extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+  float* const as_lds = reinterpret_cast<float*>(lds + kRing * kSlot);
+  float* const bs_lds = as_lds + 4 * BM;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = wave_in_block();
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  const uint32_t tiles = a.map.tiles;
+  const int kt_count = K > 0 ? int((K + kBK - 1) / kBK) : 1;
+
+  // ---- load side: byte offsets of this lane's chunks at K step 0, for both halves
+  uint32_t ld_a[2][kLA], ld_b[2][kLB];
+  uint32_t kc_a[kLA], kc_b[kLB];
+  const int r_in = lane / 8, u_in = lane % 8;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = i32x4{0, 0, 0, 0};
-  const int r = tid / 4, c = (tid % 4) * 16;
-  for (int64_t k0 = 0; k0 < a.K; k0 += kStep) {
-    u32x4 va = {0u, 0u, 0u, 0u}, vb = {0u, 0u, 0u, 0u};
-    if (m0 + r < a.M) va = row_piece(a.a + (m0 + r) * a.a_pitch, k0 + c, a.K);
-    if constexpr (TR) {
-      if (k0 + r < a.K) vb = row_piece(a.b + (k0 + r) * a.N, n0 + c, a.N);
-    } else {
-      if (n0 + r < a.N) vb = row_piece(a.b + (n0 + r) * a.K, k0 + c, a.K);
-    }
-    __syncthreads();
-    *reinterpret_cast<u32x4*>(la + r * kRow + c) = va;
-    if constexpr (TR) {
-      for (int i = 0; i < 16; ++i) lb[(c + i) * kRow + r] = int8_t(vb[i / 4] >> (8 * (i % 4)));
-    } else {
-      *reinterpret_cast<u32x4*>(lb + r * kRow + c) = vb;
-    }
-    __syncthreads();
-    const i32x4 fa = *reinterpret_cast<const i32x4*>(la + (wave * 16 + (lane & 15)) * kRow + (lane >> 4) * 16);
+  for (int q = 0; q < kLA; ++q) {
+    const int lr = (wave + kWaves * q) * 8 + r_in;
+    kc_a[q] = (u_in ^ ((lr >> 1) & 7)) * 16;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const i32x4 fb = *reinterpret_cast<const i32x4*>(lb + (j * 16 + (lane & 15)) * kRow + (lane >> 4) * 16);
-      acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb, fa, acc[j], 0, 0, 0);
-    }
+    for (int h = 0; h < 2; ++h) ld_a[h][q] = uint32_t((lr / HM) * 2 * HM + h * HM + lr % HM) * K + kc_a[q];
   }
-  // The lane holds row lane % 16 and columns 4 (lane / 16) + 0 .. 3 of each 16 x 16 results.
-  const int64_t m = m0 + wave * 16 + (lane & 15);
-  if (m >= a.M) return;
-  const float as = a.a_scale != nullptr ? a.a_scale[m] : 1.0f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int q = 0; q < kLB; ++q) {
+    const int lr = (wave + kWaves * q) * 8 + r_in;
+    kc_b[q] = (u_in ^ (((lr >> 1) & 1) | (((lr >> 3) & 3) << 1))) * 16;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t n = n0 + j * 16 + (lane >> 4) * 4 + e;
-      if (n < a.N) {
-        const float sc = a.b_scale != nullptr ? as * a.b_scale[n] : as;
-        OUT::store1(a.y, m * a.N + n,
-                    __builtin_fmaf(float(acc[j][e]), sc, a.bias != nullptr ? OUT::load1(a.bias, n) : 0.0f));
+    for (int h = 0; h < 2; ++h) ld_b[h][q] = uint32_t((lr / 8) * 16 + h * 8 + lr % 8) * K + kc_b[q];
+  }
+  // Load cursor: tile l_tile (l_seq-th of this block), K step l_k. Past the last tile the
+  // resources are empty and the loads read zeros into slots that nothing reads.
+  uint32_t l_tile = blockIdx.x;
+  int l_seq = 0, l_k = 0;
+  __amdgpu_buffer_rsrc_t ra, rb;
+  auto enter_tile = [&]() {
+    uint32_t tm = 0, tn = 0;
+    const bool in = l_tile < tiles;
+    if (in) tile_of(l_tile, a.map, tm, tn);
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+    const int64_t rows_a = !in ? 0 : (M - m0 < BM) ? M - m0 : BM;
+    const int64_t rows_b = !in ? 0 : (N - n0 < BN) ? N - n0 : BN;
+    ra = make_rsrc(a.a + m0 * K, rows_a * K);
+    rb = make_rsrc(a.b + n0 * K, rows_b * K);
+    // The tile's scales, into one of four places: the cursor runs at most two tiles ahead of
+    // the tile being computed. Issued before the tile's first operands, they have landed when
+    // those have.
+    for (int v = wave; v < BM / 64; v += kWaves)
+      load_lds4(make_rsrc(a.a_scale + m0, rows_a * 4), as_lds + (l_seq & 3) * BM + v * 64, uint32_t(v * 256 + lane * 4));
+    for (int v = wave; v < BN / 64; v += kWaves)
+      load_lds4(make_rsrc(a.b_scale + n0, rows_b * 4), bs_lds + (l_seq & 3) * BN + v * 64, uint32_t(v * 256 + lane * 4));
+  };
+  auto issue = [&](int h, int8_t* S) {
+    const uint32_t k0 = uint32_t(l_k) * kBK;
+#pragma unroll
+    for (int q = 0; q < kLA; ++q)
+      load_lds16(ra, S + (wave + kWaves * q) * 1024, k0 + kc_a[q] < K ? ld_a[h][q] + k0 : kOutOfRange);
+#pragma unroll
+    for (int q = 0; q < kLB; ++q)
+      load_lds16(rb, S + BM / 2 * kBK + (wave + kWaves * q) * 1024, k0 + kc_b[q] < K ? ld_b[h][q] + k0 : kOutOfRange);
+  };
+  auto advance = [&]() {
+    if (++l_k == kt_count) {
+      l_k = 0;
+      l_tile += gridDim.x;
+      ++l_seq;
+      enter_tile();
+    }
+  };
+
+  // ---- compute side
+  const int a_off = (wm * HM + (lane & 15)) * kBK;
+  const int b_off = BM / 2 * kBK + (wn * HN + ((lane & 15) >> 2) * 8 + (lane & 3)) * kBK;
+  const int swa = (lane & 15) >> 1;
+  const int swb = ((lane >> 1) & 1) | (((lane >> 2) & 3) << 1);
+  const int ua[2] = {((lane >> 4) ^ swa) * 16, ((4 + (lane >> 4)) ^ swa) * 16};
+  const int ub[2] = {((lane >> 4) ^ swb) * 16, ((4 + (lane >> 4)) ^ swb) * 16};
+  i32x4 fa[2][TMH][2], fb[2][TNH][2];
+  auto read_a = [&](const int8_t* S, int h) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < TMH; ++i) fa[h][i][kk] = *reinterpret_cast<const i32x4*>(S + a_off + i * 16 * kBK + ua[kk]);
+  };
+  auto read_b = [&](const int8_t* S, int h) {   // tile j: columns 4 (j % 2) of the wave's (j / 2)-th 64
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int j = 0; j < TNH; ++j)
+        fb[h][j][kk] = *reinterpret_cast<const i32x4*>(S + b_off + ((j / 2) * 32 + (j % 2) * 4) * kBK + ub[kk]);
+  };
+  i32x4 acc[TM][TN];
+  auto quad = [&](int ha, int hb) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < TMH; ++i)
+#pragma unroll
+        for (int j = 0; j < TNH; ++j)
+          acc[ha * TMH + i][hb * TNH + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+              fb[hb][j][kk], fa[ha][i][kk], acc[ha * TMH + i][hb * TNH + j], 0, 0, 0);
+  };
+  constexpr int MF = TMH * TNH * 2, RA = TMH * 2, RB = TNH * 2;
+
+  // An odd ring has its second-half slots loaded in first half steps and the other way round.
+  enter_tile();
+  constexpr bool kOdd = kRing % 2 != 0;
+#pragma unroll
+  for (int d = 0; d < kRing; ++d) {
+    issue(d & 1, lds + d * kSlot);
+    if (d & 1) advance();
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kRing - 2) * kL) : "memory");
+  asm volatile("s_barrier" ::: "memory");
+
+  int slot = 0;   // of the half step's first data unit
+  auto next = [&](int v, int d) { v += d; return v >= kRing ? v - kRing : v; };
+  int seq = 0;
+  for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++seq) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    // The tile's first fragments; no wave may load over them before all have read them.
+    read_a(lds + slot * kSlot, 0);
+    read_b(lds + slot * kSlot, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("s_barrier" ::: "memory");
+
+    for (int kt = 0; kt < kt_count; ++kt) {
+      int8_t* S = lds + slot * kSlot;
+      int8_t* S1 = lds + next(slot, 1) * kSlot;
+      slot = next(slot, 2);
+      int8_t* Sn = lds + slot * kSlot;
+      __builtin_amdgcn_s_setprio(1);
+      issue(kOdd ? 1 : 0, S);
+      read_b(S1, 1);
+      read_a(S1, 1);
+      quad(0, 0);
+      quad(0, 1);
+      spread<2 * MF, kL, RA + RB>();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kRing - 2) * kL) : "memory");
+      asm volatile("s_barrier" ::: "memory");
+      if constexpr (kOdd) advance();
+      issue(kOdd ? 0 : 1, S1);
+      read_a(Sn, 0);
+      quad(1, 0);
+      spread<MF, kL, RA>();
+      __builtin_amdgcn_sched_barrier(0);
+      read_b(Sn, 0);
+      quad(1, 1);
+      spread<MF, 0, RB>();
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kRing - 2) * kL) : "memory");
+      asm volatile("s_barrier" ::: "memory");
+      if constexpr (!kOdd) advance();
+    }
+
+    // ---- epilogue; no ring slot is touched, so the next tile's loads run on
+    uint32_t tm, tn;
+    tile_of(tile, a.map, tm, tn);
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+    int lane_e = lane;   // new in every tile: addresses formed from it ahead of the loop would be spilled
+    asm volatile("" : "+v"(lane_e));
+    const int g = lane_e >> 4;
+    const float* const as = as_lds + (seq & 3) * BM;
+#pragma unroll
+    for (int gr = 0; gr < HN / 32; ++gr) {
+      const int in_tile = wn * 2 * HN + gr * 64 + g * 16;
+      const int64_t col = n0 + in_tile;
+      float ws[16], b[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        ws[e] = bs_lds[(seq & 3) * BN + in_tile + e];
+        b[e] = 0.0f;
+      }
+      if (a.bias != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) b[e] = col + e < N ? OUT::load1(a.bias, col + e) : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int row = wm * 2 * HM + i * 16 + (lane_e & 15);
+        const float sc = as[row];
+        float f[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e)   // column 4 j + r of the 16: j = e / 4, half j / 2, tile j % 2 of the half
+          f[e] = __builtin_fmaf(float(acc[i][(e / 8) * TNH + gr * 2 + (e / 4) % 2][e % 4]), sc * ws[e], b[e]);
+        if (m0 + row < M) store16<OUT>(a, m0 + row, col, f);
       }
     }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives the block
 }
 
-template <class OUT, bool TR>
-hipError_t launch(const Args& a, hipStream_t s) {
-  const int64_t blocks = ((a.M + 63) / 64) * ((a.N + 63) / 64);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((product_any<OUT, TR>), dim3(unsigned(blocks)), dim3(256), 0, s, a);
+template <class C, class OUT>
+hipError_t launch_tile(Args a, int dev, int cus, hipStream_t s) {
+  if (!map_tiles(a, C::BM, C::BN)) return hipErrorInvalidValue;
+  const hipError_t e = allow_lds<product_tile<C, OUT>>(dev, C::kLdsBytes);
+  if (e != hipSuccess) return e;
+  const uint32_t slots = uint32_t(cus) * C::kBlocksPerCu;
+  hipLaunchKernelGGL((product_tile<C, OUT>), dim3(a.map.tiles < slots ? a.map.tiles : slots), dim3(C::kThreads),
+                     C::kLdsBytes, s, a);
   return hipGetLastError();
 }
 
-int64_t pitch_of(int64_t n) { return (n + 127) / 128 * 128; }
+using BigTile = Tile<256, 256, 2, 4, 2>;      // one block of 8 waves per CU
+using MidTile = Tile<128, 256, 1, 4, 2, 3>;   // two blocks of 4 waves
+using SmallTile = Tile<128, 128, 2, 2, 2>;    // two blocks of 4 waves
+using LowTile = Tile<64, 128, 2, 2, 3>;       // three blocks of 4 waves
+
+// Few rows: a block of 4 waves takes MT x 16 rows of x and NB x 16 of W; its waves take the K
+// steps in turn, each through an LDS ring of its own, and the partial sums meet in LDS.
+constexpr int kRowsWaves = 4;
+template <int MT, int NB, int D>
+constexpr int kRowsLds = kRowsWaves * D * (NB + MT) * 16 * kBK;
+
+template <int MT, int NB, int D, bool NT, class OUT>
+__global__ __launch_bounds__(kRowsWaves * kWave) void product_rows(Args a) {
+  constexpr int kWaves = kRowsWaves, kRows = MT * 16, kOut = NB * 16;
+  constexpr int kTiles = MT * NB, kSumWaves = kTiles < kWaves ? kTiles : kWaves;
+  static_assert(kTiles % kSumWaves == 0 && kRowsLds<MT, NB, D> <= 160 * 1024, "result tiles per wave; LDS");
+  static_assert(kRowsLds<MT, NB, D> >= kWaves * kTiles * 1024, "room for the partial sums");
+  const int64_t M = a.M, N = a.N;
+  const uint32_t K = uint32_t(a.K);
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = wave_in_block();
+  // Row blocks of one column block run on one XCD, next to each other.
+  const uint32_t b = blockIdx.x;
+  const uint32_t id = (b < a.map.per_xcd * kXcds) ? (b % kXcds) * a.map.per_xcd + b / kXcds : b;
+  const int64_t m0 = int64_t(id % a.map.tiles_m) * kRows, n0 = int64_t(id / a.map.tiles_m) * kOut;
+  const int64_t rows_a = (M - m0 < kRows) ? M - m0 : kRows, rows_b = (N - n0 < kOut) ? N - n0 : kOut;
+  const auto ra = make_rsrc(a.a + m0 * K, rows_a * K), rb = make_rsrc(a.b + n0 * K, rows_b * K);
+  const int g = lane >> 4;
+  // This wave's ring: D steps of kOut rows of W and kRows of x. No other wave touches it: no
+  // barrier in the K loop.
+  constexpr int kStep = (kOut + kRows) * kBK, kLoads = 2 * (NB + MT);
+  extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+  int8_t* const ring = lds + wave * D * kStep;
+  const int r_in = lane / 8;   // rows 8 q + r_in of the load q: even and odd q differ in their swizzle
+  const uint32_t kc[2] = {uint32_t((lane % 8) ^ (r_in >> 1)) * 16, uint32_t((lane % 8) ^ (4 + (r_in >> 1))) * 16};
+  const uint32_t off[2] = {r_in * K + kc[0], (8 + r_in) * K + kc[1]}, tile_off = 16 * K;
+  auto load = [&](int step, int d) {
+    int8_t* S = ring + d * kStep;
+    const uint32_t k0 = uint32_t(step) * kBK;
+#pragma unroll
+    for (int q = 0; q < 2 * NB; ++q)
+      load_lds16<NT ? 2 : 0>(rb, S + q * 1024, k0 + kc[q % 2] < K ? off[q % 2] + k0 + (q / 2) * tile_off : kOutOfRange);
+#pragma unroll
+    for (int q = 0; q < 2 * MT; ++q)
+      load_lds16(ra, S + kOut * kBK + q * 1024, k0 + kc[q % 2] < K ? off[q % 2] + k0 + (q / 2) * tile_off : kOutOfRange);
+  };
+  i32x4 acc[MT][NB];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  const int steps = int((K + kBK - 1) / kBK);
+#pragma unroll
+  for (int d = 0; d < D; ++d) load(wave + d * kWaves, d);   // steps past the end read zeros
+  const int frag = (lane & 15) * kBK, sw = (lane & 15) >> 1;
+  const int u[2] = {(g ^ sw) * 16, ((4 + g) ^ sw) * 16};
+  int d = 0;
+  for (int st = wave; st < steps; st += kWaves) {
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"((D - 1) * kLoads) : "memory");
+    const int8_t* S = ring + d * kStep + frag;
+    i32x4 fw[NB][2], fx[MT][2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) fw[j][kk] = *reinterpret_cast<const i32x4*>(S + j * 16 * kBK + u[kk]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fx[i][kk] = *reinterpret_cast<const i32x4*>(S + (NB + i) * 16 * kBK + u[kk]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is loaded over
+    load(st + D * kWaves, d);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[j][kk], fx[i][kk], acc[i][j], 0, 0, 0);
+    d = d + 1 == D ? 0 : d + 1;
+  }
+  // The rings' place holds the sums from here on: no load may still land there (a barrier
+  // alone does not promise that), and every ring must have been read.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  auto part = reinterpret_cast<i32x4 (*)[MT][NB][kWave]>(lds);
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) part[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kTiles / kSumWaves; ++q) {
+    const int tile = wave + q * kSumWaves, i = tile / NB, j = tile % NB;
+    if (tile >= kTiles) return;
+    i32x4 v = part[0][i][j][lane];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v += part[w][i][j][lane];
+    const int64_t row = m0 + i * 16 + (lane & 15), col = n0 + j * 16 + g * 4;
+    if (row >= M) continue;
+    const float sc = a.a_scale[row];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < N)
+        OUT::store1(a.y, row * N + col + e,
+                    __builtin_fmaf(float(v[e]), sc * a.b_scale[col + e], a.bias != nullptr ? OUT::load1(a.bias, col + e) : 0.0f));
+  }
+}
+
+template <int MT, int NB, int D, bool NT, class OUT>
+hipError_t launch_rows(Args a, int dev, hipStream_t s) {
+  if (!map_tiles(a, MT * 16, NB * 16)) return hipErrorInvalidValue;
+  const hipError_t e = allow_lds<product_rows<MT, NB, D, NT, OUT>>(dev, kRowsLds<MT, NB, D>);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((product_rows<MT, NB, D, NT, OUT>), dim3(a.map.tiles), dim3(kRowsWaves * kWave), (kRowsLds<MT, NB, D>),
+                     s, a);
+  return hipGetLastError();
+}
+
+// One or two rows: a wave takes one row of W, 1 KiB at a time (16 bytes to a lane), against the
+// same pieces of all MT rows of x, and adds up its lanes' sums at the end.
+constexpr int kFewWaves = 4;
+template <int MT, class OUT>
+__global__ __launch_bounds__(kFewWaves * kWave) void product_few(Args a) {
+  constexpr int kDeep = 4;   // pieces of a row in flight
+  const uint32_t K = uint32_t(a.K);
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t n = int64_t(blockIdx.x) * kFewWaves + wave_in_block();
+  if (n >= a.N) return;
+  const auto rb = make_rsrc(a.b + n * K, K), ra = make_rsrc(a.a, a.M * K);
+  int sum[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) sum[i] = 0;
+  for (uint32_t k0 = 0; k0 < K; k0 += kDeep * 1024) {
+    u32x4 w[kDeep], x[kDeep][MT];
+#pragma unroll
+    for (int p = 0; p < kDeep; ++p) {
+      const uint32_t k = k0 + p * 1024 + lane * 16;
+      w[p] = __builtin_amdgcn_raw_buffer_load_b128(rb, k < K ? k : kOutOfRange, 0, 2);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        x[p][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, k < K ? i * K + k : kOutOfRange, 0, 0);
+    }
+#pragma unroll
+    for (int p = 0; p < kDeep; ++p)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[i] = __builtin_amdgcn_sdot4(int(w[p][e]), int(x[p][i][e]), sum[i], false);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) sum[i] += __shfl_xor(sum[i], off, kWave);
+    if (lane == i && i < a.M)
+      OUT::store1(a.y, i * a.N + n,
+                  __builtin_fmaf(float(sum[i]), a.a_scale[i] * a.b_scale[n], a.bias != nullptr ? OUT::load1(a.bias, n) : 0.0f));
+  }
+}
+
+template <int MT, class OUT>
+hipError_t launch_few(const Args& a, hipStream_t s) {
+  hipLaunchKernelGGL((product_few<MT, OUT>), dim3(unsigned((a.N + kFewWaves - 1) / kFewWaves)), dim3(kFewWaves * kWave), 0,
+                     s, a);
+  return hipGetLastError();
+}
+
+enum Form { kFew, kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
+
+Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
+  if (const char* f = getenv("Q8FORM")) return Form(atoi(f));
+  if (M <= 2) return kFew;
+  if (M <= 32) return kRows16;
+  if (M <= 64) return kRows32;
+  if (M <= 160) return kRows64;
+  auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  if (tiles(256, 256) >= 2 * cus) return kBig;
+  if (tiles(128, 256) >= cus) return kMid;
+  if (tiles(128, 128) >= cus) return kSmall;
+  return kLow;
+}
+
+template <class OUT>
+hipError_t launch_fwd(const Args& a, hipStream_t s) {
+  const bool aligned = a.K > 0 && a.K % 16 == 0 && reinterpret_cast<uintptr_t>(a.a) % 16 == 0 &&
+                       reinterpret_cast<uintptr_t>(a.b) % 16 == 0;
+  if (!aligned) return launch_any<OUT, false>(a, s);
+  int dev = 0, cus = 0;
+  const hipError_t e = current_device(dev, cus);
+  if (e != hipSuccess) return e;
+  // Weights by non-temporal loads when one row block reads them and they are large (see product_rows).
+  const bool nt = a.N * a.K > (int64_t(32) << 20);
+  switch (choose_form(a.M, a.N, a.K, cus)) {
+    case kFew: return a.M == 1 ? launch_few<1, OUT>(a, s) : launch_few<2, OUT>(a, s);
+    case kRows16:
+      return nt && a.M <= 16 ? launch_rows<1, 2, 2, true, OUT>(a, dev, s) : launch_rows<1, 2, 2, false, OUT>(a, dev, s);
+    case kRows32: return launch_rows<2, 2, 2, false, OUT>(a, dev, s);
+    case kRows64: return launch_rows<4, 2, 2, false, OUT>(a, dev, s);
+    case kLow: return launch_tile<LowTile, OUT>(a, dev, cus, s);
+    case kSmall: return launch_tile<SmallTile, OUT>(a, dev, cus, s);
+    case kMid: return launch_tile<MidTile, OUT>(a, dev, cus, s);
+    default: return launch_tile<BigTile, OUT>(a, dev, cus, s);
+  }
+}
 
 }  // namespace lq8
 
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
                                 const int8_t* w, const float* w_scale, const void* bias, void* y, hipStream_t s) {
-  const lq8::Args a{q, w, scale, w_scale, bias, y, M, N, K, K};
-  return bf16 ? lq8::launch<BF16, false>(a, s) : lq8::launch<F32, false>(a, s);
-}
-
-size_t linear_q8_bwd_workspace(int64_t M, int64_t N) {
-  return size_t(M) * size_t(lq8::pitch_of(N)) + size_t(M) * 4;
-}
-
-hipError_t launch_linear_q8_bwd(bool bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
-                                const float* w_scale, void* dx, void* workspace, hipStream_t s) {
-  const int64_t pitch = lq8::pitch_of(N);
-  int8_t* const p = static_cast<int8_t*>(workspace);
-  float* const p_scale = reinterpret_cast<float*>(p + M * pitch);
-  if (N > 0) {
-    const hipError_t e = launch_q8_rows(bf16, M, N, pitch, dy, w_scale, p, p_scale, s);
-    if (e != hipSuccess) return e;
-  }
-  const lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, dx, M, K, N, pitch};
-  return bf16 ? lq8::launch<BF16, true>(a, s) : lq8::launch<F32, true>(a, s);
+  const bool vec = reinterpret_cast<uintptr_t>(y) % 16 == 0 && N * (bf16 ? 2 : 4) % 16 == 0;
+  const lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, vec, {}};
+  return bf16 ? lq8::launch_fwd<BF16>(a, s) : lq8::launch_fwd<F32>(a, s);
 }
 
 }  // namespace lmbp

@@ -491,22 +491,24 @@ lmbp_status msrms_q8_fwd_impl(lmbp_dtype dt, int64_t rows, int64_t cols, float e
                                             static_cast<hipStream_t>(stream)));
 }
 
-lmbp_status msrms_q8_bwd_impl(lmbp_dtype dt, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
-                              const float* scale, const float* rstd, const void* ds, void* dx, void* stream) {
-  if (!known_dtype(dt)) return LMBP_EDTYPE;
+lmbp_status msrms_q8_bwd_impl(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t cols, const void* dz,
+                              const int8_t* q, const float* scale, const float* rstd, const void* ds, void* dx,
+                              void* stream) {
+  if (!known_dtype(dt_dz) || !known_dtype(dt) || (dt_dz == LMBP_BF16 && dt == LMBP_FP32)) return LMBP_EDTYPE;
   if (bad_matrix(rows, cols)) return LMBP_EINVAL;
   if (rows == 0) return LMBP_OK;
   if (cols == 0 || !dz || !q || !scale || !rstd || !dx) return LMBP_EINVAL;
   const int eb = elem_bytes(dt);
-  if (!aligned(dz, eb) || !aligned(dx, eb) || (ds && !aligned(ds, eb)) || !aligned(scale, 4) || !aligned(rstd, 4))
+  if (!aligned(dz, elem_bytes(dt_dz)) || !aligned(dx, eb) || (ds && !aligned(ds, eb)) || !aligned(scale, 4) ||
+      !aligned(rstd, 4))
     return LMBP_EINVAL;
   const uint64_t count = uint64_t(rows) * uint64_t(cols);
   const Span sd = span(dx, count * eb);
-  if (bad_pair(sd, span(dz, count * eb), true) || bad_pair(sd, span(ds, ds ? count * eb : 0), true) ||
+  if (bad_pair(sd, span(dz, count * elem_bytes(dt_dz)), dt == dt_dz) || bad_pair(sd, span(ds, ds ? count * eb : 0), true) ||
       overlaps(sd, span(q, count)) || overlaps(sd, span(scale, uint64_t(rows) * 4)) ||
       overlaps(sd, span(rstd, uint64_t(rows) * 4)))
     return LMBP_EOVERLAP;
-  return from_hip(lmbp::launch_msrms_q8_bwd(dt == LMBP_BF16, rows, cols, dz, q, scale, rstd, ds, dx,
+  return from_hip(lmbp::launch_msrms_q8_bwd(dt_dz == LMBP_BF16, dt == LMBP_BF16, rows, cols, dz, q, scale, rstd, ds, dx,
                                             static_cast<hipStream_t>(stream)));
 }
 
@@ -533,26 +535,28 @@ lmbp_status linear_q8_fwd_impl(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, c
                                              static_cast<hipStream_t>(stream)));
 }
 
-lmbp_status linear_q8_bwd_impl(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const void* dy, const int8_t* w,
-                               const float* w_scale, void* dx, void* workspace, int64_t workspace_bytes,
-                               void* stream) {
-  if (!known_dtype(dt)) return LMBP_EDTYPE;
+lmbp_status linear_q8_bwd_impl(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n, int64_t k, const void* dy,
+                               const int8_t* w, const float* w_scale, const void* add, void* dx, void* workspace,
+                               int64_t workspace_bytes, void* stream) {
+  if (!known_dtype(dt) || !known_dtype(dt_dx)) return LMBP_EDTYPE;
   if (bad_layer(m, n, k) || n > lmbp::kQ8MaxDepth || bad_matrix(m, k)) return LMBP_EINVAL;
   if (m == 0 || k == 0) return LMBP_OK;
   if (!dx || (n > 0 && (!dy || !w || !w_scale))) return LMBP_EINVAL;
-  const int eb = elem_bytes(dt);
-  if (!aligned(dx, eb) || (n > 0 && (!aligned(dy, eb) || !aligned(w_scale, 4)))) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt), eb_dx = elem_bytes(dt_dx);
+  if (!aligned(dx, eb_dx) || (add && !aligned(add, eb_dx)) || (n > 0 && (!aligned(dy, eb) || !aligned(w_scale, 4)))) return LMBP_EINVAL;
   const uint64_t need = lmbp_linear_q8_bwd_bytes(m, n, k);
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || uint64_t(workspace_bytes) < need)
     return LMBP_EINVAL;
-  const Span sd = span(dx, uint64_t(m) * uint64_t(k) * eb), sp = span(workspace, need);
+  const uint64_t mk = uint64_t(m) * uint64_t(k) * eb_dx;
+  const Span sd = span(dx, mk), sp = span(workspace, need), sa = span(add, add ? mk : 0);
+  if (bad_pair(sd, sa, true) || overlaps(sp, sa)) return LMBP_EOVERLAP;
   const Span ins[3] = {span(dy, n > 0 ? uint64_t(m) * uint64_t(n) * eb : 0),
                        span(w, n > 0 ? uint64_t(n) * uint64_t(k) : 0), span(w_scale, uint64_t(n) * 4)};
   if (overlaps(sd, sp)) return LMBP_EOVERLAP;
   for (const Span& in : ins)
     if (overlaps(sd, in) || overlaps(sp, in)) return LMBP_EOVERLAP;
-  return from_hip(lmbp::launch_linear_q8_bwd(dt == LMBP_BF16, m, n, k, dy, w, w_scale, dx, workspace,
-                                             static_cast<hipStream_t>(stream)));
+  return from_hip(lmbp::launch_linear_q8_bwd(dt == LMBP_BF16, dt_dx == LMBP_BF16, m, n, k, dy, w, w_scale, add, dx,
+                                             workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
@@ -695,9 +699,9 @@ lmbp_status msrms_q8_fwd(lmbp_dtype dt, int64_t rows, int64_t cols, float eps, c
                          int8_t* q, float* scale, float* rstd, void* stream) {
   return msrms_q8_fwd_impl(dt, rows, cols, eps, x, res, s, q, scale, rstd, stream);
 }
-lmbp_status msrms_q8_bwd(lmbp_dtype dt, int64_t rows, int64_t cols, const void* dz, const int8_t* q, const float* scale,
-                         const float* rstd, const void* ds, void* dx, void* stream) {
-  return msrms_q8_bwd_impl(dt, rows, cols, dz, q, scale, rstd, ds, dx, stream);
+lmbp_status msrms_q8_bwd(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
+                         const float* scale, const float* rstd, const void* ds, void* dx, void* stream) {
+  return msrms_q8_bwd_impl(dt_dz, dt, rows, cols, dz, q, scale, rstd, ds, dx, stream);
 }
 lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t* q, const float* scale,
                           const int8_t* w, const float* w_scale, const void* bias, void* y, void* stream) {
@@ -707,9 +711,10 @@ size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k) {
   if (m <= 0 || k <= 0 || bad_layer(m, n, k) || n > lmbp::kQ8MaxDepth) return 0;
   return lmbp::linear_q8_bwd_workspace(m, n);
 }
-lmbp_status linear_q8_bwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const void* dy, const int8_t* w,
-                          const float* w_scale, void* dx, void* workspace, int64_t workspace_bytes, void* stream) {
-  return linear_q8_bwd_impl(dt, m, n, k, dy, w, w_scale, dx, workspace, workspace_bytes, stream);
+lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n, int64_t k, const void* dy,
+                          const int8_t* w, const float* w_scale, const void* add, void* dx, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+  return linear_q8_bwd_impl(dt, dt_dx, m, n, k, dy, w, w_scale, add, dx, workspace, workspace_bytes, stream);
 }
 
 lmbp_status lmbp_copy(const void* src, void* dst, int64_t bytes, void* stream) {

@@ -117,18 +117,19 @@ hipError_t launch_q8_values(bool bf16, int64_t rows, int64_t cols, const int8_t*
 // MS-RMSNorm of x, or of sum = x + res (res and sum both null or both given), in 8 bits.
 hipError_t launch_msrms_q8_fwd(bool bf16, int64_t rows, int64_t cols, float eps, const void* x, const void* res,
                                void* sum, int8_t* q, float* scale, float* rstd, hipStream_t s);
-hipError_t launch_msrms_q8_bwd(bool bf16, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
+// dz_bf16: the type of dz; bf16 that of ds and dx (not fp32 with a bf16 dz).
+hipError_t launch_msrms_q8_bwd(bool dz_bf16, bool bf16, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
                                const float* scale, const float* rstd, const void* ds, void* dx, hipStream_t s);
 
-// Linear layers of 8-bit rows and weights; bf16: the type of y, bias, dy and dx. No more than
-// kQ8MaxDepth products to a sum: 128 * 128 * kQ8MaxDepth < 2^31. Workspace of
+// Linear layers of 8-bit rows and weights; bf16: the type of y and bias, or of dy; dx_bf16 that of
+// add (may be null, or dx) and dx. No more than kQ8MaxDepth products to a sum: 128 * 128 * kQ8MaxDepth < 2^31. Workspace of
 // linear_q8_bwd_workspace bytes, 16-byte aligned.
 constexpr int64_t kQ8MaxDepth = 131071;
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
                                 const int8_t* w, const float* w_scale, const void* bias, void* y, hipStream_t s);
 size_t linear_q8_bwd_workspace(int64_t M, int64_t N);
-hipError_t launch_linear_q8_bwd(bool bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
-                                const float* w_scale, void* dx, void* workspace, hipStream_t s);
+hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
+                                const float* w_scale, const void* add, void* dx, void* workspace, hipStream_t s);
 
 hipError_t launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);
 

@@ -11,6 +11,8 @@
 #include "lmbp_launch.hpp"
 #include "q8_device.hpp"
 
+#include <type_traits>
+
 namespace lmbp {
 namespace q8 {
 
@@ -27,6 +29,317 @@ struct FwdArgs {
   int64_t rows, cols, pitch;   // pitch: bytes from one row of q to the next, zeros behind the row
   float eps;
 };
+
+// Threads per block of the register kernels: 256, or one row of WPR waves where that is wider.
+template <int WPR>
+constexpr int block_of() { return WPR * kWave > 256 ? WPR * kWave : 256; }
+
+// P consecutive elements of a row in storage form; RAGGED: at any element's address.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <class IO, int P, bool RAGGED>
+struct Piece {
+  static constexpr int kVecs = P * IO::kBytes / 16, E = IO::kPerVec;
+  u32x4 v[kVecs];
+  __device__ inline void clear() {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) v[k] = u32x4{0u, 0u, 0u, 0u};
+  }
+  __device__ inline void load(const void* base, int64_t elem) {
+    const char* p = static_cast<const char*>(base) + elem * IO::kBytes;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      if constexpr (RAGGED) v[k] = reinterpret_cast<const u32x4_any*>(p)[k];
+      else v[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + k);
+    }
+  }
+  __device__ inline void store(void* base, int64_t elem) const {
+    char* p = static_cast<char*>(base) + elem * IO::kBytes;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      if constexpr (RAGGED) reinterpret_cast<u32x4_any*>(p)[k] = v[k];
+      else __builtin_nontemporal_store(v[k], reinterpret_cast<u32x4*>(p) + k);
+    }
+  }
+  __device__ inline void get(float (&f)[P]) const {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float e[E];
+      IO::unpack(v[k], e);
+#pragma unroll
+      for (int i = 0; i < E; ++i) f[k * E + i] = e[i];
+    }
+  }
+  __device__ inline void set(const float (&f)[P]) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float e[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[i] = f[k * E + i];
+      v[k] = IO::pack(e);
+    }
+  }
+};
+
+// P bytes of q (4 or 8).
+template <int P, bool RAGGED>
+struct Bytes {
+  typedef uint32_t any __attribute__((ext_vector_type(P / 4), aligned(RAGGED ? 1 : P)));
+  uint32_t v[P / 4];
+  __device__ inline void load(const int8_t* p) {
+    const any b = *reinterpret_cast<const any*>(p);
+#pragma unroll
+    for (int k = 0; k < P / 4; ++k) v[k] = b[k];
+  }
+  __device__ inline void store(int8_t* p) const {
+    any b;
+#pragma unroll
+    for (int k = 0; k < P / 4; ++k) b[k] = v[k];
+    if constexpr (!RAGGED) __builtin_nontemporal_store(b, reinterpret_cast<any*>(p));
+    else *reinterpret_cast<any*>(p) = b;
+  }
+  __device__ inline void get(float (&f)[P]) const {
+#pragma unroll
+    for (int k = 0; k < P; ++k) f[k] = float(int8_t(v[k / 4] >> (8 * (k % 4))));
+  }
+  __device__ inline void set(const float (&t)[P], float r) {   // q8_device.hpp
+#pragma unroll
+    for (int k = 0; k < P / 4; ++k) {
+      const uint32_t lo = __builtin_amdgcn_perm(to_q8(t[4 * k + 1], r), to_q8(t[4 * k], r), 0x0c0c0400u);
+      const uint32_t hi = __builtin_amdgcn_perm(to_q8(t[4 * k + 3], r), to_q8(t[4 * k + 2], r), 0x04000c0cu);
+      v[k] = lo | hi;
+    }
+  }
+};
+
+// Rows in registers: WPR waves to a row, thread t of the row holding pieces t, t + 64 WPR, ...
+// (VPL of them); RAGGED rows have fewer than a piece's elements left, one to a thread.
+template <class IO, int MODE, int VPL, int WPR, bool RAGGED>
+__global__ __launch_bounds__(block_of<WPR>()) void fwd_rows(FwdArgs a) {
+  constexpr int P = IO::kPerVec, TPR = kWave * WPR, RPB = block_of<WPR>() / TPR;
+  constexpr bool kIsNorm = MODE == kNorm || MODE == kNormRes;
+  __shared__ uint32_t most_lds[block_of<WPR>() / kWave];
+  __shared__ float sum_lds[block_of<WPR>() / kWave];
+  const int t = threadIdx.x % TPR;
+  const int64_t row = int64_t(blockIdx.x) * RPB + wave_in_block() / WPR;
+  const bool active = row < a.rows;
+  if constexpr (WPR == 1) {
+    if (!active) return;   // no barriers in the single-wave form
+  }
+  const int cols = int(a.cols), pieces = cols / P;
+  const int64_t base = row * a.cols;
+  Piece<IO, P, RAGGED> x[VPL], y[MODE == kNormRes ? VPL : 1];
+  float c[MODE == kColumns ? VPL : 1][P];
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int idx = j * TPR + t;
+    x[j].clear();
+    if constexpr (MODE == kNormRes) y[j].clear();
+    if (active && idx < pieces) {
+      x[j].load(a.x, base + idx * P);
+      if constexpr (MODE == kNormRes) y[j].load(a.res, base + idx * P);
+    }
+    if constexpr (MODE == kColumns) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) c[j][e] = idx < pieces ? a.columns[idx * P + e] : 0.0f;
+    }
+  }
+  const bool rest = RAGGED && active && pieces * P + t < cols;
+  float last = 0.0f;
+  if (rest) {
+    const int64_t at = base + pieces * P + t;
+    last = IO::load1(a.x, at);
+    if constexpr (MODE == kNormRes) {
+      IO::store1(a.s, at, last + IO::load1(a.res, at));
+      last = IO::load1(a.s, at);
+    }
+    if constexpr (MODE == kColumns) last *= a.columns[pieces * P + t];
+  }
+  uint32_t most = magnitude(last);
+  float sum = last * last;
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    float f[P];
+    x[j].get(f);
+    if constexpr (MODE == kNormRes) {
+      float g[P];
+      y[j].get(g);
+#pragma unroll
+      for (int e = 0; e < P; ++e) f[e] += g[e];
+      x[j].set(f);
+      const int idx = j * TPR + t;
+      if (active && idx < pieces) x[j].store(a.s, base + idx * P);
+      x[j].get(f);   // as stored
+    }
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      if constexpr (MODE == kColumns) f[e] *= c[j][e];
+      most = umax(most, magnitude(f[e]));
+      if constexpr (kIsNorm) sum = __builtin_fmaf(f[e], f[e], sum);
+    }
+  }
+  most = wave_umax(most);
+  if constexpr (kIsNorm) sum = wave_sum(sum);
+  if constexpr (WPR > 1) {
+    const int wave = threadIdx.x / kWave, first = wave / WPR * WPR;
+    if ((threadIdx.x & (kWave - 1)) == 0) {
+      most_lds[wave] = most;
+      if constexpr (kIsNorm) sum_lds[wave] = sum;
+    }
+    __syncthreads();
+    most = 0;
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WPR; ++k) {
+      most = umax(most, most_lds[first + k]);
+      if constexpr (kIsNorm) sum += sum_lds[first + k];
+    }
+    if (!active) return;
+  }
+  const Q8Row w = q8_row(most);
+  int8_t* const q = a.q + row * a.pitch;
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int idx = j * TPR + t;
+    if (idx < pieces) {
+      float f[P];
+      x[j].get(f);
+      if constexpr (MODE == kColumns) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) f[e] *= c[j][e];
+      }
+      Bytes<P, RAGGED> b;
+      b.set(f, w.r);
+#pragma unroll
+      for (int k = 0; k < P / 4; ++k) b.v[k] = w.finite ? b.v[k] : 0u;
+      b.store(q + idx * P);
+    }
+  }
+  if (rest) q[pieces * P + t] = int8_t(w.finite ? to_q8(last, w.r) : 0u);
+  if constexpr (MODE == kColumns) {
+    for (int k = cols + t; k < a.pitch; k += TPR) q[k] = 0;
+  }
+  if (t == 0) {
+    if constexpr (kIsNorm) {
+      const float rs = rsqrtf(sum / float(cols) + a.eps);
+      a.rstd[row] = rs;
+      a.scale[row] = w.a * rs / 127.0f;
+    } else {
+      a.scale[row] = w.a / 127.0f;
+    }
+  }
+}
+
+template <class IO, int VPL, int WPR, bool RAGGED>
+__global__ __launch_bounds__(block_of<WPR>()) void values_rows(const int8_t* q, const float* __restrict__ scale, void* v,
+                                                               int64_t rows, int cols) {
+  constexpr int P = IO::kPerVec, TPR = kWave * WPR, RPB = block_of<WPR>() / TPR;
+  const int t = threadIdx.x % TPR;
+  const int64_t row = int64_t(blockIdx.x) * RPB + wave_in_block() / WPR;
+  if (row >= rows) return;
+  const int pieces = cols / P;
+  const int64_t base = row * cols;
+  const float sc = scale[row];
+  Bytes<P, RAGGED> b[VPL];
+#pragma unroll
+  for (int j = 0; j < VPL; ++j)
+    if (j * TPR + t < pieces) b[j].load(q + base + (j * TPR + t) * P);
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int idx = j * TPR + t;
+    if (idx < pieces) {
+      float f[P];
+      b[j].get(f);
+#pragma unroll
+      for (int e = 0; e < P; ++e) f[e] *= sc;
+      Piece<IO, P, RAGGED> o;
+      o.set(f);
+      o.store(v, base + idx * P);
+    }
+  }
+  const int at = pieces * P + t;
+  if (RAGGED && at < cols) IO::store1(v, base + at, float(q[base + at]) * sc);
+}
+
+struct BwdArgs {
+  const void* dz;
+  const int8_t* q;
+  const float* scale;
+  const float* rstd;
+  const void* ds;
+  void* dx;
+  int64_t rows, cols;
+};
+
+template <class DZ, class IO, int VPL, int WPR, bool RAGGED>
+__global__ __launch_bounds__(block_of<WPR>()) void norm_bwd_rows(BwdArgs a) {
+  constexpr int P = IO::kPerVec, TPR = kWave * WPR, RPB = block_of<WPR>() / TPR;
+  __shared__ float sum_lds[block_of<WPR>() / kWave];
+  const int t = threadIdx.x % TPR;
+  const int64_t row = int64_t(blockIdx.x) * RPB + wave_in_block() / WPR;
+  const bool active = row < a.rows;
+  if constexpr (WPR == 1) {
+    if (!active) return;
+  }
+  const int cols = int(a.cols), pieces = cols / P;
+  const int64_t base = row * a.cols;
+  Piece<DZ, P, RAGGED> dz[VPL];
+  Piece<IO, P, RAGGED> ds[VPL];
+  Bytes<P, RAGGED> q[VPL];
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int idx = j * TPR + t;
+    dz[j].clear();
+    ds[j].clear();
+#pragma unroll
+    for (int k = 0; k < P / 4; ++k) q[j].v[k] = 0u;
+    if (active && idx < pieces) {
+      dz[j].load(a.dz, base + idx * P);
+      q[j].load(a.q + base + idx * P);
+      if (a.ds != nullptr) ds[j].load(a.ds, base + idx * P);
+    }
+  }
+  const int at = pieces * P + t;
+  const bool rest = RAGGED && active && at < cols;
+  const float last_dz = rest ? DZ::load1(a.dz, base + at) : 0.0f, last_q = rest ? float(a.q[base + at]) : 0.0f;
+  const float last_ds = rest && a.ds != nullptr ? IO::load1(a.ds, base + at) : 0.0f;
+  const float sc = active ? a.scale[row] : 0.0f, rs = active ? a.rstd[row] : 0.0f;
+  float sum = last_dz * last_q;
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    float g[P], z[P];
+    dz[j].get(g);
+    q[j].get(z);
+#pragma unroll
+    for (int e = 0; e < P; ++e) sum = __builtin_fmaf(z[e], g[e], sum);
+  }
+  sum = wave_sum(sum);
+  if constexpr (WPR > 1) {
+    const int wave = threadIdx.x / kWave, first = wave / WPR * WPR;
+    if ((threadIdx.x & (kWave - 1)) == 0) sum_lds[wave] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WPR; ++k) sum += sum_lds[first + k];
+    if (!active) return;
+  }
+  const float b = sc * (sc * (sum / float(cols)));
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int idx = j * TPR + t;
+    if (idx < pieces) {
+      float g[P], z[P], d[P];
+      dz[j].get(g);
+      q[j].get(z);
+      ds[j].get(d);
+#pragma unroll
+      for (int e = 0; e < P; ++e) g[e] = __builtin_fmaf(rs, __builtin_fmaf(-z[e], b, g[e]), d[e]);
+      Piece<IO, P, RAGGED> o;
+      o.set(g);
+      o.store(a.dx, base + idx * P);
+    }
+  }
+  if (rest) IO::store1(a.dx, base + at, __builtin_fmaf(rs, __builtin_fmaf(-last_q, b, last_dz), last_ds));
+}
 
 // Maximum of v and sum of t over the block's 4 waves.
 __device__ inline void block_max_sum(uint32_t& v, float& t, uint32_t* most, float* sum) {
@@ -89,42 +402,113 @@ __global__ __launch_bounds__(256) void values_any(const int8_t* q, const float* 
   for (int64_t k = threadIdx.x; k < cols; k += 256) IO::store1(v, base + k, float(q[base + k]) * sc);
 }
 
-template <class IO>
+template <class DZ, class IO>
 __global__ __launch_bounds__(256) void norm_bwd_any(const void* dz, const int8_t* q, const float* __restrict__ scale,
                                                     const float* __restrict__ rstd, const void* ds, void* dx,
                                                     int64_t cols) {
   __shared__ float red[256 / kWave];
   const int64_t row = blockIdx.x, base = row * cols;
   float s = 0.0f;
-  for (int64_t k = threadIdx.x; k < cols; k += 256) s = __builtin_fmaf(float(q[base + k]), IO::load1(dz, base + k), s);
+  for (int64_t k = threadIdx.x; k < cols; k += 256) s = __builtin_fmaf(float(q[base + k]), DZ::load1(dz, base + k), s);
   const float sc = scale[row], rs = rstd[row];
   const float b = sc * (sc * (block_sum(s, red) / float(cols)));
   for (int64_t k = threadIdx.x; k < cols; k += 256) {
-    const float g = __builtin_fmaf(-float(q[base + k]), b, IO::load1(dz, base + k));
+    const float g = __builtin_fmaf(-float(q[base + k]), b, DZ::load1(dz, base + k));
     IO::store1(dx, base + k, ds != nullptr ? __builtin_fmaf(rs, g, IO::load1(ds, base + k)) : rs * g);
   }
 }
 
+// Launch shapes of the register kernels: the fewest waves to a row that hold it in kTarget
+// pieces per thread, or 16 waves with up to 8.
+constexpr int kVpl[] = {1, 2, 3, 4, 6, 8};
+constexpr int kWpr[] = {1, 2, 4, 8, 16};
+constexpr int kShapes = 30;
+constexpr int kTarget = 3;
+constexpr bool reachable(int vpl, int wpr) { return vpl <= kTarget || wpr == 16; }
+
+// Calls f(shape of VPL, shape of WPR) for the shape that holds `pieces`; false if none does.
+template <int I = 0, class F>
+bool with_shape(int64_t pieces, F f) {
+  if constexpr (I < kShapes) {
+    constexpr int wpr = kWpr[I / 6], vpl = kVpl[I % 6];
+    if constexpr (reachable(vpl, wpr)) {
+      if (pieces <= int64_t(kWave) * wpr * vpl) {
+        f(std::integral_constant<int, vpl>{}, std::integral_constant<int, wpr>{});
+        return true;
+      }
+    }
+    return with_shape<I + 1>(pieces, f);
+  } else {
+    return false;
+  }
+}
+
+// Blocks for `rows` of them at WPR waves each.
+template <int WPR>
+int64_t blocks_of(int64_t rows) {
+  constexpr int rpb = block_of<WPR>() / (kWave * WPR);
+  return (rows + rpb - 1) / rpb;
+}
+
+bool at16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
 template <class IO, int MODE>
 hipError_t launch_fwd(const FwdArgs& a, hipStream_t s) {
-  if (a.rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((fwd_any<IO, MODE>), dim3(unsigned(a.rows)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  const bool ragged = a.cols % IO::kPerVec != 0 || !at16(a.x) || (MODE == kNormRes && (!at16(a.res) || !at16(a.s))) ||
+                      reinterpret_cast<uintptr_t>(a.q) % IO::kPerVec != 0;
+  int64_t blocks = 0;
+  const bool held = a.cols < (1 << 24) && with_shape(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+    constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
+    blocks = blocks_of<W>(a.rows);
+    if (blocks > 0x7fffffff) return;
+    const auto kernel = ragged ? fwd_rows<IO, MODE, V, W, true> : fwd_rows<IO, MODE, V, W, false>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, a);
+  });
+  if (!held) {
+    blocks = a.rows;
+    if (blocks <= 0x7fffffff) hipLaunchKernelGGL((fwd_any<IO, MODE>), dim3(unsigned(blocks)), dim3(256), 0, s, a);
+  }
+  return blocks > 0x7fffffff ? hipErrorInvalidValue : hipGetLastError();
 }
 
 template <class IO>
 hipError_t launch_values(int64_t rows, int64_t cols, const int8_t* q, const float* scale, void* v, hipStream_t s) {
-  if (rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((values_any<IO>), dim3(unsigned(rows)), dim3(256), 0, s, q, scale, v, cols);
-  return hipGetLastError();
+  const bool ragged = cols % IO::kPerVec != 0 || !at16(v) || reinterpret_cast<uintptr_t>(q) % IO::kPerVec != 0;
+  int64_t blocks = 0;
+  const bool held = cols < (1 << 24) && with_shape(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+    constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
+    blocks = blocks_of<W>(rows);
+    if (blocks > 0x7fffffff) return;
+    const auto kernel = ragged ? values_rows<IO, V, W, true> : values_rows<IO, V, W, false>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, q, scale, v, rows, int(cols));
+  });
+  if (!held) {
+    blocks = rows;
+    if (blocks <= 0x7fffffff) hipLaunchKernelGGL((values_any<IO>), dim3(unsigned(blocks)), dim3(256), 0, s, q, scale, v, cols);
+  }
+  return blocks > 0x7fffffff ? hipErrorInvalidValue : hipGetLastError();
 }
 
-template <class IO>
+template <class DZ, class IO>
 hipError_t launch_norm_bwd(int64_t rows, int64_t cols, const void* dz, const int8_t* q, const float* scale,
                            const float* rstd, const void* ds, void* dx, hipStream_t s) {
-  if (rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((norm_bwd_any<IO>), dim3(unsigned(rows)), dim3(256), 0, s, dz, q, scale, rstd, ds, dx, cols);
-  return hipGetLastError();
+  const bool ragged = cols % IO::kPerVec != 0 || !at16(dz) || !at16(ds) || !at16(dx) ||
+                      reinterpret_cast<uintptr_t>(q) % IO::kPerVec != 0;
+  int64_t blocks = 0;
+  const BwdArgs a{dz, q, scale, rstd, ds, dx, rows, cols};
+  const bool held = cols < (1 << 24) && with_shape(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+    constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
+    blocks = blocks_of<W>(rows);
+    if (blocks > 0x7fffffff) return;
+    const auto kernel = ragged ? norm_bwd_rows<DZ, IO, V, W, true> : norm_bwd_rows<DZ, IO, V, W, false>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, a);
+  });
+  if (!held) {
+    blocks = rows;
+    if (blocks <= 0x7fffffff)
+      hipLaunchKernelGGL((norm_bwd_any<DZ, IO>), dim3(unsigned(blocks)), dim3(256), 0, s, dz, q, scale, rstd, ds, dx, cols);
+  }
+  return blocks > 0x7fffffff ? hipErrorInvalidValue : hipGetLastError();
 }
 
 }  // namespace q8
@@ -150,10 +534,11 @@ hipError_t launch_msrms_q8_fwd(bool bf16, int64_t rows, int64_t cols, float eps,
   return bf16 ? q8::launch_fwd<BF16, q8::kNorm>(a, s) : q8::launch_fwd<F32, q8::kNorm>(a, s);
 }
 
-hipError_t launch_msrms_q8_bwd(bool bf16, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
+hipError_t launch_msrms_q8_bwd(bool dz_bf16, bool bf16, int64_t rows, int64_t cols, const void* dz, const int8_t* q,
                                const float* scale, const float* rstd, const void* ds, void* dx, hipStream_t s) {
-  return bf16 ? q8::launch_norm_bwd<BF16>(rows, cols, dz, q, scale, rstd, ds, dx, s)
-              : q8::launch_norm_bwd<F32>(rows, cols, dz, q, scale, rstd, ds, dx, s);
+  if (!bf16) return q8::launch_norm_bwd<F32, F32>(rows, cols, dz, q, scale, rstd, ds, dx, s);
+  return dz_bf16 ? q8::launch_norm_bwd<BF16, BF16>(rows, cols, dz, q, scale, rstd, ds, dx, s)
+                 : q8::launch_norm_bwd<F32, BF16>(rows, cols, dz, q, scale, rstd, ds, dx, s);
 }
 
 }  // namespace lmbp

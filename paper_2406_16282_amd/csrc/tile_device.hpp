@@ -37,6 +37,25 @@ __device__ inline void load_lds4(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t o
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)dst, 4, offset, 0, 0, 0);
 }
 
+// A buffer resource as its four words.
+__device__ inline u32x4 rsrc_words(uint64_t base, uint32_t bytes) {
+  return u32x4{uint32_t(base), uint32_t(base >> 32) & 0xffffu, bytes, kBufferGDword3};
+}
+// The same load as load_lds16, written as asm, for kernels that read LDS with transposing reads:
+// of the builtin the compiler knows that it writes LDS, and it waits for all of them before
+// every such read. `dst`: LDS address (lds_addr). The waits are the kernel's own. The wait states
+// cover a resource whose registers a VALU operation has just written (5, with the move).
+// The compiler reserves m0 for itself and warns that it cannot keep a value there across
+// the asm; the clobber is to say just that, so that it never counts on one.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ inline void load_lds16_asm(const u32x4& r, uint32_t dst, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(dst), "v"(offset), "s"(r) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ inline uint32_t lds_addr(const void* p) { return uint32_t(uintptr_t((const lds_void*)p)); }
+
 // Scheduling groups for MF MFMAs, with VM buffer loads and then DS LDS reads spread over
 // the first half of them (so the reads have landed before the next wait).
 template <int MF, int VM, int DS, int I = 0>
@@ -55,9 +74,9 @@ __device__ inline void spread() {
 }
 
 // Tile coordinates of the t-th tile: XCD by XCD (consecutive blocks go to the 8 XCDs in turn),
-// in groups of kGroupM row tiles. tiles_n is divided by with a
-// host-made reciprocal (floor(2^32 / tiles_n), at most one short of the quotient for
-// t < 2^30) instead of an integer division.
+// in groups of kGroupM row tiles. tiles_n is divided by with a host-made reciprocal
+// (floor(2^32 / tiles_n), at most one short of the quotient for t < 2^30) instead of an integer
+// division.
 __device__ inline void tile_of(uint32_t t, const TileMap& m, uint32_t& tm, uint32_t& tn) {
   const uint32_t id = (t < m.per_xcd * kXcds) ? (t % kXcds) * m.per_xcd + t / kXcds : t;
   const uint32_t id8 = id / kGroupM;

@@ -330,6 +330,7 @@ class _NormLinearQ8(torch.autograd.Function):
         out = binding.msrms_q8_fwd(_flat(x), eps, None if res is None else _flat(res))
         q, q_scale, rstd = out[:3]
         ctx.set_materialize_grads(False)
+        ctx.dtype = x.dtype
         ctx.bias_dtypes = [b.dtype if b is not None else None for b in layers[2::3]]
         ctx.save_for_backward(q, q_scale, rstd, *(t for i, t in enumerate(layers) if i % 3 != 2))
         ys = [_product_q8(q, q_scale, w, sc, b, x.dtype) for w, sc, b in zip(*(layers[i::3] for i in range(3)))]
@@ -345,14 +346,14 @@ class _NormLinearQ8(torch.autograd.Function):
         dx = None
         if need_x or need_res:
             dz = None
+            # The layers' gradients add up in fp32, and the norm's backward takes the sum as it is.
             for dy, w, sc in zip(grads, weights[::2], weights[1::2]):
                 if dy is not None:
-                    part = binding.linear_q8_bwd(_flat(dy), w, sc)
-                    dz = part if dz is None else dz.add_(part)
+                    dz = binding.linear_q8_bwd(_flat(dy), w, sc, add=dz, dx=dz, dtype=torch.float32)
             if dz is None:
                 dx = ds
             else:
-                dx = binding.msrms_q8_bwd(dz, q, q_scale, rstd, None if ds is None else _flat(ds), dx=dz)
+                dx = binding.msrms_q8_bwd(dz, q, q_scale, rstd, None if ds is None else _flat(ds), dtype=ctx.dtype)
         db = [_bias_grad(grads[i], t) if ctx.needs_input_grad[5 + 3 * i] and grads[i] is not None else None
               for i, t in enumerate(ctx.bias_dtypes)]
         return (dx if need_x else None, dx if need_res else None, None,

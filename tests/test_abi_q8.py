@@ -58,13 +58,16 @@ def test_msrms_q8_fwd(L):
 
 
 def test_msrms_q8_bwd(L):
-    def f(dt=B.BF16, rows=4, cols=32, dz=at(0), q=at(1), scale=at(2), rstd=at(3), ds=at(4), dx=at(5)):
-        return L.msrms_q8_bwd(dt, rows, cols, dz, q, scale, rstd, ds, dx, None)
+    def f(dt=B.BF16, rows=4, cols=32, dz=at(0), q=at(1), scale=at(2), rstd=at(3), ds=at(4), dx=at(5), dt_dz=None):
+        return L.msrms_q8_bwd(dt if dt_dz is None else dt_dz, dt, rows, cols, dz, q, scale, rstd, ds, dx, None)
     assert f(dt=5) == B.EDTYPE
     assert f(rows=-1) == f(cols=-1) == f(cols=0) == B.EINVAL
     assert f(rows=0, dz=None, q=None, scale=None, rstd=None, ds=None, dx=None) == B.OK
     assert f(dz=None) == f(q=None) == f(scale=None) == f(rstd=None) == f(dx=None) == B.EINVAL
     assert f(dz=at(0) + 1) == f(ds=at(4) + 1) == f(dx=at(5) + 1) == f(scale=at(2) + 1) == B.EINVAL
+    assert f(dt_dz=5) == f(dt=B.FP32, dt_dz=B.BF16) == B.EDTYPE
+    assert f(dt_dz=B.FP32, dz=at(0) + 2) == B.EINVAL
+    assert f(dt_dz=B.FP32, dx=at(0)) == B.EOVERLAP          # in place only where the types are the same
     assert f(dx=at(0) + 2) == f(dx=at(4) + 2) == f(dx=at(1)) == f(dx=at(2)) == f(dx=at(3)) == B.EOVERLAP
 
 
@@ -85,9 +88,11 @@ def test_linear_q8_bwd(L):
     assert need >= 4 * 32 + 4 * 4
     assert [L.lmbp_linear_q8_bwd_bytes(*s) for s in ((0, 32, 64), (4, 32, 0), (-1, 2, 3), (4, 131072, 64))] == [0] * 4
 
-    def f(dt=B.BF16, m=4, n=32, k=64, dy=at(0), w=at(1), w_scale=at(2), dx=at(3), work=at(4), size=need):
-        return L.linear_q8_bwd(dt, m, n, k, dy, w, w_scale, dx, work, size, None)
-    assert f(dt=5) == B.EDTYPE
+    def f(dt=B.BF16, m=4, n=32, k=64, dy=at(0), w=at(1), w_scale=at(2), dx=at(3), work=at(4), size=need, add=None, dt_dx=B.BF16):
+        return L.linear_q8_bwd(dt, dt_dx, m, n, k, dy, w, w_scale, add, dx, work, size, None)
+    assert f(dt=5) == f(dt_dx=5) == B.EDTYPE
+    assert f(add=at(5) + 1) == f(dt_dx=B.FP32, dx=at(3) + 2) == f(dt_dx=B.FP32, add=at(5) + 2) == B.EINVAL
+    assert f(add=at(3) + 2) == f(add=at(4)) == B.EOVERLAP
     assert f(m=-1) == f(n=-1) == f(k=-1) == f(m=1 << 31) == f(n=131072) == B.EINVAL
     assert f(m=0, dy=None, dx=None, work=None, size=0) == f(k=0, w=None, dx=None, work=None, size=0) == B.OK
     assert f(dy=None) == f(w=None) == f(w_scale=None) == f(dx=None) == B.EINVAL

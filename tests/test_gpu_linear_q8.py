@@ -100,6 +100,23 @@ def test_input_gradient(m, n, k, dtype):
     assert ((dx.double() - real).abs() <= room + 1e-5 * real.abs() + 1e-38).all()
 
 
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32"), ("fp32", "bf16")])
+@pytest.mark.parametrize("m,k,n", SIZES)
+def test_input_gradients_that_add_up(m, n, k, dtype, out):
+    """dx = product + add with one rounding (u of the sum in the multiply-add, h in the store)."""
+    w, w_scale = weight(n, k, 4)
+    dy = (torch.randn(m, n, device=DEV) * 1e-3).to(TYPES[dtype])
+    add = torch.randn(m, k, device=DEV).to(TYPES[out])
+    part, _, _ = plain_bwd(dy, w, w_scale)
+    want = part + add.double()
+    dx = lmbp.linear_q8_bwd(dy, w, w_scale, add)
+    assert dx.dtype == TYPES[out]
+    room = 1.01 * (3 * U * part.abs() + (U + half(dx.dtype)) * want.abs()) + 1e-38
+    assert ((dx.double() - want).abs() <= room).all()
+    assert torch.equal(lmbp.linear_q8_bwd(dy, w, w_scale, add, dx=add), dx) and torch.equal(add, dx)   # in place
+    assert lmbp.linear_q8_bwd(dy, w, w_scale, dtype=TYPES[out]).dtype == TYPES[out]
+
+
 @pytest.mark.parametrize("m,n,k", [(4096, 4096, 2048), (2048, 11008, 4096), (300, 4096, 11008), (20, 11008, 4096)])
 def test_large_layers(m, n, k):
     (q, scale), (w, w_scale) = rows(m, k, 6), weight(n, k, 7)
@@ -180,7 +197,7 @@ def test_any_address_and_nothing_beside_the_result(m, n, k, shift, dtype):
     assert torch.equal(by[1].view(m, n), lmbp.linear_q8_fwd(q, scale, w, w_scale, bias, t))
     need = L.lmbp_linear_q8_bwd_bytes(m, n, k)
     work = torch.full((need + 64,), 77, dtype=torch.uint8, device=DEV)
-    assert L.linear_q8_bwd(dt, m, n, k, bdy[2], bw[2], bws[2], bdx[2], ctypes.c_void_p(work.data_ptr()), need, st) == B.OK
+    assert L.linear_q8_bwd(dt, dt, m, n, k, bdy[2], bw[2], bws[2], None, bdx[2], ctypes.c_void_p(work.data_ptr()), need, st) == B.OK
     assert torch.equal(bdx[1].view(m, k), lmbp.linear_q8_bwd(dy, w, w_scale))
     torch.cuda.synchronize()
     assert all(whole(b) for b in (bq, bs, bw, bws, bb, by, bdx, bdy)) and (work[need:] == 77).all()
@@ -240,6 +257,9 @@ def test_shapes_and_refusals():
         (ValueError, lambda: lmbp.linear_q8_bwd(y[..., :16].contiguous(), w, w_scale)),
         (ValueError, lambda: lmbp.linear_q8_bwd(y, w, w_scale.bfloat16())),
         (ValueError, lambda: lmbp.linear_q8_bwd(y.transpose(0, 1), w, w_scale)),
+        (ValueError, lambda: lmbp.linear_q8_bwd(y, w, w_scale, add=dx[:1])),
+        (ValueError, lambda: lmbp.linear_q8_bwd(y, w, w_scale, add=dx, dx=dx.float())),
+        (TypeError, lambda: lmbp.linear_q8_bwd(y, w, w_scale, dtype=torch.float16)),
     ]
     for error, call in cases:
         with pytest.raises(error):

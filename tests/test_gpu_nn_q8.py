@@ -113,7 +113,8 @@ def test_outputs_that_are_not_used():
     dy = torch.randn_like(y1)
     g, = torch.autograd.grad(y1, res, dy, retain_graph=True)
     q, scale, rstd = lmbp.msrms_q8_fwd((x + res).detach(), block.eps)
-    assert torch.equal(g, lmbp.msrms_q8_bwd(lmbp.linear_q8_bwd(dy, mods[1].weight, mods[1].scale), q, scale, rstd))
+    dz = lmbp.linear_q8_bwd(dy, mods[1].weight, mods[1].scale, dtype=torch.float32)
+    assert torch.equal(g, lmbp.msrms_q8_bwd(dz, q, scale, rstd))
     x2 = x.detach()
     assert block(x2)[0].grad_fn is None and block(x2, res)[2].requires_grad
     with torch.no_grad():
@@ -167,7 +168,8 @@ def test_mlp_block_step_by_step():
     y1 = lmbp.linear_q8_fwd(hq, hs, down.weight, down.scale)
     dh = lmbp.linear_q8_bwd(dy, down.weight, down.scale)
     dg, du = lmbp.reswiglu2_bwd(dh, u, act, codes)
-    dz = lmbp.linear_q8_bwd(dg, gate.weight, gate.scale) + lmbp.linear_q8_bwd(du, up.weight, up.scale)
+    dz = lmbp.linear_q8_bwd(dg, gate.weight, gate.scale, dtype=torch.float32)
+    dz = lmbp.linear_q8_bwd(du, up.weight, up.scale, add=dz)
     dx1 = lmbp.msrms_q8_bwd(dz, q, sc, rstd, ds)
     for got, want in ((y, y1), (s, s1), (dx, dx1), (dres, dx1)):
         assert torch.equal(got, want)
@@ -207,9 +209,9 @@ def test_graph_of_the_block(rows):
         y = lmbp.linear_q8_fwd(hq, hs, down.weight, down.scale)
         dh = lmbp.linear_q8_bwd(dy, down.weight, down.scale)
         dg, du = lmbp.reswiglu2_bwd(dh, u, act, codes)
-        dz = lmbp.linear_q8_bwd(dg, gate.weight, gate.scale)
-        dz2 = lmbp.linear_q8_bwd(du, up.weight, up.scale)
-        return y, s, dz2, lmbp.q8_values(q, sc), lmbp.msrms_q8_bwd(dz, q, sc, rstd, ds)
+        dz = lmbp.linear_q8_bwd(dg, gate.weight, gate.scale, dtype=torch.float32)
+        dz2 = lmbp.linear_q8_bwd(du, up.weight, up.scale, add=dz)
+        return y, s, dz2, lmbp.q8_values(q, sc), lmbp.msrms_q8_bwd(dz2, q, sc, rstd, ds)
 
     ins = [[torch.randn(rows, k, device=DEV).to(torch.bfloat16) for _ in range(4)] for _ in range(2)]
     for i in ins:

@@ -191,7 +191,7 @@ def test_any_address_and_nothing_beside_the_rows(rows, cols, shift, dtype):
     assert ((brs.t - want_rs).abs() <= room * want_rs).all() and ((bsc.t - want_sc).abs() <= room * want_sc).all()
     assert L.q8_values(dt, rows, cols, bq.ptr, bsc.ptr, bv.ptr, st) == B.OK
     assert torch.equal(bv.t.view(rows, cols), lmbp.q8_values(want_q, bsc.t.clone(), t))
-    assert L.msrms_q8_bwd(dt, rows, cols, bdz.ptr, bq.ptr, bsc.ptr, brs.ptr, bres.ptr, bdx.ptr, st) == B.OK
+    assert L.msrms_q8_bwd(dt, dt, rows, cols, bdz.ptr, bq.ptr, bsc.ptr, brs.ptr, bres.ptr, bdx.ptr, st) == B.OK
     dx_o = q8.msrms_bwd(n64(dz), n64(want_q), n64(bsc.t), n64(brs.t), n64(res))
     got = n64(bdx.t).reshape(rows, cols)
     assert (np.abs(got - dx_o) <= bwd_bound(dz, want_q, bsc.t, brs.t, dx_o, cols, dtype)).all()
@@ -247,6 +247,9 @@ def test_shapes_and_refusals():
         (ValueError, lambda: lmbp.msrms_q8_bwd(x, q, scale[:3], rstd)),
         (ValueError, lambda: lmbp.msrms_q8_bwd(x, q, scale, rstd.double())),
         (ValueError, lambda: lmbp.msrms_q8_bwd(x, q, scale, rstd, x[:3])),
+        (ValueError, lambda: lmbp.msrms_q8_bwd(x, q, scale, rstd, dx=x.float())),
+        (TypeError, lambda: lmbp.msrms_q8_bwd(x, q, scale, rstd, dtype=torch.float16)),
+        (lmbp.LmbpError, lambda: lmbp.msrms_q8_bwd(x, q, scale, rstd, x.float())),   # bf16 dz, fp32 dx
         (TypeError, lambda: lmbp.q8_values(q, scale, torch.float16)),
         (ValueError, lambda: lmbp.q8_values(q, scale[:2])),
         (ValueError, lambda: lmbp.q8_values(x, scale)),
@@ -254,6 +257,20 @@ def test_shapes_and_refusals():
     for error, call in cases:
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("with_ds", [False, True])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_norm_backward_from_a_sum_in_fp32(rows, cols, with_ds):
+    x = draw(rows, cols, "bf16", 1)
+    q, scale, rstd = lmbp.msrms_q8_fwd(x, EPS)
+    dz, ds = draw(rows, cols, "fp32", 4, 1e-3), draw(rows, cols, "bf16", 5, 1e-3) if with_ds else None
+    dx = lmbp.msrms_q8_bwd(dz, q, scale, rstd, ds, dtype=torch.bfloat16)
+    assert dx.dtype == torch.bfloat16
+    dx_o = q8.msrms_bwd(n64(dz), n64(q), n64(scale), n64(rstd), None if ds is None else n64(ds))
+    assert (np.abs(n64(dx) - dx_o) <= bwd_bound(dz, q, scale, rstd, dx_o, cols, "bf16")).all()
+    if with_ds:   # in place of the gradient of the sum
+        assert torch.equal(lmbp.msrms_q8_bwd(dz, q, scale, rstd, ds, dx=ds), dx)
 
 
 def test_any_bytes_have_values():
