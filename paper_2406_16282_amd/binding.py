@@ -144,7 +144,7 @@ def _bind_fast(L):
                       "`python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning, stacklevel=3)
         return
     for name in (*ACT_OPS, *NORM_OPS, *GLU_OPS, "linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd",
-                 "msrms_linear_swiglu_fwd"):
+                 "msrms_linear_swiglu_fwd", *Q8_OPS, "lmbp_linear_q8_bwd_bytes"):
         _address[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
     _fast = module
 
@@ -737,6 +737,9 @@ def _q8_rows_cols(t):
     return math.prod(t.shape[:-1]), t.shape[-1]   # rows of no columns are the library's to refuse
 
 
+_CODES = {torch.float32: FP32, torch.bfloat16: BF16}
+
+
 def _q8_in(q, ref, what, shape=None):
     """An int8 tensor on the same device as ``ref`` (of the given shape)."""
     _on(q, ref, what)
@@ -770,6 +773,10 @@ def q8_rows(x, stream=None):
     """Rows (the last dimension) in 8 bits: returns (q, scale), q int8 of x's shape and one
     fp32 scale per row; x is q * scale up to half a scale. Also for a weight [n, k]: one
     scale per output channel."""
+    if _fast is not None and stream is None:
+        out = _fast.q8_rows(_address["q8_rows"], x)
+        if out is not None:
+            return _done("q8_rows", out)
     _dev(x, "x")
     dt = _dtype_code(x)
     rows, cols = _q8_rows_cols(x)
@@ -782,6 +789,10 @@ def q8_rows(x, stream=None):
 
 def q8_values(q, scale, dtype=torch.bfloat16, stream=None):
     """The values that rows in 8 bits stand for: q * scale in ``dtype``."""
+    if _fast is not None and stream is None and dtype in _CODES:
+        out = _fast.q8_values(_address["q8_values"], _CODES[dtype], q, scale)
+        if out is not None:
+            return _done("q8_values", out)
     _q8_in(q, q, "q")
     rows, cols = _q8_rows_cols(q)
     _per_row(scale, q, rows, "scale")
@@ -796,6 +807,10 @@ def msrms_q8_fwd(x, eps, res=None, s=None, stream=None):
     """MS-RMSNorm over the last dimension with its output in 8 bits: returns (q, scale, rstd),
     z = q * scale. With a residual, of s = x + res (rounded to x's type): returns (q, scale,
     rstd, s); s may be given, x and res themselves included (the sum in place)."""
+    if _fast is not None and s is None and stream is None:
+        out = _fast.msrms_q8_fwd(_address["msrms_q8_fwd"], x, eps, res)
+        if out is not None:
+            return _done("msrms_q8_fwd", out)
     _dev(x, "x")
     dt = _dtype_code(x)
     rows, cols = _q8_rows_cols(x)
@@ -820,6 +835,11 @@ def msrms_q8_bwd(dz, q, scale, rstd, ds=None, dx=None, dtype=None, stream=None):
     gradient that reaches their sum past the norm. dx has the type of ds, else ``dtype``, else
     that of dz; dz may be fp32 where they are bf16. dx may be given, dz (of one type) or ds
     included."""
+    if _fast is not None and dx is None and stream is None:
+        code = _CODES.get(getattr(ds, "dtype", None) or dtype or getattr(dz, "dtype", None))
+        out = _fast.msrms_q8_bwd(_address["msrms_q8_bwd"], code, dz, q, scale, rstd, ds) if code is not None else None
+        if out is not None:
+            return _done("msrms_q8_bwd", out)
     _dev(dz, "dz")
     dt_dz = _dtype_code(dz)
     dtype = ds.dtype if isinstance(ds, torch.Tensor) else dtype or dz.dtype
@@ -849,6 +869,10 @@ def linear_q8_fwd(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=
     """Linear layer of 8-bit rows q [..., k] (one scale per row) and an 8-bit weight w [n, k]
     (one scale per output channel): y = (q w^T) scale w_scale + bias in ``dtype``, the sums
     exact. bias [n] of that dtype or None."""
+    if _fast is not None and stream is None and dtype in _CODES:
+        out = _fast.linear_q8_fwd(_address["linear_q8_fwd"], _CODES[dtype], q, scale, w, w_scale, bias)
+        if out is not None:
+            return _done("linear_q8_fwd", out)
     _q8_in(q, q, "q")
     n, k = _q8_weight(w, w_scale, q)
     if q.dim() == 0 or q.shape[-1] != k:
@@ -871,6 +895,12 @@ def linear_q8_bwd(dy, w, w_scale, add=None, dx=None, dtype=None, stream=None):
     brought to 8 bits first (one scale per row). dx [..., k] has the type of ``add`` (None: none),
     else ``dtype``, else that of dy; it may be given, ``add`` itself included (the sum of several
     layers' gradients)."""
+    if _fast is not None and add is None and dx is None and stream is None:
+        code = _CODES.get(dtype or getattr(dy, "dtype", None))
+        out = (_fast.linear_q8_bwd(_address["linear_q8_bwd"], _address["lmbp_linear_q8_bwd_bytes"], code, dy, w, w_scale)
+               if code is not None else None)
+        if out is not None:
+            return _done("linear_q8_bwd", out)
     _dev(dy, "dy")
     dt = _dtype_code(dy)
     n, k = _q8_weight(w, w_scale, dy)

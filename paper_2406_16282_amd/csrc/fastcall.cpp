@@ -361,6 +361,195 @@ PyObject* norm_linear_swiglu_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- rows and weights in 8 bits
+bool f32_of(PyObject* o, const at::Tensor& like, int64_t count, at::Tensor& t) {
+  return plain(o, t) && t.scalar_type() == at::kFloat && t.numel() == count && t.device() == like.device();
+}
+at::ScalarType type_of(int dt) { return dt == kBf16 ? at::kBFloat16 : at::kFloat; }
+// Rows and columns of a tensor of at least one dimension; the sizes without the last one.
+bool rows_of(const at::Tensor& t, int64_t& rows, int64_t& cols, at::IntArrayRef& lead) {
+  if (t.dim() == 0) return false;
+  cols = t.size(-1);
+  lead = t.sizes().slice(0, size_t(t.dim() - 1));
+  rows = 1;
+  for (const int64_t v : lead) rows *= v;
+  return true;
+}
+
+// (function, x) -> (q, scale)
+PyObject* q8_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor x;
+  int64_t rows, cols;
+  at::IntArrayRef lead;
+  if (n != 2 || !plain(a[1], x) || !rows_of(x, rows, cols, lead)) Py_RETURN_NONE;
+  const int dt = dtype_of(x);
+  if (dt < 0 || !on_current_device(x)) Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(x, s)) return nullptr;
+  at::Tensor q, scale;
+  const auto f = address<int (*)(int, int64_t, int64_t, const void*, void*, void*, void*)>(a[0]);
+  int status;
+  {
+    NoGil released;
+    q = at::empty(x.sizes(), x.options().dtype(at::kChar));
+    scale = at::empty(lead, x.options().dtype(at::kFloat));
+    status = f(dt, rows, cols, x.data_ptr(), q.data_ptr(), scale.data_ptr(), s);
+  }
+  return result(status, q, scale);
+  END_HANDLE_TH_ERRORS
+}
+
+// (function, type, q, scale) -> v
+PyObject* q8_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor q, scale;
+  int64_t rows, cols;
+  at::IntArrayRef lead;
+  if (n != 4 || !plain(a[2], q) || q.scalar_type() != at::kChar || !rows_of(q, rows, cols, lead) || !on_current_device(q) ||
+      !f32_of(a[3], q, rows, scale))
+    Py_RETURN_NONE;
+  const int dt = int(PyLong_AsLong(a[1]));
+  void* s;
+  if (!stream_of(q, s)) return nullptr;
+  at::Tensor v;
+  const auto f = address<int (*)(int, int64_t, int64_t, const void*, const void*, void*, void*)>(a[0]);
+  int status;
+  {
+    NoGil released;
+    v = at::empty(q.sizes(), q.options().dtype(type_of(dt)));
+    status = f(dt, rows, cols, q.data_ptr(), scale.data_ptr(), v.data_ptr(), s);
+  }
+  return result(status, v);
+  END_HANDLE_TH_ERRORS
+}
+
+// (function, x, eps, residual or None) -> (q, scale, rstd[, sum])
+PyObject* msrms_q8_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor x, res;
+  int64_t rows, cols;
+  at::IntArrayRef lead;
+  if (n != 4 || !PyFloat_CheckExact(a[2]) || !plain(a[1], x) || !rows_of(x, rows, cols, lead)) Py_RETURN_NONE;
+  const int dt = dtype_of(x);
+  if (dt < 0 || !on_current_device(x)) Py_RETURN_NONE;
+  if (a[3] != Py_None && (!plain(a[3], res) || !same(res, x) || res.sizes() != x.sizes())) Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(x, s)) return nullptr;
+  at::Tensor q, scale, rstd, sum;
+  const auto f = address<int (*)(int, int64_t, int64_t, float, const void*, const void*, void*, void*, void*, void*, void*)>(
+      a[0]);
+  int status;
+  {
+    NoGil released;
+    q = at::empty(x.sizes(), x.options().dtype(at::kChar));
+    scale = at::empty(lead, x.options().dtype(at::kFloat));
+    rstd = at::empty(lead, x.options().dtype(at::kFloat));
+    if (res.defined()) sum = at::empty(x.sizes(), x.options());
+    status = f(dt, rows, cols, float(PyFloat_AS_DOUBLE(a[2])), x.data_ptr(), res.defined() ? res.data_ptr() : nullptr,
+               sum.defined() ? sum.data_ptr() : nullptr, q.data_ptr(), scale.data_ptr(), rstd.data_ptr(), s);
+  }
+  return sum.defined() ? result(status, q, scale, rstd, sum) : result(status, q, scale, rstd);
+  END_HANDLE_TH_ERRORS
+}
+
+// (function, type of dx, dz, q, scale, rstd, ds or None) -> dx
+PyObject* msrms_q8_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor dz, q, scale, rstd, ds;
+  int64_t rows, cols;
+  at::IntArrayRef lead;
+  if (n != 7 || !plain(a[2], dz) || !rows_of(dz, rows, cols, lead)) Py_RETURN_NONE;
+  const int dt_dz = dtype_of(dz), dt = int(PyLong_AsLong(a[1]));
+  if (dt_dz < 0 || !on_current_device(dz) || !plain(a[3], q) || q.scalar_type() != at::kChar || q.device() != dz.device() ||
+      q.sizes() != dz.sizes() || !f32_of(a[4], dz, rows, scale) || !f32_of(a[5], dz, rows, rstd))
+    Py_RETURN_NONE;
+  if (a[6] != Py_None && (!plain(a[6], ds) || ds.scalar_type() != type_of(dt) || ds.device() != dz.device() ||
+                          ds.sizes() != dz.sizes()))
+    Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(dz, s)) return nullptr;
+  at::Tensor dx;
+  const auto f = address<int (*)(int, int, int64_t, int64_t, const void*, const void*, const void*, const void*, const void*,
+                                 void*, void*)>(a[0]);
+  int status;
+  {
+    NoGil released;
+    dx = at::empty(dz.sizes(), dz.options().dtype(type_of(dt)));
+    status = f(dt_dz, dt, rows, cols, dz.data_ptr(), q.data_ptr(), scale.data_ptr(), rstd.data_ptr(),
+               ds.defined() ? ds.data_ptr() : nullptr, dx.data_ptr(), s);
+  }
+  return result(status, dx);
+  END_HANDLE_TH_ERRORS
+}
+
+// An 8-bit weight [n, k] and its scales on the device of `like`.
+bool q8_weight(PyObject* ow, PyObject* os, const at::Tensor& like, at::Tensor& w, at::Tensor& w_scale) {
+  return plain(ow, w) && w.scalar_type() == at::kChar && w.dim() == 2 && w.device() == like.device() &&
+         f32_of(os, like, w.size(0), w_scale);
+}
+
+// (function, type, q, scale, w, w_scale, bias or None) -> y
+PyObject* linear_q8_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor q, scale, w, w_scale, b;
+  int64_t m, k;
+  at::IntArrayRef lead;
+  if (n != 7 || !plain(a[2], q) || q.scalar_type() != at::kChar || !rows_of(q, m, k, lead) || !on_current_device(q) ||
+      !f32_of(a[3], q, m, scale) || !q8_weight(a[4], a[5], q, w, w_scale) || w.size(1) != k)
+    Py_RETURN_NONE;
+  const int dt = int(PyLong_AsLong(a[1]));
+  if (a[6] != Py_None && (!plain(a[6], b) || b.scalar_type() != type_of(dt) || b.numel() != w.size(0) ||
+                          b.device() != q.device()))
+    Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(q, s)) return nullptr;
+  c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
+  shape.push_back(w.size(0));
+  at::Tensor y;
+  const auto f = address<int (*)(int, int64_t, int64_t, int64_t, const void*, const void*, const void*, const void*,
+                                 const void*, void*, void*)>(a[0]);
+  int status;
+  {
+    NoGil released;
+    y = at::empty(shape, q.options().dtype(type_of(dt)));
+    status = f(dt, m, w.size(0), k, q.data_ptr(), scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
+               b.defined() ? b.data_ptr() : nullptr, y.data_ptr(), s);
+  }
+  return result(status, y);
+  END_HANDLE_TH_ERRORS
+}
+
+// (function, the workspace's size function, type of dx, dy, w, w_scale) -> dx
+PyObject* linear_q8_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor dy, w, w_scale;
+  int64_t m, cols;
+  at::IntArrayRef lead;
+  if (n != 6 || !plain(a[3], dy) || !rows_of(dy, m, cols, lead)) Py_RETURN_NONE;
+  const int dt = dtype_of(dy), dt_dx = int(PyLong_AsLong(a[2]));
+  if (dt < 0 || !on_current_device(dy) || !q8_weight(a[4], a[5], dy, w, w_scale) || w.size(0) != cols) Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(dy, s)) return nullptr;
+  c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
+  shape.push_back(w.size(1));
+  at::Tensor dx, work;
+  const auto f = address<int (*)(int, int, int64_t, int64_t, int64_t, const void*, const void*, const void*, const void*,
+                                 void*, void*, int64_t, void*)>(a[0]);
+  const auto bytes_of = address<size_t (*)(int64_t, int64_t, int64_t)>(a[1]);
+  int status;
+  {
+    NoGil released;
+    const int64_t bytes = int64_t(bytes_of(m, cols, w.size(1)));
+    work = at::empty({bytes}, dy.options().dtype(at::kByte));
+    dx = at::empty(shape, dy.options().dtype(type_of(dt_dx)));
+    status = f(dt, dt_dx, m, cols, w.size(1), dy.data_ptr(), w.data_ptr(), w_scale.data_ptr(), nullptr, dx.data_ptr(),
+               work.data_ptr(), bytes, s);
+  }
+  return result(status, dx);
+  END_HANDLE_TH_ERRORS
+}
+
 // (torch's raw-stream accessor)
 PyObject* bind(PyObject*, PyObject* accessor) {
   Py_INCREF(accessor);
@@ -372,7 +561,9 @@ PyObject* bind(PyObject*, PyObject* accessor) {
 PyMethodDef kMethods[] = {LMBP_FAST(act_fwd), LMBP_FAST(act_bwd), LMBP_FAST(glu_fwd), LMBP_FAST(glu_bwd),
                           LMBP_FAST(norm_fwd), LMBP_FAST(norm_bwd), LMBP_FAST(linear_act_fwd),
                           LMBP_FAST(linear_swiglu_fwd), LMBP_FAST(norm_linear_act_fwd),
-                          LMBP_FAST(norm_linear_swiglu_fwd), {"bind", bind, METH_O, nullptr},
+                          LMBP_FAST(norm_linear_swiglu_fwd), LMBP_FAST(q8_rows), LMBP_FAST(q8_values),
+                          LMBP_FAST(msrms_q8_fwd), LMBP_FAST(msrms_q8_bwd), LMBP_FAST(linear_q8_fwd),
+                          LMBP_FAST(linear_q8_bwd), {"bind", bind, METH_O, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

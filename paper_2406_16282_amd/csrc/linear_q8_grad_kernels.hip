@@ -7,7 +7,6 @@
 // features, N for its input features. The sums are exact, as the forward's.
 #include "linear_q8_device.hpp"
 
-#include <cstdlib>
 #include <type_traits>
 
 namespace lmbp {
@@ -403,7 +402,6 @@ hipError_t launch_rows(Args a, int dev, hipStream_t s) {
 enum Form { kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
 
 Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
-  if (const char* f = getenv("Q8FORM")) return Form(atoi(f));
   if (M <= 100) return kRows16;
   auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   if (tiles(256, 256) >= 2 * cus) return kBig;

@@ -8,7 +8,6 @@
 #include "linear_q8_device.hpp"
 
 #include <algorithm>
-#include <cstdlib>
 
 namespace lmbp {
 namespace lq8 {
@@ -38,19 +37,21 @@ struct Tile {
 template <class OUT>
 __device__ inline void store16(const Args& a, int64_t row, int64_t col, const float (&f)[16]) {
   const int64_t base = row * a.N + col;
+  int left = int(a.N - col);   // columns that there are; new in every call: 16 masks kept would be spilled
+  asm volatile("" : "+v"(left));
   if (a.vec) {
 #pragma unroll
     for (int p = 0; p < 16 / OUT::kPerVec; ++p) {
       float v[OUT::kPerVec];
 #pragma unroll
       for (int e = 0; e < OUT::kPerVec; ++e) v[e] = f[p * OUT::kPerVec + e];
-      if (col + p * OUT::kPerVec < a.N)
+      if (p * OUT::kPerVec < left)
         *reinterpret_cast<u32x4*>(static_cast<char*>(a.y) + (base + p * OUT::kPerVec) * OUT::kBytes) = OUT::pack(v);
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      if (col + e < a.N) OUT::store1(a.y, base + e, f[e]);
+      if (e < left) OUT::store1(a.y, base + e, f[e]);
   }
 }
 
@@ -59,8 +60,7 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tile(Args a
   constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, TMH = C::TMH, TNH = C::TNH;
   constexpr int HM = C::HM, HN = C::HN, kWaves = C::kWaves;
   constexpr int kLA = C::kLA, kLB = C::kLB, kL = kLA + kLB, kSlot = C::kSlot, kRing = C::kRing;
-  const int64_t M = a.M, N = a.N;
-  const uint32_t K = uint32_t(a.K);
+  const uint32_t M = uint32_t(a.M), N = uint32_t(a.N), K = uint32_t(a.K);   // below 2^31
   extern __shared__ __attribute__((aligned(16))) int8_t lds[];
   float* const as_lds = reinterpret_cast<float*>(lds + kRing * kSlot);
   float* const bs_lds = as_lds + 4 * BM;
@@ -97,11 +97,11 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tile(Args a
     uint32_t tm = 0, tn = 0;
     const bool in = l_tile < tiles;
     if (in) tile_of(l_tile, a.map, tm, tn);
-    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
-    const int64_t rows_a = !in ? 0 : (M - m0 < BM) ? M - m0 : BM;
-    const int64_t rows_b = !in ? 0 : (N - n0 < BN) ? N - n0 : BN;
-    ra = make_rsrc(a.a + m0 * K, rows_a * K);
-    rb = make_rsrc(a.b + n0 * K, rows_b * K);
+    const uint32_t m0 = tm * BM, n0 = tn * BN;
+    const uint32_t rows_a = !in ? 0u : (M - m0 < BM) ? M - m0 : BM;
+    const uint32_t rows_b = !in ? 0u : (N - n0 < BN) ? N - n0 : BN;
+    ra = make_rsrc(a.a + uint64_t(m0) * K, rows_a * K);
+    rb = make_rsrc(a.b + uint64_t(n0) * K, rows_b * K);
     // The tile's scales, into one of four places: the cursor runs at most two tiles ahead of
     // the tile being computed. Issued before the tile's first operands, they have landed when
     // those have.
@@ -436,7 +436,6 @@ hipError_t launch_few(const Args& a, hipStream_t s) {
 enum Form { kFew, kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
 
 Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
-  if (const char* f = getenv("Q8FORM")) return Form(atoi(f));
   if (M <= 2) return kFew;
   if (M <= 32) return kRows16;
   if (M <= 64) return kRows32;

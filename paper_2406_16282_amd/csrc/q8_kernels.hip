@@ -418,26 +418,28 @@ __global__ __launch_bounds__(256) void norm_bwd_any(const void* dz, const int8_t
   }
 }
 
-// Launch shapes of the register kernels: the fewest waves to a row that hold it in kTarget
-// pieces per thread, or 16 waves with up to 8.
-constexpr int kVpl[] = {1, 2, 3, 4, 6, 8};
-constexpr int kWpr[] = {1, 2, 4, 8, 16};
-constexpr int kShapes = 30;
-constexpr int kTarget = 3;
-constexpr bool reachable(int vpl, int wpr) { return vpl <= kTarget || wpr == 16; }
+// Launch shapes of the register kernels, by the pieces that they hold: the fewest waves to a row
+// that hold it in 3 pieces per thread, or 16 waves with up to MOST (what a kernel has registers
+// for).
+struct Shape {
+  int wpr, vpl;
+};
+constexpr Shape kShapes[] = {{1, 1}, {1, 2}, {1, 3}, {2, 2},  {2, 3},  {4, 2},  {4, 3},
+                             {8, 2}, {8, 3}, {16, 2}, {16, 3}, {16, 4}, {16, 6}, {16, 8}};
+constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]);
 
-// Calls f(shape of VPL, shape of WPR) for the shape that holds `pieces`; false if none does.
-template <int I = 0, class F>
+// Calls f(VPL, WPR) for the shape that holds `pieces`; false if none does.
+template <int MOST, int I = 0, class F>
 bool with_shape(int64_t pieces, F f) {
-  if constexpr (I < kShapes) {
-    constexpr int wpr = kWpr[I / 6], vpl = kVpl[I % 6];
-    if constexpr (reachable(vpl, wpr)) {
+  if constexpr (I < kNumShapes) {
+    constexpr int wpr = kShapes[I].wpr, vpl = kShapes[I].vpl;
+    if constexpr (vpl <= MOST) {
       if (pieces <= int64_t(kWave) * wpr * vpl) {
         f(std::integral_constant<int, vpl>{}, std::integral_constant<int, wpr>{});
         return true;
       }
     }
-    return with_shape<I + 1>(pieces, f);
+    return with_shape<MOST, I + 1>(pieces, f);
   } else {
     return false;
   }
@@ -457,7 +459,7 @@ hipError_t launch_fwd(const FwdArgs& a, hipStream_t s) {
   const bool ragged = a.cols % IO::kPerVec != 0 || !at16(a.x) || (MODE == kNormRes && (!at16(a.res) || !at16(a.s))) ||
                       reinterpret_cast<uintptr_t>(a.q) % IO::kPerVec != 0;
   int64_t blocks = 0;
-  const bool held = a.cols < (1 << 24) && with_shape(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+  const bool held = a.cols < (1 << 24) && with_shape<8>(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
     blocks = blocks_of<W>(a.rows);
     if (blocks > 0x7fffffff) return;
@@ -475,7 +477,7 @@ template <class IO>
 hipError_t launch_values(int64_t rows, int64_t cols, const int8_t* q, const float* scale, void* v, hipStream_t s) {
   const bool ragged = cols % IO::kPerVec != 0 || !at16(v) || reinterpret_cast<uintptr_t>(q) % IO::kPerVec != 0;
   int64_t blocks = 0;
-  const bool held = cols < (1 << 24) && with_shape(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+  const bool held = cols < (1 << 24) && with_shape<8>(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
     blocks = blocks_of<W>(rows);
     if (blocks > 0x7fffffff) return;
@@ -496,7 +498,7 @@ hipError_t launch_norm_bwd(int64_t rows, int64_t cols, const void* dz, const int
                       reinterpret_cast<uintptr_t>(q) % IO::kPerVec != 0;
   int64_t blocks = 0;
   const BwdArgs a{dz, q, scale, rstd, ds, dx, rows, cols};
-  const bool held = cols < (1 << 24) && with_shape(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+  const bool held = cols < (1 << 24) && with_shape<IO::kPerVec == 8 ? 4 : 8>(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
     blocks = blocks_of<W>(rows);
     if (blocks > 0x7fffffff) return;

@@ -274,3 +274,47 @@ def test_the_same_twice():
                *lmbp.msrms_q8_fwd(x, 1e-5), lmbp.msrms_q8_bwd(x, q, s, r))
         first = first or out
         assert all(torch.equal(a, b) for a, b in zip(out, first))
+
+
+def calls(shape, dtype):
+    torch.manual_seed(0)
+    here = torch.cuda.current_stream()
+    x, res, dz, ds = (torch.randn(shape, device=DEV).to(dtype) for _ in range(4))
+    q, scale, rstd = lmbp.msrms_q8_fwd(x, 1e-5, stream=here)
+    w = torch.randint(-127, 128, (33, shape[-1]), device=DEV, dtype=torch.int8)
+    w_scale, bias = torch.rand(33, device=DEV), torch.randn(33, device=DEV).to(dtype)
+    dy = torch.randn(*shape[:-1], 33, device=DEV).to(dtype)
+    yield lmbp.q8_rows, (x,), {}
+    yield lmbp.q8_values, (q, scale), {}
+    yield lmbp.q8_values, (q, scale, dtype), {}
+    yield lmbp.msrms_q8_fwd, (x, 1e-5), {}
+    yield lmbp.msrms_q8_fwd, (x, 1e-5, res), {}
+    yield lmbp.msrms_q8_bwd, (dz, q, scale, rstd), {}
+    yield lmbp.msrms_q8_bwd, (dz, q, scale, rstd, ds), {}
+    yield lmbp.msrms_q8_bwd, (dz.float(), q, scale, rstd), {"dtype": dtype}
+    yield lmbp.linear_q8_fwd, (q, scale, w, w_scale, None, dtype), {}
+    yield lmbp.linear_q8_fwd, (q, scale, w, w_scale, bias, dtype), {}
+    yield lmbp.linear_q8_bwd, (dy, w, w_scale), {}
+    yield lmbp.linear_q8_bwd, (dy, w, w_scale), {"dtype": torch.float32}
+
+
+class Sub(torch.Tensor):
+    pass
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", [(1,), (3, 40), (2, 5, 64), (0, 16), (7, 1023)])
+def test_native_calls_and_the_python_path(shape, dtype):
+    """The same results from the native form of a call, from the Python path (a stream given) and
+    from a call that the native form declines (a subclass)."""
+    from paper_2406_16282_amd import binding
+    lmbp.lib()
+    assert binding._fast is not None
+    for op, args, more in calls(shape, dtype):
+        outs = (op(*args, **more), op(*args, **more, stream=torch.cuda.current_stream()),
+                op(args[0].as_subclass(Sub), *args[1:], **more))
+        outs = [o if isinstance(o, tuple) else (o,) for o in outs]
+        for a, b, c in zip(*outs):
+            assert type(a) is torch.Tensor and a.shape == b.shape and a.dtype == b.dtype and a.stride() == b.stride()
+            assert torch.equal(a.reshape(-1).view(torch.uint8), b.reshape(-1).view(torch.uint8)), op.__name__
+            assert torch.equal(b.reshape(-1).view(torch.uint8), c.reshape(-1).view(torch.uint8)), op.__name__
