@@ -895,10 +895,10 @@ def linear_q8_bwd(dy, w, w_scale, add=None, dx=None, dtype=None, stream=None):
     brought to 8 bits first (one scale per row). dx [..., k] has the type of ``add`` (None: none),
     else ``dtype``, else that of dy; it may be given, ``add`` itself included (the sum of several
     layers' gradients)."""
-    if _fast is not None and add is None and dx is None and stream is None:
-        code = _CODES.get(dtype or getattr(dy, "dtype", None))
-        out = (_fast.linear_q8_bwd(_address["linear_q8_bwd"], _address["lmbp_linear_q8_bwd_bytes"], code, dy, w, w_scale)
-               if code is not None else None)
+    if _fast is not None and (dx is None or dx is add) and stream is None:
+        code = _CODES.get(getattr(add, "dtype", None) or dtype or getattr(dy, "dtype", None))
+        out = (_fast.linear_q8_bwd(_address["linear_q8_bwd"], _address["lmbp_linear_q8_bwd_bytes"], code, dy, w, w_scale, add,
+                                   dx is not None) if code is not None else None)
         if out is not None:
             return _done("linear_q8_bwd", out)
     _dev(dy, "dy")

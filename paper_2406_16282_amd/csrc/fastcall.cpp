@@ -520,19 +520,22 @@ PyObject* linear_q8_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// (function, the workspace's size function, type of dx, dy, w, w_scale) -> dx
+// (function, the workspace's size function, type of dx, dy, w, w_scale, add or None, in place) -> dx
 PyObject* linear_q8_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  at::Tensor dy, w, w_scale;
+  at::Tensor dy, w, w_scale, add;
   int64_t m, cols;
   at::IntArrayRef lead;
-  if (n != 6 || !plain(a[3], dy) || !rows_of(dy, m, cols, lead)) Py_RETURN_NONE;
+  if (n != 8 || !plain(a[3], dy) || !rows_of(dy, m, cols, lead)) Py_RETURN_NONE;
   const int dt = dtype_of(dy), dt_dx = int(PyLong_AsLong(a[2]));
   if (dt < 0 || !on_current_device(dy) || !q8_weight(a[4], a[5], dy, w, w_scale) || w.size(0) != cols) Py_RETURN_NONE;
   void* s;
   if (!stream_of(dy, s)) return nullptr;
   c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
   shape.push_back(w.size(1));
+  if (a[6] != Py_None && (!plain(a[6], add) || add.scalar_type() != type_of(dt_dx) || add.device() != dy.device() ||
+                          add.sizes() != at::IntArrayRef(shape)))
+    Py_RETURN_NONE;
   at::Tensor dx, work;
   const auto f = address<int (*)(int, int, int64_t, int64_t, int64_t, const void*, const void*, const void*, const void*,
                                  void*, void*, int64_t, void*)>(a[0]);
@@ -542,9 +545,9 @@ PyObject* linear_q8_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     NoGil released;
     const int64_t bytes = int64_t(bytes_of(m, cols, w.size(1)));
     work = at::empty({bytes}, dy.options().dtype(at::kByte));
-    dx = at::empty(shape, dy.options().dtype(type_of(dt_dx)));
-    status = f(dt, dt_dx, m, cols, w.size(1), dy.data_ptr(), w.data_ptr(), w_scale.data_ptr(), nullptr, dx.data_ptr(),
-               work.data_ptr(), bytes, s);
+    dx = a[7] == Py_True ? add : at::empty(shape, dy.options().dtype(type_of(dt_dx)));
+    status = f(dt, dt_dx, m, cols, w.size(1), dy.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
+               add.defined() ? add.data_ptr() : nullptr, dx.data_ptr(), work.data_ptr(), bytes, s);
   }
   return result(status, dx);
   END_HANDLE_TH_ERRORS

@@ -11,6 +11,7 @@
 #include "lmbp_launch.hpp"
 #include "q8_device.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lmbp {
@@ -112,120 +113,129 @@ struct Bytes {
 };
 
 // Rows in registers: WPR waves to a row, thread t of the row holding pieces t, t + 64 WPR, ...
-// (VPL of them); RAGGED rows have fewer than a piece's elements left, one to a thread.
+// (VPL of them); RAGGED rows have fewer than a piece's elements left, one to a thread. With a
+// factor per column the blocks walk the rows, each with its columns' factors in registers.
 template <class IO, int MODE, int VPL, int WPR, bool RAGGED>
 __global__ __launch_bounds__(block_of<WPR>()) void fwd_rows(FwdArgs a) {
   constexpr int P = IO::kPerVec, TPR = kWave * WPR, RPB = block_of<WPR>() / TPR;
   constexpr bool kIsNorm = MODE == kNorm || MODE == kNormRes;
-  __shared__ uint32_t most_lds[block_of<WPR>() / kWave];
+  __shared__ uint32_t most_lds[2][block_of<WPR>() / kWave];
   __shared__ float sum_lds[block_of<WPR>() / kWave];
   const int t = threadIdx.x % TPR;
-  const int64_t row = int64_t(blockIdx.x) * RPB + wave_in_block() / WPR;
-  const bool active = row < a.rows;
-  if constexpr (WPR == 1) {
-    if (!active) return;   // no barriers in the single-wave form
-  }
   const int cols = int(a.cols), pieces = cols / P;
-  const int64_t base = row * a.cols;
-  Piece<IO, P, RAGGED> x[VPL], y[MODE == kNormRes ? VPL : 1];
-  float c[MODE == kColumns ? VPL : 1][P];
+  float c[MODE == kColumns ? VPL : 1][P], c_last = 1.0f;
+  if constexpr (MODE == kColumns) {
 #pragma unroll
-  for (int j = 0; j < VPL; ++j) {
-    const int idx = j * TPR + t;
-    x[j].clear();
-    if constexpr (MODE == kNormRes) y[j].clear();
-    if (active && idx < pieces) {
-      x[j].load(a.x, base + idx * P);
-      if constexpr (MODE == kNormRes) y[j].load(a.res, base + idx * P);
+    for (int j = 0; j < VPL; ++j) {
+      Piece<F32, P, true> f;
+      f.clear();
+      if (j * TPR + t < pieces) f.load(a.columns, (j * TPR + t) * P);
+      f.get(c[j]);
     }
-    if constexpr (MODE == kColumns) {
-#pragma unroll
-      for (int e = 0; e < P; ++e) c[j][e] = idx < pieces ? a.columns[idx * P + e] : 0.0f;
-    }
+    if (RAGGED && pieces * P + t < cols) c_last = a.columns[pieces * P + t];
   }
-  const bool rest = RAGGED && active && pieces * P + t < cols;
-  float last = 0.0f;
-  if (rest) {
-    const int64_t at = base + pieces * P + t;
-    last = IO::load1(a.x, at);
-    if constexpr (MODE == kNormRes) {
-      IO::store1(a.s, at, last + IO::load1(a.res, at));
-      last = IO::load1(a.s, at);
-    }
-    if constexpr (MODE == kColumns) last *= a.columns[pieces * P + t];
-  }
-  uint32_t most = magnitude(last);
-  float sum = last * last;
+  const int64_t groups = (a.rows + RPB - 1) / RPB;
+  int turn = 0;   // LDS place: a wave can be at most one barrier ahead of another
+  for (int64_t group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
+    const int64_t row = group * RPB + wave_in_block() / WPR;
+    const bool active = row < a.rows;
+    const int64_t base = row * a.cols;
+    Piece<IO, P, RAGGED> x[VPL], y[MODE == kNormRes ? VPL : 1];
 #pragma unroll
-  for (int j = 0; j < VPL; ++j) {
-    float f[P];
-    x[j].get(f);
-    if constexpr (MODE == kNormRes) {
-      float g[P];
-      y[j].get(g);
-#pragma unroll
-      for (int e = 0; e < P; ++e) f[e] += g[e];
-      x[j].set(f);
+    for (int j = 0; j < VPL; ++j) {
       const int idx = j * TPR + t;
-      if (active && idx < pieces) x[j].store(a.s, base + idx * P);
-      x[j].get(f);   // as stored
+      x[j].clear();
+      if constexpr (MODE == kNormRes) y[j].clear();
+      if (active && idx < pieces) {
+        x[j].load(a.x, base + idx * P);
+        if constexpr (MODE == kNormRes) y[j].load(a.res, base + idx * P);
+      }
     }
+    const bool rest = RAGGED && active && pieces * P + t < cols;
+    float last = 0.0f;
+    if (rest) {
+      const int64_t at = base + pieces * P + t;
+      last = IO::load1(a.x, at);
+      if constexpr (MODE == kNormRes) {
+        IO::store1(a.s, at, last + IO::load1(a.res, at));
+        last = IO::load1(a.s, at);
+      }
+      if constexpr (MODE == kColumns) last *= c_last;
+    }
+    uint32_t most = magnitude(last);
+    float sum = last * last;
 #pragma unroll
-    for (int e = 0; e < P; ++e) {
-      if constexpr (MODE == kColumns) f[e] *= c[j][e];
-      most = umax(most, magnitude(f[e]));
-      if constexpr (kIsNorm) sum = __builtin_fmaf(f[e], f[e], sum);
-    }
-  }
-  most = wave_umax(most);
-  if constexpr (kIsNorm) sum = wave_sum(sum);
-  if constexpr (WPR > 1) {
-    const int wave = threadIdx.x / kWave, first = wave / WPR * WPR;
-    if ((threadIdx.x & (kWave - 1)) == 0) {
-      most_lds[wave] = most;
-      if constexpr (kIsNorm) sum_lds[wave] = sum;
-    }
-    __syncthreads();
-    most = 0;
-    sum = 0.0f;
-#pragma unroll
-    for (int k = 0; k < WPR; ++k) {
-      most = umax(most, most_lds[first + k]);
-      if constexpr (kIsNorm) sum += sum_lds[first + k];
-    }
-    if (!active) return;
-  }
-  const Q8Row w = q8_row(most);
-  int8_t* const q = a.q + row * a.pitch;
-#pragma unroll
-  for (int j = 0; j < VPL; ++j) {
-    const int idx = j * TPR + t;
-    if (idx < pieces) {
+    for (int j = 0; j < VPL; ++j) {
       float f[P];
       x[j].get(f);
-      if constexpr (MODE == kColumns) {
+      if constexpr (MODE == kNormRes) {
+        float g[P];
+        y[j].get(g);
 #pragma unroll
-        for (int e = 0; e < P; ++e) f[e] *= c[j][e];
+        for (int e = 0; e < P; ++e) f[e] += g[e];
+        x[j].set(f);
+        const int idx = j * TPR + t;
+        if (active && idx < pieces) x[j].store(a.s, base + idx * P);
+        x[j].get(f);   // as stored
       }
-      Bytes<P, RAGGED> b;
-      b.set(f, w.r);
 #pragma unroll
-      for (int k = 0; k < P / 4; ++k) b.v[k] = w.finite ? b.v[k] : 0u;
-      b.store(q + idx * P);
+      for (int e = 0; e < P; ++e) {
+        if constexpr (MODE == kColumns) f[e] *= c[j][e];
+        most = umax(most, magnitude(f[e]));
+        if constexpr (kIsNorm) sum = __builtin_fmaf(f[e], f[e], sum);
+      }
     }
-  }
-  if (rest) q[pieces * P + t] = int8_t(w.finite ? to_q8(last, w.r) : 0u);
-  if constexpr (MODE == kColumns) {
-    for (int k = cols + t; k < a.pitch; k += TPR) q[k] = 0;
-  }
-  if (t == 0) {
-    if constexpr (kIsNorm) {
-      const float rs = rsqrtf(sum / float(cols) + a.eps);
-      a.rstd[row] = rs;
-      a.scale[row] = w.a * rs / 127.0f;
-    } else {
-      a.scale[row] = w.a / 127.0f;
+    most = wave_umax(most);
+    if constexpr (kIsNorm) sum = wave_sum(sum);
+    if constexpr (WPR > 1) {
+      const int wave = threadIdx.x / kWave, first = wave / WPR * WPR;
+      if ((threadIdx.x & (kWave - 1)) == 0) {
+        most_lds[turn][wave] = most;
+        if constexpr (kIsNorm) sum_lds[wave] = sum;
+      }
+      __syncthreads();
+      most = 0;
+      sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < WPR; ++k) {
+        most = umax(most, most_lds[turn][first + k]);
+        if constexpr (kIsNorm) sum += sum_lds[first + k];
+      }
     }
+    if (!active) continue;   // the last group: no barrier follows
+    const Q8Row w = q8_row(most);
+    int8_t* const q = a.q + row * a.pitch;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) {
+      const int idx = j * TPR + t;
+      if (idx < pieces) {
+        float f[P];
+        x[j].get(f);
+        if constexpr (MODE == kColumns) {
+#pragma unroll
+          for (int e = 0; e < P; ++e) f[e] *= c[j][e];
+        }
+        Bytes<P, RAGGED> b;
+        b.set(f, w.r);
+#pragma unroll
+        for (int k = 0; k < P / 4; ++k) b.v[k] = w.finite ? b.v[k] : 0u;
+        b.store(q + idx * P);
+      }
+    }
+    if (rest) q[pieces * P + t] = int8_t(w.finite ? to_q8(last, w.r) : 0u);
+    if constexpr (MODE == kColumns) {
+      for (int k = cols + t; k < a.pitch; k += TPR) q[k] = 0;
+    }
+    if (t == 0) {
+      if constexpr (kIsNorm) {
+        const float rs = rsqrtf(sum / float(cols) + a.eps);
+        a.rstd[row] = rs;
+        a.scale[row] = w.a * rs / 127.0f;
+      } else {
+        a.scale[row] = w.a / 127.0f;
+      }
+    }
+    if constexpr (MODE != kColumns) return;   // a block for every group
   }
 }
 
@@ -459,9 +469,15 @@ hipError_t launch_fwd(const FwdArgs& a, hipStream_t s) {
   const bool ragged = a.cols % IO::kPerVec != 0 || !at16(a.x) || (MODE == kNormRes && (!at16(a.res) || !at16(a.s))) ||
                       reinterpret_cast<uintptr_t>(a.q) % IO::kPerVec != 0;
   int64_t blocks = 0;
+  int dev = 0, cus = 0;
+  if (MODE == kColumns) {
+    const hipError_t e = current_device(dev, cus);
+    if (e != hipSuccess) return e;
+  }
   const bool held = a.cols < (1 << 24) && with_shape<8>(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
     blocks = blocks_of<W>(a.rows);
+    if (MODE == kColumns) blocks = std::min<int64_t>(blocks, int64_t(cus) * (1024 / block_of<W>()));
     if (blocks > 0x7fffffff) return;
     const auto kernel = ragged ? fwd_rows<IO, MODE, V, W, true> : fwd_rows<IO, MODE, V, W, false>;
     hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, a);

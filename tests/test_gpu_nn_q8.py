@@ -296,6 +296,7 @@ def calls(shape, dtype):
     yield lmbp.linear_q8_fwd, (q, scale, w, w_scale, bias, dtype), {}
     yield lmbp.linear_q8_bwd, (dy, w, w_scale), {}
     yield lmbp.linear_q8_bwd, (dy, w, w_scale), {"dtype": torch.float32}
+    yield lmbp.linear_q8_bwd, (dy, w, w_scale, res), {}
 
 
 class Sub(torch.Tensor):
