@@ -6,7 +6,9 @@
 #include "lmbp_launch.hpp"
 #include "tile_device.hpp"
 
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 
 namespace lmbp {
 namespace lq8 {
@@ -32,69 +34,164 @@ struct Args {
   void* y;                // [M x N]
   int64_t M, N, K, a_pitch;
   bool vec;               // forward: y takes 16-byte stores
+  int32_t* part;          // input gradient: [splits][M x N] sums over shares of K, or null
+  int32_t share;          // steps of K to a share
   TileMap map;
 };
 
-// 16 bytes of a row from byte k0 on, zeros from byte `end` on; any alignment.
-__device__ inline u32x4 row_piece(const int8_t* row, int64_t k0, int64_t end) {
-  if (k0 + 16 <= end) return *reinterpret_cast<const u32x4_at1*>(row + k0);
+// 16 bytes of a matrix of `total` bytes (16 at least) from byte `at` on, at any alignment; those
+// that start less than 16 before its end are read from 16 before its end (mend shifts them).
+__device__ inline u32x4 fetch(const int8_t* base, int64_t total, int64_t at) {
+  return *reinterpret_cast<const u32x4_at1*>(base + (at < total - 16 ? at : total - 16));
+}
+// What `fetch` read, with byte `at` first and zeros from the count-th on.
+__device__ inline u32x4 mend(const u32x4& v, int64_t total, int64_t at, int64_t count) {
+  uint64_t lo = uint64_t(v[1]) << 32 | v[0], hi = uint64_t(v[3]) << 32 | v[2];
+  const int by = at > total - 16 ? 8 * int(at - (total - 16)) : 0;   // bits
+  const int keep = count <= 0 ? 0 : count < 16 ? 8 * int(count) : 128;
+  if (by >= 64) {
+    lo = by < 128 ? hi >> (by - 64) : 0;
+    hi = 0;
+  } else if (by > 0) {
+    lo = lo >> by | hi << (64 - by);
+    hi >>= by;
+  }
+  if (keep < 64) {
+    lo &= (uint64_t(1) << keep) - 1;
+    hi = 0;
+  } else if (keep < 128) {
+    hi &= (uint64_t(1) << (keep - 64)) - 1;
+  }
+  return u32x4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
+}
+// The same of a matrix of any size.
+__device__ inline u32x4 few_bytes(const int8_t* base, int64_t at, int64_t count) {
   u32x4 v = {0u, 0u, 0u, 0u};
-  for (int i = 0; i < 16 && k0 + i < end; ++i) v[i / 4] |= uint32_t(uint8_t(row[k0 + i])) << (8 * (i % 4));
+  for (int i = 0; i < 16 && i < count; ++i) v[i / 4] |= uint32_t(uint8_t(base[at + i])) << (8 * (i % 4));
   return v;
 }
 
-// Any sizes and alignments: a block of 4 waves takes 64 x 64 results, 64 products at a time,
-// both operands staged through registers into LDS with the products contiguous.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+// Transposing LDS read: of 16 lanes, lane q passes the address of columns 8 (q % 2) .. + 7 of row
+// q / 2 and lane i gets the 8 rows of column i (checked on the hardware).
+__device__ inline i32x2 read_tr8(const int8_t* p) {
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(p));
+}
+
+// Any sizes and alignments. A block takes 64 x 64 results; its 4 waves take the steps of 64 products
+// in turn, each through registers (the next step's loads under way) and LDS of its own, so that the
+// loop has no barrier, and the partial sums meet in LDS. Rows that do not start on 16-byte
+// boundaries rule out the loads straight into LDS.
+constexpr int kAnyRow = 80;   // LDS bytes to a row of 64: 16 rows' pieces in distinct banks
 template <class OUT, bool TR>
 __global__ __launch_bounds__(256) void product_any(Args a) {
-  constexpr int kStep = 64, kRow = kStep + 16;
-  __shared__ __attribute__((aligned(16))) int8_t la[64 * kRow], lb[64 * kRow];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_in_block();
+  __shared__ __attribute__((aligned(16))) int8_t lds[64 * 1024];
+  const int lane = threadIdx.x & (kWave - 1), wave = wave_in_block();
   const int64_t tiles_n = (a.N + 63) / 64;
   const int64_t m0 = int64_t(blockIdx.x) / tiles_n * 64, n0 = int64_t(blockIdx.x) % tiles_n * 64;
-  i32x4 acc[4];
+  int8_t* const la = lds + wave * 2 * 64 * kAnyRow;
+  int8_t* const lb = la + 64 * kAnyRow;
+  const int r = lane / 4, c = (lane % 4) * 16, g = lane >> 4, i16 = lane & 15;
+  const int64_t a_bytes = a.M * a.a_pitch, b_bytes = a.N * a.K;
+  const bool tiny = a_bytes < 16 || b_bytes < 16;
+  // Rows beyond the matrices are read as their last ones (their results are not stored, and the
+  // backward's a holds zeros there), so that every load is made: 8 of them under way, no branch.
+  int64_t row_a[4], row_b[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = i32x4{0, 0, 0, 0};
-  const int r = tid / 4, c = (tid % 4) * 16;
-  for (int64_t k0 = 0; k0 < a.K; k0 += kStep) {
-    u32x4 va = {0u, 0u, 0u, 0u}, vb = {0u, 0u, 0u, 0u};
-    if (m0 + r < a.M) va = row_piece(a.a + (m0 + r) * a.a_pitch, k0 + c, a.K);
-    if constexpr (TR) {
-      if (k0 + r < a.K) vb = row_piece(a.b + (k0 + r) * a.N, n0 + c, a.N);
-    } else {
-      if (n0 + r < a.N) vb = row_piece(a.b + (n0 + r) * a.K, k0 + c, a.K);
-    }
-    __syncthreads();
-    *reinterpret_cast<u32x4*>(la + r * kRow + c) = va;
-    if constexpr (TR) {
-      for (int i = 0; i < 16; ++i) lb[(c + i) * kRow + r] = int8_t(vb[i / 4] >> (8 * (i % 4)));
-    } else {
-      *reinterpret_cast<u32x4*>(lb + r * kRow + c) = vb;
-    }
-    __syncthreads();
-    const i32x4 fa = *reinterpret_cast<const i32x4*>(la + (wave * 16 + (lane & 15)) * kRow + (lane >> 4) * 16);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const i32x4 fb = *reinterpret_cast<const i32x4*>(lb + (j * 16 + (lane & 15)) * kRow + (lane >> 4) * 16);
-      acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb, fa, acc[j], 0, 0, 0);
-    }
+  for (int q = 0; q < 4; ++q) {
+    row_a[q] = std::min<int64_t>(m0 + q * 16 + r, a.M - 1) * a.a_pitch;
+    row_b[q] = TR ? 0 : std::min<int64_t>(n0 + q * 16 + r, a.N - 1) * a.K;
   }
-  // The lane holds row lane % 16 and columns 4 (lane / 16) + 0 .. 3 of each 16 x 16 results.
-  const int64_t m = m0 + wave * 16 + (lane & 15);
-  if (m >= a.M) return;
-  const float as = a.a_scale != nullptr ? a.a_scale[m] : 1.0f;
+  auto at_a = [&](int q, int64_t k0) { return row_a[q] + k0 + c; };
+  auto at_b = [&](int q, int64_t k0) {
+    return TR ? std::min<int64_t>(k0 + q * 16 + r, a.K - 1) * a.N + n0 + c : row_b[q] + k0 + c;
+  };
+  u32x4 va[4], vb[4];
+  auto load = [&](int64_t k0) {
+    if (tiny) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+      for (int q = 0; q < 4; ++q) {
+        va[q] = few_bytes(a.a, at_a(q, k0), a.K - k0 - c);
+        vb[q] = few_bytes(a.b, at_b(q, k0), TR ? a.N - n0 - c : a.K - k0 - c);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        va[q] = fetch(a.a, a_bytes, at_a(q, k0));
+        vb[q] = fetch(a.b, b_bytes, at_b(q, k0));
+      }
+    }
+  };
+  i32x4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  int64_t k0 = int64_t(wave) * 64;
+  if (k0 < a.K) load(k0);
+  for (; k0 < a.K; k0 += 256) {
+    // The step that ends the rows of both, or (TR) that holds rows of b within 16 bytes of its end:
+    // one of its last 17 rows, where it is one byte wide.
+    if (!tiny && k0 + (TR ? 80 : 64) >= a.K) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        va[q] = mend(va[q], a_bytes, at_a(q, k0), a.K - k0 - c);
+        vb[q] = mend(vb[q], b_bytes, at_b(q, k0), TR ? 16 : a.K - k0 - c);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      *reinterpret_cast<u32x4*>(la + (q * 16 + r) * kAnyRow + c) = va[q];
+      *reinterpret_cast<u32x4*>(lb + (q * 16 + r) * kAnyRow + c) = vb[q];
+    }
+    if (k0 + 256 < a.K) load(k0 + 256);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // written by this wave's other lanes
+    i32x4 fa[4], fb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      fa[i] = *reinterpret_cast<const i32x4*>(la + (i * 16 + i16) * kAnyRow + g * 16);
+      if constexpr (TR) {
+        const int8_t* p = lb + (16 * g + (i16 >> 1)) * kAnyRow + i * 16 + (i16 & 1) * 8;
+        const i32x2 lo = read_tr8(p), hi = read_tr8(p + 8 * kAnyRow);
+        fb[i] = i32x4{lo[0], lo[1], hi[0], hi[1]};
+      } else {
+        fb[i] = *reinterpret_cast<const i32x4*>(lb + (i * 16 + i16) * kAnyRow + g * 16);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is written over
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+  }
+  __syncthreads();
+  auto part = reinterpret_cast<i32x4 (*)[4][4][kWave]>(lds);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+  // The lane holds row lane % 16 and columns 4 (lane / 16) + 0 .. 3 of each 16 x 16 results.
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    i32x4 v = part[0][wave][j][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) v += part[w][wave][j][lane];
+    const int64_t m = m0 + wave * 16 + i16;
+    if (m >= a.M) return;
+    const float as = a.a_scale != nullptr ? a.a_scale[m] : 1.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int64_t n = n0 + j * 16 + (lane >> 4) * 4 + e;
+      const int64_t n = n0 + j * 16 + g * 4 + e;
       if (n < a.N) {
         const float sc = TR ? as : as * a.b_scale[n];
         const float more = TR ? (a.add != nullptr ? OUT::load1(a.add, m * a.N + n) : 0.0f)
                               : (a.bias != nullptr ? OUT::load1(a.bias, n) : 0.0f);
-        OUT::store1(a.y, m * a.N + n, __builtin_fmaf(float(acc[j][e]), sc, more));
+        OUT::store1(a.y, m * a.N + n, __builtin_fmaf(float(v[e]), sc, more));
       }
     }
+  }
 }
 
 template <class OUT, bool TR>
@@ -124,6 +221,40 @@ inline bool map_tiles(Args& a, int bm, int bn) {
   a.map = {uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles), uint32_t(tiles / kXcds),
            uint32_t((uint64_t(1) << 32) / uint64_t(tiles_n) - (tiles_n == 1))};
   return true;
+}
+
+// Estimated times, in us, by which a form is chosen. Tiles: full rounds of the resident blocks and a
+// partial one, in which a CU with one block (or two of three) is faster; the bytes of the weight and
+// the results. Rows forms: the chain of a wave's K steps, longer where a CU has several blocks, in
+// every further round of them, and with a weight that the caches do not hold; the bytes that all
+// blocks take in; a second kernel and the partial sums' bytes where K is split over blocks.
+struct TileCost {
+  float base, step_full, step_first, step_second, step_third, w_mb, out_mb;
+};
+template <class C>
+float tile_cost(int64_t M, int64_t N, int64_t K, int k_step, int cus, const TileCost& c) {
+  const int64_t tiles = ((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN), slots = int64_t(cus) * C::kBlocksPerCu;
+  const int64_t rest = tiles % slots;
+  const float per_step = c.step_full * float(tiles / slots) + c.step_first * float(rest > 0) +
+                         c.step_second * float(rest > cus) + c.step_third * float(rest > 2 * int64_t(cus));
+  return c.base + float((K + k_step - 1) / k_step) * per_step + c.w_mb * float(N) * float(K) * 1e-6f +
+         c.out_mb * float(M) * float(N) * 2e-6f;
+}
+struct RowsCost {
+  float base, chain, chain_second, chain_round, chain_w, mb, w_mb, out_mb, split, part_mb;
+};
+// blocks_per_cu: those that fit by their LDS.
+inline float rows_cost(int64_t M, int64_t N, int64_t K, int bm, int bn, int k_step, int blocks_per_cu, int shares, int cus,
+                       const RowsCost& c) {
+  const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), steps = (K + k_step - 1) / k_step;
+  const float chain = float(((steps + shares - 1) / shares + 3) / 4);   // 4 waves take the steps in turn
+  const float per_cu = float(tiles * shares) / float(cus), w_mb = float(N) * float(K) * 1e-6f;
+  const float rounds = std::ceil(per_cu / float(blocks_per_cu)) - 1.0f;
+  const float out = float(M) * float(N);
+  return c.base + chain * (c.chain + c.chain_second * float(per_cu > 1.0f) + c.chain_round * rounds +
+                           c.chain_w * std::min(w_mb, 64.0f)) +
+         c.mb * float(tiles) * float(steps) * float((bm + bn) * k_step) * 1e-6f + c.w_mb * w_mb + c.out_mb * out * 2e-6f +
+         (shares > 1 ? c.split + c.part_mb * float(shares) * out * 4e-6f : 0.0f);
 }
 
 }  // namespace lq8

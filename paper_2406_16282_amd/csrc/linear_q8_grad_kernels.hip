@@ -36,11 +36,6 @@ __device__ inline void store4(void* p, int64_t i, const float (&f)[4]) {
   else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = uint2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
 }
 
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-__device__ inline i32x2 read_tr8(const int8_t* p) {
-  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(p));
-}
 // Scheduling groups: DS LDS reads spread over the first half of MF MFMAs.
 template <int MF, int DS, int I = 0>
 __device__ inline void spread_reads() {
@@ -295,11 +290,12 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
   const int64_t M = a.M, N = a.N;
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = wave_in_block();
-  const uint32_t blk = blockIdx.x;
+  const uint32_t blk = blockIdx.x, split = blockIdx.y;
   const uint32_t id = (blk < a.map.per_xcd * kXcds) ? (blk % kXcds) * a.map.per_xcd + blk / kXcds : blk;
   const int64_t m0 = int64_t(id % a.map.tiles_m) * kRows, n0 = int64_t(id / a.map.tiles_m) * 64;
   const uint32_t rows_a = uint32_t(M - m0 < kRows ? M - m0 : kRows);
-  const int steps = int((a.K + kTrStep - 1) / kTrStep);
+  const int all_steps = int((a.K + kTrStep - 1) / kTrStep), first = int(split) * a.share;
+  const int steps = all_steps < first + a.share ? all_steps : first + a.share;   // this share's end
   constexpr int kStep = (kRows + 64) * kTrStep, kLoads = MT + 4;
   extern __shared__ __attribute__((aligned(16))) int8_t lds[];
   int8_t* const ring = lds + wave * D * kStep;
@@ -321,7 +317,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
   const uint64_t pa = reinterpret_cast<uint64_t>(a.a + m0 * a.a_pitch), pb = reinterpret_cast<uint64_t>(a.b + n0);
   auto load = [&](int step, int d) {
     const uint32_t S = ring_at + d * kStep;
-    const int64_t left = a.K - int64_t(step) * kTrStep;   // rows of b from this step on
+    const int64_t left = step < steps ? a.K - int64_t(step) * kTrStep : 0;   // rows of b from this step on
     const uint32_t rows_b = left <= 0 ? 0u : left < kTrStep ? uint32_t(left) : uint32_t(kTrStep);
     const u32x4 ra = rsrc_words(pa + uint64_t(step) * kTrStep, rows_b == 0 ? 0u : rows_a * uint32_t(a.a_pitch) - uint32_t(step) * kTrStep);
     const u32x4 rb = rsrc_words(pb + uint64_t(step) * kTrStep * uint64_t(N), rows_b == 0 ? 0u : rows_b * uint32_t(N) - uint32_t(n0));
@@ -337,9 +333,9 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int d = 0; d < D; ++d) load(wave + d * kWaves, d);   // steps past the end read zeros
+  for (int d = 0; d < D; ++d) load(first + wave + d * kWaves, d);   // steps past the end read zeros
   int d = 0;
-  for (int st = wave; st < steps; st += kWaves) {
+  for (int st = first + wave; st < steps; st += kWaves) {
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"((D - 1) * kLoads) : "memory");
     const int8_t* S = ring + d * kStep;
     i32x4 fa[MT], fb[NB];
@@ -381,6 +377,10 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
     for (int w = 1; w < kWaves; ++w) v += part[w][i][j][lane];
     const int64_t row = m0 + i * 16 + i16, col = n0 + j * 16 + g * 4;
     if (row >= M || col >= N) continue;   // N is a multiple of 16
+    if (a.part != nullptr) {
+      *reinterpret_cast<i32x4*>(a.part + (int64_t(split) * M + row) * N + col) = v;
+      continue;
+    }
     const float sc = a.a_scale[row];
     float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (a.add != nullptr) load4<OUT>(a.add, row * N + col, f);
@@ -390,25 +390,72 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
   }
 }
 
+// The shares' sums, added up in order (4 columns to a thread).
+template <class OUT>
+__global__ __launch_bounds__(256) void add_shares(Args a, int shares) {
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= a.M * a.N) return;
+  i32x4 v = {0, 0, 0, 0};
+  for (int p = 0; p < shares; ++p) v += *reinterpret_cast<const i32x4*>(a.part + int64_t(p) * a.M * a.N + i);
+  const float sc = a.a_scale[i / a.N];
+  float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (a.add != nullptr) load4<OUT>(a.add, i, f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf(float(v[e]), sc, f[e]);
+  store4<OUT>(a.y, i, f);
+}
+
 template <int MT, int D, class OUT>
-hipError_t launch_rows(Args a, int dev, hipStream_t s) {
+hipError_t launch_rows(Args a, int shares, hipStream_t s) {
   if (!map_tiles(a, MT * 16, 64)) return hipErrorInvalidValue;
-  const hipError_t e = allow_lds<product_tr_rows<MT, D, OUT>>(dev, kTrRowsLds<MT, D>);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((product_tr_rows<MT, D, OUT>), dim3(a.map.tiles), dim3(kRowsWaves * kWave), (kTrRowsLds<MT, D>), s, a);
+  const int steps = int((a.K + kTrStep - 1) / kTrStep);
+  a.share = (steps + shares - 1) / shares;
+  if (shares == 1) a.part = nullptr;
+  static_assert(kTrRowsLds<MT, D> <= 64 * 1024, "no more than is allowed without asking");
+  hipLaunchKernelGGL((product_tr_rows<MT, D, OUT>), dim3(a.map.tiles, unsigned(shares)), dim3(kRowsWaves * kWave),
+                     (kTrRowsLds<MT, D>), s, a);
+  if (shares > 1) {
+    const int64_t blocks = (a.M * a.N + 1023) / 1024;
+    hipLaunchKernelGGL((add_shares<OUT>), dim3(unsigned(blocks)), dim3(256), 0, s, a, shares);
+  }
   return hipGetLastError();
 }
 
 enum Form { kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
+struct Plan {
+  Form form;
+  int shares;   // of K, for the rows forms
+};
 
-Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
-  if (M <= 100) return kRows16;
-  auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  if (tiles(256, 256) >= 2 * cus) return kBig;
-  if (tiles(128, 256) >= cus) return kMid;
-  if (tiles(128, 128) >= cus) return kSmall;
-  if (tiles(64, 128) >= cus) return kLow;
-  return kRows32;
+constexpr RowsCost kRows16Cost = {2.625f, 0.2748f, 0.2102f, 0.6503f, 0.002209f, 0.02494f, 0.1602f, 0.6891f, 2.522f, 0.6569f};
+constexpr RowsCost kRows32Cost = {3.002f, 0.3285f, 0.2874f, 0.6502f, 0.002858f, 0.0204f, 0.1366f, 0.5392f, 2.5f, 0.5556f};
+constexpr RowsCost kRows64Cost = {3.865f, 0.44f, 0.4022f, 0.6351f, 0.004338f, 0.01361f, 0.08103f, 0.5614f, 2.518f, 0.5743f};
+constexpr TileCost kLowCost = {3.546f, 0.5144f, 0.2777f, 0.1192f, 0.1853f, 0.01071f, 0.2907f};
+constexpr TileCost kSmallCost = {4.609f, 0.546f, 0.3394f, 0.1923f, 0, 0, 0.2672f};
+constexpr TileCost kMidCost = {6.925f, 0.8417f, 0.492f, 0.3107f, 0, 0, 0.2087f};
+constexpr TileCost kBigCost = {7.826f, 0.8177f, 0.7358f, 0, 0, 0, 0.2235f};
+
+// The form by the estimates (linear_q8_device.hpp); the partial sums of a split K stay below 32 MiB.
+Plan make_plan(int64_t M, int64_t N, int64_t K, int cus) {
+  Plan best{kLow, 1};
+  float least = tile_cost<LowTile>(M, N, K, kTrStep, cus, kLowCost);
+  auto take = [&](Form f, int shares, float t) {
+    if (t < least) {
+      least = t;
+      best = {f, shares};
+    }
+  };
+  take(kSmall, 1, tile_cost<SmallTile>(M, N, K, kTrStep, cus, kSmallCost));
+  take(kMid, 1, tile_cost<MidTile>(M, N, K, kTrStep, cus, kMidCost));
+  take(kBig, 1, tile_cost<BigTile>(M, N, K, kTrStep, cus, kBigCost));
+  if (M > 1024) return best;
+  for (int shares = 1; shares <= 8; shares *= 2) {
+    if (shares > 1 && (K < 1024 || int64_t(shares) * M * N * 4 > (int64_t(32) << 20))) break;
+    take(kRows16, shares, rows_cost(M, N, K, 16, 64, kTrStep, 4, shares, cus, kRows16Cost));
+    take(kRows32, shares, rows_cost(M, N, K, 32, 64, kTrStep, 3, shares, cus, kRows32Cost));
+    take(kRows64, shares, rows_cost(M, N, K, 64, 64, kTrStep, 2, shares, cus, kRows64Cost));
+  }
+  return best;
 }
 
 template <class OUT>
@@ -420,10 +467,11 @@ hipError_t launch(const Args& a, hipStream_t s) {
   int dev = 0, cus = 0;
   const hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;
-  switch (choose_form(a.M, a.N, a.K, cus)) {
-    case kRows16: return launch_rows<1, 2, OUT>(a, dev, s);
-    case kRows32: return launch_rows<2, 2, OUT>(a, dev, s);
-    case kRows64: return launch_rows<4, 2, OUT>(a, dev, s);
+  const Plan plan = make_plan(a.M, a.N, a.K, cus);
+  switch (plan.form) {
+    case kRows16: return launch_rows<1, 2, OUT>(a, plan.shares, s);
+    case kRows32: return launch_rows<2, 2, OUT>(a, plan.shares, s);
+    case kRows64: return launch_rows<4, 2, OUT>(a, plan.shares, s);
     case kLow: return launch_tile<LowTile, OUT>(a, dev, cus, s);
     case kSmall: return launch_tile<SmallTile, OUT>(a, dev, cus, s);
     case kMid: return launch_tile<MidTile, OUT>(a, dev, cus, s);
@@ -433,12 +481,17 @@ hipError_t launch(const Args& a, hipStream_t s) {
 
 // Rows of p start on 128-byte lines and are padded with zeros to whole K steps.
 int64_t pitch_of(int64_t n) { return (n + 127) / 128 * 128; }
+size_t part_at(int64_t m, int64_t n) { return (size_t(m) * size_t(pitch_of(n)) + size_t(m) * 4 + 15) / 16 * 16; }
 
 }  // namespace tr
 }  // namespace lq8
 
-size_t linear_q8_bwd_workspace(int64_t M, int64_t N) {
-  return size_t(M) * size_t(lq8::tr::pitch_of(N)) + size_t(M) * 4;
+// p, its scales, and the sums of the shares, 16-byte aligned.
+size_t linear_q8_bwd_workspace(int64_t M, int64_t N, int64_t K) {
+  int dev = 0, cus = 256;
+  if (current_device(dev, cus) != hipSuccess) cus = 256;   // no device here
+  const lq8::tr::Plan plan = lq8::tr::make_plan(M, K, N, cus);
+  return lq8::tr::part_at(M, N) + (plan.shares > 1 ? size_t(plan.shares) * size_t(M) * size_t(K) * 4 : 0);
 }
 
 hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
@@ -450,7 +503,8 @@ hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, i
     const hipError_t e = launch_q8_rows(bf16, M, N, pitch, dy, w_scale, p, p_scale, s);
     if (e != hipSuccess) return e;
   }
-  const lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, true, {}};
+  const lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, true,
+                    reinterpret_cast<int32_t*>(p + lq8::tr::part_at(M, N)), 0, {}};
   return dx_bf16 ? lq8::tr::launch<BF16>(a, s) : lq8::tr::launch<F32>(a, s);
 }
 

@@ -385,26 +385,31 @@ hipError_t launch_rows(Args a, int dev, hipStream_t s) {
   return hipGetLastError();
 }
 
-// One or two rows: a wave takes one row of W, 1 KiB at a time (16 bytes to a lane), against the
-// same pieces of all MT rows of x, and adds up its lanes' sums at the end.
+// One or two rows: a wave takes R rows of W, 1 KiB of each at a time (16 bytes to a lane), against
+// the same pieces of all MT rows of x, and adds up its lanes' sums at the end.
 constexpr int kFewWaves = 4;
-template <int MT, class OUT>
+template <int MT, int R, class OUT>
 __global__ __launch_bounds__(kFewWaves * kWave) void product_few(Args a) {
-  constexpr int kDeep = 4;   // pieces of a row in flight
+  constexpr int kDeep = R > 1 ? 4 / R : 4;   // pieces of a row in flight
   const uint32_t K = uint32_t(a.K);
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t n = int64_t(blockIdx.x) * kFewWaves + wave_in_block();
-  if (n >= a.N) return;
-  const auto rb = make_rsrc(a.b + n * K, K), ra = make_rsrc(a.a, a.M * K);
-  int sum[MT];
+  const int64_t n0 = (int64_t(blockIdx.x) * kFewWaves + wave_in_block()) * R;
+  if (n0 >= a.N) return;
+  const int rows_b = a.N - n0 < R ? int(a.N - n0) : R;
+  const auto rb = make_rsrc(a.b + n0 * K, int64_t(rows_b) * K), ra = make_rsrc(a.a, a.M * K);
+  int sum[R][MT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) sum[i] = 0;
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sum[r][i] = 0;
   for (uint32_t k0 = 0; k0 < K; k0 += kDeep * 1024) {
-    u32x4 w[kDeep], x[kDeep][MT];
+    u32x4 w[kDeep][R], x[kDeep][MT];
 #pragma unroll
     for (int p = 0; p < kDeep; ++p) {
       const uint32_t k = k0 + p * 1024 + lane * 16;
-      w[p] = __builtin_amdgcn_raw_buffer_load_b128(rb, k < K ? k : kOutOfRange, 0, 2);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        w[p][r] = __builtin_amdgcn_raw_buffer_load_b128(rb, k < K ? r * K + k : kOutOfRange, 0, 2);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
         x[p][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, k < K ? i * K + k : kOutOfRange, 0, 0);
@@ -412,39 +417,63 @@ __global__ __launch_bounds__(kFewWaves * kWave) void product_few(Args a) {
 #pragma unroll
     for (int p = 0; p < kDeep; ++p)
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[i] = __builtin_amdgcn_sdot4(int(w[p][e]), int(x[p][i][e]), sum[i], false);
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sum[r][i] = __builtin_amdgcn_sdot4(int(w[p][r][e]), int(x[p][i][e]), sum[r][i], false);
   }
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
+  for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) sum[i] += __shfl_xor(sum[i], off, kWave);
-    if (lane == i && i < a.M)
-      OUT::store1(a.y, i * a.N + n,
-                  __builtin_fmaf(float(sum[i]), a.a_scale[i] * a.b_scale[n], a.bias != nullptr ? OUT::load1(a.bias, n) : 0.0f));
-  }
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) sum[r][i] += __shfl_xor(sum[r][i], off, kWave);
+      const int64_t n = n0 + r;
+      if (lane == r * MT + i && i < a.M && n < a.N)
+        OUT::store1(a.y, i * a.N + n,
+                    __builtin_fmaf(float(sum[r][i]), a.a_scale[i] * a.b_scale[n],
+                                   a.bias != nullptr ? OUT::load1(a.bias, n) : 0.0f));
+    }
 }
 
 template <int MT, class OUT>
 hipError_t launch_few(const Args& a, hipStream_t s) {
-  hipLaunchKernelGGL((product_few<MT, OUT>), dim3(unsigned((a.N + kFewWaves - 1) / kFewWaves)), dim3(kFewWaves * kWave), 0,
-                     s, a);
-  return hipGetLastError();
+  auto launch = [&](auto kernel, int rows) {
+    const int64_t per = int64_t(kFewWaves) * rows;
+    hipLaunchKernelGGL(kernel, dim3(unsigned((a.N + per - 1) / per)), dim3(kFewWaves * kWave), 0, s, a);
+    return hipGetLastError();
+  };
+  if (a.K <= 1024) return launch(product_few<MT, 4, OUT>, 4);
+  if (a.K <= 2048 || MT > 1) return launch(product_few<MT, 2, OUT>, 2);
+  return launch(product_few<MT, 1, OUT>, 1);
 }
 
 enum Form { kFew, kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
 
+constexpr RowsCost kRows16Cost = {2.685f, 0.2485f, 0.2127f, 0.578f, 0.001916f, 0.009501f, 0.0643f, 1.986f, 0, 0};
+constexpr RowsCost kRows32Cost = {3.018f, 0.2897f, 0.338f, 0.4889f, 0.003409f, 0.009262f, 0.04509f, 1.318f, 0, 0};
+constexpr RowsCost kRows64Cost = {3.573f, 0.4323f, 0.1489f, 0.6175f, 0.003602f, 0.005212f, 0.01158f, 2.154f, 0, 0};
+constexpr TileCost kLowCost = {3.156f, 0.8615f, 0.3726f, 0.1655f, 0.3679f, 0.08068f, 0.2468f};
+constexpr TileCost kSmallCost = {3.676f, 0.8739f, 0.4877f, 0.312f, 0, 0.05597f, 0.2539f};
+constexpr TileCost kMidCost = {4.706f, 1.471f, 0.7827f, 0.561f, 0, 0.08527f, 0.2501f};
+constexpr TileCost kBigCost = {5.923f, 1.435f, 1.257f, 0, 0, 0.003937f, 0.2741f};
+
 Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
   if (M <= 2) return kFew;
-  if (M <= 32) return kRows16;
-  if (M <= 64) return kRows32;
-  if (M <= 160) return kRows64;
-  auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  if (tiles(256, 256) >= 2 * cus) return kBig;
-  if (tiles(128, 256) >= cus) return kMid;
-  if (tiles(128, 128) >= cus) return kSmall;
-  return kLow;
+  auto rows = [&](int bm, int blocks_per_cu, const RowsCost& c) {
+    return M <= 2048 ? rows_cost(M, N, K, bm, 32, kBK, blocks_per_cu, 1, cus, c) : INFINITY;
+  };
+  const float t[kForms] = {INFINITY,
+                           rows(16, 3, kRows16Cost),
+                           rows(32, 2, kRows32Cost),
+                           rows(64, 1, kRows64Cost),
+                           tile_cost<LowTile>(M, N, K, kBK, cus, kLowCost),
+                           tile_cost<SmallTile>(M, N, K, kBK, cus, kSmallCost),
+                           tile_cost<MidTile>(M, N, K, kBK, cus, kMidCost),
+                           tile_cost<BigTile>(M, N, K, kBK, cus, kBigCost)};
+  return Form(std::min_element(t, t + kForms) - t);
 }
 
 template <class OUT>
@@ -475,7 +504,7 @@ hipError_t launch_fwd(const Args& a, hipStream_t s) {
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
                                 const int8_t* w, const float* w_scale, const void* bias, void* y, hipStream_t s) {
   const bool vec = reinterpret_cast<uintptr_t>(y) % 16 == 0 && N * (bf16 ? 2 : 4) % 16 == 0;
-  const lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, vec, {}};
+  const lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, vec, nullptr, 0, {}};
   return bf16 ? lq8::launch_fwd<BF16>(a, s) : lq8::launch_fwd<F32>(a, s);
 }
 

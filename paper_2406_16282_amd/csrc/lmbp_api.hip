@@ -709,7 +709,7 @@ lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const 
 }
 size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k) {
   if (m <= 0 || k <= 0 || bad_layer(m, n, k) || n > lmbp::kQ8MaxDepth) return 0;
-  return lmbp::linear_q8_bwd_workspace(m, n);
+  return lmbp::linear_q8_bwd_workspace(m, n, k);
 }
 lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n, int64_t k, const void* dy,
                           const int8_t* w, const float* w_scale, const void* add, void* dx, void* workspace,

@@ -127,7 +127,7 @@ hipError_t launch_msrms_q8_bwd(bool dz_bf16, bool bf16, int64_t rows, int64_t co
 constexpr int64_t kQ8MaxDepth = 131071;
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
                                 const int8_t* w, const float* w_scale, const void* bias, void* y, hipStream_t s);
-size_t linear_q8_bwd_workspace(int64_t M, int64_t N);
+size_t linear_q8_bwd_workspace(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
                                 const float* w_scale, const void* add, void* dx, void* workspace, hipStream_t s);
 

@@ -474,7 +474,7 @@ hipError_t launch_fwd(const FwdArgs& a, hipStream_t s) {
     const hipError_t e = current_device(dev, cus);
     if (e != hipSuccess) return e;
   }
-  const bool held = a.cols < (1 << 24) && with_shape<8>(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
+  const bool held = a.cols < (1 << 24) && with_shape<MODE == kColumns && IO::kPerVec == 8 ? 4 : 8>(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
     blocks = blocks_of<W>(a.rows);
     if (MODE == kColumns) blocks = std::min<int64_t>(blocks, int64_t(cus) * (1024 / block_of<W>()));

@@ -20,7 +20,7 @@ U = 2.0 ** -24
 TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
 
 # (m, n, k): every remainder of tiles and vectors, single rows and columns, long sums
-SIZES = [(1, 1, 1), (1, 16, 16), (2, 3, 5), (1, 4096, 512), (3, 1001, 1023), (7, 48, 64), (16, 64, 256), (17, 80, 272),
+SIZES = [(3, 5, 65), (4, 1, 130), (2, 7, 193), (5, 3, 67), (70, 15, 66), (1, 1, 1), (1, 16, 16), (2, 3, 5), (1, 4096, 512), (3, 1001, 1023), (7, 48, 64), (16, 64, 256), (17, 80, 272),
          (31, 2048, 1040), (33, 24, 48), (64, 130, 257), (65, 1000, 4096), (100, 272, 11008), (127, 255, 129),
          (128, 256, 128), (129, 257, 144), (200, 768, 768), (256, 512, 1024), (257, 528, 1024), (333, 1001, 1023),
          (513, 1040, 2064), (700, 96, 131056), (1000, 8, 32), (1025, 2064, 528), (2100, 4112, 784)]
