@@ -358,14 +358,17 @@ lmbp_status msrms_q8_bwd(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t 
  *   q [m x k], w [n x k]: any values; scale [m], w_scale [n]; bias [n] or NULL; y, dy [m x n];
  *            add, dx [m x k], add NULL for none; dx == add is allowed (the sum of several
  *            layers' gradients).
- *   workspace : lmbp_linear_q8_bwd_bytes(m, n, k) bytes, 16-byte aligned. Its contents do
- *            not matter before or after.
- * q and w with k a multiple of 16 on 16-byte aligned pointers take the fast path, anything
- * else a slower one with the same results. No other output overlaps another buffer.
+ *   workspace : lmbp_linear_q8_fwd_bytes / lmbp_linear_q8_bwd_bytes(m, n, k) bytes on the
+ *            calling thread's current device, 16-byte aligned, NULL if that is 0. Its contents
+ *            do not matter before or after.
+ * k a multiple of 16 and 16-byte aligned q, w and results are the fast case, anything else
+ * slower with the same results. No other output overlaps another buffer.
  * ------------------------------------------------------------------------ */
 lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t *q,
                           const float *scale, const int8_t *w, const float *w_scale,
-                          const void *bias, void *y, void *stream);
+                          const void *bias, void *y, void *workspace, int64_t workspace_bytes,
+                          void *stream);
+size_t lmbp_linear_q8_fwd_bytes(int64_t m, int64_t n, int64_t k);
 size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k);
 lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n, int64_t k,
                           const void *dy, const int8_t *w, const float *w_scale,
@@ -380,9 +383,15 @@ lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n,
  *                      that one block computes. -1 for sizes that run nothing.
  *   lmbp_linear_grad_form : 0 .. 2 tiles of 256 x 256, 128 x 256, 128 x 128; *splits (or
  *                      NULL): the shares of the rows; *rounds (or NULL): as above.
+ *   lmbp_linear_q8_form : the 8-bit layers' forward, or (grad) input gradient, on 16-byte
+ *                      aligned tensors: 0 dot products (forward), 1 .. 3 split-K with 16, 32,
+ *                      64 rows to a block, 4 .. 7 tiles of 64 x 128, 128 x 128, 128 x 256,
+ *                      256 x 256, 8 the general form; *shares (or NULL): the blocks that share
+ *                      a sum; *copies (or NULL): 1 if rows are copied to aligned ones first.
  * ------------------------------------------------------------------------ */
 int lmbp_linear_form(int64_t m, int64_t n, int64_t k, int gated, int64_t *rounds);
 int lmbp_linear_grad_form(int64_t m, int64_t n, int64_t k, int64_t *splits, int64_t *rounds);
+int lmbp_linear_q8_form(int64_t m, int64_t n, int64_t k, int grad, int64_t *shares, int64_t *copies);
 
 /* ------------------------------------------------------------------------
  * Measurement utility (not part of the method): copies `bytes` bytes from src

@@ -112,11 +112,12 @@ def lib():
     L.q8_rows.argtypes = L.q8_values.argtypes = [i32, i64, i64, vp, vp, vp, vp]
     L.msrms_q8_fwd.argtypes = [i32, i64, i64, f32, vp, vp, vp, vp, vp, vp, vp]
     L.msrms_q8_bwd.argtypes = [i32, i32, i64, i64, vp, vp, vp, vp, vp, vp, vp]
-    L.linear_q8_fwd.argtypes = [i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
-    L.lmbp_linear_q8_bwd_bytes.argtypes = [i64, i64, i64]
-    L.lmbp_linear_q8_bwd_bytes.restype = ctypes.c_size_t
+    L.linear_q8_fwd.argtypes = [i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.lmbp_linear_q8_fwd_bytes.argtypes = L.lmbp_linear_q8_bwd_bytes.argtypes = [i64, i64, i64]
+    L.lmbp_linear_q8_fwd_bytes.restype = L.lmbp_linear_q8_bwd_bytes.restype = ctypes.c_size_t
     L.linear_q8_bwd.argtypes = [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
-    for name in Q8_OPS:
+    L.lmbp_linear_q8_form.argtypes = [i64, i64, i64, i32, counts, counts]
+    for name in (*Q8_OPS, "lmbp_linear_q8_form"):
         getattr(L, name).restype = i32
     L.lmbp_copy.argtypes = [vp, vp, i64, vp]
     L.lmbp_copy.restype = i32
@@ -144,7 +145,7 @@ def _bind_fast(L):
                       "`python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning, stacklevel=3)
         return
     for name in (*ACT_OPS, *NORM_OPS, *GLU_OPS, "linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd",
-                 "msrms_linear_swiglu_fwd", *Q8_OPS, "lmbp_linear_q8_bwd_bytes"):
+                 "msrms_linear_swiglu_fwd", *Q8_OPS, "lmbp_linear_q8_fwd_bytes", "lmbp_linear_q8_bwd_bytes"):
         _address[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
     _fast = module
 
@@ -870,7 +871,8 @@ def linear_q8_fwd(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=
     (one scale per output channel): y = (q w^T) scale w_scale + bias in ``dtype``, the sums
     exact. bias [n] of that dtype or None."""
     if _fast is not None and stream is None and dtype in _CODES:
-        out = _fast.linear_q8_fwd(_address["linear_q8_fwd"], _CODES[dtype], q, scale, w, w_scale, bias)
+        out = _fast.linear_q8_fwd(_address["linear_q8_fwd"], _address["lmbp_linear_q8_fwd_bytes"], _CODES[dtype], q, scale, w,
+                                  w_scale, bias)
         if out is not None:
             return _done("linear_q8_fwd", out)
     _q8_in(q, q, "q")
@@ -884,9 +886,13 @@ def linear_q8_fwd(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=
         if bias.dtype != dtype or bias.numel() != n:
             raise ValueError(f"bias must be a {dtype} tensor of n elements")
     y = torch.empty((*q.shape[:-1], n), dtype=dtype, device=q.device)
+    L = lib()
     with _device_of(q):   # launches go to the tensors' GPU
-        _check("linear_q8_fwd", lib().linear_q8_fwd(_dtype_code(y), m, n, k, _ptr(q), _ptr(scale), _ptr(w), _ptr(w_scale),
-                                                    _opt(bias), _ptr(y), _stream(q, stream)))
+        nbytes = L.lmbp_linear_q8_fwd_bytes(m, n, k)
+        handle = _stream(q, stream)
+        work = _workspace(nbytes, q, stream) if nbytes else None
+        _check("linear_q8_fwd", L.linear_q8_fwd(_dtype_code(y), m, n, k, _ptr(q), _ptr(scale), _ptr(w), _ptr(w_scale),
+                                                _opt(bias), _ptr(y), _opt(work), nbytes, handle))
     return y
 
 

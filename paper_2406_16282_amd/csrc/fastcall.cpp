@@ -489,32 +489,35 @@ bool q8_weight(PyObject* ow, PyObject* os, const at::Tensor& like, at::Tensor& w
          f32_of(os, like, w.size(0), w_scale);
 }
 
-// (function, type, q, scale, w, w_scale, bias or None) -> y
+// (function, the workspace's size function, type, q, scale, w, w_scale, bias or None) -> y
 PyObject* linear_q8_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   at::Tensor q, scale, w, w_scale, b;
   int64_t m, k;
   at::IntArrayRef lead;
-  if (n != 7 || !plain(a[2], q) || q.scalar_type() != at::kChar || !rows_of(q, m, k, lead) || !on_current_device(q) ||
-      !f32_of(a[3], q, m, scale) || !q8_weight(a[4], a[5], q, w, w_scale) || w.size(1) != k)
+  if (n != 8 || !plain(a[3], q) || q.scalar_type() != at::kChar || !rows_of(q, m, k, lead) || !on_current_device(q) ||
+      !f32_of(a[4], q, m, scale) || !q8_weight(a[5], a[6], q, w, w_scale) || w.size(1) != k)
     Py_RETURN_NONE;
-  const int dt = int(PyLong_AsLong(a[1]));
-  if (a[6] != Py_None && (!plain(a[6], b) || b.scalar_type() != type_of(dt) || b.numel() != w.size(0) ||
+  const int dt = int(PyLong_AsLong(a[2]));
+  if (a[7] != Py_None && (!plain(a[7], b) || b.scalar_type() != type_of(dt) || b.numel() != w.size(0) ||
                           b.device() != q.device()))
     Py_RETURN_NONE;
   void* s;
   if (!stream_of(q, s)) return nullptr;
   c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
   shape.push_back(w.size(0));
-  at::Tensor y;
+  at::Tensor y, work;
   const auto f = address<int (*)(int, int64_t, int64_t, int64_t, const void*, const void*, const void*, const void*,
-                                 const void*, void*, void*)>(a[0]);
+                                 const void*, void*, void*, int64_t, void*)>(a[0]);
+  const auto bytes_of = address<size_t (*)(int64_t, int64_t, int64_t)>(a[1]);
   int status;
   {
     NoGil released;
+    const int64_t bytes = int64_t(bytes_of(m, w.size(0), k));
+    if (bytes > 0) work = at::empty({bytes}, q.options().dtype(at::kByte));
     y = at::empty(shape, q.options().dtype(type_of(dt)));
     status = f(dt, m, w.size(0), k, q.data_ptr(), scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
-               b.defined() ? b.data_ptr() : nullptr, y.data_ptr(), s);
+               b.defined() ? b.data_ptr() : nullptr, y.data_ptr(), bytes > 0 ? work.data_ptr() : nullptr, bytes, s);
   }
   return result(status, y);
   END_HANDLE_TH_ERRORS

@@ -32,12 +32,20 @@ struct Args {
   const void* bias;       // forward: per column, of the result's type, or null
   const void* add;        // input gradient: [M x N] of the result's type, or null; may be y
   void* y;                // [M x N]
-  int64_t M, N, K, a_pitch;
-  bool vec;               // forward: y takes 16-byte stores
+  int64_t M, N, K, a_pitch, b_pitch;   // bytes from one row to the next
   int32_t* part;          // input gradient: [splits][M x N] sums over shares of K, or null
   int32_t share;          // steps of K to a share
   TileMap map;
 };
+
+// 16 and 8 bytes at any element's address (global memory takes such accesses).
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+__device__ inline void store_16(void* p, const u32x4& v) { *static_cast<u32x4_at2*>(p) = v; }
+template <class IO>
+__device__ inline char* elem(const void* p, int64_t i) {
+  return const_cast<char*>(static_cast<const char*>(p)) + i * IO::kBytes;
+}
 
 // 16 bytes of a matrix of `total` bytes (16 at least) from byte `at` on, at any alignment; those
 // that start less than 16 before its end are read from 16 before its end (mend shifts them).
@@ -221,6 +229,42 @@ inline bool map_tiles(Args& a, int bm, int bn) {
   a.map = {uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles), uint32_t(tiles / kXcds),
            uint32_t((uint64_t(1) << 32) / uint64_t(tiles_n) - (tiles_n == 1))};
   return true;
+}
+
+// Rows of `cols` bytes at any address, copied to rows `pitch` (a multiple of 16) bytes apart with
+// zeros behind them: those of `src`, then those of `src2`. A wave to a row.
+__global__ inline __launch_bounds__(256) void pad_rows(const int8_t* src, int64_t rows, const int8_t* src2, int64_t rows2,
+                                                       int64_t cols, int8_t* dst, int64_t pitch) {
+  int64_t row = int64_t(blockIdx.x) * 4 + wave_in_block();
+  if (row >= rows + rows2) return;
+  int8_t* const to = dst + row * pitch;
+  if (row >= rows) {
+    row -= rows;
+    src = src2;
+    rows = rows2;
+  }
+  const int64_t total = rows * cols;
+  for (int64_t k = int64_t(threadIdx.x & (kWave - 1)) * 16; k < pitch; k += kWave * 16) {
+    const int64_t at = row * cols + k;
+    const u32x4 v = total < 16 ? few_bytes(src, at, cols - k) : mend(fetch(src, total, at), total, at, cols - k);
+    *reinterpret_cast<u32x4*>(to + k) = v;
+  }
+}
+inline hipError_t launch_pad(const int8_t* src, int64_t rows, const int8_t* src2, int64_t rows2, int64_t cols, int8_t* dst,
+                             int64_t pitch, hipStream_t s) {
+  const int64_t blocks = (rows + rows2 + 3) / 4;
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(pad_rows, dim3(unsigned(blocks)), dim3(256), 0, s, src, rows, src2, rows2, cols, dst, pitch);
+  return hipGetLastError();
+}
+inline int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+// Whether rows of k bytes that are no multiple of 16 are worth a copy to ones that are: `fast` is the
+// estimated time of the product after it, `copied` the rows. The general form takes a chain of K
+// steps and 450 TOPS, the copy a launch and 3 TB/s.
+inline bool pad_pays(int64_t M, int64_t N, int64_t K, int64_t copied, int64_t k, float fast) {
+  const float any = 5.5f + 0.65f * float((K + 255) / 256) + float(M) * float(N) * float(K) * (2.0f / 450e6f);
+  return fast + 2.5f + float(copied) * float(k) * (1.0f / 3e6f) < any;
 }
 
 // Estimated times, in us, by which a form is chosen. Tiles: full rounds of the resident blocks and a

@@ -17,23 +17,51 @@ using lin::lds_addr;
 using lin::load_lds16_asm;
 using lin::rsrc_words;
 
-// 4 consecutive elements from a multiple of 4 on, of a 16-byte aligned tensor.
+// 4 consecutive elements at any element's address.
 template <class IO>
 __device__ inline void load4(const void* p, int64_t i, float (&f)[4]) {
   if constexpr (IO::kBytes == 4) {
-    F32::unpack(*reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + i), f);
+    F32::unpack(*reinterpret_cast<const u32x4_at2*>(elem<IO>(p, i)), f);
   } else {
-    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-    f[0] = __uint_as_float(v.x << 16);
-    f[1] = __uint_as_float(v.x & 0xffff0000u);
-    f[2] = __uint_as_float(v.y << 16);
-    f[3] = __uint_as_float(v.y & 0xffff0000u);
+    const u32x2_at2 v = *reinterpret_cast<const u32x2_at2*>(elem<IO>(p, i));
+    f[0] = __uint_as_float(v[0] << 16);
+    f[1] = __uint_as_float(v[0] & 0xffff0000u);
+    f[2] = __uint_as_float(v[1] << 16);
+    f[3] = __uint_as_float(v[1] & 0xffff0000u);
   }
 }
 template <class IO>
 __device__ inline void store4(void* p, int64_t i, const float (&f)[4]) {
-  if constexpr (IO::kBytes == 4) *reinterpret_cast<u32x4*>(static_cast<float*>(p) + i) = F32::pack(f);
-  else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = uint2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+  if constexpr (IO::kBytes == 4) store_16(elem<IO>(p, i), F32::pack(f));
+  else *reinterpret_cast<u32x2_at2*>(elem<IO>(p, i)) = u32x2_at2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+}
+
+// Results of a row at 4 columns from `col` on, f = sum * scale + add; columns from N on are 0.
+template <class OUT>
+__device__ inline void results4(const Args& a, int64_t row, int64_t col, const i32x4& v, float sc, float (&f)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = 0.0f;
+  if (a.add != nullptr) {
+    if (col + 4 <= a.N) load4<OUT>(a.add, row * a.N + col, f);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = col + e < a.N ? OUT::load1(a.add, row * a.N + col + e) : 0.0f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf(float(v[e]), sc, f[e]);
+}
+// The same, stored.
+template <class OUT>
+__device__ inline void finish4(const Args& a, int64_t row, int64_t col, const i32x4& v, float sc) {
+  float f[4];
+  results4<OUT>(a, row, col, v, sc, f);
+  if (col + 4 <= a.N) {
+    store4<OUT>(a.y, row * a.N + col, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.N) OUT::store1(a.y, row * a.N + col + e, f[e]);
+  }
 }
 
 // Scheduling groups: DS LDS reads spread over the first half of MF MFMAs.
@@ -70,6 +98,7 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
   constexpr int kLA = C::kLA, kLB = C::kLB, kL = kLA + kLB, kRing = C::kRing, kSlot = C::kSlot;
   constexpr int kUnits = BN / 16;   // 16-byte units in a row of b's slot
   const int64_t M = a.M, N = a.N;
+  const uint32_t pitch = uint32_t(a.b_pitch);
   extern __shared__ __attribute__((aligned(16))) int8_t lds[];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = wave_in_block();
@@ -88,14 +117,14 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
 #pragma unroll
   for (int q = 0; q < kLB; ++q) {
     const int p = (wave + kWaves * q) * 64 + lane, r = p / kUnits;
-    ld_b[q] = uint32_t(r) * uint32_t(N) + ((p % kUnits) ^ swz_b(r)) * 16;
+    ld_b[q] = uint32_t(r) * pitch + ((p % kUnits) ^ swz_b(r)) * 16;
   }
   // Load cursor: slots of the tile still to load.
   uint32_t l_tile = blockIdx.x;
   int l_slots = 0;
   uint64_t pa = 0, pb = 0;
   uint32_t na = 0, nb = 0;   // records: bytes in range
-  const uint32_t nb_step = uint32_t(kTrStep * N);
+  const uint32_t nb_step = kTrStep * pitch;
   const int last_rows = int(a.K - int64_t(steps - 1) * kTrStep);
   auto enter = [&]() {
     uint32_t tm = 0, tn = 0;
@@ -106,7 +135,7 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
     pa = reinterpret_cast<uint64_t>(a.a + m0 * a.a_pitch);
     pb = reinterpret_cast<uint64_t>(a.b + n0);
     na = in ? (left < uint32_t(BM) ? left : uint32_t(BM)) * uint32_t(a.a_pitch) : 0u;
-    nb = in ? uint32_t(steps == 1 ? last_rows : kTrStep) * uint32_t(N) - uint32_t(n0) : 0u;
+    nb = in ? uint32_t(steps == 1 ? last_rows : kTrStep) * pitch - uint32_t(n0) : 0u;
     l_slots = in ? steps : 0x7fffffff;
   };
   auto load = [&](uint32_t S, int q) {
@@ -121,7 +150,7 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
       pa += kTrStep;
       na -= kTrStep;   // the rows are padded to whole slots
       pb += nb_step;
-      if (l_slots == 1) nb -= uint32_t(kTrStep - last_rows) * uint32_t(N);
+      if (l_slots == 1) nb -= uint32_t(kTrStep - last_rows) * pitch;
     }
   };
 
@@ -225,26 +254,16 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
       const float sc = row < M ? a.a_scale[row] : 0.0f;
       if constexpr (OUT::kBytes == 4) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int64_t col = n0 + j * 16 + (lane_e >> 4) * 4;
-          const bool ok = row < M && col < N;
-          float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (ok && a.add != nullptr) load4<OUT>(a.add, row * N + col, f);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf(float(acc[i][j][e]), sc, f[e]);
-          if (ok) store4<OUT>(a.y, row * N + col, f);
-        }
+        for (int j = 0; j < TN; ++j)
+          if (row < M) finish4<OUT>(a, row, n0 + j * 16 + (lane_e >> 4) * 4, acc[i][j], sc);
       } else {   // neighbouring lane groups exchange halves: 8 consecutive columns to a lane
 #pragma unroll
         for (int j = 0; j < TN; j += 2) {
           uint32_t v[2][2];
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const int64_t at = n0 + (j + t) * 16 + (lane_e >> 4) * 4;
             float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (a.add != nullptr && row < M && at < N) load4<OUT>(a.add, row * N + at, f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf(float(acc[i][j + t][e]), sc, f[e]);
+            if (row < M) results4<OUT>(a, row, n0 + (j + t) * 16 + (lane_e >> 4) * 4, acc[i][j + t], sc, f);
             v[t][0] = pack_bf16x2(f[0], f[1]);
             v[t][1] = pack_bf16x2(f[2], f[3]);
           }
@@ -252,8 +271,16 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
           const auto s1 = __builtin_amdgcn_permlane16_swap(v[0][1], v[1][1], false, false);
           const int g4 = lane_e >> 4;
           const int64_t col = n0 + (j + (g4 & 1)) * 16 + (g4 >> 1) * 8;
-          if (row < M && col < N)
-            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + row * N + col) = u32x4{s0[0], s1[0], s0[1], s1[1]};
+          const u32x4 out = {s0[0], s1[0], s0[1], s1[1]};
+          if (row < M) {
+            if (col + 8 <= N) {
+              store_16(elem<OUT>(a.y, row * N + col), out);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (col + e < N) static_cast<uint16_t*>(a.y)[row * N + col + e] = uint16_t(out[e / 2] >> (16 * (e % 2)));
+            }
+          }
         }
       }
     }
@@ -288,6 +315,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
   constexpr int kWaves = kRowsWaves, kRows = MT * 16, NB = 4;
   static_assert(kTrRowsLds<MT, D> <= 160 * 1024 && kTrRowsLds<MT, D> >= kWaves * MT * NB * 1024, "LDS; the partial sums");
   const int64_t M = a.M, N = a.N;
+  const uint32_t pitch = uint32_t(a.b_pitch);
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = wave_in_block();
   const uint32_t blk = blockIdx.x, split = blockIdx.y;
@@ -312,7 +340,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int r = q * 16 + lane / 4;
-    off_b[q] = uint32_t(r) * uint32_t(N) + ((lane % 4) ^ swz_b(r)) * 16;
+    off_b[q] = uint32_t(r) * pitch + ((lane % 4) ^ swz_b(r)) * 16;
   }
   const uint64_t pa = reinterpret_cast<uint64_t>(a.a + m0 * a.a_pitch), pb = reinterpret_cast<uint64_t>(a.b + n0);
   auto load = [&](int step, int d) {
@@ -320,7 +348,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
     const int64_t left = step < steps ? a.K - int64_t(step) * kTrStep : 0;   // rows of b from this step on
     const uint32_t rows_b = left <= 0 ? 0u : left < kTrStep ? uint32_t(left) : uint32_t(kTrStep);
     const u32x4 ra = rsrc_words(pa + uint64_t(step) * kTrStep, rows_b == 0 ? 0u : rows_a * uint32_t(a.a_pitch) - uint32_t(step) * kTrStep);
-    const u32x4 rb = rsrc_words(pb + uint64_t(step) * kTrStep * uint64_t(N), rows_b == 0 ? 0u : rows_b * uint32_t(N) - uint32_t(n0));
+    const u32x4 rb = rsrc_words(pb + uint64_t(step) * kTrStep * pitch, rows_b == 0 ? 0u : rows_b * pitch - uint32_t(n0));
 #pragma unroll
     for (int q = 0; q < MT; ++q) load_lds16_asm(ra, S + q * 1024, off_a[q]);
 #pragma unroll
@@ -376,17 +404,12 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) v += part[w][i][j][lane];
     const int64_t row = m0 + i * 16 + i16, col = n0 + j * 16 + g * 4;
-    if (row >= M || col >= N) continue;   // N is a multiple of 16
-    if (a.part != nullptr) {
-      *reinterpret_cast<i32x4*>(a.part + (int64_t(split) * M + row) * N + col) = v;
+    if (row >= M || col >= N) continue;
+    if (a.part != nullptr) {   // rows of partial sums are b's, so whole fours
+      *reinterpret_cast<i32x4*>(a.part + (int64_t(split) * M + row) * a.b_pitch + col) = v;
       continue;
     }
-    const float sc = a.a_scale[row];
-    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.add != nullptr) load4<OUT>(a.add, row * N + col, f);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf(float(v[e]), sc, f[e]);
-    store4<OUT>(a.y, row * N + col, f);
+    finish4<OUT>(a, row, col, v, a.a_scale[row]);
   }
 }
 
@@ -394,15 +417,11 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
 template <class OUT>
 __global__ __launch_bounds__(256) void add_shares(Args a, int shares) {
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (i >= a.M * a.N) return;
+  if (i >= a.M * a.b_pitch) return;
   i32x4 v = {0, 0, 0, 0};
-  for (int p = 0; p < shares; ++p) v += *reinterpret_cast<const i32x4*>(a.part + int64_t(p) * a.M * a.N + i);
-  const float sc = a.a_scale[i / a.N];
-  float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (a.add != nullptr) load4<OUT>(a.add, i, f);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf(float(v[e]), sc, f[e]);
-  store4<OUT>(a.y, i, f);
+  for (int p = 0; p < shares; ++p) v += *reinterpret_cast<const i32x4*>(a.part + int64_t(p) * a.M * a.b_pitch + i);
+  const int64_t row = i / a.b_pitch;
+  finish4<OUT>(a, row, i - row * a.b_pitch, v, a.a_scale[row]);
 }
 
 template <int MT, int D, class OUT>
@@ -415,7 +434,7 @@ hipError_t launch_rows(Args a, int shares, hipStream_t s) {
   hipLaunchKernelGGL((product_tr_rows<MT, D, OUT>), dim3(a.map.tiles, unsigned(shares)), dim3(kRowsWaves * kWave),
                      (kTrRowsLds<MT, D>), s, a);
   if (shares > 1) {
-    const int64_t blocks = (a.M * a.N + 1023) / 1024;
+    const int64_t blocks = (a.M * a.b_pitch + 1023) / 1024;
     hipLaunchKernelGGL((add_shares<OUT>), dim3(unsigned(blocks)), dim3(256), 0, s, a, shares);
   }
   return hipGetLastError();
@@ -436,7 +455,7 @@ constexpr TileCost kMidCost = {6.925f, 0.8417f, 0.492f, 0.3107f, 0, 0, 0.2087f};
 constexpr TileCost kBigCost = {7.826f, 0.8177f, 0.7358f, 0, 0, 0, 0.2235f};
 
 // The form by the estimates (linear_q8_device.hpp); the partial sums of a split K stay below 32 MiB.
-Plan make_plan(int64_t M, int64_t N, int64_t K, int cus) {
+Plan make_plan(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr) {
   Plan best{kLow, 1};
   float least = tile_cost<LowTile>(M, N, K, kTrStep, cus, kLowCost);
   auto take = [&](Form f, int shares, float t) {
@@ -448,26 +467,33 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, int cus) {
   take(kSmall, 1, tile_cost<SmallTile>(M, N, K, kTrStep, cus, kSmallCost));
   take(kMid, 1, tile_cost<MidTile>(M, N, K, kTrStep, cus, kMidCost));
   take(kBig, 1, tile_cost<BigTile>(M, N, K, kTrStep, cus, kBigCost));
-  if (M > 1024) return best;
-  for (int shares = 1; shares <= 8; shares *= 2) {
+  for (int shares = 1; shares <= 8 && M <= 1024; shares *= 2) {
     if (shares > 1 && (K < 1024 || int64_t(shares) * M * N * 4 > (int64_t(32) << 20))) break;
     take(kRows16, shares, rows_cost(M, N, K, 16, 64, kTrStep, 4, shares, cus, kRows16Cost));
     take(kRows32, shares, rows_cost(M, N, K, 32, 64, kTrStep, 3, shares, cus, kRows32Cost));
     take(kRows64, shares, rows_cost(M, N, K, 64, 64, kTrStep, 2, shares, cus, kRows64Cost));
   }
+  if (time) *time = least;
   return best;
+}
+
+// Whether b's rows are copied to aligned ones first.
+bool pads(int64_t M, int64_t N, int64_t K, int cus) {
+  if (N % 16 == 0 || M == 0 || K == 0 || N >= (1 << 24)) return false;
+  float fast;
+  make_plan(M, padded(N), K, cus, &fast);
+  return pad_pays(M, N, K, K, N, fast);
 }
 
 template <class OUT>
 hipError_t launch(const Args& a, hipStream_t s) {
   // b's rows start on 16-byte boundaries and a ring slot's 64 rows fit a buffer resource.
-  const bool aligned = a.K > 0 && a.N % 16 == 0 && a.N < (1 << 24) && reinterpret_cast<uintptr_t>(a.b) % 16 == 0 &&
-                       reinterpret_cast<uintptr_t>(a.y) % 16 == 0 && reinterpret_cast<uintptr_t>(a.add) % 16 == 0;
+  const bool aligned = a.K > 0 && a.b_pitch % 16 == 0 && a.b_pitch <= (1 << 24) && reinterpret_cast<uintptr_t>(a.b) % 16 == 0;
   if (!aligned) return launch_any<OUT, true>(a, s);
   int dev = 0, cus = 0;
   const hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;
-  const Plan plan = make_plan(a.M, a.N, a.K, cus);
+  const Plan plan = make_plan(a.M, a.b_pitch, a.K, cus);
   switch (plan.form) {
     case kRows16: return launch_rows<1, 2, OUT>(a, plan.shares, s);
     case kRows32: return launch_rows<2, 2, OUT>(a, plan.shares, s);
@@ -481,17 +507,27 @@ hipError_t launch(const Args& a, hipStream_t s) {
 
 // Rows of p start on 128-byte lines and are padded with zeros to whole K steps.
 int64_t pitch_of(int64_t n) { return (n + 127) / 128 * 128; }
-size_t part_at(int64_t m, int64_t n) { return (size_t(m) * size_t(pitch_of(n)) + size_t(m) * 4 + 15) / 16 * 16; }
+size_t more_at(int64_t m, int64_t n) { return (size_t(m) * size_t(pitch_of(n)) + size_t(m) * 4 + 15) / 16 * 16; }
 
 }  // namespace tr
 }  // namespace lq8
 
-// p, its scales, and the sums of the shares, 16-byte aligned.
+LinearQ8Form linear_q8_bwd_form(int64_t M, int64_t N, int64_t K) {
+  int dev = 0, cus = 256;
+  if (current_device(dev, cus) != hipSuccess) cus = 256;   // no device here
+  const bool copies = lq8::tr::pads(M, K, N, cus);
+  if (N == 0 || (K % 16 != 0 && !copies)) return {8, 1, false};
+  const lq8::tr::Plan plan = lq8::tr::make_plan(M, lq8::padded(K), N, cus);
+  return {int(plan.form) + 1, plan.shares, copies};
+}
+
+// p, its scales, the copy of w, and the sums of the shares, 16-byte aligned.
 size_t linear_q8_bwd_workspace(int64_t M, int64_t N, int64_t K) {
   int dev = 0, cus = 256;
   if (current_device(dev, cus) != hipSuccess) cus = 256;   // no device here
-  const lq8::tr::Plan plan = lq8::tr::make_plan(M, K, N, cus);
-  return lq8::tr::part_at(M, N) + (plan.shares > 1 ? size_t(plan.shares) * size_t(M) * size_t(K) * 4 : 0);
+  const size_t pitch = size_t(lq8::padded(K)), copy = lq8::tr::pads(M, K, N, cus) ? size_t(N) * pitch : 0;
+  const lq8::tr::Plan plan = lq8::tr::make_plan(M, int64_t(pitch), N, cus);
+  return lq8::tr::more_at(M, N) + copy + (plan.shares > 1 ? size_t(plan.shares) * size_t(M) * pitch * 4 : 0);
 }
 
 hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
@@ -503,8 +539,19 @@ hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, i
     const hipError_t e = launch_q8_rows(bf16, M, N, pitch, dy, w_scale, p, p_scale, s);
     if (e != hipSuccess) return e;
   }
-  const lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, true,
-                    reinterpret_cast<int32_t*>(p + lq8::tr::part_at(M, N)), 0, {}};
+  int8_t* more = p + lq8::tr::more_at(M, N);
+  lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, K, nullptr, 0, {}};
+  int dev = 0, cus = 0;
+  const hipError_t e = current_device(dev, cus);
+  if (e != hipSuccess) return e;
+  if (lq8::tr::pads(M, K, N, cus)) {
+    a.b_pitch = lq8::padded(K);
+    const hipError_t ep = lq8::launch_pad(w, N, nullptr, 0, K, more, a.b_pitch, s);
+    if (ep != hipSuccess) return ep;
+    a.b = more;
+    more += N * a.b_pitch;
+  }
+  a.part = reinterpret_cast<int32_t*>(more);
   return dx_bf16 ? lq8::tr::launch<BF16>(a, s) : lq8::tr::launch<F32>(a, s);
 }
 

@@ -36,22 +36,22 @@ struct Tile {
 // 16 consecutive results of a row from column `col` on; those from N on are not stored.
 template <class OUT>
 __device__ inline void store16(const Args& a, int64_t row, int64_t col, const float (&f)[16]) {
+  constexpr int E = OUT::kPerVec;
   const int64_t base = row * a.N + col;
   int left = int(a.N - col);   // columns that there are; new in every call: 16 masks kept would be spilled
   asm volatile("" : "+v"(left));
-  if (a.vec) {
 #pragma unroll
-    for (int p = 0; p < 16 / OUT::kPerVec; ++p) {
-      float v[OUT::kPerVec];
+  for (int p = 0; p < 16; p += E) {
+    if (p + E <= left) {
+      float v[E];
 #pragma unroll
-      for (int e = 0; e < OUT::kPerVec; ++e) v[e] = f[p * OUT::kPerVec + e];
-      if (p * OUT::kPerVec < left)
-        *reinterpret_cast<u32x4*>(static_cast<char*>(a.y) + (base + p * OUT::kPerVec) * OUT::kBytes) = OUT::pack(v);
+      for (int e = 0; e < E; ++e) v[e] = f[p + e];
+      store_16(elem<OUT>(a.y, base + p), OUT::pack(v));
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (p + e < left) OUT::store1(a.y, base + p + e, f[p + e]);
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (e < left) OUT::store1(a.y, base + e, f[e]);
   }
 }
 
@@ -460,8 +460,11 @@ constexpr TileCost kSmallCost = {3.676f, 0.8739f, 0.4877f, 0.312f, 0, 0.05597f, 
 constexpr TileCost kMidCost = {4.706f, 1.471f, 0.7827f, 0.561f, 0, 0.08527f, 0.2501f};
 constexpr TileCost kBigCost = {5.923f, 1.435f, 1.257f, 0, 0, 0.003937f, 0.2741f};
 
-Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
-  if (M <= 2) return kFew;
+Form choose_form(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr) {
+  if (M <= 2) {
+    if (time) *time = 3.2f + float(N) * float(K) * (1.0f / 5.5e6f);
+    return kFew;
+  }
   auto rows = [&](int bm, int blocks_per_cu, const RowsCost& c) {
     return M <= 2048 ? rows_cost(M, N, K, bm, 32, kBK, blocks_per_cu, 1, cus, c) : INFINITY;
   };
@@ -473,7 +476,17 @@ Form choose_form(int64_t M, int64_t N, int64_t K, int cus) {
                            tile_cost<SmallTile>(M, N, K, kBK, cus, kSmallCost),
                            tile_cost<MidTile>(M, N, K, kBK, cus, kMidCost),
                            tile_cost<BigTile>(M, N, K, kBK, cus, kBigCost)};
-  return Form(std::min_element(t, t + kForms) - t);
+  const float* const least = std::min_element(t, t + kForms);
+  if (time) *time = *least;
+  return Form(least - t);
+}
+
+// Whether a layer's rows are copied to aligned ones first.
+bool pads(int64_t M, int64_t N, int64_t K, int cus) {
+  if (K % 16 == 0 || M == 0 || N == 0) return false;
+  float fast;
+  choose_form(M, N, padded(K), cus, &fast);
+  return pad_pays(M, N, K, M + N, K, fast);
 }
 
 template <class OUT>
@@ -501,10 +514,35 @@ hipError_t launch_fwd(const Args& a, hipStream_t s) {
 
 }  // namespace lq8
 
+LinearQ8Form linear_q8_fwd_form(int64_t M, int64_t N, int64_t K) {
+  int dev = 0, cus = 256;
+  if (current_device(dev, cus) != hipSuccess) cus = 256;   // no device here
+  const bool copies = lq8::pads(M, N, K, cus);
+  if (K == 0 || (K % 16 != 0 && !copies)) return {8, 1, false};
+  return {int(lq8::choose_form(M, N, lq8::padded(K), cus)), 1, copies};
+}
+
+size_t linear_q8_fwd_workspace(int64_t M, int64_t N, int64_t K) {
+  int dev = 0, cus = 256;
+  if (current_device(dev, cus) != hipSuccess) cus = 256;   // no device here
+  return lq8::pads(M, N, K, cus) ? size_t(M + N) * size_t(lq8::padded(K)) : 0;
+}
+
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
-                                const int8_t* w, const float* w_scale, const void* bias, void* y, hipStream_t s) {
-  const bool vec = reinterpret_cast<uintptr_t>(y) % 16 == 0 && N * (bf16 ? 2 : 4) % 16 == 0;
-  const lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, vec, nullptr, 0, {}};
+                                const int8_t* w, const float* w_scale, const void* bias, void* y, void* workspace,
+                                hipStream_t s) {
+  lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, K, nullptr, 0, {}};
+  int dev = 0, cus = 0;
+  hipError_t e = current_device(dev, cus);
+  if (e != hipSuccess) return e;
+  if (lq8::pads(M, N, K, cus)) {   // zeros behind the rows add nothing to the sums
+    a.K = a.a_pitch = a.b_pitch = lq8::padded(K);
+    int8_t* const rows = static_cast<int8_t*>(workspace);
+    e = lq8::launch_pad(q, M, w, N, K, rows, a.K, s);
+    if (e != hipSuccess) return e;
+    a.a = rows;
+    a.b = rows + M * a.K;
+  }
   return bf16 ? lq8::launch_fwd<BF16>(a, s) : lq8::launch_fwd<F32>(a, s);
 }
 

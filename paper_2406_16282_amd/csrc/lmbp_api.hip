@@ -518,20 +518,25 @@ bool bad_layer(int64_t m, int64_t n, int64_t k) {
 }
 
 lmbp_status linear_q8_fwd_impl(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t* q, const float* scale,
-                               const int8_t* w, const float* w_scale, const void* bias, void* y, void* stream) {
+                               const int8_t* w, const float* w_scale, const void* bias, void* y, void* workspace,
+                               int64_t workspace_bytes, void* stream) {
   if (!known_dtype(dt)) return LMBP_EDTYPE;
   if (bad_layer(m, n, k) || k > lmbp::kQ8MaxDepth || bad_matrix(m, n)) return LMBP_EINVAL;
   if (m == 0 || n == 0) return LMBP_OK;
   if (!y || !scale || !w_scale || (k > 0 && (!q || !w))) return LMBP_EINVAL;
   const int eb = elem_bytes(dt);
   if (!aligned(y, eb) || !aligned(scale, 4) || !aligned(w_scale, 4) || (bias && !aligned(bias, eb))) return LMBP_EINVAL;
-  const Span sy = span(y, uint64_t(m) * uint64_t(n) * eb);
+  const uint64_t need = lmbp_linear_q8_fwd_bytes(m, n, k);
+  if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || uint64_t(workspace_bytes) < need))
+    return LMBP_EINVAL;
+  const Span sy = span(y, uint64_t(m) * uint64_t(n) * eb), sp = span(workspace, need);
+  if (overlaps(sy, sp)) return LMBP_EOVERLAP;
   const Span ins[5] = {span(q, q ? uint64_t(m) * uint64_t(k) : 0), span(w, w ? uint64_t(n) * uint64_t(k) : 0),
                        span(scale, uint64_t(m) * 4), span(w_scale, uint64_t(n) * 4),
                        span(bias, bias ? uint64_t(n) * eb : 0)};
   for (const Span& in : ins)
-    if (overlaps(sy, in)) return LMBP_EOVERLAP;
-  return from_hip(lmbp::launch_linear_q8_fwd(dt == LMBP_BF16, m, n, k, q, scale, w, w_scale, bias, y,
+    if (overlaps(sy, in) || overlaps(sp, in)) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_linear_q8_fwd(dt == LMBP_BF16, m, n, k, q, scale, w, w_scale, bias, y, workspace,
                                              static_cast<hipStream_t>(stream)));
 }
 
@@ -704,8 +709,20 @@ lmbp_status msrms_q8_bwd(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t 
   return msrms_q8_bwd_impl(dt_dz, dt, rows, cols, dz, q, scale, rstd, ds, dx, stream);
 }
 lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t* q, const float* scale,
-                          const int8_t* w, const float* w_scale, const void* bias, void* y, void* stream) {
-  return linear_q8_fwd_impl(dt, m, n, k, q, scale, w, w_scale, bias, y, stream);
+                          const int8_t* w, const float* w_scale, const void* bias, void* y, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+  return linear_q8_fwd_impl(dt, m, n, k, q, scale, w, w_scale, bias, y, workspace, workspace_bytes, stream);
+}
+int lmbp_linear_q8_form(int64_t m, int64_t n, int64_t k, int grad, int64_t* shares, int64_t* copies) {
+  if (m <= 0 || n < 0 || k < 0 || (grad ? k : n) == 0 || bad_layer(m, n, k)) return -1;
+  const lmbp::LinearQ8Form f = grad ? lmbp::linear_q8_bwd_form(m, n, k) : lmbp::linear_q8_fwd_form(m, n, k);
+  if (shares) *shares = f.shares;
+  if (copies) *copies = f.copies;
+  return f.form;
+}
+size_t lmbp_linear_q8_fwd_bytes(int64_t m, int64_t n, int64_t k) {
+  if (m <= 0 || n <= 0 || k <= 0 || bad_layer(m, n, k) || k > lmbp::kQ8MaxDepth) return 0;
+  return lmbp::linear_q8_fwd_workspace(m, n, k);
 }
 size_t lmbp_linear_q8_bwd_bytes(int64_t m, int64_t n, int64_t k) {
   if (m <= 0 || k <= 0 || bad_layer(m, n, k) || n > lmbp::kQ8MaxDepth) return 0;

@@ -122,14 +122,27 @@ hipError_t launch_msrms_q8_bwd(bool dz_bf16, bool bf16, int64_t rows, int64_t co
                                const float* scale, const float* rstd, const void* ds, void* dx, hipStream_t s);
 
 // Linear layers of 8-bit rows and weights; bf16: the type of y and bias, or of dy; dx_bf16 that of
-// add (may be null, or dx) and dx. No more than kQ8MaxDepth products to a sum: 128 * 128 * kQ8MaxDepth < 2^31. Workspace of
-// linear_q8_bwd_workspace bytes, 16-byte aligned.
+// add (may be null, or dx) and dx. No more than kQ8MaxDepth products to a sum: 128 * 128 * kQ8MaxDepth < 2^31. Workspaces of
+// the functions' bytes, 16-byte aligned.
 constexpr int64_t kQ8MaxDepth = 131071;
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
-                                const int8_t* w, const float* w_scale, const void* bias, void* y, hipStream_t s);
+                                const int8_t* w, const float* w_scale, const void* bias, void* y, void* workspace,
+                                hipStream_t s);
+size_t linear_q8_fwd_workspace(int64_t M, int64_t N, int64_t K);
 size_t linear_q8_bwd_workspace(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, int64_t K, const void* dy, const int8_t* w,
                                 const float* w_scale, const void* add, void* dx, void* workspace, hipStream_t s);
+
+// The form that aligned tensors of these sizes take on the current device (256 CUs without one): 0
+// dot products, 1 .. 3 split-K with 16, 32, 64 rows to a block, 4 .. 7 tiles of 64 x 128, 128 x
+// 128, 128 x 256, 256 x 256, 8 the general form; the blocks that share a sum's length; whether rows
+// are copied to aligned ones first.
+struct LinearQ8Form {
+  int form, shares;
+  bool copies;
+};
+LinearQ8Form linear_q8_fwd_form(int64_t M, int64_t N, int64_t K);
+LinearQ8Form linear_q8_bwd_form(int64_t M, int64_t N, int64_t K);
 
 hipError_t launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);
 

@@ -72,8 +72,14 @@ def test_msrms_q8_bwd(L):
 
 
 def test_linear_q8_fwd(L):
-    def f(dt=B.BF16, m=4, n=32, k=64, q=at(0), scale=at(1), w=at(2), w_scale=at(3), bias=at(4), y=at(5)):
-        return L.linear_q8_fwd(dt, m, n, k, q, scale, w, w_scale, bias, y, None)
+    def f(dt=B.BF16, m=4, n=32, k=64, q=at(0), scale=at(1), w=at(2), w_scale=at(3), bias=at(4), y=at(5), work=None, size=0):
+        return L.linear_q8_fwd(dt, m, n, k, q, scale, w, w_scale, bias, y, work, size, None)
+    assert L.lmbp_linear_q8_fwd_bytes(4, 32, 64) == L.lmbp_linear_q8_fwd_bytes(0, 32, 65) == 0   # whole vectors; nothing
+    need = L.lmbp_linear_q8_fwd_bytes(4096, 4096, 1023)
+    assert need == 8192 * 1024
+    odd = dict(m=4096, n=4096, k=1023, work=at(6), size=need)
+    assert f(**{**odd, "work": None}) == f(**{**odd, "size": need - 1}) == f(**{**odd, "work": at(6) + 8}) == B.EINVAL
+    assert f(**{**odd, "work": at(5)}) == f(**{**odd, "work": at(2)}) == f(**{**odd, "work": at(4)}) == B.EOVERLAP
     assert f(dt=5) == B.EDTYPE
     assert f(m=-1) == f(n=-1) == f(k=-1) == f(m=1 << 31) == f(n=1 << 31) == B.EINVAL
     assert f(k=131072) == B.EINVAL                       # 128 * 128 * 131072 = 2^31

@@ -20,10 +20,11 @@ U = 2.0 ** -24
 TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
 
 # (m, n, k): every remainder of tiles and vectors, single rows and columns, long sums
-SIZES = [(3, 5, 65), (4, 1, 130), (2, 7, 193), (5, 3, 67), (70, 15, 66), (1, 1, 1), (1, 16, 16), (2, 3, 5), (1, 4096, 512), (3, 1001, 1023), (7, 48, 64), (16, 64, 256), (17, 80, 272),
+SIZES = [(3000, 33, 65), (64, 9001, 301), (3, 5, 65), (4, 1, 130), (2, 7, 193), (5, 3, 67), (70, 15, 66), (1, 1, 1), (1, 16, 16), (2, 3, 5), (1, 4096, 512), (3, 1001, 1023), (7, 48, 64), (16, 64, 256), (17, 80, 272),
          (31, 2048, 1040), (33, 24, 48), (64, 130, 257), (65, 1000, 4096), (100, 272, 11008), (127, 255, 129),
          (128, 256, 128), (129, 257, 144), (200, 768, 768), (256, 512, 1024), (257, 528, 1024), (333, 1001, 1023),
-         (513, 1040, 2064), (700, 96, 131056), (1000, 8, 32), (1025, 2064, 528), (2100, 4112, 784)]
+         (300, 1003, 4099), (700, 1001, 1023), (1100, 1027, 2051), (20, 100, 4096), (40, 272, 8192), (3000, 272, 272),
+         (1100, 2050, 2000), (513, 1040, 2064), (700, 96, 131056), (1000, 8, 32), (1025, 2064, 528), (2100, 4112, 784)]
 
 
 def half(t):
@@ -117,12 +118,30 @@ def test_input_gradients_that_add_up(m, n, k, dtype, out):
     assert lmbp.linear_q8_bwd(dy, w, w_scale, dtype=TYPES[out]).dtype == TYPES[out]
 
 
-@pytest.mark.parametrize("m,n,k", [(4096, 4096, 2048), (2048, 11008, 4096), (300, 4096, 11008), (20, 11008, 4096)])
+LARGE = [(4096, 4096, 2048), (2048, 11008, 4096), (300, 4096, 11008), (20, 11008, 4096), (40, 13824, 1024), (400, 4096, 4096),
+         (1000, 8208, 2064), (1000, 2064, 8208), (40, 4112, 4112), (70, 8208, 2064), (100, 1040, 4112)]
+
+
+@pytest.mark.parametrize("m,n,k", LARGE)
 def test_large_layers(m, n, k):
     (q, scale), (w, w_scale) = rows(m, k, 6), weight(n, k, 7)
     check_fwd(lmbp.linear_q8_fwd(q, scale, w, w_scale), q, scale, w, w_scale, None, "forward")
     dy = torch.randn(m, n, device=DEV).to(torch.bfloat16)
     check_bwd(lmbp.linear_q8_bwd(dy, w, w_scale), dy, w, w_scale, "gradient")
+
+
+def forms(grad, sizes):
+    shares, copies = ctypes.c_int64(), ctypes.c_int64()
+    for m, n, k in sizes:
+        yield lmbp.lib().lmbp_linear_q8_form(m, n, k, grad, shares, copies), shares.value, copies.value
+
+
+def test_the_sizes_take_every_form():
+    fwd = set(forms(0, SIZES + LARGE))
+    assert {f for f, _, _ in fwd} == set(range(9)) and {c for _, _, c in fwd} == {0, 1}, fwd
+    bwd = set(forms(1, [(m, n, k) for m, k, n in SIZES] + LARGE))
+    assert {f for f, _, _ in bwd} == set(range(1, 9)) and {c for _, _, c in bwd} == {0, 1}, bwd
+    assert {s for f, s, _ in bwd if f <= 3} >= {1, 2, 4, 8}, bwd
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 32, 131071), (70, 64, 131056), (3, 9, 131071)])
@@ -193,7 +212,8 @@ def test_any_address_and_nothing_beside_the_result(m, n, k, shift, dtype):
     bdy = band(dy)
     L, dt = lmbp.lib(), B.BF16 if dtype == "bf16" else B.FP32
     st = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-    assert L.linear_q8_fwd(dt, m, n, k, bq[2], bs[2], bw[2], bws[2], bb[2], by[2], st) == B.OK
+    assert L.lmbp_linear_q8_fwd_bytes(m, n, k) == 0
+    assert L.linear_q8_fwd(dt, m, n, k, bq[2], bs[2], bw[2], bws[2], bb[2], by[2], None, 0, st) == B.OK
     assert torch.equal(by[1].view(m, n), lmbp.linear_q8_fwd(q, scale, w, w_scale, bias, t))
     need = L.lmbp_linear_q8_bwd_bytes(m, n, k)
     work = torch.full((need + 64,), 77, dtype=torch.uint8, device=DEV)
