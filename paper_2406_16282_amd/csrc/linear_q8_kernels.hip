@@ -390,7 +390,7 @@ hipError_t launch_rows(Args a, int dev, hipStream_t s) {
 constexpr int kFewWaves = 4;
 template <int MT, int R, class OUT>
 __global__ __launch_bounds__(kFewWaves * kWave) void product_few(Args a) {
-  constexpr int kDeep = R > 1 ? 4 / R : 4;   // pieces of a row in flight
+  constexpr int kDeep = 4 / R;   // pieces of a row in flight
   const uint32_t K = uint32_t(a.K);
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t n0 = (int64_t(blockIdx.x) * kFewWaves + wave_in_block()) * R;
@@ -445,9 +445,10 @@ hipError_t launch_few(const Args& a, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(unsigned((a.N + per - 1) / per)), dim3(kFewWaves * kWave), 0, s, a);
     return hipGetLastError();
   };
-  if (a.K <= 1024) return launch(product_few<MT, 4, OUT>, 4);
-  if (a.K <= 2048 || MT > 1) return launch(product_few<MT, 2, OUT>, 2);
-  return launch(product_few<MT, 1, OUT>, 1);
+  // Two rows of W to a wave where they are short. One row of x, two against one: 11008 x 1024 4.65 and
+  // 6.1 us, 11008 x 2048 6.0 and 7.0; 11008 x 4096 9.8 and 9.1 (two rows of x: 10.6 and 10.0). Four were
+  // never the best (11008 x 1024 4.72, 4096 x 1024 3.64 against 3.40).
+  return a.K <= 2048 ? launch(product_few<MT, 2, OUT>, 2) : launch(product_few<MT, 1, OUT>, 1);
 }
 
 enum Form { kFew, kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };

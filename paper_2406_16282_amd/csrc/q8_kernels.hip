@@ -429,13 +429,17 @@ __global__ __launch_bounds__(256) void norm_bwd_any(const void* dz, const int8_t
 }
 
 // Launch shapes of the register kernels, by the pieces that they hold: the fewest waves to a row
-// that hold it in 3 pieces per thread, or 16 waves with up to MOST (what a kernel has registers
-// for).
+// that hold it in 3 pieces per thread (4 with 8 waves), or 16 waves with up to MOST (what a kernel
+// has registers for). Measured in us as waves x pieces, bf16, 8192 rows, q8_rows and msrms_q8_fwd with
+// a residual: 768 columns 1x2 5.5 and 8.8, 2x2 7.5 and 10.0; 4096 columns 4x2 18.4 and 30.7, 8x2
+// 23.0 and 32.5, 16x2 34.7 and 47.1, 2x4 18.9 and 32.4; 11008 columns 8x3 43.5 and 79, 16x2 52 and 82; 13824
+// columns 8x4 54.2 and 96.9, 16x2 59.9 and 99.6 (with factors per column 56.8 against 70). In 32 bits 8192
+// columns 8x4 56 and 102, 16x2 57 and 103 (with factors 58 against 66).
 struct Shape {
   int wpr, vpl;
 };
-constexpr Shape kShapes[] = {{1, 1}, {1, 2}, {1, 3}, {2, 2},  {2, 3},  {4, 2},  {4, 3},
-                             {8, 2}, {8, 3}, {16, 2}, {16, 3}, {16, 4}, {16, 6}, {16, 8}};
+constexpr Shape kShapes[] = {{1, 1}, {1, 2}, {1, 3}, {2, 2},  {2, 3},  {4, 2}, {4, 3},
+                             {8, 2}, {8, 3}, {8, 4}, {16, 3}, {16, 4}, {16, 6}, {16, 8}};
 constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]);
 
 // Calls f(VPL, WPR) for the shape that holds `pieces`; false if none does.

@@ -24,7 +24,8 @@ SIZES = [(3000, 33, 65), (64, 9001, 301), (3, 5, 65), (4, 1, 130), (2, 7, 193), 
          (31, 2048, 1040), (33, 24, 48), (64, 130, 257), (65, 1000, 4096), (100, 272, 11008), (127, 255, 129),
          (128, 256, 128), (129, 257, 144), (200, 768, 768), (256, 512, 1024), (257, 528, 1024), (333, 1001, 1023),
          (300, 1003, 4099), (700, 1001, 1023), (1100, 1027, 2051), (20, 100, 4096), (40, 272, 8192), (3000, 272, 272),
-         (1100, 2050, 2000), (513, 1040, 2064), (700, 96, 131056), (1000, 8, 32), (1025, 2064, 528), (2100, 4112, 784)]
+         (1100, 2050, 2000), (513, 1040, 2064), (700, 96, 131056), (1000, 8, 32), (1025, 2064, 528), (2100, 4112, 784),
+         (2, 33, 2048), (1, 1001, 2064), (2, 13, 4112)]
 
 
 def half(t):

@@ -28,7 +28,7 @@ U = 2.0 ** -24
 EPS = 1e-5
 TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
 SHAPES = [(1, 1), (3, 1), (5, 2), (1, 8), (2, 33), (1, 4096), (64, 768), (7, 1023), (33, 1025), (130, 96), (4, 5120),
-          (3, 8191), (2, 11008), (3, 13824), (2, 16392), (2, 30011), (1, 40000), (2, 65536), (1, 131080)]
+          (3, 8191), (2, 11008), (3, 13824), (5, 12345), (2, 16392), (2, 30011), (1, 40000), (2, 65536), (1, 131080)]
 
 
 def half(dtype):
