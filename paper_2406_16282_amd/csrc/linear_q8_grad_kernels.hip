@@ -105,8 +105,9 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
   const int wm = wave / C::WN, wn = wave % C::WN;
   const uint32_t tiles = a.map.tiles;
   const int steps = int((a.K + kTrStep - 1) / kTrStep);
-  // Unit u of row r of the slot is stored at u ^ swz(r).
-  auto swz_a = [](int r) { return (r >> 2) & 3; };
+  // Unit u of row r of the slot is stored at u ^ swz(r): no read meets a bank conflict (bits 2 and 3 of r
+  // for a cost one more pass in each of its reads, 364 us instead of 355 for 8192 rows of 11008 x 4096).
+  auto swz_a = [](int r) { return (r >> 1) & 3; };
   auto swz_b = [](int r) { return BN == 256 ? (r & 7) | (((r >> 4) & 1) << 3) : ((r >> 1) & 3) | (((r >> 4) & 1) << 2); };
   uint32_t ld_a[kLA], ld_b[kLB];
 #pragma unroll
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
   int8_t* const ring = lds + wave * D * kStep;
   const uint32_t ring_at = lds_addr(lds) + wave * D * kStep;
   // Unit u (of 4) of row r at u ^ swz(r), 16 rows of 64 bytes to a load.
-  auto swz_a = [](int r) { return (r >> 2) & 3; };
+  auto swz_a = [](int r) { return (r >> 1) & 3; };
   auto swz_b = [](int r) { return ((r >> 2) & 1) | (((r >> 4) & 1) << 1); };
   uint32_t off_a[MT], off_b[4];
 #pragma unroll
