@@ -354,14 +354,14 @@ lmbp_status msrms_q8_bwd(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t 
  *
  *   dt     : type of y and bias, or of dy; dt_dx: type of add and dx.
  *   m,n,k  : any sizes >= 0 below 2^31; the length of the sums (k forward, n backward) at
- *            most 131071. k = 0 gives y = bias (0 without), n = 0 gives dx = 0.
+ *            most 131071. k = 0 gives y = bias (0 without), n = 0 dx = add (0 without).
  *   q [m x k], w [n x k]: any values; scale [m], w_scale [n]; bias [n] or NULL; y, dy [m x n];
  *            add, dx [m x k], add NULL for none; dx == add is allowed (the sum of several
  *            layers' gradients).
  *   workspace : lmbp_linear_q8_fwd_bytes / lmbp_linear_q8_bwd_bytes(m, n, k) bytes on the
  *            calling thread's current device, 16-byte aligned, NULL if that is 0. Its contents
  *            do not matter before or after.
- * k a multiple of 16 and 16-byte aligned q, w and results are the fast case, anything else
+ * k a multiple of 16 and 16-byte aligned q and w are the fast case, anything else
  * slower with the same results. No other output overlaps another buffer.
  * ------------------------------------------------------------------------ */
 lmbp_status linear_q8_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t k, const int8_t *q,

@@ -5,6 +5,22 @@
 //
 // Here the product is y = a b with a = p [M x K], b = w [K x N]: K stands for the layer's output
 // features, N for its input features. The sums are exact, as the forward's.
+//
+// What bounds it. Many rows: the card's power, as the forward; 8192 rows of 11008 x 4096 355 us, 44 of
+// them dy to 8 bits (270 MB, 6.1 TB/s) and 311 the product (2380 TOPS); with its operands laid out this
+// way the library's int8 product takes 475 to 496 us. 2000 rows of 4096 x 11008 97 us in a row, 114
+// from memory: 688 tiles of 128 x 256 on 512 places. Few rows: the weight's bytes and the chain of K steps.
+//
+// b's columns are K-strided: its rows are staged as they lie in memory and read with the transposing
+// LDS read (8 bytes to a lane). A ring slot holds 64 products, whole (that read wants 8 rows of each
+// column), and a step has four segments of MFMAs with the loads of a later slot and the reads of the
+// next fragments between them. After LDS loads issued by the compiler's builtin it waits for all of
+// them before each such read; the loads are written as asm for that reason (they have no output
+// registers, and every wait is written out). bf16 results are exchanged between neighbouring lane groups, so
+// that a lane stores 8 consecutive ones.
+//
+// dy is brought to 8 bits by a kernel of its own: a row's scale is known only after the whole row,
+// and every tile of columns needs the row. add (the other layers' gradients) is read in the epilogue.
 #include "linear_q8_device.hpp"
 
 #include <type_traits>
@@ -455,7 +471,14 @@ constexpr TileCost kSmallCost = {4.609f, 0.546f, 0.3394f, 0.1923f, 0, 0, 0.2672f
 constexpr TileCost kMidCost = {6.925f, 0.8417f, 0.492f, 0.3107f, 0, 0, 0.2087f};
 constexpr TileCost kBigCost = {7.826f, 0.8177f, 0.7358f, 0, 0, 0, 0.2235f};
 
-// The form by the estimates (linear_q8_device.hpp); the partial sums of a split K stay below 32 MiB.
+// The form by the estimates (linear_q8_device.hpp), their constants fitted to 420 sizes of 15 layers as
+// the forward's: 1.0% slower than the best on average, 30% at worst (1.1% on layers left out). Both sides,
+// us, dy's rows included: 11008 x 4096 at 16 rows 16-row blocks 45.3, K split over 2 of them 29.5, 4 21.3,
+// 8 22.9; at 64 rows 64-row blocks 52.6, over 4 25.3; 197 rows 64-row blocks 44.4, 64x128 tiles 53.1; 1024
+// rows 64x128 90, 128x128 80, 128x256 99; 1576 rows 128x128 122, 128x256 107; 8192 rows 128x256 388, 256x256 364.
+// 768 x 768 at 1024 rows 32-row blocks 9.9, 64x128 10.3; at 1576 rows 12.5 and 11.3.
+// The partial sums of a split K stay below 32 MiB, and K below 1024 is not split (at 16 rows of 768 x 768
+// 8.3 us against 6.4).
 Plan make_plan(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr) {
   Plan best{kLow, 1};
   float least = tile_cost<LowTile>(M, N, K, kTrStep, cus, kLowCost);

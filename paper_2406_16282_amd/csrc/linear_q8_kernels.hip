@@ -5,6 +5,38 @@
 // The sums are whole numbers in 32 bits and exact for up to kQ8MaxDepth products (128 * 128 *
 // kQ8MaxDepth < 2^31); one conversion to fp32, one product of the scales, one fused
 // multiply-add with the bias, one rounding to the output's type.
+//
+// What bounds it. Many rows: the card's power. A loop of nothing but 16x16x64 products of random
+// bytes runs at 3404 TOPS, of 32x32x32 ones at 3087 (4419 and 3986 on zeros), so the smaller shape
+// is taken although it needs as many operand reads. [8192 x 4096] x 11008 takes 305 to 340 us by the
+// card's state (2170 to 2420 TOPS; the library's int8 product without scales 392 to 413, its bf16
+// product 686 to 704, in the same runs), 8192^3 422 to 437 us (2510 to 2600; library 446 to 453):
+// matrix cores busy 63 to 67% of the cycles, no bank conflicts, a clock of 1.6 to 1.85 GHz. Few rows:
+// the weight's bytes. One row of 11008 x 4096 9.1 us with weights that the caches do not hold
+// (5.0 TB/s; one load's way and the launch are 3 of them), 16384 x 16384 40 us (6.7 TB/s), 16 rows
+// of the first 12.5 us.
+//
+// Tiles (product_tile). The loop is that of the bf16 layers (linear_kernels.hip): K in steps of
+// 128 bytes, each in two half steps; a ring of slots of half a step's operands (half of every wave's
+// rows of x and of W), filled straight from memory by buffer loads into LDS that return zeros past
+// the operands' ends; a half step multiplies fragments in registers, reads the next ones and loads
+// into the slot that was read before, with one barrier and a wait that leaves kRing - 2 slots in
+// flight. An LDS row is 128 bytes = eight 16-byte units, unit u of row r at u ^ swz(r), so that the
+// 16 rows of a read fall into distinct banks: (r >> 1) % 8 for x, bit 1 and bits 3, 4 of r for W.
+// Blocks are persistent and the loads run on from one tile into the next. MFMA rows are rows of W,
+// dealt to the tiles so that a lane ends with 16 consecutive columns of a row: whole vectors are
+// stored from registers. The tiles' scales travel with the operands, in LDS.
+// Tried on 8192 rows of 11008 x 4096 without gain: the MFMAs in a fixed order with the reads and
+// loads between them (2 to 5% faster as long as it spilled two registers, slower without), 256 x 256
+// by 4 waves.
+//
+// Some rows (product_rows). Too few tiles to fill the card: a block takes 16, 32 or 64 rows and 32
+// columns, its four waves the K steps in turn, each through a ring of its own without barriers.
+// 16 rows, us: rings of two steps 13.3 (11008 x 4096) and 15.9 (4096 x 11008), of three 13.8 and 16.0; 64
+// columns to a block 12.9 and 21.6 (768 x 768 4.7 against 3.9).
+//
+// One or two rows (product_few). Dot products: the matrix form would load as much and compute 16
+// rows; 9.1 us against 11.7 for 11008 x 4096 (2 rows: 10.0 and 12.0; 3 rows would take 12 either way).
 #include "linear_q8_device.hpp"
 
 #include <algorithm>
@@ -451,6 +483,13 @@ hipError_t launch_few(const Args& a, hipStream_t s) {
   return a.K <= 2048 ? launch(product_few<MT, 2, OUT>, 2) : launch(product_few<MT, 1, OUT>, 1);
 }
 
+// The form by estimated times (linear_q8_device.hpp), their constants fitted to the times of every
+// form at 420 sizes of 15 layers. The choice is 0.8% slower than the best form on average and 27% at
+// worst (0.9% on layers that were left out of the fit). Both sides, us: 11008 x 4096 at 16 rows
+// rows16 12.5, 64x128 tiles 19.8; at 32 rows rows32 15.3, 64x128 20.0; at 128 rows rows64 30, 64x128
+// 20.7; 197 rows 64x128 26.5, 128x128 23.5; 512 rows 128x128 38.4, 128x256 36.5; 2048 rows 128x256 91,
+// 256x256 105; 4096 rows 174 and 163; 8192 rows 318 and 318. 768 x 768 at 1576 rows 64x128 6.4, 128x128
+// 7.4, 256x256 14.8. 4096 x 11008 at 128 rows rows64 22.7, 64x128 43.9; 8192 rows 128x256 298, 256x256 281.
 enum Form { kFew, kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
 
 constexpr RowsCost kRows16Cost = {2.685f, 0.2485f, 0.2127f, 0.578f, 0.001916f, 0.009501f, 0.0643f, 1.986f, 0, 0};
@@ -482,7 +521,7 @@ Form choose_form(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr
   return Form(least - t);
 }
 
-// Whether a layer's rows are copied to aligned ones first.
+// Whether a layer's rows, of both operands, are copied to aligned ones first (pad_pays).
 bool pads(int64_t M, int64_t N, int64_t K, int cus) {
   if (K % 16 == 0 || M == 0 || N == 0) return false;
   float fast;
@@ -498,7 +537,10 @@ hipError_t launch_fwd(const Args& a, hipStream_t s) {
   int dev = 0, cus = 0;
   const hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;
-  // Weights by non-temporal loads when one row block reads them and they are large (see product_rows).
+  // Weights by non-temporal loads where one row block reads them and they are more than the caches are
+  // likely to hold until the next call. 16 rows, without and with, weights cold / in the caches: 11008 x
+  // 4096 14.1 and 12.7 / 10.4 and 10.6 us, 16384 x 16384 51 and 44 / 40 and 43; 8192 x 4096 (32 MiB) 9.7 and
+  // 8.9 / 5.8 and 6.3.
   const bool nt = a.N * a.K > (int64_t(32) << 20);
   switch (choose_form(a.M, a.N, a.K, cus)) {
     case kFew: return a.M == 1 ? launch_few<1, OUT>(a, s) : launch_few<2, OUT>(a, s);
