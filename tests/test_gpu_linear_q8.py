@@ -256,6 +256,63 @@ def test_inputs_behind_the_2_31st_byte():
     check_bwd(lmbp.linear_q8_bwd(dy, q[:, :64].contiguous(), scale), dy, q[:, :64].contiguous(), scale, "long sums")
 
 
+@pytest.mark.parametrize("m,n,k,what", [(333, 1001, 1023, "copies"), (16, 11008, 512, "shares")])
+def test_two_graphs_at_once_with_workspaces(m, n, k, what):
+    """Two graphs of one size, each with workspaces of its own, replayed on two streams at the same
+    time, with eager calls between: every replay against the eager result."""
+    shares, copies = ctypes.c_int64(), ctypes.c_int64()
+    lmbp.lib().lmbp_linear_q8_form(m, n, k, 1, shares, copies)
+    assert copies.value == 1 if what == "copies" else shares.value > 1
+    w, w_scale = weight(n, k, 1)
+
+    def run(q, scale, dy):
+        return lmbp.linear_q8_fwd(q, scale, w, w_scale), lmbp.linear_q8_bwd(dy, w, w_scale)
+
+    ins = [[*rows(m, k, s), torch.randn(m, n, device=DEV)] for s in (2, 3)]
+    for i in ins:
+        run(*i)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for i in ins:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(run(*i))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for replay in range(4):
+        for q, _, dy in ins:
+            q.random_(-127, 128)
+            dy.normal_()
+        want = [run(*i) for i in ins]
+        for o in outs:
+            for v in o:
+                v.fill_(7.0)
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        run(*ins[0])
+        torch.cuda.synchronize()
+        for o, v in zip(outs, want):
+            assert all(torch.equal(a, b) for a, b in zip(o, v)), f"replay {replay}"
+
+
+@pytest.mark.parametrize("m,n,k", [(333, 1001, 1023), (16, 11008, 512)])
+def test_workspaces_on_another_stream(m, n, k):
+    """The stream argument: what the default stream allocates next is not the launch's workspace."""
+    (q, scale), (w, w_scale) = rows(m, k, 1), weight(n, k, 2)
+    dy = torch.randn(m, n, device=DEV)
+    want = lmbp.linear_q8_fwd(q, scale, w, w_scale), lmbp.linear_q8_bwd(dy, w, w_scale)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = (lmbp.linear_q8_fwd(q, scale, w, w_scale, stream=side), lmbp.linear_q8_bwd(dy, w, w_scale, stream=side))
+        for nbytes in (1 << 16, 1 << 20, 1 << 22, 1 << 24):
+            torch.full((nbytes,), 255, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_shapes_and_refusals():
     (q, scale), (w, w_scale) = rows(6, 32, 1), weight(48, 32, 2)
     y = lmbp.linear_q8_fwd(q.view(2, 3, 32), scale.view(2, 3), w, w_scale)

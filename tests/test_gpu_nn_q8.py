@@ -263,6 +263,72 @@ def test_on_another_stream():
         assert torch.equal(dx, lmbp.linear_q8_bwd(dy, down.weight, down.scale))
 
 
+def test_two_threads_on_two_streams():
+    """Calls made at the same time by two host threads, each on a stream of its own."""
+    import threading
+    torch.manual_seed(3)
+    (_, mod) = layer(1001, 1023, 1)
+    xs = [torch.randn(130, 1023, device=DEV) for _ in range(2)]
+    dys = [torch.randn(130, 1001, device=DEV) for _ in range(2)]
+
+    def run(x, dy):
+        q, scale, rstd = lmbp.msrms_q8_fwd(x, 1e-5)
+        dz = lmbp.linear_q8_bwd(dy, mod.weight, mod.scale)
+        return lmbp.linear_q8_fwd(q, scale, mod.weight, mod.scale), lmbp.msrms_q8_bwd(dz, q, scale, rstd)
+
+    want = [run(x, dy) for x, dy in zip(xs, dys)]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got = run(xs[i], dys[i])
+                s.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not bad
+
+
+@pytest.mark.parametrize("shape", [(0, 144), (2, 0, 144), (144,), (1, 1, 144)])
+def test_modules_of_no_rows_and_of_one(shape):
+    (_, a), (_, b) = layer(272, 144, 1, True), layer(33, 144, 2)
+    a.bias.requires_grad_()
+    x, res = (torch.randn(shape, device=DEV, requires_grad=True) for _ in range(2))
+    block = MSRMSNormLinearQ8([a, b])
+    ya, yb, s = block(x, res)
+    assert ya.shape == (*shape[:-1], 272) and yb.shape == (*shape[:-1], 33) and s.shape == x.shape
+    (ya.sum() + yb.sum() + s.sum() + a(x).sum()).backward()      # gradients that are expanded numbers
+    assert x.grad.shape == x.shape and res.grad.shape == x.shape
+    rows = x.numel() // 144
+    assert torch.equal(a.bias.grad, torch.full((272,), 2.0 * rows, device=DEV))
+    q, scale, rstd, s1 = lmbp.msrms_q8_fwd(x.detach(), block.eps, res.detach())
+    dz = lmbp.linear_q8_bwd(torch.ones_like(ya), a.weight, a.scale)
+    dz = lmbp.linear_q8_bwd(torch.ones_like(yb), b.weight, b.scale, add=dz)
+    assert torch.equal(res.grad, lmbp.msrms_q8_bwd(dz, q, scale, rstd, torch.ones_like(s1)))
+    if rows == 0:
+        assert x.grad.numel() == 0
+
+
+def test_one_layer_twice_and_frozen_inputs():
+    (_, a) = layer(48, 64, 1, True)
+    a.bias.requires_grad_()
+    x = torch.randn(9, 64, device=DEV)
+    y0, y1 = MSRMSNormLinearQ8([a, a])(x)
+    assert torch.equal(y0, y1)
+    d0, d1 = torch.randn_like(y0), torch.randn_like(y1)
+    torch.autograd.backward((y0, y1), (d0, d1))       # no input asks for a gradient, the bias does
+    want = (d0.double() + d1.double()).sum(0)
+    assert ((a.bias.grad - want).abs() <= 20 * U * (d0.abs() + d1.abs()).double().sum(0)).all()
+
+
 def test_the_same_twice():
     """No result depends on the order in which blocks run."""
     (_, mod), x = layer(1040, 2064, 1), torch.randn(300, 2064, device=DEV)
