@@ -33,7 +33,8 @@ struct Args {
   const void* add;        // input gradient: [M x N] of the result's type, or null; may be y
   void* y;                // [M x N]
   int64_t M, N, K, a_pitch, b_pitch;   // bytes from one row to the next
-  int32_t* part;          // input gradient: [splits][M x N] sums over shares of K, or null
+  int32_t* part;          // [shares][M x part_pitch] sums over shares of K, or null
+  int64_t part_pitch;     // N in whole sixteens
   int32_t share;          // steps of K to a share
   TileMap map;
 };
@@ -233,6 +234,12 @@ inline bool map_tiles(Args& a, int bm, int bn) {
   return true;
 }
 
+// Steps to a share, and the shares that then hold any.
+inline int share_out(Args& a, int steps, int shares) {
+  a.share = (steps + shares - 1) / shares;
+  return (steps + a.share - 1) / a.share;
+}
+
 // Rows of `cols` bytes at any address, copied to rows `pitch` (a multiple of 16) bytes apart with
 // zeros behind them: those of `src`, then those of `src2`. A wave to a row.
 __global__ inline __launch_bounds__(256) void pad_rows(const int8_t* src, int64_t rows, const int8_t* src2, int64_t rows2,
@@ -274,18 +281,19 @@ inline bool pad_pays(int64_t M, int64_t N, int64_t K, int64_t copied, int64_t k,
 // partial one, in which a CU with one block (or two of three) is faster; the bytes of the weight and
 // the results. Rows forms: the chain of a wave's K steps, longer where a CU has several blocks, in
 // every further round of them, and with a weight that the caches do not hold; the bytes that all
-// blocks take in; a second kernel and the partial sums' bytes where K is split over blocks.
+// blocks take in. Both: a second kernel and the partial sums' bytes where K is split over blocks.
 struct TileCost {
-  float base, step_full, step_first, step_second, step_third, w_mb, out_mb;
+  float base, step_full, step_first, step_second, step_third, w_mb, out_mb, split, part_mb;
 };
 template <class C>
-float tile_cost(int64_t M, int64_t N, int64_t K, int k_step, int cus, const TileCost& c) {
-  const int64_t tiles = ((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN), slots = int64_t(cus) * C::kBlocksPerCu;
-  const int64_t rest = tiles % slots;
+float tile_cost(int64_t M, int64_t N, int64_t K, int k_step, int shares, int cus, const TileCost& c) {
+  const int64_t tiles = ((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN) * shares, slots = int64_t(cus) * C::kBlocksPerCu;
+  const int64_t rest = tiles % slots, steps = (K + k_step - 1) / k_step;
   const float per_step = c.step_full * float(tiles / slots) + c.step_first * float(rest > 0) +
                          c.step_second * float(rest > cus) + c.step_third * float(rest > 2 * int64_t(cus));
-  return c.base + float((K + k_step - 1) / k_step) * per_step + c.w_mb * float(N) * float(K) * 1e-6f +
-         c.out_mb * float(M) * float(N) * 2e-6f;
+  const float out = float(M) * float(N);
+  return c.base + float((steps + shares - 1) / shares) * per_step + c.w_mb * float(N) * float(K) * 1e-6f + c.out_mb * out * 2e-6f +
+         (shares > 1 ? c.split + c.part_mb * float(shares) * out * 4e-6f : 0.0f);
 }
 struct RowsCost {
   float base, chain, chain_second, chain_round, chain_w, mb, w_mb, out_mb, split, part_mb;

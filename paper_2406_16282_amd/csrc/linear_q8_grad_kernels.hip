@@ -109,7 +109,8 @@ struct TrTile {
   static_assert(kLdsBytes * kBlocksPerCu <= 160 * 1024, "LDS per CU");
 };
 
-template <class C, class OUT>
+// SPLIT: a share of K per blockIdx.y, the sums to a.part.
+template <class C, bool SPLIT, class OUT>
 __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Args a) {
   constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, kWaves = C::kWaves;
   constexpr int kLA = C::kLA, kLB = C::kLB, kL = kLA + kLB, kRing = C::kRing, kSlot = C::kSlot;
@@ -121,7 +122,8 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
   const int wave = wave_in_block();
   const int wm = wave / C::WN, wn = wave % C::WN;
   const uint32_t tiles = a.map.tiles;
-  const int steps = int((a.K + kTrStep - 1) / kTrStep);
+  const int first = SPLIT ? int(blockIdx.y) * a.share : 0, all_steps = int((a.K + kTrStep - 1) / kTrStep);
+  const int steps = SPLIT && all_steps - first > a.share ? a.share : all_steps - first;   // of this share
   // Unit u of row r of the slot is stored at u ^ swz(r): no read meets a bank conflict (bits 2 and 3 of r
   // for a cost one more pass in each of its reads, 364 us instead of 355 for 8192 rows of 11008 x 4096).
   auto swz_a = [](int r) { return (r >> 1) & 3; };
@@ -143,16 +145,17 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
   uint64_t pa = 0, pb = 0;
   uint32_t na = 0, nb = 0;   // records: bytes in range
   const uint32_t nb_step = kTrStep * pitch;
-  const int last_rows = int(a.K - int64_t(steps - 1) * kTrStep);
+  const int64_t rows_left = a.K - int64_t(first + steps - 1) * kTrStep;
+  const int last_rows = rows_left < kTrStep ? int(rows_left) : kTrStep;
   auto enter = [&]() {
     uint32_t tm = 0, tn = 0;
     const bool in = l_tile < tiles;   // past the last tile: zeros
     if (in) tile_of(l_tile, a.map, tm, tn);
     const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
     const uint32_t left = uint32_t(M - m0);   // M < 2^31
-    pa = reinterpret_cast<uint64_t>(a.a + m0 * a.a_pitch);
-    pb = reinterpret_cast<uint64_t>(a.b + n0);
-    na = in ? (left < uint32_t(BM) ? left : uint32_t(BM)) * uint32_t(a.a_pitch) : 0u;
+    pa = reinterpret_cast<uint64_t>(a.a + m0 * a.a_pitch) + uint64_t(first) * kTrStep;
+    pb = reinterpret_cast<uint64_t>(a.b + n0) + uint64_t(first) * nb_step;
+    na = in ? (left < uint32_t(BM) ? left : uint32_t(BM)) * uint32_t(a.a_pitch) - uint32_t(first) * kTrStep : 0u;
     nb = in ? uint32_t(steps == 1 ? last_rows : kTrStep) * pitch - uint32_t(n0) : 0u;
     l_slots = in ? steps : 0x7fffffff;
   };
@@ -266,6 +269,19 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
     const int64_t m0 = int64_t(tm) * BM + wm * TM * 16, n0 = int64_t(tn) * BN + wn * TN * 16;
     int lane_e = lane;
     asm volatile("" : "+v"(lane_e));
+    if constexpr (SPLIT) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int64_t row = m0 + i * 16 + (lane_e & 15);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const int64_t col = n0 + j * 16 + (lane_e >> 4) * 4;
+          if (row < M && col < N)
+            *reinterpret_cast<i32x4*>(a.part + (int64_t(blockIdx.y) * M + row) * a.part_pitch + col) = acc[i][j];
+        }
+      }
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t row = m0 + i * 16 + (lane_e & 15);
@@ -306,15 +322,33 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tr_tile(Arg
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives the block
 }
 
-template <class C, class OUT>
-hipError_t launch_tile(Args a, int dev, int cus, hipStream_t s) {
-  if (!map_tiles(a, C::BM, C::BN)) return hipErrorInvalidValue;
-  const hipError_t e = allow_lds<product_tr_tile<C, OUT>>(dev, C::kLdsBytes);
-  if (e != hipSuccess) return e;
-  const uint32_t slots = uint32_t(cus) * C::kBlocksPerCu;
-  hipLaunchKernelGGL((product_tr_tile<C, OUT>), dim3(a.map.tiles < slots ? a.map.tiles : slots), dim3(C::kThreads),
-                     C::kLdsBytes, s, a);
+// The shares' sums, added up in order (4 columns to a thread).
+template <class OUT>
+__global__ __launch_bounds__(256) void add_shares(Args a, int shares) {
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4, all = a.M * a.part_pitch;
+  if (i >= all) return;
+  i32x4 v = {0, 0, 0, 0};
+  for (int p = 0; p < shares; ++p) v += *reinterpret_cast<const i32x4*>(a.part + p * all + i);
+  const int64_t row = i / a.part_pitch;
+  finish4<OUT>(a, row, i - row * a.part_pitch, v, a.a_scale[row]);
+}
+template <class OUT>
+hipError_t launch_add_shares(const Args& a, int shares, hipStream_t s) {
+  const int64_t blocks = (a.M * a.part_pitch + 1023) / 1024;
+  hipLaunchKernelGGL((add_shares<OUT>), dim3(unsigned(blocks)), dim3(256), 0, s, a, shares);
   return hipGetLastError();
+}
+
+template <class C, bool SPLIT, class OUT>
+hipError_t launch_tile(Args a, int shares, int dev, int cus, hipStream_t s) {
+  if (!map_tiles(a, C::BM, C::BN)) return hipErrorInvalidValue;
+  const hipError_t e = allow_lds<product_tr_tile<C, SPLIT, OUT>>(dev, C::kLdsBytes);
+  if (e != hipSuccess) return e;
+  shares = share_out(a, int((a.K + kTrStep - 1) / kTrStep), shares);
+  const uint32_t slots = uint32_t(cus) * C::kBlocksPerCu;
+  hipLaunchKernelGGL((product_tr_tile<C, SPLIT, OUT>), dim3(a.map.tiles < slots ? a.map.tiles : slots, unsigned(shares)),
+                     dim3(C::kThreads), C::kLdsBytes, s, a);
+  return SPLIT ? launch_add_shares<OUT>(a, shares, s) : hipGetLastError();
 }
 
 using BigTile = TrTile<256, 256, 2, 4, 2>;      // one block of 8 waves per CU
@@ -425,80 +459,66 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
     for (int w = 1; w < kWaves; ++w) v += part[w][i][j][lane];
     const int64_t row = m0 + i * 16 + i16, col = n0 + j * 16 + g * 4;
     if (row >= M || col >= N) continue;
-    if (a.part != nullptr) {   // rows of partial sums are b's, so whole fours
-      *reinterpret_cast<i32x4*>(a.part + (int64_t(split) * M + row) * a.b_pitch + col) = v;
+    if (a.part != nullptr) {
+      *reinterpret_cast<i32x4*>(a.part + (int64_t(split) * M + row) * a.part_pitch + col) = v;
       continue;
     }
     finish4<OUT>(a, row, col, v, a.a_scale[row]);
   }
 }
 
-// The shares' sums, added up in order (4 columns to a thread).
-template <class OUT>
-__global__ __launch_bounds__(256) void add_shares(Args a, int shares) {
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (i >= a.M * a.b_pitch) return;
-  i32x4 v = {0, 0, 0, 0};
-  for (int p = 0; p < shares; ++p) v += *reinterpret_cast<const i32x4*>(a.part + int64_t(p) * a.M * a.b_pitch + i);
-  const int64_t row = i / a.b_pitch;
-  finish4<OUT>(a, row, i - row * a.b_pitch, v, a.a_scale[row]);
-}
-
 template <int MT, int D, class OUT>
 hipError_t launch_rows(Args a, int shares, hipStream_t s) {
   if (!map_tiles(a, MT * 16, 64)) return hipErrorInvalidValue;
-  const int steps = int((a.K + kTrStep - 1) / kTrStep);
-  a.share = (steps + shares - 1) / shares;
+  shares = share_out(a, int((a.K + kTrStep - 1) / kTrStep), shares);
   if (shares == 1) a.part = nullptr;
   static_assert(kTrRowsLds<MT, D> <= 64 * 1024, "no more than is allowed without asking");
   hipLaunchKernelGGL((product_tr_rows<MT, D, OUT>), dim3(a.map.tiles, unsigned(shares)), dim3(kRowsWaves * kWave),
                      (kTrRowsLds<MT, D>), s, a);
-  if (shares > 1) {
-    const int64_t blocks = (a.M * a.b_pitch + 1023) / 1024;
-    hipLaunchKernelGGL((add_shares<OUT>), dim3(unsigned(blocks)), dim3(256), 0, s, a, shares);
-  }
-  return hipGetLastError();
+  return shares > 1 ? launch_add_shares<OUT>(a, shares, s) : hipGetLastError();
 }
 
 enum Form { kRows16, kRows32, kRows64, kLow, kSmall, kMid, kBig, kForms };
 struct Plan {
   Form form;
-  int shares;   // of K, for the rows forms
+  int shares;   // of K, for the rows forms and the lowest tiles
 };
 
-constexpr RowsCost kRows16Cost = {2.625f, 0.2748f, 0.2102f, 0.6503f, 0.002209f, 0.02494f, 0.1602f, 0.6891f, 2.522f, 0.6569f};
-constexpr RowsCost kRows32Cost = {3.002f, 0.3285f, 0.2874f, 0.6502f, 0.002858f, 0.0204f, 0.1366f, 0.5392f, 2.5f, 0.5556f};
-constexpr RowsCost kRows64Cost = {3.865f, 0.44f, 0.4022f, 0.6351f, 0.004338f, 0.01361f, 0.08103f, 0.5614f, 2.518f, 0.5743f};
-constexpr TileCost kLowCost = {3.546f, 0.5144f, 0.2777f, 0.1192f, 0.1853f, 0.01071f, 0.2907f};
-constexpr TileCost kSmallCost = {4.609f, 0.546f, 0.3394f, 0.1923f, 0, 0, 0.2672f};
-constexpr TileCost kMidCost = {6.925f, 0.8417f, 0.492f, 0.3107f, 0, 0, 0.2087f};
-constexpr TileCost kBigCost = {7.826f, 0.8177f, 0.7358f, 0, 0, 0, 0.2235f};
+constexpr RowsCost kRows16Cost = {2.6f, 0.2819f, 0.1857f, 0.6247f, 0.002049f, 0.02439f, 0.1592f, 0.7644f, 2.624f, 0.6724f};
+constexpr RowsCost kRows32Cost = {3.066f, 0.3273f, 0.2738f, 0.6311f, 0.00255f, 0.02104f, 0.1365f, 0.5573f, 2.53f, 0.5608f};
+constexpr RowsCost kRows64Cost = {3.941f, 0.4253f, 0.4258f, 0.6417f, 0.004474f, 0.01234f, 0.07593f, 0.5821f, 2.654f, 0.5531f};
+constexpr TileCost kLowCost = {4.0f, 0.5062f, 0.2452f, 0.1427f, 0.1589f, 0.08949f, 0.2922f, 2.38f, 0.4422f};
+constexpr TileCost kSmallCost = {5.062f, 0.5398f, 0.3443f, 0.1797f, 0, 0, 0.3102f, 0, 0};
+constexpr TileCost kMidCost = {7.429f, 0.8145f, 0.4905f, 0.2797f, 0, 0.006095f, 0.2591f, 0, 0};
+constexpr TileCost kBigCost = {8.289f, 0.793f, 0.7208f, 0, 0, 0, 0.2536f, 0, 0};
 
 // The form by the estimates (linear_q8_device.hpp), their constants fitted to 420 sizes of 15 layers as
-// the forward's: 1.0% slower than the best on average, 30% at worst (1.1% on layers left out). Both sides,
+// the forward's: 0.8% slower than the best on average, 16% at worst (0.8% on layers left out). Both sides,
 // us, dy's rows included: 11008 x 4096 at 16 rows 16-row blocks 45.3, K split over 2 of them 29.5, 4 21.3,
-// 8 22.9; at 64 rows 64-row blocks 52.6, over 4 25.3; 197 rows 64-row blocks 44.4, 64x128 tiles 53.1; 1024
+// 8 22.9; at 64 rows 64-row blocks 57.7, over 4 26.8, 64x128 tiles over 8 24.1; 128 rows 64-row blocks over
+// 2 36.0, 64x128 64.8, over 2 41.1, over 4 29.4; 197 rows 64-row blocks 46.2, 64x128 54.0, over 2 36.8; 1024
 // rows 64x128 90, 128x128 80, 128x256 99; 1576 rows 128x128 122, 128x256 107; 8192 rows 128x256 388, 256x256 364.
 // 768 x 768 at 1024 rows 32-row blocks 9.9, 64x128 10.3; at 1576 rows 12.5 and 11.3.
 // The partial sums of a split K stay below 32 MiB, and K below 1024 is not split (at 16 rows of 768 x 768
-// 8.3 us against 6.4).
+// 8.3 us against 6.4). The forward's K is not split over blocks: over the same sizes it gave 0.3%.
 Plan make_plan(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr) {
   Plan best{kLow, 1};
-  float least = tile_cost<LowTile>(M, N, K, kTrStep, cus, kLowCost);
+  float least = tile_cost<LowTile>(M, N, K, kTrStep, 1, cus, kLowCost);
   auto take = [&](Form f, int shares, float t) {
     if (t < least) {
       least = t;
       best = {f, shares};
     }
   };
-  take(kSmall, 1, tile_cost<SmallTile>(M, N, K, kTrStep, cus, kSmallCost));
-  take(kMid, 1, tile_cost<MidTile>(M, N, K, kTrStep, cus, kMidCost));
-  take(kBig, 1, tile_cost<BigTile>(M, N, K, kTrStep, cus, kBigCost));
+  take(kSmall, 1, tile_cost<SmallTile>(M, N, K, kTrStep, 1, cus, kSmallCost));
+  take(kMid, 1, tile_cost<MidTile>(M, N, K, kTrStep, 1, cus, kMidCost));
+  take(kBig, 1, tile_cost<BigTile>(M, N, K, kTrStep, 1, cus, kBigCost));
   for (int shares = 1; shares <= 8 && M <= 1024; shares *= 2) {
     if (shares > 1 && (K < 1024 || int64_t(shares) * M * N * 4 > (int64_t(32) << 20))) break;
     take(kRows16, shares, rows_cost(M, N, K, 16, 64, kTrStep, 4, shares, cus, kRows16Cost));
     take(kRows32, shares, rows_cost(M, N, K, 32, 64, kTrStep, 3, shares, cus, kRows32Cost));
     take(kRows64, shares, rows_cost(M, N, K, 64, 64, kTrStep, 2, shares, cus, kRows64Cost));
+    if (shares > 1) take(kLow, shares, tile_cost<LowTile>(M, N, K, kTrStep, shares, cus, kLowCost));
   }
   if (time) *time = least;
   return best;
@@ -525,10 +545,12 @@ hipError_t launch(const Args& a, hipStream_t s) {
     case kRows16: return launch_rows<1, 2, OUT>(a, plan.shares, s);
     case kRows32: return launch_rows<2, 2, OUT>(a, plan.shares, s);
     case kRows64: return launch_rows<4, 2, OUT>(a, plan.shares, s);
-    case kLow: return launch_tile<LowTile, OUT>(a, dev, cus, s);
-    case kSmall: return launch_tile<SmallTile, OUT>(a, dev, cus, s);
-    case kMid: return launch_tile<MidTile, OUT>(a, dev, cus, s);
-    default: return launch_tile<BigTile, OUT>(a, dev, cus, s);
+    case kLow:
+      return plan.shares > 1 ? launch_tile<LowTile, true, OUT>(a, plan.shares, dev, cus, s)
+                             : launch_tile<LowTile, false, OUT>(a, 1, dev, cus, s);
+    case kSmall: return launch_tile<SmallTile, false, OUT>(a, 1, dev, cus, s);
+    case kMid: return launch_tile<MidTile, false, OUT>(a, 1, dev, cus, s);
+    default: return launch_tile<BigTile, false, OUT>(a, 1, dev, cus, s);
   }
 }
 
@@ -567,7 +589,7 @@ hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, i
     if (e != hipSuccess) return e;
   }
   int8_t* more = p + lq8::tr::more_at(M, N);
-  lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, K, nullptr, 0, {}};
+  lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, K, nullptr, lq8::padded(K), 0, {}};
   int dev = 0, cus = 0;
   const hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;

@@ -36,7 +36,8 @@
 // columns to a block 12.9 and 21.6 (768 x 768 4.7 against 3.9).
 //
 // One or two rows (product_few). Dot products: the matrix form would load as much and compute 16
-// rows; 9.1 us against 11.7 for 11008 x 4096 (2 rows: 10.0 and 12.0; 3 rows would take 12 either way).
+// rows; 9.1 us against 11.7 for 11008 x 4096 (2 rows: 10.0 and 12.0). Reloading each piece as soon as it
+// is used instead of four at a time gave nothing (one row) or cost 10% (two).
 #include "linear_q8_device.hpp"
 
 #include <algorithm>
@@ -501,7 +502,10 @@ constexpr TileCost kMidCost = {4.706f, 1.471f, 0.7827f, 0.561f, 0, 0.08527f, 0.2
 constexpr TileCost kBigCost = {5.923f, 1.435f, 1.257f, 0, 0, 0.003937f, 0.2741f};
 
 Form choose_form(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr) {
-  if (M <= 2) {
+  // Two rows of x take twice the loads of x against each of W; with large weights (which the caches do not
+  // hold) the matrix form is ahead: 13824 x 5120 19.3 and 15.5 us, 5120 x 13824 17.3 and 16.6, but 11008 x 4096
+  // 10.3 and 12.3, 4096 x 11008 12.6 and 14.2.
+  if (M == 1 || (M == 2 && N * K <= (int64_t(56) << 20))) {
     if (time) *time = 3.2f + float(N) * float(K) * (1.0f / 5.5e6f);
     return kFew;
   }
@@ -512,10 +516,10 @@ Form choose_form(int64_t M, int64_t N, int64_t K, int cus, float* time = nullptr
                            rows(16, 3, kRows16Cost),
                            rows(32, 2, kRows32Cost),
                            rows(64, 1, kRows64Cost),
-                           tile_cost<LowTile>(M, N, K, kBK, cus, kLowCost),
-                           tile_cost<SmallTile>(M, N, K, kBK, cus, kSmallCost),
-                           tile_cost<MidTile>(M, N, K, kBK, cus, kMidCost),
-                           tile_cost<BigTile>(M, N, K, kBK, cus, kBigCost)};
+                           tile_cost<LowTile>(M, N, K, kBK, 1, cus, kLowCost),
+                           tile_cost<SmallTile>(M, N, K, kBK, 1, cus, kSmallCost),
+                           tile_cost<MidTile>(M, N, K, kBK, 1, cus, kMidCost),
+                           tile_cost<BigTile>(M, N, K, kBK, 1, cus, kBigCost)};
   const float* const least = std::min_element(t, t + kForms);
   if (time) *time = *least;
   return Form(least - t);
@@ -574,7 +578,7 @@ size_t linear_q8_fwd_workspace(int64_t M, int64_t N, int64_t K) {
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
                                 const int8_t* w, const float* w_scale, const void* bias, void* y, void* workspace,
                                 hipStream_t s) {
-  lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, K, nullptr, 0, {}};
+  lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, K, nullptr, 0, 0, {}};
   int dev = 0, cus = 0;
   hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;

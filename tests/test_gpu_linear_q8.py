@@ -25,7 +25,8 @@ SIZES = [(3000, 33, 65), (64, 9001, 301), (3, 5, 65), (4, 1, 130), (2, 7, 193), 
          (128, 256, 128), (129, 257, 144), (200, 768, 768), (256, 512, 1024), (257, 528, 1024), (333, 1001, 1023),
          (300, 1003, 4099), (700, 1001, 1023), (1100, 1027, 2051), (20, 100, 4096), (40, 272, 8192), (3000, 272, 272),
          (1100, 2050, 2000), (513, 1040, 2064), (700, 96, 131056), (1000, 8, 32), (1025, 2064, 528), (2100, 4112, 784),
-         (2, 33, 2048), (1, 1001, 2064), (2, 13, 4112)]
+         (2, 33, 2048), (1, 1001, 2064), (2, 13, 4112), (276, 880, 5378), (577, 464, 7414), (347, 809, 7223),
+         (130, 784, 6611), (581, 2448, 9527), (2, 13824, 4352)]
 
 
 def half(t):
@@ -143,6 +144,7 @@ def test_the_sizes_take_every_form():
     bwd = set(forms(1, [(m, n, k) for m, k, n in SIZES] + LARGE))
     assert {f for f, _, _ in bwd} == set(range(1, 9)) and {c for _, _, c in bwd} == {0, 1}, bwd
     assert {s for f, s, _ in bwd if f <= 3} >= {1, 2, 4, 8}, bwd
+    assert {s for f, s, _ in bwd if f == 4} >= {1, 2, 4, 8}, bwd
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 32, 131071), (70, 64, 131056), (3, 9, 131071)])
