@@ -19,6 +19,7 @@
  *   q8_rows / q8_values            rows in 8 bits with one scale each, and back
  *   msrms_q8_fwd / msrms_q8_bwd    MS-RMSNorm with the residual's addition, output in 8 bits
  *   linear_q8_fwd / linear_q8_bwd  a frozen linear layer of 8-bit rows and 8-bit weights
+ *   linear_bias_grad               the gradient of a linear layer's bias
  *
  * Conventions shared by every call
  * --------------------------------
@@ -374,6 +375,20 @@ lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n,
                           const void *dy, const int8_t *w, const float *w_scale,
                           const void *add, void *dx, void *workspace, int64_t workspace_bytes,
                           void *stream);
+
+/* ------------------------------------------------------------------------
+ * Gradient of a linear layer's bias: db[n] = sum over the rows of dy [m x n], added up in fp32 in
+ * a fixed order, one rounding to dt_db. (linear_act_bwd has it with the activation's backward.)
+ *
+ *   dt, dt_db : types of dy and db, any two.
+ *   m, n      : any sizes >= 0, n below 2^31; m = 0 gives db = 0.
+ *   workspace : lmbp_linear_bias_grad_bytes(m, n) bytes on the calling thread's current device,
+ *               16-byte aligned, NULL if that is 0.
+ * Nothing overlaps.
+ * ------------------------------------------------------------------------ */
+lmbp_status linear_bias_grad(lmbp_dtype dt, lmbp_dtype dt_db, int64_t m, int64_t n, const void *dy,
+                             void *db, void *workspace, int64_t workspace_bytes, void *stream);
+size_t lmbp_linear_bias_grad_bytes(int64_t m, int64_t n);
 
 /* ------------------------------------------------------------------------
  * Test utilities (host only, no launch): the kernel form that a size takes on the calling

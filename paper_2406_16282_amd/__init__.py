@@ -23,6 +23,7 @@ from .binding import (  # noqa: F401
     lib,
     linear_act_bwd,
     linear_act_fwd,
+    linear_bias_grad,
     linear_q8_bwd,
     linear_q8_fwd,
     linear_swiglu_fwd,

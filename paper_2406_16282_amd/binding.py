@@ -116,6 +116,10 @@ def lib():
     L.lmbp_linear_q8_fwd_bytes.argtypes = L.lmbp_linear_q8_bwd_bytes.argtypes = [i64, i64, i64]
     L.lmbp_linear_q8_fwd_bytes.restype = L.lmbp_linear_q8_bwd_bytes.restype = ctypes.c_size_t
     L.linear_q8_bwd.argtypes = [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.linear_bias_grad.argtypes = [i32, i32, i64, i64, vp, vp, vp, i64, vp]
+    L.linear_bias_grad.restype = i32
+    L.lmbp_linear_bias_grad_bytes.argtypes = [i64, i64]
+    L.lmbp_linear_bias_grad_bytes.restype = ctypes.c_size_t
     L.lmbp_linear_q8_form.argtypes = [i64, i64, i64, i32, counts, counts]
     for name in (*Q8_OPS, "lmbp_linear_q8_form"):
         getattr(L, name).restype = i32
@@ -928,3 +932,20 @@ def linear_q8_bwd(dy, w, w_scale, add=None, dx=None, dtype=None, stream=None):
         _check("linear_q8_bwd", L.linear_q8_bwd(dt, dt_dx, m, n, k, _ptr(dy), _ptr(w), _ptr(w_scale), _opt(add), _ptr(dx),
                                                 _ptr(work), nbytes, handle))
     return dx
+
+
+def linear_bias_grad(dy, dtype=None, stream=None):
+    """Gradient of a linear layer's bias: the sum of dy [..., n] over its rows, added up in fp32 in a
+    fixed order, in ``dtype`` (dy's unless given)."""
+    _dev(dy, "dy")
+    dt = _dtype_code(dy)
+    m, n = _q8_rows_cols(dy)
+    db = torch.empty(n, dtype=dtype or dy.dtype, device=dy.device)
+    dt_db = _dtype_code(db)
+    L = lib()
+    with _device_of(dy):   # launches go to the tensors' GPU
+        nbytes = L.lmbp_linear_bias_grad_bytes(m, n)
+        handle = _stream(dy, stream)
+        work = _workspace(nbytes, dy, stream) if nbytes else None
+        _check("linear_bias_grad", L.linear_bias_grad(dt, dt_db, m, n, _ptr(dy), _ptr(db), _opt(work), nbytes, handle))
+    return db

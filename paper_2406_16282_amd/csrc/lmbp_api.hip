@@ -512,6 +512,23 @@ lmbp_status msrms_q8_bwd_impl(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int
                                             static_cast<hipStream_t>(stream)));
 }
 
+lmbp_status linear_bias_grad_impl(lmbp_dtype dt, lmbp_dtype dt_db, int64_t m, int64_t n, const void* dy, void* db,
+                                  void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!known_dtype(dt) || !known_dtype(dt_db)) return LMBP_EDTYPE;
+  if (n >= int64_t(1) << 31 || bad_matrix(m, n)) return LMBP_EINVAL;
+  if (n == 0) return LMBP_OK;
+  if (!db || (m > 0 && !dy)) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt), eb_db = elem_bytes(dt_db);
+  if (!aligned(db, eb_db) || (m > 0 && !aligned(dy, eb))) return LMBP_EINVAL;
+  const uint64_t need = lmbp_linear_bias_grad_bytes(m, n);
+  if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || uint64_t(workspace_bytes) < need))
+    return LMBP_EINVAL;
+  const Span sy = span(dy, uint64_t(m) * uint64_t(n) * eb), sd = span(db, uint64_t(n) * eb_db), sp = span(workspace, need);
+  if (overlaps(sd, sy) || overlaps(sp, sy) || overlaps(sp, sd)) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_linear_bias_grad(dt == LMBP_BF16, dt_db == LMBP_BF16, m, n, dy, db, workspace,
+                                                static_cast<hipStream_t>(stream)));
+}
+
 bool bad_layer(int64_t m, int64_t n, int64_t k) {
   const int64_t lim = int64_t(1) << 31;
   return m < 0 || n < 0 || k < 0 || m >= lim || n >= lim || k >= lim;
@@ -693,6 +710,14 @@ lmbp_status msrms_linear_swiglu_fwd(lmbp_dtype dt, int64_t m, int64_t n, int64_t
                                       stream);
 }
 
+size_t lmbp_linear_bias_grad_bytes(int64_t m, int64_t n) {
+  if (m <= 0 || n <= 0 || n >= int64_t(1) << 31 || bad_matrix(m, n)) return 0;
+  return lmbp::linear_bias_grad_workspace(m, n);
+}
+lmbp_status linear_bias_grad(lmbp_dtype dt, lmbp_dtype dt_db, int64_t m, int64_t n, const void* dy, void* db,
+                             void* workspace, int64_t workspace_bytes, void* stream) {
+  return linear_bias_grad_impl(dt, dt_db, m, n, dy, db, workspace, workspace_bytes, stream);
+}
 lmbp_status q8_rows(lmbp_dtype dt, int64_t rows, int64_t cols, const void* x, int8_t* q, float* scale, void* stream) {
   return q8_rows_impl(dt, rows, cols, x, q, scale, stream);
 }

@@ -144,6 +144,11 @@ struct LinearQ8Form {
 LinearQ8Form linear_q8_fwd_form(int64_t M, int64_t N, int64_t K);
 LinearQ8Form linear_q8_bwd_form(int64_t M, int64_t N, int64_t K);
 
+// Sums over the rows of dy; db_bf16: the type of db. A workspace of the function's bytes, 16-byte aligned.
+size_t linear_bias_grad_workspace(int64_t m, int64_t n);
+hipError_t launch_linear_bias_grad(bool bf16, bool db_bf16, int64_t m, int64_t n, const void* dy, void* db, void* workspace,
+                                   hipStream_t s);
+
 hipError_t launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);
 
 }  // namespace lmbp

@@ -270,7 +270,8 @@ def _product_q8(q, q_scale, weight, scale, bias, dtype):
 
 
 def _bias_grad(dy, dtype):
-    return dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32).to(dtype)
+    kept = dtype if dtype in (torch.float32, torch.bfloat16) else torch.float32
+    return binding.linear_bias_grad(_flat(dy), kept).to(dtype)
 
 
 class LinearQ8(nn.Module):

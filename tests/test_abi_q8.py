@@ -107,11 +107,27 @@ def test_linear_q8_bwd(L):
     assert f(dx=at(0)) == f(dx=at(1)) == f(dx=at(2)) == f(dx=at(4)) == f(work=at(0)) == f(work=at(1)) == B.EOVERLAP
 
 
+def test_linear_bias_grad(L):
+    assert [L.lmbp_linear_bias_grad_bytes(*s) for s in ((0, 8), (8, 0), (-1, 8), (1, 1 << 31), (4, 8))] == [0] * 5
+    need = L.lmbp_linear_bias_grad_bytes(1 << 17, 8)
+    assert need > 0
+
+    def f(dt=B.BF16, dt_db=B.BF16, m=4, n=32, dy=at(0), db=at(1), work=None, size=0):
+        return L.linear_bias_grad(dt, dt_db, m, n, dy, db, work, size, None)
+    assert f(dt=5) == f(dt_db=5) == B.EDTYPE
+    assert f(m=-1) == f(n=-1) == f(n=1 << 31) == f(m=1 << 60, n=1 << 20) == B.EINVAL
+    assert f(n=0, dy=None, db=None) == B.OK
+    assert f(dy=None) == f(db=None) == f(dy=at(0) + 1) == f(dt_db=B.FP32, db=at(1) + 2) == B.EINVAL
+    big = dict(m=1 << 17, n=8, db=at(0) - 64)
+    assert f(**big) == f(**big, work=at(0) - 4096, size=need - 1) == f(**big, work=at(0) - 4088, size=need) == B.EINVAL
+    assert f(**big, work=at(0), size=need) == f(db=at(0)) == B.EOVERLAP
+
+
 def test_the_binding_refuses_what_is_not_on_a_gpu():
     x, q, one = torch.zeros(2, 16), torch.zeros(2, 16, dtype=torch.int8), torch.ones(2)
     for call in (lambda: lmbp.q8_rows(x), lambda: lmbp.q8_values(q, one), lambda: lmbp.msrms_q8_fwd(x, 1e-5),
                  lambda: lmbp.msrms_q8_bwd(x, q, one, one), lambda: lmbp.linear_q8_fwd(q, one, q, one),
-                 lambda: lmbp.linear_q8_bwd(x, q, one)):
+                 lambda: lmbp.linear_q8_bwd(x, q, one), lambda: lmbp.linear_bias_grad(x)):
         with pytest.raises(ValueError, match="GPU tensor"):
             call()
 

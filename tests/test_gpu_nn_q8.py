@@ -239,6 +239,61 @@ def test_graph_of_the_block(rows):
             assert all(torch.equal(a, b) for a, b in zip(o, w)), f"replay {replay}"
 
 
+def test_captured_training_step():
+    """The modules' forward and backward in one graph. The eager steps have leaves of their own and
+    their graphs are gone before the capture; every replay against an eager step."""
+    parts = mlp(256, 688, torch.bfloat16)
+    ins = [torch.randn(130, 256, device=DEV, dtype=torch.bfloat16) for _ in range(4)]
+
+    def eager():
+        x, res, dy, ds = (v.clone() for v in ins)
+        return [v.detach() for v in step(parts, x.requires_grad_(), res.requires_grad_(), dy, ds)]
+
+    eager()
+    torch.cuda.synchronize()
+    x, res = (v.clone().requires_grad_() for v in ins[:2])
+    dy, ds = (v.clone() for v in ins[2:])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = [v.detach() for v in step(parts, x, res, dy, ds)]
+    for replay in range(3):
+        with torch.no_grad():
+            for v, to in zip(ins, (x, res, dy, ds)):
+                v.normal_()
+                to.copy_(v)
+            for v in out:
+                v.fill_(7.0)
+        want = eager()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), f"replay {replay}"
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n", [(130, 272), (20011, 48), (6000, 1024), (100000, 16), (70000, 1)])
+def test_captured_bias_gradients(rows, n, dtype):
+    """The biases' gradients, sums over all rows, in a graph. Of small whole numbers, so that every
+    order of additions in fp32 is exact: every replay against the sum in 64 bits."""
+    torch.manual_seed(5)
+    mod = LinearQ8.from_linear(torch.nn.Linear(64, n, device=DEV, dtype=dtype))
+    mod.bias.requires_grad_()
+    x = torch.randn(rows, 64, device=DEV, dtype=dtype)
+    dy = torch.randint(-8, 9, (rows, n), device=DEV).to(dtype)
+    torch.autograd.grad(mod(x), mod.bias, dy)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        db, = torch.autograd.grad(mod(x), mod.bias, dy)
+    for replay in range(4):
+        dy.copy_(torch.randint(-8, 9, (rows, n), device=DEV))
+        eager, = torch.autograd.grad(mod(x), mod.bias, dy)
+        db.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = dy.double().sum(0).to(dtype)
+        assert torch.equal(db, want) and torch.equal(eager, want), f"replay {replay}"
+
+
 def test_on_another_stream():
     parts = mlp(256, 688, torch.bfloat16)
     x, res = (torch.randn(200, 256, device=DEV, dtype=torch.bfloat16, requires_grad=True) for _ in range(2))
