@@ -364,7 +364,10 @@ class _NormLinearQ8(torch.autograd.Function):
 class MSRMSNormLinearQ8(nn.Module):
     """Residual addition, RMSNorm without weight (Alg. 3; its affine merged into the layers)
     and the ``LinearQ8`` layers behind it. ``forward(x, res)`` returns the layers' outputs and
-    s = x + res; ``forward(x)`` the outputs alone (one tensor for a single layer)."""
+    s = x + res; ``forward(x)`` the outputs alone (one tensor for a single layer).
+
+    To capture forward and backward in a graph, let go of the eager graphs of the same leaves
+    first: autograd would wait for the stream that they ran on."""
 
     def __init__(self, layers, eps=1e-5):
         super().__init__()
