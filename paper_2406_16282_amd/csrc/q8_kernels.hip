@@ -15,7 +15,10 @@
 //
 // msrms_q8_fwd, per row: s = x + res rounded to the storage type, rstd = 1 / sqrt(p^-1 |s|^2
 // + eps), z = s rstd. z is a multiple of s, so q comes from s itself and rstd only enters
-// the scale: scale = a rstd / 127 with a the largest |s|.
+// the scale: scale = a rstd / 127 with a the largest |s|. Squares that add up to 2^128 or more (a
+// value above 2^64, or many near it) are added up again as (s 2^-96)^2, which no row overflows; what
+// falls below the smallest number there is less than 2^-60 of the sum. One wave does so for its row,
+// from memory and behind everything else: of the pieces in registers it cost every call 10 to 20 registers.
 // msrms_q8_bwd: with z = q scale, dx = rstd (dz - z p^-1 z^T dz) + ds.
 #include "lmbp_launch.hpp"
 #include "q8_device.hpp"
@@ -39,6 +42,21 @@ struct FwdArgs {
   int64_t rows, cols, pitch;   // pitch: bytes from one row of q to the next, zeros behind the row
   float eps;
 };
+
+__device__ inline bool overflowed(float sum) { return !(fabsf(sum) < INFINITY); }   // or NaN
+
+// rstd of a row, and the scale of one whose largest magnitude is a, of its mean square + eps; that mean
+// may be one of unit^2 times the squares.
+constexpr float kDown = 0x1p-96f;
+__device__ inline float add_square_down(float v, float sum) { return __builtin_fmaf(v * kDown, v * kDown, sum); }
+__device__ inline float mean_down(float sum_down, int64_t cols, float eps) {
+  return sum_down / float(cols) + eps * kDown * kDown;
+}
+__device__ inline void store_stats(const FwdArgs& f, int64_t row, float mean, float unit, float a) {
+  const float rs = rsqrtf(mean);
+  f.rstd[row] = rs * unit;
+  f.scale[row] = a * unit * rs / 127.0f;
+}
 
 // Threads per block of the register kernels: 256, or one row of WPR waves where that is wider.
 template <int WPR>
@@ -128,6 +146,10 @@ template <class IO, int MODE, int VPL, int WPR, bool RAGGED>
 __global__ __launch_bounds__(block_of<WPR>()) void fwd_rows(FwdArgs a) {
   constexpr int P = IO::kPerVec, TPR = kWave * WPR, RPB = block_of<WPR>() / TPR;
   constexpr bool kIsNorm = MODE == kNorm || MODE == kNormRes;
+  // Rows of 8 waves and more with many pieces: the waves' sums are read behind the pieces' use, not held in
+  // 8 or 16 registers meanwhile ([4096 x 20000] fp32 66.7 us, else 76.9; elsewhere that only ends the block
+  // later, [8192 x 4096] fp32 30.1 us against 28.8).
+  constexpr bool kSumLate = WPR == 16 || (WPR == 8 && VPL == 4);
   __shared__ uint32_t most_lds[2][block_of<WPR>() / kWave];
   __shared__ float sum_lds[block_of<WPR>() / kWave];
   const int t = threadIdx.x % TPR;
@@ -208,7 +230,7 @@ __global__ __launch_bounds__(block_of<WPR>()) void fwd_rows(FwdArgs a) {
 #pragma unroll
       for (int k = 0; k < WPR; ++k) {
         most = umax(most, most_lds[turn][first + k]);
-        if constexpr (kIsNorm) sum += sum_lds[first + k];
+        if constexpr (kIsNorm && !kSumLate) sum += sum_lds[first + k];
       }
     }
     if (!active) continue;   // the last group: no barrier follows
@@ -235,14 +257,26 @@ __global__ __launch_bounds__(block_of<WPR>()) void fwd_rows(FwdArgs a) {
     if constexpr (MODE == kColumns) {
       for (int k = cols + t; k < a.pitch; k += TPR) q[k] = 0;
     }
-    if (t == 0) {
-      if constexpr (kIsNorm) {
-        const float rs = rsqrtf(sum / float(cols) + a.eps);
-        a.rstd[row] = rs;
-        a.scale[row] = w.a * rs / 127.0f;
-      } else {
-        a.scale[row] = w.a / 127.0f;
+    if constexpr (kIsNorm) {
+      if (t < kWave) {   // the row's first wave
+        if constexpr (kSumLate) {
+          const int first = threadIdx.x / kWave;
+#pragma unroll
+          for (int k = 0; k < WPR; ++k) sum += sum_lds[first + k];
+        }
+        float mean = sum / float(cols) + a.eps, unit = 1.0f;
+        if (w.finite && overflowed(mean)) {
+          __threadfence_block();   // s is read as other lanes and waves stored it
+          float down = 0.0f;
+#pragma unroll 1
+          for (int k = t; k < cols; k += kWave) down = add_square_down(IO::load1(MODE == kNormRes ? a.s : a.x, base + k), down);
+          mean = mean_down(wave_sum(down), cols, a.eps);
+          unit = kDown;
+        }
+        if (t == 0) store_stats(a, row, mean, unit, w.a);
       }
+    } else if (t == 0) {
+      a.scale[row] = w.a / 127.0f;
     }
     if constexpr (MODE != kColumns) return;   // a block for every group
   }
@@ -394,6 +428,18 @@ __global__ __launch_bounds__(256) void fwd_any(FwdArgs a) {
   }
   block_max_sum(most, sum, most_lds, sum_lds);
   const Q8Row w = q8_row(most);
+  float mean = sum / float(a.cols) + a.eps, unit = 1.0f;
+  if constexpr (MODE == kNorm || MODE == kNormRes) {
+    if (w.finite && overflowed(mean)) {   // for all threads or none
+      unit = kDown;
+      float down = 0.0f;
+      for (int64_t k = tid; k < a.cols; k += 256)
+        down = add_square_down(IO::load1(MODE == kNormRes ? a.s : a.x, base + k), down);
+      __syncthreads();   // the sums of before have been read
+      block_max_sum(most, down, most_lds, sum_lds);
+      mean = mean_down(down, a.cols, a.eps);
+    }
+  }
   for (int64_t k = tid; k < a.pitch; k += 256) {
     uint32_t v = 0;
     if (k < a.cols) {
@@ -404,13 +450,8 @@ __global__ __launch_bounds__(256) void fwd_any(FwdArgs a) {
     a.q[row * a.pitch + k] = int8_t(v);
   }
   if (tid == 0) {
-    if constexpr (MODE == kNorm || MODE == kNormRes) {
-      const float rs = rsqrtf(sum / float(a.cols) + a.eps);
-      a.rstd[row] = rs;
-      a.scale[row] = w.a * rs / 127.0f;
-    } else {
-      a.scale[row] = w.a / 127.0f;
-    }
+    if constexpr (MODE == kNorm || MODE == kNormRes) store_stats(a, row, mean, unit, w.a);
+    else a.scale[row] = w.a / 127.0f;
   }
 }
 

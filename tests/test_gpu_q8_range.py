@@ -1,0 +1,64 @@
+"""Rows of every size through MS-RMSNorm into 8 bits.
+
+A finite row stands for s rstd whatever its size, also where its squares add up to more than
+fp32 holds. The bounds are those of test_gpu_q8_rows.py
+(chains of p / 64 + 24 additions, then the roundings counted there: scaling by a power of two
+rounds nothing), and half a step of the smallest numbers, 2^-150, where rstd is one of them.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_16282_amd as lmbp
+from oracle import q8
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+# the register form with 1, 2, 4, 8 and 16 waves to a row, rows at any address, and a block per row
+COLS = [1, 40, 768, 1025, 2049, 4096, 12345, 13824, 30011, 70000, 140001]
+SIZES = [1.0, 2.0 ** 60, 2.0 ** 64, 2.0 ** 100, 2.0 ** 122, 2.0 ** -40, 2.0 ** -90, 0.0]
+
+
+def n64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def draw(rows, cols, dtype, seed, sizes):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g).clamp_(-8, 8)
+    x *= torch.tensor([sizes[i % len(sizes)] for i in range(rows)])[:, None]
+    return x.to(TYPES[dtype]).to(DEV)
+
+
+def rows_of_every_size(cols, dtype, seed):
+    x = draw(13, cols, dtype, seed, SIZES)
+    x[8:] = draw(5, cols, dtype, seed + 1, [1.0])
+    x[8, cols // 2] = 2.0 ** 80          # one value far above the rest of its row
+    x[9, cols - 1] = -2.0 ** 127
+    x[10, 0] = 2.0 ** 66
+    x[11] = 2.0 ** 127                   # all of them as large as they come
+    x[12, : (cols + 1) // 2] *= 2.0 ** -60
+    return x
+
+
+@pytest.mark.parametrize("eps", [1e-5, 1e-30, 1e30])
+@pytest.mark.parametrize("with_res", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", COLS)
+def test_norm(cols, dtype, with_res, eps):
+    print(f"[q8] range {cols} {dtype} res {with_res} eps {eps}", flush=True)
+    x = rows_of_every_size(cols, dtype, 1)
+    res = draw(13, cols, dtype, 3, [1.0, 2.0 ** 58, 2.0 ** 30, 2.0 ** 99]) if with_res else None
+    q, scale, rstd, *s = lmbp.msrms_q8_fwd(x, eps, res)
+    torch.cuda.synchronize()
+    q_o, sc_o, r_o, s_o = q8.msrms_fwd(n64(x), None if res is None else n64(res), float(np.float32(eps)), dtype)
+    assert np.isfinite(s_o).all()
+    if with_res:
+        assert np.array_equal(n64(s[0]), s_o)
+    assert np.array_equal(n64(q), q_o)
+    c = cols / 64 + 24
+    assert (np.abs(n64(rstd) - r_o) <= 1.01 * U * (c / 2 + 4) * r_o + 2.0 ** -149).all()
+    assert (np.abs(n64(scale) - sc_o) <= 1.01 * U * (c / 2 + 6) * sc_o + 2.0 ** -149).all()
