@@ -326,6 +326,7 @@ lmbp_status q8_values(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t *q
  * Backward: with z = q scale,  dx = rstd (dz - z mean(z dz)) + ds.
  *           dx is the gradient of x and of res alike; ds is the gradient that reaches s
  *           past the norm.
+ *           dz of any size, as long as dz - z mean(z dz) is one of fp32's numbers.
  *
  *   x, res, s : rows x cols of dtype. res and s both NULL or both given; s == x and
  *               s == res are allowed, x == res too.

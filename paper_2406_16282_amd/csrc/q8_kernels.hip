@@ -19,6 +19,7 @@
 // value above 2^64, or many near it) are added up again as (s 2^-96)^2, which no row overflows; what
 // falls below the smallest number there is less than 2^-60 of the sum. One wave does so for its row,
 // from memory and behind everything else: of the pieces in registers it cost every call 10 to 20 registers.
+// The backward's sum of q dz is formed again of dz 2^-56 in the same case, by each wave for its pieces.
 // msrms_q8_bwd: with z = q scale, dx = rstd (dz - z p^-1 z^T dz) + ds.
 #include "lmbp_launch.hpp"
 #include "q8_device.hpp"
@@ -43,7 +44,11 @@ struct FwdArgs {
   float eps;
 };
 
-__device__ inline bool overflowed(float sum) { return !(fabsf(sum) < INFINITY); }   // or NaN
+// Infinite or NaN, of a sum that is the same in all lanes: a scalar condition, so that the other side of the
+// branch costs no registers.
+__device__ inline bool overflowed(float sum) {
+  return (uint32_t(__builtin_amdgcn_readfirstlane(__float_as_int(sum))) & 0x7f800000u) == 0x7f800000u;
+}
 
 // rstd of a row, and the scale of one whose largest magnitude is a, of its mean square + eps; that mean
 // may be one of unit^2 times the squares.
@@ -313,6 +318,15 @@ __global__ __launch_bounds__(block_of<WPR>()) void values_rows(const int8_t* q, 
   if (RAGGED && at < cols) IO::store1(v, base + at, float(q[base + at]) * sc);
 }
 
+// b = sc^2 p^-1 sum, the factor of q in z mean(z dz); down: the sum of q (dz kDownDz), for a sum that
+// has overflowed.
+constexpr float kDownDz = 0x1p-56f;
+__device__ inline float along(float sum, float down, int64_t cols, float sc) {
+  // A branch: a choice of values takes 7 registers more ([8192 x 11008] bf16 72.5 us against 65.6).
+  if (overflowed(sum)) return sc * (sc * (down / float(cols))) / kDownDz;
+  return sc * (sc * (sum / float(cols)));
+}
+
 struct BwdArgs {
   const void* dz;
   const int8_t* q;
@@ -326,7 +340,7 @@ struct BwdArgs {
 template <class DZ, class IO, int VPL, int WPR, bool RAGGED>
 __global__ __launch_bounds__(block_of<WPR>()) void norm_bwd_rows(BwdArgs a) {
   constexpr int P = IO::kPerVec, TPR = kWave * WPR, RPB = block_of<WPR>() / TPR;
-  __shared__ float sum_lds[block_of<WPR>() / kWave];
+  __shared__ float sum_lds[2][block_of<WPR>() / kWave];
   const int t = threadIdx.x % TPR;
   const int64_t row = int64_t(blockIdx.x) * RPB + wave_in_block() / WPR;
   const bool active = row < a.rows;
@@ -366,16 +380,36 @@ __global__ __launch_bounds__(block_of<WPR>()) void norm_bwd_rows(BwdArgs a) {
     for (int e = 0; e < P; ++e) sum = __builtin_fmaf(z[e], g[e], sum);
   }
   sum = wave_sum(sum);
+  float down = sum * kDownDz;
+  if (overflowed(sum)) {
+    down = last_dz * kDownDz * last_q;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) {
+      float g[P], z[P];
+      dz[j].get(g);
+      q[j].get(z);
+#pragma unroll
+      for (int e = 0; e < P; ++e) down = __builtin_fmaf(z[e], g[e] * kDownDz, down);
+    }
+    down = wave_sum(down);
+  }
   if constexpr (WPR > 1) {
     const int wave = threadIdx.x / kWave, first = wave / WPR * WPR;
-    if ((threadIdx.x & (kWave - 1)) == 0) sum_lds[wave] = sum;
+    if ((threadIdx.x & (kWave - 1)) == 0) {
+      sum_lds[0][wave] = sum;
+      sum_lds[1][wave] = down;
+    }
     __syncthreads();
     sum = 0.0f;
+    down = 0.0f;
 #pragma unroll
-    for (int k = 0; k < WPR; ++k) sum += sum_lds[first + k];
+    for (int k = 0; k < WPR; ++k) {
+      sum += sum_lds[0][first + k];
+      down += sum_lds[1][first + k];
+    }
     if (!active) return;
   }
-  const float b = sc * (sc * (sum / float(cols)));
+  const float b = along(sum, down, cols, sc);
 #pragma unroll
   for (int j = 0; j < VPL; ++j) {
     const int idx = j * TPR + t;
@@ -471,7 +505,14 @@ __global__ __launch_bounds__(256) void norm_bwd_any(const void* dz, const int8_t
   float s = 0.0f;
   for (int64_t k = threadIdx.x; k < cols; k += 256) s = __builtin_fmaf(float(q[base + k]), DZ::load1(dz, base + k), s);
   const float sc = scale[row], rs = rstd[row];
-  const float b = sc * (sc * (block_sum(s, red) / float(cols)));
+  const float sum = block_sum(s, red);
+  float down = 0.0f;
+  if (overflowed(sum)) {   // for all threads or none
+    for (int64_t k = threadIdx.x; k < cols; k += 256)
+      down = __builtin_fmaf(float(q[base + k]), DZ::load1(dz, base + k) * kDownDz, down);
+    down = block_sum(down, red);
+  }
+  const float b = along(sum, down, cols, sc);
   for (int64_t k = threadIdx.x; k < cols; k += 256) {
     const float g = __builtin_fmaf(-float(q[base + k]), b, DZ::load1(dz, base + k));
     IO::store1(dx, base + k, ds != nullptr ? __builtin_fmaf(rs, g, IO::load1(ds, base + k)) : rs * g);

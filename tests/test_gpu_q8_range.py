@@ -1,7 +1,7 @@
-"""Rows of every size through MS-RMSNorm into 8 bits.
+"""Rows of every size through MS-RMSNorm into 8 bits and back.
 
 A finite row stands for s rstd whatever its size, also where its squares add up to more than
-fp32 holds. The bounds are those of test_gpu_q8_rows.py
+fp32 holds, and so does the backward's sum of q dz. The bounds are those of test_gpu_q8_rows.py
 (chains of p / 64 + 24 additions, then the roundings counted there: scaling by a power of two
 rounds nothing), and half a step of the smallest numbers, 2^-150, where rstd is one of them.
 """
@@ -62,3 +62,24 @@ def test_norm(cols, dtype, with_res, eps):
     c = cols / 64 + 24
     assert (np.abs(n64(rstd) - r_o) <= 1.01 * U * (c / 2 + 4) * r_o + 2.0 ** -149).all()
     assert (np.abs(n64(scale) - sc_o) <= 1.01 * U * (c / 2 + 6) * sc_o + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("dt_dz,dtype", [("bf16", "bf16"), ("fp32", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("cols", COLS)
+def test_norm_backward(cols, dt_dz, dtype):
+    x = draw(13, cols, dtype, 5, [1.0, 2.0 ** 3, 2.0 ** 70, 2.0 ** -3, 2.0 ** 110])
+    q, scale, rstd = lmbp.msrms_q8_fwd(x, 1e-5)
+    dz = draw(13, cols, dt_dz, 6, [1e-3, 2.0 ** 121, 2.0 ** 118, 2.0 ** -60, 2.0 ** 100, 2.0 ** 122])
+    ds = draw(13, cols, dtype, 7, [1e-3, 2.0 ** 100])
+    for more in (None, ds):
+        dx = lmbp.msrms_q8_bwd(dz, q, scale, rstd, more, dtype=TYPES[dtype])
+        torch.cuda.synchronize()
+        dx_o = q8.msrms_bwd(n64(dz), n64(q), n64(scale), n64(rstd), None if more is None else n64(more))
+        c = cols / 64 + 24
+        g, w, sc, rs = n64(dz), n64(q), n64(scale)[:, None], n64(rstd)[:, None]
+        most = np.abs(w) * sc * sc / cols * np.abs(w * g).sum(axis=1, keepdims=True)
+        # what passes the largest number of the type (2^128) is none of this test's: no value here does
+        assert (np.abs(dx_o) < 2.0 ** 127).all() and (np.abs(g) + most < 2.0 ** 127).all()
+        room = rs * most * (c + 4) * U + 3 * U * (rs * (np.abs(g) + most) + np.abs(dx_o))
+        room = 1.01 * (room + torch.finfo(TYPES[dtype]).eps / 2 * np.abs(dx_o)) + 2.0 ** -133
+        assert (np.abs(n64(dx) - dx_o) <= room).all()
