@@ -36,12 +36,13 @@ __device__ inline void load(const void* p, int64_t i, float (&f)[P]) {
 }
 
 // pieces: threads across columns (a power of two up to 64); a group of `share` rows per blockIdx.y,
-// its sums to row blockIdx.y of out.
+// its sums to row blockIdx.y of out. first_block: blocks across columns of the launches before.
 template <class IO, class OUT, int P>
-__global__ __launch_bounds__(256) void column_sums(const void* dy, int64_t m, int64_t n, int pieces, int64_t share, void* out) {
+__global__ __launch_bounds__(256) void column_sums(const void* dy, int64_t m, int64_t n, int pieces, int64_t share, void* out,
+                                                   int64_t first_block) {
   __shared__ float lds[256 * P];
   const int tx = threadIdx.x & (pieces - 1), ty = threadIdx.x / pieces, rows = 256 / pieces;
-  const int64_t col = (int64_t(blockIdx.x) * pieces + tx) * P;
+  const int64_t col = ((first_block + blockIdx.x) * pieces + tx) * P;
   const int64_t first = int64_t(blockIdx.y) * share, end = m - first < share ? m : first + share;
   float sum[P];
 #pragma unroll
@@ -87,10 +88,10 @@ Plan make_plan(int64_t m, int64_t n, bool wide, int cus) {
 
 template <class IO, class OUT>
 hipError_t launch(const Plan& a, int64_t m, int64_t n, const void* dy, void* out, hipStream_t s) {
-  if (a.blocks > 0x7fffffff) return hipErrorInvalidValue;
   const auto kernel = a.p == 4 ? column_sums<IO, OUT, 4> : column_sums<IO, OUT, 1>;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(a.blocks), unsigned(a.groups)), dim3(256), 0, s, dy, m, n, a.pieces, a.share, out);
-  return hipGetLastError();
+  return in_parts(a.blocks, most_blocks(256), [&](int64_t first, int64_t count) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(count), unsigned(a.groups)), dim3(256), 0, s, dy, m, n, a.pieces, a.share, out, first);
+  });
 }
 template <class OUT>
 hipError_t launch_from(bool bf16, const Plan& a, int64_t m, int64_t n, const void* dy, void* out, hipStream_t s) {

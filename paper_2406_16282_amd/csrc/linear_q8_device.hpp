@@ -37,6 +37,7 @@ struct Args {
   int64_t part_pitch;     // N in whole sixteens
   int32_t share;          // steps of K to a share
   TileMap map;
+  uint32_t first;         // product_any, product_few: blocks of the launches before (in_parts)
 };
 
 // 16 and 8 bytes at any element's address (global memory takes such accesses).
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(256) void product_any(Args a) {
   __shared__ __attribute__((aligned(16))) int8_t lds[64 * 1024];
   const int lane = threadIdx.x & (kWave - 1), wave = wave_in_block();
   const int64_t tiles_n = (a.N + 63) / 64;
-  const int64_t m0 = int64_t(blockIdx.x) / tiles_n * 64, n0 = int64_t(blockIdx.x) % tiles_n * 64;
+  const int64_t block = int64_t(a.first) + blockIdx.x, m0 = block / tiles_n * 64, n0 = block % tiles_n * 64;
   int8_t* const la = lds + wave * 2 * 64 * kAnyRow;
   int8_t* const lb = la + 64 * kAnyRow;
   const int r = lane / 4, c = (lane % 4) * 16, g = lane >> 4, i16 = lane & 15;
@@ -206,11 +207,13 @@ __global__ __launch_bounds__(256) void product_any(Args a) {
 }
 
 template <class OUT, bool TR>
-hipError_t launch_any(const Args& a, hipStream_t s) {
+hipError_t launch_any(Args a, hipStream_t s) {
   const int64_t blocks = ((a.M + 63) / 64) * ((a.N + 63) / 64);
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((product_any<OUT, TR>), dim3(unsigned(blocks)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return in_parts(blocks, most_blocks(256), [&](int64_t first, int64_t count) {
+    a.first = uint32_t(first);
+    hipLaunchKernelGGL((product_any<OUT, TR>), dim3(unsigned(count)), dim3(256), 0, s, a);
+  });
 }
 
 // More than 64 KiB of dynamic LDS must be allowed explicitly, per kernel and device: done on the
@@ -243,8 +246,8 @@ inline int share_out(Args& a, int steps, int shares) {
 // Rows of `cols` bytes at any address, copied to rows `pitch` (a multiple of 16) bytes apart with
 // zeros behind them: those of `src`, then those of `src2`. A wave to a row.
 __global__ inline __launch_bounds__(256) void pad_rows(const int8_t* src, int64_t rows, const int8_t* src2, int64_t rows2,
-                                                       int64_t cols, int8_t* dst, int64_t pitch) {
-  int64_t row = int64_t(blockIdx.x) * 4 + wave_in_block();
+                                                       int64_t cols, int8_t* dst, int64_t pitch, int64_t first) {
+  int64_t row = (first + blockIdx.x) * 4 + wave_in_block();
   if (row >= rows + rows2) return;
   int8_t* const to = dst + row * pitch;
   if (row >= rows) {
@@ -261,10 +264,9 @@ __global__ inline __launch_bounds__(256) void pad_rows(const int8_t* src, int64_
 }
 inline hipError_t launch_pad(const int8_t* src, int64_t rows, const int8_t* src2, int64_t rows2, int64_t cols, int8_t* dst,
                              int64_t pitch, hipStream_t s) {
-  const int64_t blocks = (rows + rows2 + 3) / 4;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(pad_rows, dim3(unsigned(blocks)), dim3(256), 0, s, src, rows, src2, rows2, cols, dst, pitch);
-  return hipGetLastError();
+  return in_parts((rows + rows2 + 3) / 4, most_blocks(256), [&](int64_t first, int64_t count) {
+    hipLaunchKernelGGL(pad_rows, dim3(unsigned(count)), dim3(256), 0, s, src, rows, src2, rows2, cols, dst, pitch, first);
+  });
 }
 inline int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 

@@ -469,7 +469,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_tr_rows(Args a) {
 
 template <int MT, int D, class OUT>
 hipError_t launch_rows(Args a, int shares, hipStream_t s) {
-  if (!map_tiles(a, MT * 16, 64)) return hipErrorInvalidValue;
+  if (!map_tiles(a, MT * 16, 64) || a.map.tiles > most_blocks(kRowsWaves * kWave)) return hipErrorInvalidValue;
   shares = share_out(a, int((a.K + kTrStep - 1) / kTrStep), shares);
   if (shares == 1) a.part = nullptr;
   static_assert(kTrRowsLds<MT, D> <= 64 * 1024, "no more than is allowed without asking");
@@ -589,7 +589,7 @@ hipError_t launch_linear_q8_bwd(bool bf16, bool dx_bf16, int64_t M, int64_t N, i
     if (e != hipSuccess) return e;
   }
   int8_t* more = p + lq8::tr::more_at(M, N);
-  lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, K, nullptr, lq8::padded(K), 0, {}};
+  lq8::Args a{p, w, N > 0 ? p_scale : nullptr, nullptr, nullptr, add, dx, M, K, N, pitch, K, nullptr, lq8::padded(K), 0, {}, 0};
   int dev = 0, cus = 0;
   const hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;

@@ -410,7 +410,7 @@ __global__ __launch_bounds__(kRowsWaves * kWave) void product_rows(Args a) {
 
 template <int MT, int NB, int D, bool NT, class OUT>
 hipError_t launch_rows(Args a, int dev, hipStream_t s) {
-  if (!map_tiles(a, MT * 16, NB * 16)) return hipErrorInvalidValue;
+  if (!map_tiles(a, MT * 16, NB * 16) || a.map.tiles > most_blocks(kRowsWaves * kWave)) return hipErrorInvalidValue;
   const hipError_t e = allow_lds<product_rows<MT, NB, D, NT, OUT>>(dev, kRowsLds<MT, NB, D>);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((product_rows<MT, NB, D, NT, OUT>), dim3(a.map.tiles), dim3(kRowsWaves * kWave), (kRowsLds<MT, NB, D>),
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void product_few(Args a) {
   constexpr int kDeep = 4 / R;   // pieces of a row in flight
   const uint32_t K = uint32_t(a.K);
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t n0 = (int64_t(blockIdx.x) * kFewWaves + wave_in_block()) * R;
+  const int64_t n0 = ((int64_t(a.first) + blockIdx.x) * kFewWaves + wave_in_block()) * R;
   if (n0 >= a.N) return;
   const int rows_b = a.N - n0 < R ? int(a.N - n0) : R;
   const auto rb = make_rsrc(a.b + n0 * K, int64_t(rows_b) * K), ra = make_rsrc(a.a, a.M * K);
@@ -472,11 +472,13 @@ __global__ __launch_bounds__(kFewWaves * kWave) void product_few(Args a) {
 }
 
 template <int MT, class OUT>
-hipError_t launch_few(const Args& a, hipStream_t s) {
+hipError_t launch_few(Args a, hipStream_t s) {
   auto launch = [&](auto kernel, int rows) {
     const int64_t per = int64_t(kFewWaves) * rows;
-    hipLaunchKernelGGL(kernel, dim3(unsigned((a.N + per - 1) / per)), dim3(kFewWaves * kWave), 0, s, a);
-    return hipGetLastError();
+    return in_parts((a.N + per - 1) / per, most_blocks(kFewWaves * kWave), [&](int64_t first, int64_t count) {
+      a.first = uint32_t(first);
+      hipLaunchKernelGGL(kernel, dim3(unsigned(count)), dim3(kFewWaves * kWave), 0, s, a);
+    });
   };
   // Two rows of W to a wave where they are short. One row of x, two against one: 11008 x 1024 4.65 and
   // 6.1 us, 11008 x 2048 6.0 and 7.0; 11008 x 4096 9.8 and 9.1 (two rows of x: 10.6 and 10.0). Four were
@@ -578,7 +580,7 @@ size_t linear_q8_fwd_workspace(int64_t M, int64_t N, int64_t K) {
 hipError_t launch_linear_q8_fwd(bool bf16, int64_t M, int64_t N, int64_t K, const int8_t* q, const float* scale,
                                 const int8_t* w, const float* w_scale, const void* bias, void* y, void* workspace,
                                 hipStream_t s) {
-  lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, K, nullptr, 0, 0, {}};
+  lq8::Args a{q, w, scale, w_scale, bias, nullptr, y, M, N, K, K, K, nullptr, 0, 0, {}, 0};
   int dev = 0, cus = 0;
   hipError_t e = current_device(dev, cus);
   if (e != hipSuccess) return e;

@@ -5,12 +5,28 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace lmbp {
 
 enum { kGelu = 0, kSilu = 1 };
 
 constexpr int kXcds = 8;          // consecutive blocks go to them in turn
 constexpr int kMaxDevices = 64;   // of one process
+
+// HIP takes fewer than 2^32 threads to a grid dimension. A launch of more reports success and runs
+// their number modulo 2^32 (measured), so where the number of blocks grows with the data the launch goes
+// out in parts: f(first, count) launches units first .. first + count - 1, at most `part` of them.
+constexpr int64_t most_blocks(int threads) { return int64_t(0xffffffff) / threads; }
+template <class F>
+hipError_t in_parts(int64_t count, int64_t part, F f) {
+  for (int64_t first = 0; first < count; first += part) {
+    f(first, std::min(part, count - first));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 // The current device and its CU count (queried once per device).
 hipError_t current_device(int& dev, int& cus);

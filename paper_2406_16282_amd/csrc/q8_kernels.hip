@@ -556,50 +556,65 @@ int64_t blocks_of(int64_t rows) {
   constexpr int rpb = block_of<WPR>() / (kWave * WPR);
   return (rows + rpb - 1) / rpb;
 }
+// Rows that one launch takes.
+template <int WPR>
+constexpr int64_t rows_at_once() { return most_blocks(block_of<WPR>()) * (block_of<WPR>() / (kWave * WPR)); }
 
 bool at16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+template <class T>
+T* moved(T* p, int64_t bytes) {   // null stays null
+  return p == nullptr ? p : reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(p) + bytes);
+}
 
 template <class IO, int MODE>
 hipError_t launch_fwd(const FwdArgs& a, hipStream_t s) {
   const bool ragged = a.cols % IO::kPerVec != 0 || !at16(a.x) || (MODE == kNormRes && (!at16(a.res) || !at16(a.s))) ||
                       reinterpret_cast<uintptr_t>(a.q) % IO::kPerVec != 0;
-  int64_t blocks = 0;
   int dev = 0, cus = 0;
+  hipError_t e = hipSuccess;
   if (MODE == kColumns) {
-    const hipError_t e = current_device(dev, cus);
+    e = current_device(dev, cus);
     if (e != hipSuccess) return e;
   }
+  auto rows_of = [&](int64_t first, int64_t rows) {
+    const int64_t at = first * a.cols * IO::kBytes;
+    return FwdArgs{moved(a.x, at), moved(a.res, at), a.columns, moved(a.s, at), a.q + first * a.pitch, a.scale + first,
+                   moved(a.rstd, first * 4), rows, a.cols, a.pitch, a.eps};
+  };
   const bool held = a.cols < (1 << 24) && with_shape<MODE == kColumns && IO::kPerVec == 8 ? 4 : 8>(a.cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
-    blocks = blocks_of<W>(a.rows);
-    if (MODE == kColumns) blocks = std::min<int64_t>(blocks, int64_t(cus) * (1024 / block_of<W>()));
-    if (blocks > 0x7fffffff) return;
     const auto kernel = ragged ? fwd_rows<IO, MODE, V, W, true> : fwd_rows<IO, MODE, V, W, false>;
-    hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, a);
+    // With a factor per column the blocks walk the rows: any number of rows in one launch.
+    e = in_parts(a.rows, MODE == kColumns ? a.rows : rows_at_once<W>(), [&](int64_t first, int64_t rows) {
+      int64_t blocks = blocks_of<W>(rows);
+      if (MODE == kColumns) blocks = std::min<int64_t>(blocks, int64_t(cus) * (1024 / block_of<W>()));
+      hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, rows_of(first, rows));
+    });
   });
-  if (!held) {
-    blocks = a.rows;
-    if (blocks <= 0x7fffffff) hipLaunchKernelGGL((fwd_any<IO, MODE>), dim3(unsigned(blocks)), dim3(256), 0, s, a);
-  }
-  return blocks > 0x7fffffff ? hipErrorInvalidValue : hipGetLastError();
+  if (held) return e;
+  return in_parts(a.rows, most_blocks(256), [&](int64_t first, int64_t rows) {
+    hipLaunchKernelGGL((fwd_any<IO, MODE>), dim3(unsigned(rows)), dim3(256), 0, s, rows_of(first, rows));
+  });
 }
 
 template <class IO>
 hipError_t launch_values(int64_t rows, int64_t cols, const int8_t* q, const float* scale, void* v, hipStream_t s) {
   const bool ragged = cols % IO::kPerVec != 0 || !at16(v) || reinterpret_cast<uintptr_t>(q) % IO::kPerVec != 0;
-  int64_t blocks = 0;
+  hipError_t e = hipSuccess;
   const bool held = cols < (1 << 24) && with_shape<8>(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
-    blocks = blocks_of<W>(rows);
-    if (blocks > 0x7fffffff) return;
     const auto kernel = ragged ? values_rows<IO, V, W, true> : values_rows<IO, V, W, false>;
-    hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, q, scale, v, rows, int(cols));
+    e = in_parts(rows, rows_at_once<W>(), [&](int64_t first, int64_t count) {
+      hipLaunchKernelGGL(kernel, dim3(unsigned(blocks_of<W>(count))), dim3(block_of<W>()), 0, s, q + first * cols, scale + first,
+                         moved(v, first * cols * IO::kBytes), count, int(cols));
+    });
   });
-  if (!held) {
-    blocks = rows;
-    if (blocks <= 0x7fffffff) hipLaunchKernelGGL((values_any<IO>), dim3(unsigned(blocks)), dim3(256), 0, s, q, scale, v, cols);
-  }
-  return blocks > 0x7fffffff ? hipErrorInvalidValue : hipGetLastError();
+  if (held) return e;
+  return in_parts(rows, most_blocks(256), [&](int64_t first, int64_t count) {
+    hipLaunchKernelGGL((values_any<IO>), dim3(unsigned(count)), dim3(256), 0, s, q + first * cols, scale + first,
+                       moved(v, first * cols * IO::kBytes), cols);
+  });
 }
 
 template <class DZ, class IO>
@@ -607,21 +622,25 @@ hipError_t launch_norm_bwd(int64_t rows, int64_t cols, const void* dz, const int
                            const float* rstd, const void* ds, void* dx, hipStream_t s) {
   const bool ragged = cols % IO::kPerVec != 0 || !at16(dz) || !at16(ds) || !at16(dx) ||
                       reinterpret_cast<uintptr_t>(q) % IO::kPerVec != 0;
-  int64_t blocks = 0;
-  const BwdArgs a{dz, q, scale, rstd, ds, dx, rows, cols};
+  hipError_t e = hipSuccess;
+  auto rows_of = [&](int64_t first, int64_t count) {
+    const int64_t at = first * cols;
+    return BwdArgs{moved(dz, at * DZ::kBytes), q + at, scale + first, rstd + first, moved(ds, at * IO::kBytes),
+                   moved(dx, at * IO::kBytes), count, cols};
+  };
   const bool held = cols < (1 << 24) && with_shape<IO::kPerVec == 8 ? 4 : 8>(cols / IO::kPerVec, [&](auto vpl, auto wpr) {
     constexpr int V = decltype(vpl)::value, W = decltype(wpr)::value;
-    blocks = blocks_of<W>(rows);
-    if (blocks > 0x7fffffff) return;
     const auto kernel = ragged ? norm_bwd_rows<DZ, IO, V, W, true> : norm_bwd_rows<DZ, IO, V, W, false>;
-    hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(block_of<W>()), 0, s, a);
+    e = in_parts(rows, rows_at_once<W>(), [&](int64_t first, int64_t count) {
+      hipLaunchKernelGGL(kernel, dim3(unsigned(blocks_of<W>(count))), dim3(block_of<W>()), 0, s, rows_of(first, count));
+    });
   });
-  if (!held) {
-    blocks = rows;
-    if (blocks <= 0x7fffffff)
-      hipLaunchKernelGGL((norm_bwd_any<DZ, IO>), dim3(unsigned(blocks)), dim3(256), 0, s, dz, q, scale, rstd, ds, dx, cols);
-  }
-  return blocks > 0x7fffffff ? hipErrorInvalidValue : hipGetLastError();
+  if (held) return e;
+  return in_parts(rows, most_blocks(256), [&](int64_t first, int64_t count) {
+    const BwdArgs a = rows_of(first, count);
+    hipLaunchKernelGGL((norm_bwd_any<DZ, IO>), dim3(unsigned(count)), dim3(256), 0, s, a.dz, a.q, a.scale, a.rstd, a.ds, a.dx,
+                       cols);
+  });
 }
 
 }  // namespace q8

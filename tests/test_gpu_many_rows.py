@@ -1,0 +1,86 @@
+"""More rows, channels or columns than one launch takes (2^32 threads in a grid dimension): narrow
+tensors, whose results are compared with those of their halves."""
+
+import ctypes
+
+import pytest
+import torch
+
+import paper_2406_16282_amd as lmbp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def same(whole, first, second):
+    half = first.shape[0]
+    return torch.equal(whole[:half], first) and torch.equal(whole[half:], second)
+
+
+@pytest.mark.parametrize("cols", [1, 8])
+def test_8_bit_rows(cols):
+    """Four rows to a block of 256 threads: 2^26 rows and more."""
+    rows, half = 2 ** 26 + 5, 2 ** 25
+    x = torch.randn(rows, cols, device=DEV).to(torch.bfloat16)
+    q, scale = lmbp.q8_rows(x)
+    (q0, s0), (q1, s1) = lmbp.q8_rows(x[:half]), lmbp.q8_rows(x[half:])
+    assert same(q, q0, q1) and same(scale, s0, s1)
+    assert same(lmbp.q8_values(q, scale), lmbp.q8_values(q0, s0), lmbp.q8_values(q1, s1))
+    print(f"[q8] rows done {cols}", flush=True)
+    del q, scale, q0, s0, q1, s1
+    res = torch.randn(rows, cols, device=DEV).to(torch.bfloat16)
+    whole = lmbp.msrms_q8_fwd(x, 1e-5, res)
+    parts = lmbp.msrms_q8_fwd(x[:half], 1e-5, res[:half]), lmbp.msrms_q8_fwd(x[half:], 1e-5, res[half:])
+    assert all(same(w, a, b) for w, a, b in zip(whole, *parts))
+    q, scale, rstd, _ = whole
+    dx = lmbp.msrms_q8_bwd(x, q, scale, rstd, res)
+    assert same(dx, *(lmbp.msrms_q8_bwd(x[p], q[p], scale[p], rstd[p], res[p]) for p in (slice(half), slice(half, None))))
+
+
+def form(m, n, k, grad=0):
+    copies = ctypes.c_int64()
+    return lmbp.lib().lmbp_linear_q8_form(m, n, k, grad, None, copies), copies.value
+
+
+def layer(m, n, k):
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q = torch.randint(-127, 128, (m, k), generator=g, device=DEV, dtype=torch.int8)
+    w = torch.randint(-127, 128, (n, k), generator=g, device=DEV, dtype=torch.int8)
+    return q, torch.rand(m, generator=g, device=DEV), w, torch.rand(n, generator=g, device=DEV)
+
+
+# A row of x against 2^27 and more channels (dot products); as many channels and no product at all
+# (the general form); 2^26 and more rows that are copied to aligned ones first.
+@pytest.mark.parametrize("m,n,k,kind", [(1, 2 ** 27 + 3, 16, (0, 0)), (1, 2 ** 30 + 5, 0, (8, 0)), (2 ** 26 + 9, 256, 255, (None, 1))])
+def test_8_bit_products(m, n, k, kind):
+    got = form(m, n, k)
+    assert kind[0] in (None, got[0]) and got[1] == kind[1], got
+    q, scale, w, w_scale = layer(m, n, k)
+    bias = torch.randn(n, device=DEV).to(torch.bfloat16)
+    y = lmbp.linear_q8_fwd(q, scale, w, w_scale, bias)
+    print(f"[q8] {m} {n} {k} done", flush=True)
+    if m == 1:
+        for at in range(0, n, 2 ** 24):
+            part = slice(at, at + 2 ** 24)
+            assert torch.equal(y[:, part], lmbp.linear_q8_fwd(q, scale, w[part], w_scale[part], bias[part]))
+        assert k > 0 or torch.equal(y[0], bias)
+    else:
+        for at in range(0, m, 2 ** 23):
+            part = slice(at, at + 2 ** 23)
+            assert torch.equal(y[part], lmbp.linear_q8_fwd(q[part], scale[part], w, w_scale, bias))
+
+
+def test_bias_gradient():
+    """A column to a thread, 64 of them to a block: 2^30 columns and more."""
+    m, n = 2, 2 ** 30 + 5
+    dy = torch.randint(-8, 9, (m, n), device=DEV, dtype=torch.int8).to(torch.bfloat16)
+    db = lmbp.linear_bias_grad(dy)
+    for at in range(0, n, 2 ** 26):
+        assert torch.equal(db[at:at + 2 ** 26], dy[0, at:at + 2 ** 26] + dy[1, at:at + 2 ** 26])
