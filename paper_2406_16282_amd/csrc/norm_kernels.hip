@@ -523,22 +523,21 @@ hipError_t fwd_dispatch(NormShape sh, bool ragged, int64_t rows, int cols, float
     if constexpr (reachable(W, V, LMBP_NORM_FWD_VPL)) {
       if (sh.wpr == W && sh.vpl == V) {
         constexpr int rpb = norm_block<W>() / (kWave * W);
-        const int64_t blocks = (rows + rpb - 1) / rpb;
-        if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-        if (ragged) {
-          hipLaunchKernelGGL((norm_fwd_vec<IO, LN, V, W, true>), dim3(unsigned(blocks)), dim3(norm_block<W>()),
-                             0, s, x, z, rstd, rows, cols, eps);
-          return hipGetLastError();
-        }
+        constexpr int64_t most = most_blocks(norm_block<W>());
         if constexpr (W <= LMBP_NORM_FWD_PIPE_WPR) {
-          const int64_t grid = persistent_grid<norm_fwd_pipe<IO, LN, V, W>>(norm_block<W>(), blocks);
-          hipLaunchKernelGGL((norm_fwd_pipe<IO, LN, V, W>), dim3(unsigned(grid)), dim3(norm_block<W>()),
-                             0, s, x, z, rstd, rows, cols, eps);
-          return hipGetLastError();
+          if (!ragged) {
+            const int64_t grid = persistent_grid<norm_fwd_pipe<IO, LN, V, W>>(norm_block<W>(), (rows + rpb - 1) / rpb);
+            hipLaunchKernelGGL((norm_fwd_pipe<IO, LN, V, W>), dim3(unsigned(std::min(grid, most))), dim3(norm_block<W>()),
+                               0, s, x, z, rstd, rows, cols, eps);
+            return hipGetLastError();
+          }
         }
-        hipLaunchKernelGGL((norm_fwd_vec<IO, LN, V, W>), dim3(unsigned(blocks)), dim3(norm_block<W>()),
-                           0, s, x, z, rstd, rows, cols, eps);
-        return hipGetLastError();
+        const auto kernel = ragged ? norm_fwd_vec<IO, LN, V, W, true> : norm_fwd_vec<IO, LN, V, W>;
+        return in_parts(rows, most * rpb, [&](int64_t first, int64_t count) {
+          const int64_t at = first * cols * IO::kBytes;
+          hipLaunchKernelGGL(kernel, dim3(unsigned((count + rpb - 1) / rpb)), dim3(norm_block<W>()), 0, s,
+                             static_cast<const char*>(x) + at, static_cast<char*>(z) + at, rstd + first, count, cols, eps);
+        });
       }
     }
     return fwd_dispatch<IO, LN, I + 1>(sh, ragged, rows, cols, eps, x, z, rstd, s);
@@ -555,15 +554,13 @@ hipError_t bwd_dispatch(NormShape sh, bool ragged, int64_t rows, int cols, const
     if constexpr (reachable(W, V, LMBP_NORM_BWD_VPL)) {
       if (sh.wpr == W && sh.vpl == V) {
         constexpr int rpb = norm_block<W>() / (kWave * W);
-        const int64_t blocks = (rows + rpb - 1) / rpb;
-        if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-        if (ragged)
-          hipLaunchKernelGGL((norm_bwd_vec<IO, LN, V, W, true>), dim3(unsigned(blocks)), dim3(norm_block<W>()),
-                             0, s, dz, z, rstd, dx, rows, cols);
-        else
-          hipLaunchKernelGGL((norm_bwd_vec<IO, LN, V, W>), dim3(unsigned(blocks)), dim3(norm_block<W>()),
-                             0, s, dz, z, rstd, dx, rows, cols);
-        return hipGetLastError();
+        const auto kernel = ragged ? norm_bwd_vec<IO, LN, V, W, true> : norm_bwd_vec<IO, LN, V, W>;
+        return in_parts(rows, most_blocks(norm_block<W>()) * rpb, [&](int64_t first, int64_t count) {
+          const int64_t at = first * cols * IO::kBytes;
+          hipLaunchKernelGGL(kernel, dim3(unsigned((count + rpb - 1) / rpb)), dim3(norm_block<W>()), 0, s,
+                             static_cast<const char*>(dz) + at, static_cast<const char*>(z) + at, rstd + first,
+                             static_cast<char*>(dx) + at, count, cols);
+        });
       }
     }
     return bwd_dispatch<IO, LN, I + 1>(sh, ragged, rows, cols, dz, z, rstd, dx, s);
@@ -575,10 +572,11 @@ hipError_t norm_fwd_t(int64_t rows, int64_t cols, float eps, const void* x, void
                       bool vec_ok, hipStream_t s) {
   const NormShape sh = pick_shape(std::max<int64_t>(1, cols / IO::kPerVec), LMBP_NORM_FWD_VPL);
   if (sh.wpr != 0) return fwd_dispatch<IO, LN, 0>(sh, !vec_ok, rows, int(cols), eps, x, z, rstd, s);
-  if (rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((norm_fwd_any<IO, LN>), dim3(unsigned(rows)), dim3(256), 0, s, x, z, rstd, rows,
-                     cols, eps);
-  return hipGetLastError();
+  return in_parts(rows, most_blocks(256), [&](int64_t first, int64_t count) {
+    const int64_t at = first * cols * IO::kBytes;
+    hipLaunchKernelGGL((norm_fwd_any<IO, LN>), dim3(unsigned(count)), dim3(256), 0, s, static_cast<const char*>(x) + at,
+                       static_cast<char*>(z) + at, rstd + first, count, cols, eps);
+  });
 }
 
 template <class IO, bool LN>
@@ -586,10 +584,11 @@ hipError_t norm_bwd_t(int64_t rows, int64_t cols, const void* dz, const void* z,
                       void* dx, bool vec_ok, hipStream_t s) {
   const NormShape sh = pick_shape(std::max<int64_t>(1, cols / IO::kPerVec), LMBP_NORM_BWD_VPL);
   if (sh.wpr != 0) return bwd_dispatch<IO, LN, 0>(sh, !vec_ok, rows, int(cols), dz, z, rstd, dx, s);
-  if (rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((norm_bwd_any<IO, LN>), dim3(unsigned(rows)), dim3(256), 0, s, dz, z, rstd, dx,
-                     rows, cols);
-  return hipGetLastError();
+  return in_parts(rows, most_blocks(256), [&](int64_t first, int64_t count) {
+    const int64_t at = first * cols * IO::kBytes;
+    hipLaunchKernelGGL((norm_bwd_any<IO, LN>), dim3(unsigned(count)), dim3(256), 0, s, static_cast<const char*>(dz) + at,
+                       static_cast<const char*>(z) + at, rstd + first, static_cast<char*>(dx) + at, count, cols);
+  });
 }
 }  // namespace
 

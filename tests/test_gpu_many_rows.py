@@ -44,6 +44,18 @@ def test_8_bit_rows(cols):
     assert same(dx, *(lmbp.msrms_q8_bwd(x[p], q[p], scale[p], rstd[p], res[p]) for p in (slice(half), slice(half, None))))
 
 
+@pytest.mark.parametrize("op", ["msln", "msrms"])
+@pytest.mark.parametrize("cols", [1, 8])
+def test_norms(op, cols):
+    rows, half = 2 ** 26 + 5, 2 ** 25
+    fwd, bwd = getattr(lmbp, f"{op}_fwd"), getattr(lmbp, f"{op}_bwd")
+    x = torch.randn(rows, cols, device=DEV).to(torch.bfloat16)
+    z, rstd = fwd(x, 1e-5)
+    (z0, r0), (z1, r1) = fwd(x[:half], 1e-5), fwd(x[half:], 1e-5)
+    assert same(z, z0, z1) and same(rstd, r0, r1)
+    assert same(bwd(x, z, rstd), bwd(x[:half], z0, r0), bwd(x[half:], z1, r1))
+
+
 def form(m, n, k, grad=0):
     copies = ctypes.c_int64()
     return lmbp.lib().lmbp_linear_q8_form(m, n, k, grad, None, copies), copies.value
