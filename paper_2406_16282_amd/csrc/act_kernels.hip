@@ -365,57 +365,57 @@ constexpr int glu_vpl() {
 }
 template <class IO>
 constexpr int act_block() { return std::is_same<IO, F32>::value ? LMBP_ACT_BLOCK_F32 : LMBP_ACT_BLOCK; }
-template <class IO, int VPL>
-int64_t tile_blocks(int64_t n) {
-  constexpr int wpb = act_block<IO>() / kWave;
-  constexpr int64_t tile = int64_t(kWave) * VPL * IO::kPerVec;
-  const int64_t waves = (n + tile - 1) / tile;
-  return (waves + wpb - 1) / wpb;
+// The launches of a tensor of n elements, VPL vectors to a thread: f(blocks, first element, elements). Parts
+// start on whole tiles, so on whole vectors and code words.
+template <class IO, int VPL, class F>
+hipError_t tile_launches(int64_t n, F f) {
+  constexpr int64_t per_block = int64_t(act_block<IO>()) * VPL * IO::kPerVec;
+  return in_parts(n, most_blocks(act_block<IO>()) * per_block, [&](int64_t first, int64_t count) {
+    f(unsigned((count + per_block - 1) / per_block), first, count);
+  });
 }
 template <class IO>
-int64_t act_blocks(int64_t n) { return tile_blocks<IO, act_vpl<IO>()>(n); }
+const void* elements(const void* p, int64_t first) { return static_cast<const char*>(p) + first * IO::kBytes; }
 template <class IO>
-int64_t glu_blocks(int64_t n) { return tile_blocks<IO, glu_vpl<IO>()>(n); }
+void* elements(void* p, int64_t first) { return static_cast<char*>(p) + first * IO::kBytes; }
 }  // namespace
 
 template <class IO, int ACT>
 hipError_t launch_act_fwd_t(int64_t n, const void* x, void* y, uint32_t* codes, bool vec_ok,
                             hipStream_t s) {
-  const int64_t blocks = act_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((act_fwd_kernel<IO, ACT, act_vpl<IO>()>), dim3(unsigned(blocks)), dim3(act_block<IO>()), 0, s,
-                     x, y, codes, n, int(vec_ok));
-  return hipGetLastError();
+  return tile_launches<IO, act_vpl<IO>()>(n, [&](unsigned blocks, int64_t at, int64_t count) {
+    hipLaunchKernelGGL((act_fwd_kernel<IO, ACT, act_vpl<IO>()>), dim3(blocks), dim3(act_block<IO>()), 0, s,
+                       elements<IO>(x, at), elements<IO>(y, at), codes + at / 16, count, int(vec_ok));
+  });
 }
 
 template <class IO, int ACT>
 hipError_t launch_act_bwd_t(int64_t n, const void* dy, const uint32_t* codes, void* dx,
                             bool vec_ok, hipStream_t s) {
-  const int64_t blocks = act_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((act_bwd_kernel<IO, ACT, act_vpl<IO>()>), dim3(unsigned(blocks)), dim3(act_block<IO>()), 0, s,
-                     dy, codes, dx, n, int(vec_ok));
-  return hipGetLastError();
+  return tile_launches<IO, act_vpl<IO>()>(n, [&](unsigned blocks, int64_t at, int64_t count) {
+    hipLaunchKernelGGL((act_bwd_kernel<IO, ACT, act_vpl<IO>()>), dim3(blocks), dim3(act_block<IO>()), 0, s,
+                       elements<IO>(dy, at), codes + at / 16, elements<IO>(dx, at), count, int(vec_ok));
+  });
 }
 
 template <class IO, int ACT>
 hipError_t launch_glu_fwd_t(int64_t n, const void* g, const void* u, void* h, void* s,
                             uint32_t* codes, bool vec_ok, hipStream_t st) {
-  const int64_t blocks = glu_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((glu_fwd_kernel<IO, ACT, glu_vpl<IO>()>), dim3(unsigned(blocks)),
-                     dim3(act_block<IO>()), 0, st, g, u, h, s, codes, n, int(vec_ok));
-  return hipGetLastError();
+  return tile_launches<IO, glu_vpl<IO>()>(n, [&](unsigned blocks, int64_t at, int64_t count) {
+    hipLaunchKernelGGL((glu_fwd_kernel<IO, ACT, glu_vpl<IO>()>), dim3(blocks), dim3(act_block<IO>()), 0, st,
+                       elements<IO>(g, at), elements<IO>(u, at), elements<IO>(h, at), elements<IO>(s, at), codes + at / 16,
+                       count, int(vec_ok));
+  });
 }
 
 template <class IO, int ACT>
 hipError_t launch_glu_bwd_t(int64_t n, const void* dh, const void* u, const void* s,
                             const uint32_t* codes, void* dg, void* du, bool vec_ok, hipStream_t st) {
-  const int64_t blocks = glu_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((glu_bwd_kernel<IO, ACT, glu_vpl<IO>()>), dim3(unsigned(blocks)),
-                     dim3(act_block<IO>()), 0, st, dh, u, s, codes, dg, du, n, int(vec_ok));
-  return hipGetLastError();
+  return tile_launches<IO, glu_vpl<IO>()>(n, [&](unsigned blocks, int64_t at, int64_t count) {
+    hipLaunchKernelGGL((glu_bwd_kernel<IO, ACT, glu_vpl<IO>()>), dim3(blocks), dim3(act_block<IO>()), 0, st,
+                       elements<IO>(dh, at), elements<IO>(u, at), elements<IO>(s, at), codes + at / 16, elements<IO>(dg, at),
+                       elements<IO>(du, at), count, int(vec_ok));
+  });
 }
 
 hipError_t launch_glu_fwd(int act, bool bf16, int64_t n, const void* g, const void* u, void* h,

@@ -584,7 +584,7 @@ hipError_t launch_linear_grad(int act, int64_t M, int64_t N, int64_t K, const vo
     if (e != hipSuccess) return e;
   }
   const int64_t dw_blocks = split ? (N * K / 8 + 255) / 256 : 0, db_blocks = db != nullptr ? N / 16 : 0;
-  if (dw_blocks + db_blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (dw_blocks + db_blocks > most_blocks(256)) return hipErrorInvalidValue;
   if (dw_blocks + db_blocks > 0) {
     hipLaunchKernelGGL(grad_reduce_kernel, dim3(unsigned(dw_blocks + db_blocks)), dim3(256), 0, s, part,
                        static_cast<uint16_t*>(dw), N * K, int(plan.splits), dw_blocks, sums,

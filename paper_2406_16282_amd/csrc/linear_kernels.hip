@@ -703,7 +703,7 @@ hipError_t launch_rows(LinArgs a, hipStream_t s) {
   constexpr int kOut = GLU ? 16 : 32;
   const int64_t tiles_m = (a.M + MT * 16 - 1) / (MT * 16), tiles_n = (a.N + kOut - 1) / kOut;
   const int64_t blocks = tiles_m * tiles_n;
-  if (blocks > 0x3fffffff) return hipErrorInvalidValue;
+  if (blocks > most_blocks(kRowsWaves * kWave)) return hipErrorInvalidValue;
   a.map = {uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(blocks), uint32_t(blocks / kXcds), 0u};
   // Non-temporal from 32 MiB of weights on, when one row block reads them (see the kernel).
   const bool nt = tiles_m == 1 && a.N * a.K * (GLU ? 4 : 2) > (int64_t(32) << 20);

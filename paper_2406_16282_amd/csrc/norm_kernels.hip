@@ -627,13 +627,12 @@ __global__ __launch_bounds__(256) void copy16_kernel(const u32x4* __restrict__ s
 hipError_t launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t s) {
   const int64_t nvec = bytes / 16;
   const int tail = int(bytes % 16);
-  const int64_t blocks = nvec > 0 ? (nvec + 255) / 256 : 1;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(copy16_kernel, dim3(unsigned(blocks)), dim3(256), 0, s,
-                     static_cast<const u32x4*>(src), static_cast<u32x4*>(dst), nvec,
-                     static_cast<const uint8_t*>(src) + nvec * 16,
-                     static_cast<uint8_t*>(dst) + nvec * 16, tail);
-  return hipGetLastError();
+  return in_parts(nvec > 0 ? nvec : 1, most_blocks(256) * 256, [&](int64_t first, int64_t count) {
+    hipLaunchKernelGGL(copy16_kernel, dim3(unsigned((count + 255) / 256)), dim3(256), 0, s,
+                       static_cast<const u32x4*>(src) + first, static_cast<u32x4*>(dst) + first, std::min(count, nvec),
+                       static_cast<const uint8_t*>(src) + nvec * 16,
+                       static_cast<uint8_t*>(dst) + nvec * 16, tail);
+  });
 }
 
 }  // namespace lmbp

@@ -319,7 +319,7 @@ template <class IO, int ACT>
 hipError_t fwd3(int64_t n, const void* x, void* y, uint32_t* codes, bool vec_ok,
                 const StepTable& tab, hipStream_t s) {
   const int64_t blocks = step3_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (blocks > most_blocks(128)) return hipErrorInvalidValue;   // more than the card's memory
   hipLaunchKernelGGL((stepact3_fwd_kernel<IO, ACT>), dim3(unsigned(blocks)), dim3(128), 0, s, x, y,
                      codes, n, int(vec_ok), tab);
   return hipGetLastError();
@@ -329,36 +329,38 @@ template <class IO>
 hipError_t bwd3(int64_t n, const void* dy, const uint32_t* codes, void* dx, bool vec_ok,
                 const StepTable& tab, hipStream_t s) {
   const int64_t blocks = step3_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (blocks > most_blocks(128)) return hipErrorInvalidValue;   // more than the card's memory
   hipLaunchKernelGGL((stepact3_bwd_kernel<IO>), dim3(unsigned(blocks)), dim3(128), 0, s, dy, codes,
                      dx, n, int(vec_ok), tab);
   return hipGetLastError();
 }
 
-template <class IO>
-int64_t step_blocks(int64_t n) {
-  const int64_t waves = (n + int64_t(kWave) * IO::kPerVec - 1) / (int64_t(kWave) * IO::kPerVec);
-  return (waves + 1) / 2;  // 2 waves per 128-thread block
+// The launches of a tensor of n elements, 128 vectors to a block: f(blocks, first element's byte, first code
+// word, elements).
+template <class IO, int BITS, class F>
+hipError_t step_launches(int64_t n, F f) {
+  constexpr int64_t per_block = 128 * IO::kPerVec;
+  return in_parts(n, most_blocks(128) * per_block, [&](int64_t first, int64_t count) {
+    f(unsigned((count + per_block - 1) / per_block), first * IO::kBytes, first * BITS / 32, count);
+  });
 }
 
 template <class IO, int ACT, int BITS>
 hipError_t fwd_t(int64_t n, const void* x, void* y, uint32_t* codes, bool vec_ok,
                  const StepTable& tab, hipStream_t s) {
-  const int64_t blocks = step_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((stepact_fwd_kernel<IO, ACT, BITS>), dim3(unsigned(blocks)), dim3(128), 0, s, x, y,
-                     codes, n, int(vec_ok), tab);
-  return hipGetLastError();
+  return step_launches<IO, BITS>(n, [&](unsigned blocks, int64_t at, int64_t word, int64_t count) {
+    hipLaunchKernelGGL((stepact_fwd_kernel<IO, ACT, BITS>), dim3(blocks), dim3(128), 0, s, static_cast<const char*>(x) + at,
+                       static_cast<char*>(y) + at, codes + word, count, int(vec_ok), tab);
+  });
 }
 
 template <class IO, int BITS>
 hipError_t bwd_t(int64_t n, const void* dy, const uint32_t* codes, void* dx, bool vec_ok,
                  const StepTable& tab, hipStream_t s) {
-  const int64_t blocks = step_blocks<IO>(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((stepact_bwd_kernel<IO, BITS>), dim3(unsigned(blocks)), dim3(128), 0, s, dy, codes,
-                     dx, n, int(vec_ok), tab);
-  return hipGetLastError();
+  return step_launches<IO, BITS>(n, [&](unsigned blocks, int64_t at, int64_t word, int64_t count) {
+    hipLaunchKernelGGL((stepact_bwd_kernel<IO, BITS>), dim3(blocks), dim3(128), 0, s, static_cast<const char*>(dy) + at,
+                       codes + word, static_cast<char*>(dx) + at, count, int(vec_ok), tab);
+  });
 }
 
 template <class IO, int ACT>

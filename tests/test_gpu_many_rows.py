@@ -96,3 +96,73 @@ def test_bias_gradient():
     db = lmbp.linear_bias_grad(dy)
     for at in range(0, n, 2 ** 26):
         assert torch.equal(db[at:at + 2 ** 26], dy[0, at:at + 2 ** 26] + dy[1, at:at + 2 ** 26])
+
+
+# Flat tensors: 4 values in fp32 to a thread, 2^34 of them and more. One block of values after the other is the
+# same; whole tensors in place of their inputs.
+BLOCK = 2 ** 20
+FLAT = 2 ** 34 + 3 * BLOCK
+
+
+def repeated(values, n=FLAT):
+    t = torch.empty(n, device=DEV)
+    t.view(-1, BLOCK).copy_(values.expand(n // BLOCK, BLOCK))
+    return t
+
+
+def repeats(t, values):
+    rows = t.view(-1, values.numel())
+    return all(bool((rows[i:i + 512] == values).all()) for i in range(0, len(rows), 512))
+
+
+def room_for(tensors):
+    free = torch.cuda.mem_get_info()[0]
+    if free < FLAT * 4 * tensors + (24 << 30):
+        pytest.skip(f"needs {tensors} tensors of {FLAT * 4 >> 30} GiB, {free >> 30} GiB are free")
+
+
+@pytest.mark.parametrize("op", ["regelu2", "resilu2"])
+def test_activations(op):
+    room_for(1)
+    fwd, bwd = getattr(lmbp, f"{op}_fwd"), getattr(lmbp, f"{op}_bwd")
+    one = torch.randn(BLOCK, device=DEV) * 3
+    y, codes = fwd(one)
+    x = repeated(one)
+    _, many = fwd(x, y=x)
+    assert repeats(x, y) and repeats(many, codes)
+    bwd(x, many, dx=x)
+    assert repeats(x, bwd(y, codes))
+
+
+@pytest.mark.parametrize("bits", [1, 2, 4])
+def test_k_bit_activations(bits):
+    room_for(1)
+    thresholds = [0.3 * (i - 2 ** (bits - 1)) + 0.1 for i in range(2 ** bits - 1)]
+    levels = [0.1 * i - 0.2 for i in range(2 ** bits)]
+    one = torch.randn(BLOCK, device=DEV) * 2
+    y, codes = lmbp.stepact_fwd(one, "gelu", thresholds, bits)
+    x = repeated(one)
+    _, many = lmbp.stepact_fwd(x, "gelu", thresholds, bits, y=x)
+    assert repeats(x, y) and repeats(many, codes)
+    lmbp.stepact_bwd(x, many, levels, bits, dx=x)
+    assert repeats(x, lmbp.stepact_bwd(y, codes, levels, bits))
+
+
+def test_swiglu():
+    room_for(3)
+    one_g, one_u = torch.randn(BLOCK, device=DEV) * 3, torch.randn(BLOCK, device=DEV)
+    h, s, codes = lmbp.reswiglu2_fwd(one_g, one_u)
+    g, u = repeated(one_g), repeated(one_u)
+    _, many_s, many = lmbp.reswiglu2_fwd(g, u, h=g)
+    assert repeats(g, h) and repeats(many_s, s) and repeats(many, codes)
+    lmbp.reswiglu2_bwd(g, u, many_s, many, dg=g, du=u)
+    dg, du = lmbp.reswiglu2_bwd(h, one_u, s, codes)
+    assert repeats(g, dg) and repeats(u, du)
+
+
+def test_copy():
+    room_for(2)
+    one = torch.randn(BLOCK, device=DEV)
+    src = repeated(one)
+    dst = torch.zeros_like(src)
+    assert repeats(lmbp.copy_bytes(src, dst), one)
