@@ -197,7 +197,8 @@ __global__ __launch_bounds__(256) void product_any(Args a) {
     for (int e = 0; e < 4; ++e) {
       const int64_t n = n0 + j * 16 + g * 4 + e;
       if (n < a.N) {
-        const float sc = TR ? as : as * a.b_scale[n];
+        // Nothing to add up (K = 0) is 0 whatever the scales are, infinite and NaN ones among them.
+        const float sc = a.K == 0 ? 0.0f : TR ? as : as * a.b_scale[n];
         const float more = TR ? (a.add != nullptr ? OUT::load1(a.add, m * a.N + n) : 0.0f)
                               : (a.bias != nullptr ? OUT::load1(a.bias, n) : 0.0f);
         OUT::store1(a.y, m * a.N + n, __builtin_fmaf(float(v[e]), sc, more));
