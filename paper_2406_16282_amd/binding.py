@@ -35,6 +35,7 @@ STEP_OPS = ("stepact_fwd", "stepact_bwd")
 LINEAR_OPS = ("linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd", "msrms_linear_swiglu_fwd")
 Q8_OPS = ("q8_rows", "q8_values", "msrms_q8_fwd", "msrms_q8_bwd", "linear_q8_fwd", "linear_q8_bwd")
 ACT_GELU, ACT_SILU = 0, 1
+Q8_MAX_SUM = 131071   # products of bytes to a sum in 32 bits
 
 
 class LmbpError(RuntimeError):
@@ -873,7 +874,7 @@ def _q8_weight(w, w_scale, ref):
 def linear_q8_fwd(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=None):
     """Linear layer of 8-bit rows q [..., k] (one scale per row) and an 8-bit weight w [n, k]
     (one scale per output channel): y = (q w^T) scale w_scale + bias in ``dtype``, the sums
-    exact. bias [n] of that dtype or None."""
+    exact. bias [n] of that dtype or None; k up to Q8_MAX_SUM."""
     if _fast is not None and stream is None and dtype in _CODES:
         out = _fast.linear_q8_fwd(_address["linear_q8_fwd"], _address["lmbp_linear_q8_fwd_bytes"], _CODES[dtype], q, scale, w,
                                   w_scale, bias)
@@ -904,7 +905,7 @@ def linear_q8_bwd(dy, w, w_scale, add=None, dx=None, dtype=None, stream=None):
     """Input gradient of linear_q8_fwd: dx = (dy w_scale) w + add, the rows of dy w_scale [..., n]
     brought to 8 bits first (one scale per row). dx [..., k] has the type of ``add`` (None: none),
     else ``dtype``, else that of dy; it may be given, ``add`` itself included (the sum of several
-    layers' gradients)."""
+    layers' gradients). n up to Q8_MAX_SUM."""
     if _fast is not None and (dx is None or dx is add) and stream is None:
         code = _CODES.get(getattr(add, "dtype", None) or dtype or getattr(dy, "dtype", None))
         out = (_fast.linear_q8_bwd(_address["linear_q8_bwd"], _address["lmbp_linear_q8_bwd_bytes"], code, dy, w, w_scale, add,

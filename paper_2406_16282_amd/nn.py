@@ -259,7 +259,7 @@ class _LinearQ8(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         weight, scale = ctx.saved_tensors
-        dx = binding.linear_q8_bwd(_flat(dy), weight, scale) if ctx.needs_input_grad[0] else None
+        dx = _input_grad_q8(dy, weight, scale, dy.dtype) if ctx.needs_input_grad[0] else None
         return dx, None, None, _bias_grad(dy, ctx.bias_dtype) if ctx.needs_input_grad[3] else None
 
 
@@ -267,6 +267,22 @@ def _product_q8(q, q_scale, weight, scale, bias, dtype):
     if bias is not None:
         bias = _flat(bias if bias.dtype == dtype else bias.to(dtype))
     return binding.linear_q8_fwd(q, q_scale, weight, scale, bias, dtype)
+
+
+def _input_grad_q8(dy, weight, scale, dtype, add=None):
+    """dx = (dy scale) weight + add in ``dtype`` (in add's place, if there is one). Of more output channels
+    than one sum holds, in shares of whole 64s (w's rows stay aligned): each brings its part of dy's rows to 8 bits,
+    with a scale of its own, and they add up in fp32."""
+    n = weight.shape[0]
+    if n <= binding.Q8_MAX_SUM:
+        return binding.linear_q8_bwd(_flat(dy), weight, scale, add=add, dx=add, dtype=dtype)
+    shares = -(-n // (binding.Q8_MAX_SUM // 64 * 64))
+    size = -(-n // (64 * shares)) * 64
+    dx = add
+    for at in range(0, n, size):
+        part = slice(at, at + size)
+        dx = binding.linear_q8_bwd(_flat(dy[..., part]), weight[part], scale[part], add=dx, dx=dx, dtype=torch.float32)
+    return dx.to(dtype)
 
 
 def _bias_grad(dy, dtype):
@@ -278,7 +294,8 @@ class LinearQ8(nn.Module):
     """Linear layer with a frozen 8-bit weight: ``weight`` int8 [n, k] and ``scale`` fp32 [n]
     (buffers; w = weight * scale), ``bias`` [n] or None (a parameter, frozen unless its
     ``requires_grad`` is set). The input's rows are brought to 8 bits, and so are the rows of
-    the output's gradient in the backward; nothing of the input is kept."""
+    the output's gradient in the backward; nothing of the input is kept. k is at most 131071 (a sum
+    in 32 bits), n any number: the gradient of more than 131071 outputs is that of several layers."""
 
     def __init__(self, weight, scale, bias=None):
         super().__init__()
@@ -350,7 +367,7 @@ class _NormLinearQ8(torch.autograd.Function):
             # The layers' gradients add up in fp32, and the norm's backward takes the sum as it is.
             for dy, w, sc in zip(grads, weights[::2], weights[1::2]):
                 if dy is not None:
-                    dz = binding.linear_q8_bwd(_flat(dy), w, sc, add=dz, dx=dz, dtype=torch.float32)
+                    dz = _input_grad_q8(dy, w, sc, torch.float32, add=dz)
             if dz is None:
                 dx = ds
             else:

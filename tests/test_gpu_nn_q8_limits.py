@@ -1,0 +1,74 @@
+"""The 8-bit modules at the ends of what their operators take: output widths beyond one exact sum."""
+
+import pytest
+import torch
+
+import paper_2406_16282_amd as lmbp
+from paper_2406_16282_amd import binding
+from paper_2406_16282_amd.nn import LinearQ8, MSRMSNormLinearQ8
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def layer(n, k, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    w = torch.randint(-127, 128, (n, k), generator=g, device=DEV, dtype=torch.int8)
+    return LinearQ8(w, torch.rand(n, generator=g, device=DEV) * 0.01 + 1e-4)
+
+
+def shares_of(n):
+    """The widths that a sum over n channels is cut into: whole 64s, as few shares as there can be."""
+    count = -(-n // (binding.Q8_MAX_SUM // 64 * 64))
+    size = -(-n // count)
+    size = -(-size // 64) * 64
+    return [(at, min(n, at + size)) for at in range(0, n, size)] if n > binding.Q8_MAX_SUM else [(0, n)]
+
+
+def grad64(dy, mod):
+    """(the gradient in 64 bits, what bounds its error): a share's rows of dy w_scale in 8 bits with a
+    scale of their own, the scale and the conversion u each and the product u; every addition u."""
+    total, size = 0.0, 0.0
+    for a, b in shares_of(mod.out_features):
+        t = (dy[:, a:b].double() * mod.scale[a:b].double()).float().double()
+        most = t.abs().amax(1, keepdim=True).clamp_min(2.0 ** -100)
+        part = (torch.round(t * (127.0 / most).float().double()) @ mod.weight[a:b].double()) * (most / 127.0)
+        total, size = total + part, size + part.abs()
+    return total, size * U * (3 + len(shares_of(mod.out_features)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [131_071, 131_072, 151_936, 262_147])
+def test_wide_layers(n, dtype):
+    mod = layer(n, 48, 1)
+    mod.scale[: n // 2] *= 20.0     # loud channels in one share
+    x = torch.randn(5, 48, device=DEV).to(dtype).requires_grad_()
+    y = mod(x)
+    dy = torch.randn(5, n, device=DEV).to(dtype)
+    dy[1] = 0.0
+    y.backward(dy)
+    want, room = grad64(dy, mod)
+    room = room + torch.finfo(dtype).eps / 2 * want.abs() * (dtype != torch.float32)
+    assert x.grad.dtype == dtype and ((x.grad - want).abs() <= 1.01 * room + 1e-38).all()
+    # behind a norm, beside a narrow layer
+    small = layer(32, 48, 2)
+    block = MSRMSNormLinearQ8([small, mod])
+    x2 = x.detach().clone().requires_grad_()
+    y0, y1 = block(x2)
+    d0 = torch.randn_like(y0)
+    torch.autograd.backward((y0, y1), (d0, dy))
+    q, scale, rstd = lmbp.msrms_q8_fwd(x.detach(), block.eps)
+    dz = lmbp.linear_q8_bwd(d0, small.weight, small.scale, dtype=torch.float32)
+    for a, b in shares_of(n):
+        dz = lmbp.linear_q8_bwd(dy[:, a:b].contiguous(), mod.weight[a:b], mod.scale[a:b], add=dz)
+    assert torch.equal(x2.grad, lmbp.msrms_q8_bwd(dz, q, scale, rstd, dtype=dtype))
+
+
+def test_the_widest_sums_do_not_overflow():
+    """Every product 127 * 127: the sum over the layer passes 2^31, a share's does not."""
+    n = 151_936
+    mod = LinearQ8(torch.full((n, 16), 127, dtype=torch.int8, device=DEV), torch.ones(n, device=DEV))
+    x = torch.zeros(3, 16, device=DEV, requires_grad=True)
+    mod(x).backward(torch.full((3, n), 2.0, device=DEV))
+    assert ((x.grad.double() - 2.0 * 127 * n).abs() <= 6 * U * 2.0 * 127 * n).all()
