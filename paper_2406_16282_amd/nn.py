@@ -383,17 +383,29 @@ class MSRMSNormLinearQ8(nn.Module):
     and the ``LinearQ8`` layers behind it. ``forward(x, res)`` returns the layers' outputs and
     s = x + res; ``forward(x)`` the outputs alone (one tensor for a single layer).
 
+    The layers' weights are read and their operators called here, not the layers themselves: what
+    only a layer's own call would run (hooks on it, a wrapper, a subclass's forward) is refused.
+
     To capture forward and backward in a graph, let go of the eager graphs of the same leaves
     first: autograd would wait for the stream that they ran on."""
 
     def __init__(self, layers, eps=1e-5):
         super().__init__()
         self.layers = nn.ModuleList(layers)
-        if not self.layers or not all(isinstance(m, LinearQ8) for m in self.layers):
+        if not self.layers:
             raise TypeError("layers must be LinearQ8 modules")
+        self._check_layers()
         self.eps = float(eps)
 
+    def _check_layers(self):
+        for m in self.layers:
+            if not isinstance(m, LinearQ8) or type(m).forward is not LinearQ8.forward or "forward" in m.__dict__:
+                raise TypeError("layers must be LinearQ8 modules with no forward of their own: it would not run")
+            if m._forward_hooks or m._forward_pre_hooks or m._backward_hooks or m._backward_pre_hooks:
+                raise RuntimeError("a hook on a layer of MSRMSNormLinearQ8 would not run: put it on the module itself")
+
     def forward(self, x, res=None):
+        self._check_layers()
         flat = [t for m in self.layers for t in (m.weight, m.scale, m.bias)]
         out = _NormLinearQ8.apply(x, res, self.eps, *flat)
         return out[0] if len(out) == 1 else out
