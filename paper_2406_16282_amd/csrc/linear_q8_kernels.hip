@@ -101,7 +101,7 @@ __global__ __launch_bounds__(C::kThreads, C::kMinWaves) void product_tile(Args a
   const int wave = wave_in_block();
   const int wm = wave / C::WN, wn = wave % C::WN;
   const uint32_t tiles = a.map.tiles;
-  const int kt_count = K > 0 ? int((K + kBK - 1) / kBK) : 1;
+  const int kt_count = int((K + kBK - 1) / kBK);   // K > 0
 
   // ---- load side: byte offsets of this lane's chunks at K step 0, for both halves
   uint32_t ld_a[2][kLA], ld_b[2][kLB];

@@ -250,7 +250,6 @@ class _LinearQ8(torch.autograd.Function):
     def forward(ctx, x, weight, scale, bias):
         x2 = _flat(x).reshape(-1, x.shape[-1])
         q, q_scale = binding.q8_rows(x2)
-        ctx.has_bias = bias is not None
         ctx.bias_dtype = bias.dtype if bias is not None else None
         ctx.save_for_backward(weight, scale)
         return _product_q8(q, q_scale, weight, scale, bias, x.dtype).reshape(*x.shape[:-1], weight.shape[0])
