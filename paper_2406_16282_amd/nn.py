@@ -24,6 +24,9 @@
   that consume its output, W~ = W diag(alpha), b~ = W beta + b (Sec. 5.2), and returns
   the parameter-free MS norm to use in its place.
 
+The modules answer in the type of their input (fp32 or bf16, the fused linear layers bf16 alone) and
+refuse others, inside an autocast region as outside: autocast casts nothing for them.
+
 Every forward and backward runs in the HIP kernels through ``binding``, except the
 product of the fused linear layers' backward for the input (torch's library GEMM) and
 the one-time weight merge.

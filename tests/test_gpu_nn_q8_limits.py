@@ -1,4 +1,5 @@
-"""The 8-bit modules at the ends of what their operators take: output widths beyond one exact sum."""
+"""The 8-bit modules at the ends of what their operators take: output widths beyond one exact sum,
+and regions of autocast."""
 
 import pytest
 import torch
@@ -72,3 +73,22 @@ def test_the_widest_sums_do_not_overflow():
     x = torch.zeros(3, 16, device=DEV, requires_grad=True)
     mod(x).backward(torch.full((3, n), 2.0, device=DEV))
     assert ((x.grad.double() - 2.0 * 127 * n).abs() <= 6 * U * 2.0 * 127 * n).all()
+
+
+def test_autocast_leaves_the_input_s_type():
+    """The modules answer in their input's type inside autocast as outside, forward and backward."""
+    a, b = layer(48, 64, 1), layer(64, 48, 2)
+    block = MSRMSNormLinearQ8([a])
+
+    def run(region, dtype):
+        torch.manual_seed(3)
+        x, res = (torch.randn(9, 64, device=DEV).to(dtype).requires_grad_() for _ in range(2))
+        with torch.autocast("cuda", dtype=torch.bfloat16, enabled=region):
+            y, s = block(x, res)
+            out = b(y)
+        torch.autograd.backward((out, s), (torch.ones_like(out), torch.ones_like(s)))
+        return out.detach(), s.detach(), x.grad, res.grad
+
+    for dtype in (torch.float32, torch.bfloat16):
+        for got, want in zip(run(True, dtype), run(False, dtype)):
+            assert got.dtype == dtype and torch.equal(got, want)
