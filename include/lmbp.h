@@ -44,7 +44,8 @@
  *   dtype. n == 0 or rows == 0 is a successful no-op. LMBP_EHIP means the kernel
  *   launch failed; lmbp_last_hip_error() then returns the hipError_t value for the
  *   calling thread. No C++ exception crosses this interface.
- * - Results are deterministic: no atomics, fixed reduction order.
+ * - Results are deterministic: no atomics, a reduction order fixed by the sizes, the
+ *   alignment of the tensors and the device.
  */
 #ifndef LMBP_H
 #define LMBP_H
@@ -315,8 +316,8 @@ lmbp_status q8_values(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t *q
 
 /* ------------------------------------------------------------------------
  * MS-RMSNorm (Appendix G Alg. 3) with the residual's addition in front and its output in 8
- * bits: the tensor that the norm and the next (merged) linear layer both keep takes one
- * byte per element. Per row:
+ * bits: what the norm keeps takes one byte per element, and linear_q8_fwd takes it as it is
+ * (a frozen layer keeps nothing of it). Per row:
  *
  * Forward:  s = x + res, rounded to dtype (s = x without res),
  *           rstd = 1 / sqrt(p^-1 |s|^2 + eps),  z = s rstd  as q scale:
@@ -354,7 +355,7 @@ lmbp_status msrms_q8_bwd(lmbp_dtype dt_dz, lmbp_dtype dt, int64_t rows, int64_t 
  *   dx = (sum_n p[m, n] w[n, k]) p_scale[m] + add,   p, p_scale the 8-bit rows of dy w_scale
  *
  * The sums are exact (whole numbers in 32 bits), everything behind them is fp32 with one
- * rounding to dtype.
+ * rounding to dtype; scale[m] w_scale[n] is formed first.
  *
  *   dt     : type of y and bias, or of dy; dt_dx: type of add and dx.
  *   m,n,k  : any sizes >= 0 below 2^31; the length of the sums (k forward, n backward) at
@@ -381,7 +382,7 @@ lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n,
 
 /* ------------------------------------------------------------------------
  * Gradient of a linear layer's bias: db[n] = sum over the rows of dy [m x n], added up in fp32 in
- * a fixed order, one rounding to dt_db. (linear_act_bwd has it with the activation's backward.)
+ * an order fixed by m, n, the alignment of dy and the device, one rounding to dt_db. (linear_act_bwd has it with the activation's backward.)
  *
  *   dt, dt_db : types of dy and db, any two.
  *   m, n      : any sizes >= 0, n below 2^31; m = 0 gives db = 0.

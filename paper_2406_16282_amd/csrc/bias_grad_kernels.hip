@@ -3,8 +3,8 @@
 // What bounds it: memory, dy once. A block takes up to 64 pieces of columns (4 elements to a lane, one
 // where n or the address does not allow that) and a group of rows, 256 / pieces of them at a time;
 // its sums meet in LDS. With several groups their sums (fp32) are added up by a second launch of the
-// same kernel. All orders are fixed: a column's chain is its rows of a thread, then the threads, then
-// the groups. bf16, us: 8192 x 11008 36 (5.0 TB/s), 8192 x 4096 18 (3.7), 12608 x 768 12.7, 1576 x 768 6.8 (two
+// same kernel. All orders are fixed by the size, the address of dy and the number of CUs: a column's chain is
+// its rows of a thread, then the threads, then the groups. bf16, us: 8192 x 11008 36 (5.0 TB/s), 8192 x 4096 18 (3.7), 12608 x 768 12.7, 1576 x 768 6.8 (two
 // launches), 16 x 4096 3.0, 8192 x 11009 (one element to a lane) 68; torch's sum over the same rows 58, 33, 23,
 // 12, 3.8 and 135.
 #include "lmbp_launch.hpp"

@@ -10,7 +10,7 @@
 // bytes runs at 3404 TOPS, of 32x32x32 ones at 3087 (4419 and 3986 on zeros), so the smaller shape
 // is taken although it needs as many operand reads. [8192 x 4096] x 11008 takes 305 to 340 us by the
 // card's state (2170 to 2420 TOPS; the library's int8 product without scales 392 to 413, its bf16
-// product 686 to 704, in the same runs), 8192^3 422 to 437 us (2510 to 2600; library 446 to 453):
+// product 686 to 704, in the same runs), 8192^3 392 to 437 us (2510 to 2806; library 430 to 453):
 // matrix cores busy 63 to 67% of the cycles, no bank conflicts, a clock of 1.6 to 1.85 GHz. Few rows:
 // the weight's bytes. One row of 11008 x 4096 9.1 us with weights that the caches do not hold
 // (5.0 TB/s; one load's way and the launch are 3 of them), 16384 x 16384 40 us (6.7 TB/s), 16 rows

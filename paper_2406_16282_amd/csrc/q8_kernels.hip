@@ -6,9 +6,9 @@
 //
 // What bounds them: memory. A row is read once and held in registers while its largest value (and
 // sum of squares) is found. On [8192 x 4096] bf16: q8_rows 18 us (5.6 TB/s), q8_values 16 (6.35),
-// msrms_q8_fwd 18 and with the residual 38 (6.2), msrms_q8_bwd 27 (6.2) and with ds 35 (6.7); on
-// [8192 x 13824] q8_rows 53 us (6.4), q8_values 50 (6.9); a copy of 1 GiB runs at 6.6 to 6.8 TB/s. On
-// [2439 x 1025] fp32, rows at any address: 5.0, 4.8, 5.4, 8.9, 6.4 and 8.5 us. q is stored past the
+// msrms_q8_fwd 18 and with the residual 38 to 40 (5.9 to 6.2), msrms_q8_bwd 27 (6.2) and with ds 35 (6.7); on
+// [8192 x 13824] 53 us (6.4), 50 to 58, 54, 128 (6.2), 83 to 91 and 113 to 124; a copy of 1 GiB runs at 6.6 to
+// 6.8 TB/s. On [2439 x 1025] fp32, rows at any address: 4.6, 4.5, 5.1, 8.7, 6.8 and 8.2 us. q is stored past the
 // caches (about 8% on q8_rows of the first). Pieces of 16 elements instead of 8 were slower; blocks
 // that walk the rows no faster than a block for each group of them, but for factors per column: there
 // the factors stay in registers over a block's rows ([8192 x 11008] 44 us; read again for every row 161).
@@ -521,11 +521,12 @@ __global__ __launch_bounds__(256) void norm_bwd_any(const void* dz, const int8_t
 
 // Launch shapes of the register kernels, by the pieces that they hold: the fewest waves to a row
 // that hold it in 3 pieces per thread (4 with 8 waves), or 16 waves with up to MOST (what a kernel
-// has registers for). Measured in us as waves x pieces, bf16, 8192 rows, q8_rows and msrms_q8_fwd with
-// a residual: 768 columns 1x2 5.5 and 8.8, 2x2 7.5 and 10.0; 4096 columns 4x2 18.4 and 30.7, 8x2
-// 23.0 and 32.5, 16x2 34.7 and 47.1, 2x4 18.9 and 32.4; 11008 columns 8x3 43.5 and 79, 16x2 52 and 82; 13824
-// columns 8x4 54.2 and 96.9, 16x2 59.9 and 99.6 (with factors per column 56.8 against 70). In 32 bits 8192
-// columns 8x4 56 and 102, 16x2 57 and 103 (with factors 58 against 66).
+// has registers for). Measured in us as waves x pieces, bf16, 8192 rows, tensors of their own throughout: q8_rows,
+// msrms_q8_fwd with a residual, msrms_q8_bwd with ds. 768 columns 1x2 5.4, 10.0, 10.2 and 2x1 7.1, 10.1, 10.1; 4096
+// columns 4x2 17.7, 38.6, 35.7, 8x1 21.1, 39.0, 36.1 and 2x4 17.7, 39.8, 36.5; 11008 columns 8x3 43.1, 102.8, 91.3 and
+// 16x2 52.2, 103.2, 93.2; 13824 columns 8x4 53.2, 128.5, 114.9, 16x2 60.1, 128.6, 115.6 and 16x3 59.7, 128.6, 148.6 (with
+// factors per column 8x4 56.8, 16x2 70). In 32 bits 4096 columns 8x2 28.0, 69.6, 65.0 and 4x4 29.0, 68.3, 65.4; 8192
+// columns 8x4 55.4, 137.5, 134.4 and 16x2 56.7, 139.4, 132.2 (with factors 58 and 66).
 struct Shape {
   int wpr, vpl;
 };

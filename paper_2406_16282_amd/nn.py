@@ -19,7 +19,9 @@
   Keeps nothing of its input.
 * ``MSRMSNormLinearQ8``: residual addition, MS-RMSNorm with its output in 8 bits, and the
   ``LinearQ8`` layers that consume it. Keeps one byte per element of the norm's output and
-  two fp32 values per row, for the norm and all its layers together.
+  two fp32 values per row for the norm's backward; the frozen layers keep nothing of it. The
+  output z itself is not handed out: where something else reads it (an adapter beside a
+  layer), ``MSRMSNorm`` and ``LinearQ8`` are the pair to use, and z stays in its own type.
 * ``merge_norm_into_linears``: folds a norm's affine (alpha, beta) into the linear layers
   that consume its output, W~ = W diag(alpha), b~ = W beta + b (Sec. 5.2), and returns
   the parameter-free MS norm to use in its place.
