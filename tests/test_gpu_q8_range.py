@@ -83,3 +83,41 @@ def test_norm_backward(cols, dt_dz, dtype):
         room = rs * most * (c + 4) * U + 3 * U * (rs * (np.abs(g) + most) + np.abs(dx_o))
         room = 1.01 * (room + torch.finfo(TYPES[dtype]).eps / 2 * np.abs(dx_o)) + 2.0 ** -133
         assert (np.abs(n64(dx) - dx_o) <= room).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", COLS)
+def test_in_place(cols, dtype):
+    """The sum in place of x or of the residual, dx in place of dz or of ds, where rows are added up again."""
+    x, res = rows_of_every_size(cols, dtype, 1), draw(13, cols, dtype, 3, [1.0, 2.0 ** 58, 2.0 ** 30, 2.0 ** 99])
+    want = lmbp.msrms_q8_fwd(x, 1e-5, res)
+    for into in ("x", "res"):
+        a, b = x.clone(), res.clone()
+        got = lmbp.msrms_q8_fwd(a, 1e-5, b, s=a if into == "x" else b)
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    q, scale, rstd, _ = want
+    dz, ds = draw(13, cols, dtype, 6, [1e-3, 2.0 ** 121, 2.0 ** 118]), draw(13, cols, dtype, 7, [1e-3, 2.0 ** 100])
+    dx = lmbp.msrms_q8_bwd(dz, q, scale, rstd, ds)
+    a, b = dz.clone(), ds.clone()
+    assert torch.equal(lmbp.msrms_q8_bwd(a, q, scale, rstd, ds, dx=a).view(torch.uint8), dx.view(torch.uint8))
+    assert torch.equal(lmbp.msrms_q8_bwd(dz, q, scale, rstd, b, dx=b).view(torch.uint8), dx.view(torch.uint8))
+
+
+@pytest.mark.parametrize("cols", [40, 1025, 4096, 13824, 30011, 140001])
+def test_rows_that_are_not_finite_beside_large_ones(cols):
+    """An infinity or a NaN stays in its row; the rows beside it are as without it."""
+    x = rows_of_every_size(cols, "fp32", 1)
+    dz = draw(13, cols, "fp32", 6, [1e-3, 2.0 ** 121, 2.0 ** 118])
+    q, scale, rstd = lmbp.msrms_q8_fwd(x, 1e-5)
+    dx = lmbp.msrms_q8_bwd(dz, q, scale, rstd)
+    bad, keep = [1, 4, 9], [i for i in range(13) if i not in (1, 4, 9)]
+    y, dy = x.clone(), dz.clone()
+    for row, value in zip(bad, (float("inf"), float("nan"), -float("inf"))):
+        y[row, cols // 3] = value
+        dy[row, cols // 2] = value
+    q1, scale1, rstd1 = lmbp.msrms_q8_fwd(y, 1e-5)
+    assert (q1[bad] == 0).all() and scale1[bad].isnan().all()
+    for a, b in zip((q1, scale1, rstd1), (q, scale, rstd)):
+        assert torch.equal(a[keep], b[keep])
+    dx1 = lmbp.msrms_q8_bwd(dy, q, scale, rstd)
+    assert torch.equal(dx1[keep], dx[keep]) and not dx1[bad].isfinite().all(dim=1).any()
