@@ -169,6 +169,8 @@ lmbp_status stepact_bwd(int bits, const double *levels, lmbp_dtype dt, int64_t n
  *   rstd    : rows fp32 values; must not overlap x, z, dz or dx.
  *   eps     : finite, > 0 (the paper uses 1e-6 or 1e-8; LLaMA-style RMSNorm 1e-5).
  *   dz, dx  : rows x cols of dtype. dx == dz is allowed; dx must not overlap z.
+ * The sums are fp32 as they are: squares that add up to 2^128 or more (values above 2^64) give
+ * rstd = 0 and z = 0 (msrms_q8_fwd has no such limit).
  * ------------------------------------------------------------------------ */
 lmbp_status msln_fwd(lmbp_dtype dt, int64_t rows, int64_t cols, float eps,
                      const void *x, void *z, float *rstd, void *stream);
