@@ -324,8 +324,8 @@ lmbp_status q8_values(lmbp_dtype dt, int64_t rows, int64_t cols, const int8_t *q
  * Forward:  s = x + res, rounded to dtype (s = x without res),
  *           rstd = 1 / sqrt(p^-1 |s|^2 + eps),  z = s rstd  as q scale:
  *           q the 8-bit row of s (as q8_rows), scale = a rstd / 127.
- *           Of finite rows of any size: squares that add up to more than fp32 holds are
- *           formed again of smaller values.
+ *           Of finite rows of any size: squares that fp32 does not hold are formed again
+ *           of smaller (larger) values.
  * Backward: with z = q scale,  dx = rstd (dz - z mean(z dz)) + ds.
  *           dx is the gradient of x and of res alike; ds is the gradient that reaches s
  *           past the norm.

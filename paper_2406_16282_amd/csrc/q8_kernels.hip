@@ -19,6 +19,7 @@
 // value above 2^64, or many near it) are added up again as (s 2^-96)^2, which no row overflows; what
 // falls below the smallest number there is less than 2^-60 of the sum. One wave does so for its row,
 // from memory and behind everything else: of the pieces in registers it cost every call 10 to 20 registers.
+// So do squares whose mean, eps included, is below 2^-90 (no eps in use is that small), as (s 2^60)^2.
 // The backward's sum of q dz is formed again of dz 2^-56 in the same case, by each wave for its pieces.
 // msrms_q8_bwd: with z = q scale, dx = rstd (dz - z p^-1 z^T dz) + ds.
 #include "lmbp_launch.hpp"
@@ -50,13 +51,10 @@ __device__ inline bool overflowed(float sum) {
   return (uint32_t(__builtin_amdgcn_readfirstlane(__float_as_int(sum))) & 0x7f800000u) == 0x7f800000u;
 }
 
-// rstd of a row, and the scale of one whose largest magnitude is a, of its mean square + eps; that mean
-// may be one of unit^2 times the squares.
-constexpr float kDown = 0x1p-96f;
-__device__ inline float add_square_down(float v, float sum) { return __builtin_fmaf(v * kDown, v * kDown, sum); }
-__device__ inline float mean_down(float sum_down, int64_t cols, float eps) {
-  return sum_down / float(cols) + eps * kDown * kDown;
-}
+// The factor in front of the squares of a row of that mean: 1, or one that keeps them in fp32's range.
+__device__ inline float unit_of(float mean) { return overflowed(mean) ? 0x1p-96f : mean < 0x1p-90f ? 0x1p60f : 1.0f; }
+__device__ inline float add_square(float v, float unit, float sum) { return __builtin_fmaf(v * unit, v * unit, sum); }
+// rstd of a row, and the scale of one whose largest magnitude is a, of its mean square + eps times unit^2.
 __device__ inline void store_stats(const FwdArgs& f, int64_t row, float mean, float unit, float a) {
   const float rs = rsqrtf(mean);
   f.rstd[row] = rs * unit;
@@ -269,14 +267,14 @@ __global__ __launch_bounds__(block_of<WPR>()) void fwd_rows(FwdArgs a) {
 #pragma unroll
           for (int k = 0; k < WPR; ++k) sum += sum_lds[first + k];
         }
-        float mean = sum / float(cols) + a.eps, unit = 1.0f;
-        if (w.finite && overflowed(mean)) {
+        float mean = sum / float(cols) + a.eps;
+        const float unit = unit_of(mean);
+        if (w.finite && unit != 1.0f) {
           __threadfence_block();   // s is read as other lanes and waves stored it
-          float down = 0.0f;
+          float again = 0.0f;
 #pragma unroll 1
-          for (int k = t; k < cols; k += kWave) down = add_square_down(IO::load1(MODE == kNormRes ? a.s : a.x, base + k), down);
-          mean = mean_down(wave_sum(down), cols, a.eps);
-          unit = kDown;
+          for (int k = t; k < cols; k += kWave) again = add_square(IO::load1(MODE == kNormRes ? a.s : a.x, base + k), unit, again);
+          mean = wave_sum(again) / float(cols) + a.eps * unit * unit;
         }
         if (t == 0) store_stats(a, row, mean, unit, w.a);
       }
@@ -462,16 +460,16 @@ __global__ __launch_bounds__(256) void fwd_any(FwdArgs a) {
   }
   block_max_sum(most, sum, most_lds, sum_lds);
   const Q8Row w = q8_row(most);
-  float mean = sum / float(a.cols) + a.eps, unit = 1.0f;
+  float mean = sum / float(a.cols) + a.eps;
+  const float unit = unit_of(mean);
   if constexpr (MODE == kNorm || MODE == kNormRes) {
-    if (w.finite && overflowed(mean)) {   // for all threads or none
-      unit = kDown;
-      float down = 0.0f;
+    if (w.finite && unit != 1.0f) {   // for all threads or none
+      float again = 0.0f;
       for (int64_t k = tid; k < a.cols; k += 256)
-        down = add_square_down(IO::load1(MODE == kNormRes ? a.s : a.x, base + k), down);
+        again = add_square(IO::load1(MODE == kNormRes ? a.s : a.x, base + k), unit, again);
       __syncthreads();   // the sums of before have been read
-      block_max_sum(most, down, most_lds, sum_lds);
-      mean = mean_down(down, a.cols, a.eps);
+      block_max_sum(most, again, most_lds, sum_lds);
+      mean = again / float(a.cols) + a.eps * unit * unit;
     }
   }
   for (int64_t k = tid; k < a.pitch; k += 256) {

@@ -1,8 +1,8 @@
 """Rows of every size through MS-RMSNorm into 8 bits and back.
 
 A finite row stands for s rstd whatever its size, also where its squares add up to more than
-fp32 holds, and so does the backward's sum of q dz. The bounds are those of test_gpu_q8_rows.py
-(chains of p / 64 + 24 additions, then the roundings counted there: scaling by a power of two
+fp32 holds or, with an eps as small, are less than it holds; and so does the backward's sum of
+q dz where it is more. The bounds are those of test_gpu_q8_rows.py (chains of p / 64 + 24 additions, then the roundings counted there: scaling by a power of two
 rounds nothing), and half a step of the smallest numbers, 2^-150, where rstd is one of them.
 """
 
@@ -19,7 +19,7 @@ U = 2.0 ** -24
 TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
 # the register form with 1, 2, 4, 8 and 16 waves to a row, rows at any address, and a block per row
 COLS = [1, 40, 768, 1025, 2049, 4096, 12345, 13824, 30011, 70000, 140001]
-SIZES = [1.0, 2.0 ** 60, 2.0 ** 64, 2.0 ** 100, 2.0 ** 122, 2.0 ** -40, 2.0 ** -90, 0.0]
+SIZES = [1.0, 2.0 ** 60, 2.0 ** 64, 2.0 ** 100, 2.0 ** 122, 2.0 ** -40, 2.0 ** -71, 0.0]
 
 
 def n64(t):
@@ -44,7 +44,7 @@ def rows_of_every_size(cols, dtype, seed):
     return x
 
 
-@pytest.mark.parametrize("eps", [1e-5, 1e-30, 1e30])
+@pytest.mark.parametrize("eps", [1e-5, 1e-30, 1e30, 1e-44])
 @pytest.mark.parametrize("with_res", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("cols", COLS)
