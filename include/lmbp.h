@@ -169,8 +169,8 @@ lmbp_status stepact_bwd(int bits, const double *levels, lmbp_dtype dt, int64_t n
  *   rstd    : rows fp32 values; must not overlap x, z, dz or dx.
  *   eps     : finite, > 0 (the paper uses 1e-6 or 1e-8; LLaMA-style RMSNorm 1e-5).
  *   dz, dx  : rows x cols of dtype. dx == dz is allowed; dx must not overlap z.
- * The sums are fp32 as they are: squares that add up to 2^128 or more (values above 2^64) give
- * rstd = 0 and z = 0 (msrms_q8_fwd has no such limit).
+ * The sums are fp32 as they are: rows whose squares add up to 2^128 or more (values above 2^64)
+ * are not handled (MS-RMSNorm gives rstd = 0 and z = 0; msrms_q8_fwd takes them).
  * ------------------------------------------------------------------------ */
 lmbp_status msln_fwd(lmbp_dtype dt, int64_t rows, int64_t cols, float eps,
                      const void *x, void *z, float *rstd, void *stream);
@@ -384,7 +384,8 @@ lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n,
 
 /* ------------------------------------------------------------------------
  * Gradient of a linear layer's bias: db[n] = sum over the rows of dy [m x n], added up in fp32 in
- * an order fixed by m, n, the alignment of dy and the device, one rounding to dt_db. (linear_act_bwd has it with the activation's backward.)
+ * an order fixed by m, n, the alignment of dy and the device, one rounding to dt_db.
+ * (linear_act_bwd has it with the activation's backward.)
  *
  *   dt, dt_db : types of dy and db, any two.
  *   m, n      : any sizes >= 0, n below 2^31; m = 0 gives db = 0.
