@@ -20,6 +20,9 @@
  *   msrms_q8_fwd / msrms_q8_bwd    MS-RMSNorm with the residual's addition, output in 8 bits
  *   linear_q8_fwd / linear_q8_bwd  a frozen linear layer of 8-bit rows and 8-bit weights
  *   linear_bias_grad               the gradient of a linear layer's bias
+ *   rope_fwd / rope_bwd            rotary positions of query and key heads, one or several axes
+ *   msrms_rope_fwd / msrms_rope_bwd  MS-RMSNorm of each head and the rotation in one pass
+ *   attention_fwd / attention_bwd  softmax(scale q k^T) v over packed, padded or equal sequences
  *
  * Conventions shared by every call
  * --------------------------------
@@ -396,6 +399,127 @@ lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n,
 lmbp_status linear_bias_grad(lmbp_dtype dt, lmbp_dtype dt_db, int64_t m, int64_t n, const void *dy,
                              void *db, void *workspace, int64_t workspace_bytes, void *stream);
 size_t lmbp_linear_bias_grad_bytes(int64_t m, int64_t n);
+
+/* ------------------------------------------------------------------------
+ * Tensors of heads: rows (tokens) of heads of `dim` columns. The columns of a head lie together; `row` and `head`
+ * are the elements from one row, one head to the next (>= 0; 0 for inputs only). So queries, keys and values
+ * may lie in the one output of a fused projection. Written tensors must not meet themselves: row at least
+ * (heads - 1) head + dim, or head at least (rows - 1) row + dim. Two tensors of a call that are interleaved
+ * without sharing an element (parts of the same rows) do not overlap.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void *data;
+  int64_t row, head;
+} lmbp_heads;
+
+/* ------------------------------------------------------------------------
+ * Rotary positions. Columns are taken in pairs; pair p of a token's head turns by the angle
+ * t = freqs[p] * positions[axes[p]][token]:  (a, b) -> (a cos t - b sin t, a sin t + b cos t).
+ *
+ *   rope_fwd : y = x turned;  rope_bwd: dx = dy turned back. fp32 arithmetic, one rounding; the angle is
+ *              right for any position (formed modulo a turn in 64-bit whole numbers).
+ *
+ *   tokens, dim : tokens >= 0; 1 <= dim <= 512.
+ *   q_heads, k_heads : heads of the two tensors; k_heads = 0: there is no second one (k, yk NULL).
+ *   pairs   : 0 <= 2 pairs <= dim; pair p is columns p and p + pairs, or (interleaved) 2 p and 2 p + 1; columns from
+ *             2 pairs on are left as they are.
+ *   freqs   : pairs finite doubles in HOST memory, radians per position; axes: pairs numbers 0 .. n_axes - 1 in
+ *             HOST memory, NULL for all 0. 1 <= n_axes <= 255. Both are read before the call returns.
+ *   positions : n_axes x tokens whole numbers in device memory, int64 (wide != 0) or int32; any values.
+ * Each y may be its x (same address, strides and heads); no other overlap.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  int64_t tokens, dim, q_heads, k_heads, pairs;
+  const double *freqs;
+  const int32_t *axes;
+  const void *positions;
+  int n_axes, wide, interleaved;
+} lmbp_rope;
+
+lmbp_status rope_fwd(lmbp_dtype dt, const lmbp_rope *r, const lmbp_heads *q, const lmbp_heads *k,
+                     const lmbp_heads *yq, const lmbp_heads *yk, void *stream);
+lmbp_status rope_bwd(lmbp_dtype dt, const lmbp_rope *r, const lmbp_heads *dq, const lmbp_heads *dk,
+                     const lmbp_heads *dxq, const lmbp_heads *dxk, void *stream);
+
+/* ------------------------------------------------------------------------
+ * MS-RMSNorm (Appendix G Alg. 3) of each head and the rotation in one pass. Per head of D columns:
+ *
+ * Forward:  rstd = 1 / sqrt(D^-1 |x|^2 + eps), z = x rstd, y = turned (gain z).
+ *           Heads of any size: squares that fp32 does not hold are formed again of smaller (larger) values.
+ * Backward: without gain from the output y, which attention keeps anyway (turning keeps products):
+ *           dx = turned back (rstd (dy - y D^-1 (y . dy))).
+ *           With gain from x: g = dy turned back, dz = gain g, dx = rstd (dz - z D^-1 (z . dz)),
+ *           dgain = sum of g z over tokens and heads, in fp32 in an order fixed by the sizes.
+ *           The products y . dy (z . dz) have to be among fp32's numbers.
+ *
+ *   eps     : finite, > 0. rstd_q, rstd_k: fp32 [tokens][heads].
+ *   q_gain, k_gain : dim values of dt_gain (fp32 or bf16), both NULL or (k_gain only with k_heads) both given;
+ *             dq_gain, dk_gain: dim values of dt_gain (outputs), NULL without gains.
+ *   kept_q, kept_k : y of the forward without gains, x with.
+ *   workspace : lmbp_msrms_rope_bwd_bytes(dim) bytes, 16-byte aligned, with gains; NULL without.
+ * y may be its x, dx its dy; no other overlap.
+ * ------------------------------------------------------------------------ */
+lmbp_status msrms_rope_fwd(lmbp_dtype dt, lmbp_dtype dt_gain, const lmbp_rope *r, float eps,
+                           const void *q_gain, const void *k_gain, const lmbp_heads *q,
+                           const lmbp_heads *k, const lmbp_heads *yq, const lmbp_heads *yk,
+                           float *rstd_q, float *rstd_k, void *stream);
+lmbp_status msrms_rope_bwd(lmbp_dtype dt, lmbp_dtype dt_gain, const lmbp_rope *r,
+                           const void *q_gain, const void *k_gain, const lmbp_heads *dq,
+                           const lmbp_heads *dk, const lmbp_heads *kept_q,
+                           const lmbp_heads *kept_k, const float *rstd_q, const float *rstd_k,
+                           const lmbp_heads *dxq, const lmbp_heads *dxk, void *dq_gain,
+                           void *dk_gain, void *workspace, int64_t workspace_bytes, void *stream);
+size_t lmbp_msrms_rope_bwd_bytes(int64_t dim);
+
+/* ------------------------------------------------------------------------
+ * Attention (bf16). Of each query (a row of q, a head) over the keys that it sees:
+ *
+ * Forward:  S = scale q k^T, P = softmax(S), o = P v, lse = log sum exp S (natural).
+ * Backward: D = sum of do o, dS = P (do v^T - D), dq = scale dS k, dk = scale dS^T q, dv = P^T do.
+ *
+ * Sums, maxima and lse are fp32; P and dS are rounded to bf16 as factors of the matrix products (the sum of P is
+ * not), results once. heads / kv_heads query heads in a row share a key head; its gradients are summed over them.
+ * Sequences: `batch` of them, one behind the other in the rows. Side by side, for queries and for keys:
+ *   starts NULL : all of one length, rows / batch (a whole number);
+ *   starts      : batch + 1 ascending row numbers in device memory, the first 0 (taken as 0), the last at most
+ *                 the rows. Rows from the last on belong to no sequence.
+ *   k_lens      : NULL, or batch numbers in device memory: only so many of a sequence's keys are in use (a
+ *                 padded cache). What lies behind them is not read.
+ * Of sequence lengths nq and nk (keys in use), query i sees keys j < nk and, if causal, j <= i + nk - nq: the
+ * last query sees all. A query that sees none has o = 0 and lse = -inf, and gives and gets no gradient.
+ * Keys that a query does not see may hold anything, infinities and NaN included.
+ * Starts or k_lens that break the rules above give wrong results, but no access outside the tensors.
+ *
+ *   dt          : LMBP_BF16 (LMBP_EDTYPE otherwise).
+ *   heads, kv_heads : kv_heads divides heads. dim: a multiple of 8, 8 .. 128.
+ *   q_rows heads / kv_heads and k_rows : below 2^31 - 1024. batch >= 1.
+ *   scale       : finite, > 0.
+ *   fill        : 0 leaves o and lse, dq, dk, dv of rows of no sequence (and dk, dv of keys not in use) as they
+ *                 were; otherwise they get zeros (lse -inf).
+ *   q, k, v, o, d_o, dq, dk, dv : 16-byte aligned, strides multiples of 8; 128 row + heads head of each below 2^30.
+ *   lse         : fp32 [q_rows][heads].
+ *   workspace   : lmbp_attention_fwd_bytes / lmbp_attention_bwd_bytes on the calling thread's current device,
+ *                 16-byte aligned, NULL if that is 0. Its contents do not matter before or after.
+ * No output overlaps another buffer. Results do not depend on the order of blocks; how keys (forward) and rows
+ * (dk, dv) are shared out goes by the sizes and the device.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  int64_t batch, heads, kv_heads, dim, q_rows, k_rows;
+  const int32_t *q_starts, *k_starts, *k_lens;
+  float scale;
+  int causal, fill;
+} lmbp_attention;
+
+lmbp_status attention_fwd(lmbp_dtype dt, const lmbp_attention *a, const lmbp_heads *q,
+                          const lmbp_heads *k, const lmbp_heads *v, const lmbp_heads *o, float *lse,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+lmbp_status attention_bwd(lmbp_dtype dt, const lmbp_attention *a, const lmbp_heads *d_o,
+                          const lmbp_heads *q, const lmbp_heads *k, const lmbp_heads *v,
+                          const lmbp_heads *o, const float *lse, const lmbp_heads *dq,
+                          const lmbp_heads *dk, const lmbp_heads *dv, void *workspace,
+                          int64_t workspace_bytes, void *stream);
+size_t lmbp_attention_fwd_bytes(const lmbp_attention *a);
+size_t lmbp_attention_bwd_bytes(const lmbp_attention *a);
 
 /* ------------------------------------------------------------------------
  * Test utilities (host only, no launch): the kernel form that a size takes on the calling

@@ -9,7 +9,8 @@ product (bf16 MFMA). MS-LN / MS-RMSNorm, with the affine merged into the next
 linear layer, save only their output and one fp32 statistic per row (Sec. 5.2);
 MS-RMSNorm also comes fused into that linear layer's matrix product, and with its output
 in 8 bits (the residual's addition in front), which linear layers of frozen 8-bit weights
-take as it is.
+take as it is. Rotary positions (with MS-RMSNorm of each head in the same pass) and attention
+are the part between a block's projections.
 
 The kernels live in liblmbp.so (C ABI in include/lmbp.h); ``binding`` marshals
 torch tensors into it. The library is loaded on first use.
@@ -17,6 +18,9 @@ torch tensors into it. The library is loaded on first use.
 
 from .binding import (  # noqa: F401
     LmbpError,
+    Rotation,
+    attention_bwd,
+    attention_fwd,
     codes_bytes,
     codes_words,
     copy_bytes,
@@ -36,6 +40,8 @@ from .binding import (  # noqa: F401
     msrms_linear_swiglu_fwd,
     msrms_q8_bwd,
     msrms_q8_fwd,
+    msrms_rope_bwd,
+    msrms_rope_fwd,
     q8_rows,
     q8_values,
     regelu2_bwd,
@@ -44,6 +50,8 @@ from .binding import (  # noqa: F401
     resilu2_fwd,
     reswiglu2_bwd,
     reswiglu2_fwd,
+    rope_bwd,
+    rope_fwd,
     stepact_bwd,
     stepact_fwd,
 )

@@ -33,9 +33,27 @@ NORM_OPS = ("msln_fwd", "msln_bwd", "msrms_fwd", "msrms_bwd")
 GLU_OPS = ("reswiglu2_fwd", "reswiglu2_bwd")
 STEP_OPS = ("stepact_fwd", "stepact_bwd")
 LINEAR_OPS = ("linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd", "msrms_linear_swiglu_fwd")
+ROPE_OPS = ("rope_fwd", "rope_bwd", "msrms_rope_fwd", "msrms_rope_bwd")
+ATTENTION_OPS = ("attention_fwd", "attention_bwd")
 Q8_OPS = ("q8_rows", "q8_values", "msrms_q8_fwd", "msrms_q8_bwd", "linear_q8_fwd", "linear_q8_bwd")
 ACT_GELU, ACT_SILU = 0, 1
 Q8_MAX_SUM = 131071   # products of bytes to a sum in 32 bits
+
+
+class _Heads(ctypes.Structure):   # lmbp_heads
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class _Rope(ctypes.Structure):   # lmbp_rope
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "dim", "q_heads", "k_heads", "pairs")] + [
+        ("freqs", ctypes.c_void_p), ("axes", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+        ("n_axes", ctypes.c_int), ("wide", ctypes.c_int), ("interleaved", ctypes.c_int)]
+
+
+class _Attention(ctypes.Structure):   # lmbp_attention
+    _fields_ = [(n, ctypes.c_int64) for n in ("batch", "heads", "kv_heads", "dim", "q_rows", "k_rows")] + [
+        ("q_starts", ctypes.c_void_p), ("k_starts", ctypes.c_void_p), ("k_lens", ctypes.c_void_p),
+        ("scale", ctypes.c_float), ("causal", ctypes.c_int), ("fill", ctypes.c_int)]
 
 
 class LmbpError(RuntimeError):
@@ -124,6 +142,18 @@ def lib():
     L.lmbp_linear_q8_form.argtypes = [i64, i64, i64, i32, counts, counts]
     for name in (*Q8_OPS, "lmbp_linear_q8_form"):
         getattr(L, name).restype = i32
+    hp, rp, ap = ctypes.POINTER(_Heads), ctypes.POINTER(_Rope), ctypes.POINTER(_Attention)
+    L.rope_fwd.argtypes = L.rope_bwd.argtypes = [i32, rp, hp, hp, hp, hp, vp]
+    L.msrms_rope_fwd.argtypes = [i32, i32, rp, f32, vp, vp, hp, hp, hp, hp, vp, vp, vp]
+    L.msrms_rope_bwd.argtypes = [i32, i32, rp, vp, vp, hp, hp, hp, hp, vp, vp, hp, hp, vp, vp, vp, i64, vp]
+    L.lmbp_msrms_rope_bwd_bytes.argtypes = [i64]
+    L.attention_fwd.argtypes = [i32, ap, hp, hp, hp, hp, vp, vp, i64, vp]
+    L.attention_bwd.argtypes = [i32, ap, hp, hp, hp, hp, hp, vp, hp, hp, hp, vp, i64, vp]
+    L.lmbp_attention_fwd_bytes.argtypes = L.lmbp_attention_bwd_bytes.argtypes = [ap]
+    for name in (*ROPE_OPS, *ATTENTION_OPS):
+        getattr(L, name).restype = i32
+    for name in ("lmbp_msrms_rope_bwd_bytes", "lmbp_attention_fwd_bytes", "lmbp_attention_bwd_bytes"):
+        getattr(L, name).restype = ctypes.c_size_t
     L.lmbp_copy.argtypes = [vp, vp, i64, vp]
     L.lmbp_copy.restype = i32
     _bind_fast(L)
@@ -950,3 +980,294 @@ def linear_bias_grad(dy, dtype=None, stream=None):
         work = _workspace(nbytes, dy, stream) if nbytes else None
         _check("linear_bias_grad", L.linear_bias_grad(dt, dt_db, m, n, _ptr(dy), _ptr(db), _opt(work), nbytes, handle))
     return db
+
+
+class Rotation:
+    """Rotary positions: pair p of a head's columns turns by ``freqs[p]`` radians per position on axis
+    ``axes[p]`` (None: one axis). The pairs are columns p and p + len(freqs), or (``interleaved``) 2p
+    and 2p + 1; columns behind the pairs are left as they are. Built once, with the model."""
+
+    def __init__(self, freqs, axes=None, interleaved=False):
+        self.freqs = tuple(float(f) for f in freqs)
+        if not all(math.isfinite(f) for f in self.freqs):
+            raise ValueError("freqs must be finite")
+        self.axes = None if axes is None else tuple(int(a) for a in axes)
+        if self.axes is not None and (len(self.axes) != len(self.freqs) or any(not 0 <= a < 255 for a in self.axes)):
+            raise ValueError("axes must hold one number from 0 to 254 for each of freqs")
+        self.interleaved = bool(interleaved)
+        self.n_axes = max(self.axes, default=0) + 1 if self.axes is not None else 1
+        self._freqs = (ctypes.c_double * len(self.freqs))(*self.freqs)
+        self._axes = None if self.axes is None else (ctypes.c_int32 * len(self.axes))(*self.axes)
+        self._freqs_at = ctypes.addressof(self._freqs)
+        self._axes_at = None if self._axes is None else ctypes.addressof(self._axes)
+
+    def __reduce__(self):   # copies and pickles are built anew, with arrays of their own
+        return Rotation, (self.freqs, self.axes, self.interleaved)
+
+    @classmethod
+    def of_base(cls, columns, base=10000.0, sections=None, interleaved=False):
+        """The usual frequencies base^(-2p / columns); ``sections``: how many pairs, one group behind the
+        other, take each axis."""
+        pairs = columns // 2
+        if columns % 2 or columns < 0:
+            raise ValueError("columns must be an even number")
+        axes = None
+        if sections is not None:
+            axes = [a for a, n in enumerate(sections) for _ in range(n)]
+            if len(axes) != pairs:
+                raise ValueError("sections must add up to the pairs")
+        return cls([base ** (-p / pairs) for p in range(pairs)], axes, interleaved)
+
+    def __repr__(self):
+        return f"Rotation(pairs={len(self.freqs)}, axes={self.n_axes}, interleaved={self.interleaved})"
+
+
+def _heads(t, what, ref=None):
+    """(rows, heads, dim, row stride, head stride) of [..., heads, dim] whose leading dimensions are one
+    behind the other."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{what} must be a GPU tensor")
+    if ref is not None and t.device != ref.device:
+        raise ValueError(f"{what} must be on {ref.device}, not {t.device}")
+    if t.dim() < 3:
+        raise ValueError(f"{what} must be [..., rows, heads, dim]")
+    shape, stride = t.shape, t.stride()
+    rows = math.prod(shape[:-2])
+    if shape[-1] > 1 and stride[-1] != 1 and t.numel():
+        raise ValueError(f"the columns of a head of {what} must lie together")
+    row = stride[-3]
+    if t.dim() > 3 and t.numel():
+        size = 0   # rows of the dimensions from the innermost of more than one on
+        for n, s in zip(reversed(shape[:-2]), reversed(stride[:-2])):
+            if n == 1:
+                continue
+            if size == 0:
+                row, size = s, n
+            elif s != row * size:
+                raise ValueError(f"the leading dimensions of {what} must lie one behind the other")
+            else:
+                size *= n
+    return rows, shape[-2], shape[-1], row if rows > 1 else shape[-2] * shape[-1], stride[-2] if shape[-2] > 1 else shape[-1]
+
+
+def _view(t, layout):
+    return ctypes.byref(_Heads(t.data_ptr(), layout[3], layout[4]))
+
+
+def _heads_out(out, like, what):
+    """An output of ``like``'s shape and type: dense unless given."""
+    if out is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    if not isinstance(out, torch.Tensor) or out.dtype != like.dtype or out.shape != like.shape:
+        raise ValueError(f"{what} must be a {like.dtype} tensor of shape {tuple(like.shape)}")
+    return out
+
+
+def _rope_sides(q, k, positions, rotation):
+    """The plan of a call, and the layouts of q and k (None)."""
+    if not isinstance(rotation, Rotation):
+        raise TypeError("rotation must be a Rotation")
+    lq = _heads(q, "q")
+    lk = None
+    if k is not None:
+        lk = _heads(k, "k", q)
+        if k.dtype != q.dtype or lk[0] != lq[0] or lk[2] != lq[2]:
+            raise ValueError("q and k must have the same type, rows and dim")
+    pairs = len(rotation.freqs)
+    if 2 * pairs > lq[2]:
+        raise ValueError(f"the rotation has {pairs} pairs, a head {lq[2]} columns")
+    where, wide, axes = None, True, 1
+    if pairs:
+        _on(positions, q, "positions")
+        if positions.dtype not in (torch.int64, torch.int32):
+            raise TypeError("positions must be int64 or int32")
+        if positions.numel() != lq[0] or rotation.n_axes > 1:   # [axes, ...], of which the pairs may take the first few
+            axes = positions.shape[0] if positions.dim() > 1 else 1
+            if axes < rotation.n_axes or axes > 255 or positions.numel() != axes * lq[0]:
+                raise ValueError("positions must hold one number per row of q, or be [axes, rows]")
+        where, wide = positions.data_ptr(), positions.dtype == torch.int64
+    plan = _Rope(lq[0], lq[2], lq[1], 0 if lk is None else lk[1], pairs, rotation._freqs_at, rotation._axes_at, where,
+                 axes, wide, rotation.interleaved)
+    return plan, lq, lk
+
+
+def _rope(op, q, k, positions, rotation, q_out, k_out, stream):
+    plan, lq, lk = _rope_sides(q, k, positions, rotation)
+    dt = _dtype_code(q)
+    yq = _heads_out(q_out, q, "q_out")
+    yk = None if k is None else _heads_out(k_out, k, "k_out")
+    vq = _view(yq, _heads(yq, "q_out", q))
+    vk = None if k is None else _view(yk, _heads(yk, "k_out", q))
+    with _device_of(q):   # launches go to the tensors' GPU
+        _check(op, getattr(lib(), op)(dt, ctypes.byref(plan), _view(q, lq), None if k is None else _view(k, lk), vq, vk,
+                                      _stream(q, stream)))
+    return yq, yk
+
+
+def rope_fwd(q, k, positions, rotation, q_out=None, k_out=None, stream=None):
+    """Rotary positions of query and key heads [..., heads, dim] (k may be None): returns both turned.
+    ``positions``: one whole number (int64 or int32) per row, or [axes, rows]. The tensors may be parts of a
+    fused projection's output; q_out and k_out may be given, q and k themselves included."""
+    return _rope("rope_fwd", q, k, positions, rotation, q_out, k_out, stream)
+
+
+def rope_bwd(dq, dk, positions, rotation, q_out=None, k_out=None, stream=None):
+    """Backward of rope_fwd: the gradients turned back."""
+    return _rope("rope_bwd", dq, dk, positions, rotation, q_out, k_out, stream)
+
+
+def _gains(q, k, q_gain, k_gain, dim):
+    """The gains' type code."""
+    if q_gain is None and k_gain is None:
+        return BF16
+    for g, what, there in ((q_gain, "q_gain", True), (k_gain, "k_gain", k is not None)):
+        if (g is not None) != there:
+            raise ValueError("a gain is given for each of q and k, or for none")
+        if there and (_on(g, q, what).numel() != dim or g.dtype != q_gain.dtype):
+            raise ValueError("q_gain and k_gain must hold dim values of one type")
+    return _dtype_code(q_gain)
+
+
+def msrms_rope_fwd(q, k, eps, positions, rotation, q_gain=None, k_gain=None, q_out=None, k_out=None, stream=None):
+    """MS-RMSNorm of each head [..., heads, dim], times a gain per column (None: none), and the rotation in one
+    pass: returns (q, k, rstd_q, rstd_k), None for a k of None."""
+    plan, lq, lk = _rope_sides(q, k, positions, rotation)
+    dt, dt_gain = _dtype_code(q), _gains(q, k, q_gain, k_gain, lq[2])
+    yq = _heads_out(q_out, q, "q_out")
+    yk = None if k is None else _heads_out(k_out, k, "k_out")
+    vq = _view(yq, _heads(yq, "q_out", q))
+    vk = None if k is None else _view(yk, _heads(yk, "k_out", q))
+    rstd_q = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+    rstd_k = None if k is None else torch.empty(k.shape[:-1], dtype=torch.float32, device=q.device)
+    with _device_of(q):   # launches go to the tensors' GPU
+        _check("msrms_rope_fwd", lib().msrms_rope_fwd(
+            dt, dt_gain, ctypes.byref(plan), float(eps), _opt(q_gain), _opt(k_gain), _view(q, lq), None if k is None else _view(k, lk),
+            vq, vk, _ptr(rstd_q), _opt(rstd_k), _stream(q, stream)))
+    return yq, yk, rstd_q, rstd_k
+
+
+def msrms_rope_bwd(dq, dk, q, k, rstd_q, rstd_k, positions, rotation, q_gain=None, k_gain=None, q_out=None, k_out=None,
+                   stream=None):
+    """Backward of msrms_rope_fwd. q and k: the forward's results without gains, its arguments with. Returns
+    (dq, dk) or, with gains, (dq, dk, dq_gain, dk_gain); q_out and k_out may be given, dq and dk included."""
+    plan, lq, lk = _rope_sides(dq, dk, positions, rotation)
+    dt, dt_gain = _dtype_code(dq), _gains(dq, dk, q_gain, k_gain, lq[2])
+    kept = []
+    for t, d, what in ((q, dq, "q"), (k, dk, "k")):
+        if (t is None) != (d is None):
+            raise ValueError("k and dk go together")
+        if t is not None and (t.dtype != d.dtype or t.shape != d.shape):
+            raise ValueError(f"{what} must match its gradient's type and shape")
+        kept.append(None if t is None else _view(t, _heads(t, what, dq)))
+    _per_row(rstd_q, dq, lq[0] * lq[1], "rstd_q")
+    if dk is not None:
+        _per_row(rstd_k, dq, lk[0] * lk[1], "rstd_k")
+    xq = _heads_out(q_out, dq, "q_out")
+    xk = None if dk is None else _heads_out(k_out, dk, "k_out")
+    vq = _view(xq, _heads(xq, "q_out", dq))
+    vk = None if dk is None else _view(xk, _heads(xk, "k_out", dq))
+    gq = None if q_gain is None else torch.empty_like(q_gain)
+    gk = None if k_gain is None else torch.empty_like(k_gain)
+    L = lib()
+    with _device_of(dq):   # launches go to the tensors' GPU
+        nbytes = L.lmbp_msrms_rope_bwd_bytes(lq[2]) if gq is not None else 0
+        handle = _stream(dq, stream)
+        work = _workspace(nbytes, dq, stream) if nbytes else None
+        _check("msrms_rope_bwd", L.msrms_rope_bwd(
+            dt, dt_gain, ctypes.byref(plan), _opt(q_gain), _opt(k_gain), _view(dq, lq), None if dk is None else _view(dk, lk), *kept,
+            _ptr(rstd_q), _opt(rstd_k) if dk is not None else None, vq, vk, _opt(gq), _opt(gk), _opt(work), nbytes, handle))
+    return (xq, xk) if gq is None else (xq, xk, gq, gk)
+
+
+def _numbers(t, ref, count, what):
+    """int32 numbers on the device, or None."""
+    if t is None:
+        return None
+    _on(t, ref, what)
+    if t.dtype != torch.int32 or t.numel() != count:
+        raise ValueError(f"{what} must be an int32 tensor of {count} elements")
+    return t.data_ptr()
+
+
+def _attention(q, k, v, causal, scale, q_starts, k_starts, k_lens, fill):
+    """The plan of a call, and the layouts of q, k and v."""
+    lq, lk, lv = _heads(q, "q"), _heads(k, "k", q), _heads(v, "v", q)
+    for t in (q, k, v):
+        if t.dtype != torch.bfloat16:
+            raise TypeError("attention takes bfloat16 tensors")
+    if k.shape != v.shape or k.shape[-1] != q.shape[-1]:
+        raise ValueError("k and v must have one shape, and q the same dim")
+    if lk[1] == 0 or lq[1] % lk[1]:
+        raise ValueError("the heads of k must divide those of q")
+    if q_starts is not None and k_starts is None and k_lens is None and k.shape[:-2] == q.shape[:-2]:
+        k_starts = q_starts   # queries and keys of the same tokens
+    batch = None
+    for t, starts, what in ((q, q_starts, "q"), (k, k_starts, "k")):
+        if starts is not None:
+            if not isinstance(starts, torch.Tensor):
+                raise TypeError(f"{what}_starts must be a torch.Tensor")
+            n = starts.numel() - 1
+        elif t.dim() > 4:
+            raise ValueError(f"{what} must be [rows, heads, dim] or [sequences, rows, heads, dim]")
+        else:
+            n = t.shape[0] if t.dim() == 4 else 1
+        if batch is not None and n != batch:
+            raise ValueError("queries and keys must have the same number of sequences")
+        batch = n
+    scale = q.shape[-1] ** -0.5 if scale is None and q.shape[-1] else scale
+    plan = _Attention(batch, lq[1], lk[1], q.shape[-1], lq[0], lk[0], _numbers(q_starts, q, batch + 1, "q_starts"),
+                      _numbers(k_starts, q, batch + 1, "k_starts"), _numbers(k_lens, q, batch, "k_lens"), float(scale or 0.0),
+                      bool(causal), bool(fill))
+    return plan, lq, lk, lv
+
+
+def attention_fwd(q, k, v, causal=False, scale=None, q_starts=None, k_starts=None, k_lens=None, o=None, lse=None, stream=None):
+    """Attention of bf16 heads, q [..., heads, dim], k and v [..., kv_heads, dim] (kv_heads divides heads):
+    returns (o, lse), lse the fp32 logarithm of each query's sum. Sequences lie side by side in [sequences, rows,
+    heads, dim], one behind the other in [rows, heads, dim] with ``q_starts`` / ``k_starts`` (int32,
+    sequences + 1, from 0 on; k_starts that are not given are q_starts where k has q's rows), and of each
+    only ``k_lens`` (int32) keys may be in use (a padded cache). Causal: the last query sees the last key. scale:
+    dim ** -0.5 unless given.
+    Rows of no sequence are zeros (lse -inf); in an o and lse given here they stay as they were."""
+    fill = o is None and lse is None
+    plan, lq, lk, lv = _attention(q, k, v, causal, scale, q_starts, k_starts, k_lens, fill)
+    o = _heads_out(o, q, "o")
+    lo = _heads(o, "o", q)
+    lse = _typed_out(q, lse, q.shape[:-1], torch.float32, "lse")
+    L = lib()
+    with _device_of(q):   # launches go to the tensors' GPU
+        nbytes = L.lmbp_attention_fwd_bytes(ctypes.byref(plan))
+        handle = _stream(q, stream)
+        work = _workspace(nbytes, q, stream) if nbytes else None
+        _check("attention_fwd", L.attention_fwd(BF16, ctypes.byref(plan), _view(q, lq), _view(k, lk), _view(v, lv), _view(o, lo),
+                                                _ptr(lse), _opt(work), nbytes, handle))
+    return o, lse
+
+
+def attention_bwd(do, q, k, v, o, lse, causal=False, scale=None, q_starts=None, k_starts=None, k_lens=None, dq=None, dk=None,
+                  dv=None, stream=None):
+    """Backward of attention_fwd from its arguments and results: returns (dq, dk, dv). They may be given (parts of
+    one tensor, too); rows of no sequence and keys not in use are zeros, and stay as they were where all
+    three are given."""
+    fill = dq is None or dk is None or dv is None
+    plan, lq, lk, lv = _attention(q, k, v, causal, scale, q_starts, k_starts, k_lens, fill)
+    parts = []
+    for t, what in ((do, "do"), (o, "o")):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.shape != q.shape:
+            raise ValueError(f"{what} must be a bfloat16 tensor of q's shape")
+        parts.append(_view(t, _heads(t, what, q)))
+    _per_row(lse, q, lq[0] * lq[1], "lse")
+    outs = []
+    for t, like, what in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        t = _heads_out(t, like, what)
+        outs.append((t, _view(t, _heads(t, what, q))))
+    L = lib()
+    with _device_of(q):   # launches go to the tensors' GPU
+        nbytes = L.lmbp_attention_bwd_bytes(ctypes.byref(plan))
+        handle = _stream(q, stream)
+        work = _workspace(nbytes, q, stream) if nbytes else None
+        _check("attention_bwd", L.attention_bwd(BF16, ctypes.byref(plan), parts[0], _view(q, lq), _view(k, lk), _view(v, lv), parts[1],
+                                                _ptr(lse), *(p for _, p in outs), _opt(work), nbytes, handle))
+    return tuple(t for t, _ in outs)

@@ -21,7 +21,8 @@ LIB_PATH = os.path.join(HERE, "liblmbp.so")
 FAST_PATH = os.path.join(HERE, "_fastcall.so")
 SOURCES = ("lmbp_api.hip", "act_kernels.hip", "norm_kernels.hip", "stepact_kernels.hip",
            "linear_kernels.hip", "linear_grad_kernels.hip", "q8_kernels.hip", "linear_q8_kernels.hip",
-           "linear_q8_grad_kernels.hip", "bias_grad_kernels.hip")
+           "linear_q8_grad_kernels.hip", "bias_grad_kernels.hip",
+           "rope_kernels.hip", "attention_kernels.hip", "attention_grad_kernels.hip")
 ARCH = "gfx950"
 
 COMMON_FLAGS = [

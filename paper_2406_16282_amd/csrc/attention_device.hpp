@@ -1,0 +1,407 @@
+// Pieces that the attention kernels share (gfx950): the tiles in LDS, how a block finds its sequence,
+// operand fragments, products that keep masked rows out of each other.
+//
+// Layout of the products. All of them are 32 x 32 x 16 MFMAs whose column is one row of the block's own
+// side (a query in the forward and dq, a key in dk / dv): lane l holds column l % 32, and of the 16 values
+// of a result the rows 8 (i / 4) + 4 (l / 32) + i % 4. As B operand of the next product the same lane needs 8
+// consecutive k of its column; k is only summed over, so slot j of half h = l / 32 is taken to be row 8 (j / 4) +
+// 4 h + j % 4 of 16: a result, rounded and packed, IS the next B operand, with nothing moved between
+// lanes. The A operand of that product lies across memory and is read with the transposing LDS read (of 16
+// lanes, lane q passes the address of columns 4 (q % 4) .. + 3 of row q / 4 and lane i gets the 4 rows of column i),
+// two of them for the rows 4 h .. + 3 and 8 + 4 h .. + 3.
+#pragma once
+
+#include "lmbp_device.hpp"
+#include "lmbp_launch.hpp"
+#include "tile_device.hpp"
+
+#include <atomic>
+
+namespace lmbp {
+namespace attn {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+using lin::kOutOfRange;
+using lin::lds_addr;
+using lin::load_lds16_asm;
+using lin::rsrc_words;
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+constexpr float kLowest = -3.0e38f;   // start of a running maximum: below every score, and finite
+constexpr uint32_t kAllRecords = 0x7fffffffu;   // rows that do not exist are passed as kOutOfRange
+
+__device__ inline f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline s16x4 read_tr(const uint16_t* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)); }
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// The value of the other lane of the same column.
+__device__ inline float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int64_t uniform(int64_t v) {
+  return int64_t(uint64_t(uint32_t(uniform(int(v)))) | uint64_t(uint32_t(uniform(int(v >> 32)))) << 32);
+}
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// As load_lds16_asm, 4 bytes to a lane.
+__device__ inline void load_lds4_asm(const u32x4& r, uint32_t dst, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :: "s"(dst), "v"(offset), "s"(r) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// All of this wave's loads into LDS have landed and its reads are done, and then all waves'.
+__device__ inline void wait_all() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ inline void wait_and_meet() {
+  wait_all();
+  asm volatile("s_barrier" ::: "memory");
+}
+
+// Heads of one tensor: element strides from row to row and from head to head; columns lie together.
+struct Heads {
+  uint16_t* p;
+  int64_t row, head;
+};
+
+// Where the sequences of one side lie: given starts (packed), or all of one length.
+struct Seqs {
+  const int32_t* starts;   // batch + 1, or null
+  int64_t rows;            // of the whole tensor
+  int64_t each;            // rows of a sequence where starts is null
+};
+
+struct Shape {
+  Seqs q, k;
+  const int32_t* k_lens;   // keys in use of each sequence, or null
+  int batch, heads, kv_heads, group, dim, causal, fill;
+  uint32_t inv_group;      // floor(2^32 / group), 2^32 - 1 for 1
+  float scale;
+};
+
+// r / group and the rest, for r < 2^31.
+__device__ inline void split_row(const Shape& s, uint32_t r, uint32_t& token, uint32_t& member) {
+  uint32_t t = __umulhi(r, s.inv_group);
+  uint32_t m = r - t * s.group;
+  if (m >= uint32_t(s.group)) {
+    m -= s.group;
+    ++t;
+  }
+  token = t;
+  member = m;
+}
+
+// Rows [first, first + len) of sequence b; b = batch: the rows behind the last one. Starts that do not
+// ascend or leave the tensor give wrong results, never an access outside it.
+__device__ inline void rows_of(const Seqs& s, int batch, int b, int64_t& first, int64_t& len) {
+  if (s.starts == nullptr) {
+    first = int64_t(b) * s.each;
+    len = b < batch ? s.each : s.rows - first;
+    return;
+  }
+  int64_t lo = b == 0 ? 0 : s.starts[b];
+  lo = lo < 0 ? 0 : lo > s.rows ? s.rows : lo;
+  int64_t hi = b < batch ? s.starts[b + 1] : s.rows;
+  hi = hi < lo ? lo : hi > s.rows ? s.rows : hi;
+  first = lo;
+  len = hi - lo;
+}
+
+// The kernel's arguments, read again from memory: what only the end of a kernel needs takes no registers before it.
+#define LMBP_CONSTANT __attribute__((address_space(4)))
+template <class A>
+__device__ inline const LMBP_CONSTANT A& late_args() {
+  uint64_t p = uint64_t(__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(p));
+  return *(const LMBP_CONSTANT A*)(p);
+}
+
+// One block's part: tile `tile` of sequence b (b = batch: rows of no sequence).
+struct Part {
+  int b, tile, tiles;
+  int64_t q0, k0;     // first rows
+  int q_len, k_len;   // k_len: keys in use
+  int k_slot;         // keys up to the next sequence
+};
+
+// The t-th tile of `per` rows, a row of the side counting `times` times. false: there is none.
+template <bool QUERIES>
+__device__ inline bool locate(const Shape& s, int64_t t, int per, int times, Part& p) {
+  const Seqs& side = QUERIES ? s.q : s.k;
+  int b = 0;
+  if (side.starts == nullptr) {
+    const int64_t tiles = (side.each * times + per - 1) / per;
+    if (t >= tiles * s.batch) return false;
+    b = int(t / tiles);
+    p.tile = int(t - b * tiles);
+    p.tiles = int(tiles);
+  } else {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int all = s.batch + (s.fill ? 1 : 0);
+    bool found = false;
+    for (int base = 0; base < all; base += kWave) {
+      int64_t first, len = 0;
+      const int i = base + lane;
+      if (i < all) rows_of(side, s.batch, i, first, len);
+      const int n = int((len * times + per - 1) / per);
+      int sum = n;
+#pragma unroll
+      for (int off = 1; off < kWave; off <<= 1) {
+        const int up = __shfl_up(sum, off, kWave);
+        if (lane >= off) sum += up;
+      }
+      const int total = uniform(__shfl(sum, kWave - 1, kWave));
+      if (t < total) {
+        const uint64_t over = __ballot(sum > int(t));
+        const int at = __builtin_ctzll(over);
+        b = base + at;
+        p.tiles = uniform(__shfl(n, at, kWave));
+        p.tile = int(t) - uniform(__shfl(sum, at, kWave)) + p.tiles;
+        found = true;
+        break;
+      }
+      t -= total;
+    }
+    if (!found) return false;
+  }
+  b = uniform(b);
+  p.b = b;
+  p.tile = uniform(p.tile);
+  p.tiles = uniform(p.tiles);
+  int64_t len, klen = 0;
+  rows_of(s.q, s.batch, b, p.q0, len);
+  p.q0 = uniform(p.q0);
+  p.q_len = uniform(int(len));
+  rows_of(s.k, s.batch, b, p.k0, klen);
+  p.k0 = uniform(p.k0);
+  p.k_slot = uniform(int(klen));
+  if (b == s.batch) {
+    klen = 0;
+  } else if (s.k_lens != nullptr) {
+    const int64_t used = s.k_lens[b];
+    klen = used < 0 ? 0 : used < klen ? used : klen;
+  }
+  p.k_len = uniform(int(klen));
+  if (QUERIES && b == s.batch) p.k_slot = 0;
+  if (!QUERIES && b == s.batch) p.q_len = 0;
+  return true;
+}
+
+// A tile of rows in LDS: D columns of 2 bytes, in pieces of 16 bytes. Piece c of row r is stored at c ^ swizzle(r): the
+// 16 rows of a row-wise read fall on 16 (D = 64: 8 in each half of a line) different places, and so do the four
+// rows of a transposing one.
+template <int D>
+struct Tile {
+  static constexpr int kPieces = D / 8;
+  static constexpr int kSteps = D / 16;    // of 16 columns
+  static constexpr int kBlocks = D / 32;   // of 32 columns
+  static constexpr int kRowsPerLoad = 64 / kPieces;
+  static __device__ inline int swizzle(int r) {
+    if constexpr (D == 128) return ((r & 3) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 3);
+    else return (((r >> 1) & 1) << 1) | (((r >> 2) & 1) << 2) | ((r >> 3) & 1);
+  }
+  // Element offset of piece c of row r.
+  static __device__ inline int at(int r, int c) { return r * D + (c ^ swizzle(r)) * 8; }
+};
+
+// Reads of fragments: this lane's element offsets within a tile. The pieces are stored under an exclusive or, so the
+// other columns are at an exclusive or of the first ones' offset.
+template <int D>
+struct Reader {
+  using T = Tile<D>;
+  int row, col;
+  __device__ inline Reader() {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int h = lane >> 5, r = lane & 31, q = lane & 15, right = (lane >> 4) & 1;
+    row = T::at(r, h);
+    col = T::at(4 * h + q / 4, 2 * right + (q % 4) / 2) + (q % 2) * 4;
+  }
+  // The offsets derived from here on are formed again, not held in registers over a loop.
+  __device__ inline void refresh() { asm volatile("" : "+v"(row), "+v"(col)); }
+  // A operand, rows first .. first + 31 (first a multiple of 32): columns 16 s + 8 h .. of row l % 32.
+  __device__ inline bf16x8 rows(const uint16_t* tile, int first, int s) const {
+    return *reinterpret_cast<const bf16x8*>(tile + first * D + (row ^ (16 * s)));
+  }
+  // A operand across: rows first .. first + 15 (first a multiple of 16) of column 32 b + l % 32.
+  __device__ inline bf16x8 across(const uint16_t* tile, int first, int b) const {
+    const s16x4 lo = read_tr(tile + first * D + (col ^ (32 * b)));
+    const s16x4 hi = read_tr(tile + (first + 8) * D + (col ^ (32 * b) ^ (T::swizzle(8) * 8)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// Loads of a tile of ROWS rows by WAVES waves, straight into LDS: rows of a tensor one behind the other
+// (keys), or packed rows (token, head of the group). The swizzle is linear in the bits of the row.
+template <int D, int ROWS, int WAVES>
+struct Loader {
+  using T = Tile<D>;
+  static constexpr int kLoads = ROWS / T::kRowsPerLoad / WAVES;   // of each wave
+  static constexpr int kStep = T::kRowsPerLoad * WAVES;           // rows from one load of a wave to its next
+  static_assert(kLoads >= 1 && kLoads * kStep == ROWS, "rows to a wave");
+  int first, piece, dim;   // this lane's row and piece of its first load
+  uint32_t at;             // where the wave's first load goes
+  __device__ inline Loader(int wave, int dim_) : dim(dim_), at(uint32_t(wave) * 1024) {
+    const int lane = threadIdx.x & (kWave - 1);
+    first = wave * T::kRowsPerLoad + lane / T::kPieces;
+    piece = (lane % T::kPieces) ^ T::swizzle(first);
+  }
+  // Rows at `base` of which `left` exist, `pitch` bytes apart.
+  __device__ inline void load(uint64_t base, uint32_t pitch, int left, uint32_t dst) const {
+    const u32x4 r = rsrc_words(base, kAllRecords);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int row = first + j * kStep, c = piece ^ T::swizzle(j * kStep);
+      const uint32_t off = uint32_t(row) * pitch + uint32_t(c) * 16;
+      load_lds16_asm(r, dst + at + j * WAVES * 1024, row < left && c * 8 < dim ? off : kOutOfRange);
+    }
+  }
+  // Packed rows row0 .. of `rows`: token t of row0 + i relative to row0's, t pitch + member * head bytes.
+  __device__ inline void load_packed(const Shape& s, uint64_t base, int64_t pitch, uint32_t head, uint32_t row0, uint32_t rows,
+                                     uint32_t dst) const {
+    uint32_t t0, m0;
+    split_row(s, row0, t0, m0);
+    t0 = uint32_t(uniform(int(t0)));
+    const u32x4 r = rsrc_words(base + uint64_t(t0) * uint64_t(pitch), kAllRecords);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const uint32_t row = row0 + first + j * kStep;
+      const int c = piece ^ T::swizzle(j * kStep);
+      uint32_t t, m;
+      split_row(s, row, t, m);
+      const uint32_t off = (t - t0) * uint32_t(pitch) + m * head + uint32_t(c) * 16;
+      load_lds16_asm(r, dst + at + j * WAVES * 1024, row < rows && c * 8 < dim ? off : kOutOfRange);
+    }
+  }
+};
+
+// Eight results of a column, rounded: the B operand of the next product.
+__device__ inline bf16x8 pack8(const f32x16& v, int first) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(v[first + 2 * i], v[first + 2 * i + 1]);
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// 1 (bf16) for those of this lane's 8 of 16 rows n0 .. that lie in [lo, hi): what its column sees.
+__device__ inline bf16x8 seen_of(int n0, int lo, int hi) {
+  const int h = (threadIdx.x >> 5) & 1;
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = n0 + 8 * (i / 2) + 4 * h + 2 * (i % 2);
+    w[i] = (n >= lo && n < hi ? 0x3f80u : 0u) | (n + 1 >= lo && n + 1 < hi ? 0x3f800000u : 0u);
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// acc += tile^T p for 16 rows of the tile of which a column sees those of `see`, and the others, where p is 0, may
+// hold anything: infinities and NaN are taken out of the product and go to the columns that see them, counted by a
+// product with ones. NANS: an infinity too makes NaN.
+template <bool NANS, int D>
+__device__ inline void add_guarded(f32x16 (&acc)[D / 32], const uint16_t* tile, const Reader<D>& rd, int first, const bf16x8& p,
+                                   const bf16x8& see) {
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) {
+    __builtin_amdgcn_sched_barrier(0);   // one block of columns at a time: registers
+    u32x4 w = __builtin_bit_cast(u32x4, rd.across(tile, first, b));
+    u32x4 odd;   // +inf 1, -inf 2^8, NaN 2^16: sums of 16 say which there are
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t part[2], rest = w[i];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t v = (w[i] >> (16 * e)) & 0xffffu;
+        const uint32_t kind = NANS ? 0x4780u : v == 0x7f80u ? 0x3f80u : v == 0xff80u ? 0x4380u : 0x4780u;
+        const bool is = (v & 0x7f80u) == 0x7f80u;
+        part[e] = is ? kind : 0u;
+        rest &= is ? (e ? 0xffffu : 0xffff0000u) : 0xffffffffu;
+      }
+      w[i] = rest;
+      odd[i] = part[0] | (part[1] << 16);
+    }
+    acc[b] = mfma(__builtin_bit_cast(bf16x8, w), p, acc[b]);
+    if (__any((odd[0] | odd[1] | odd[2] | odd[3]) != 0u)) {
+      const f32x16 n = mfma(__builtin_bit_cast(bf16x8, odd), see, f32x16{});
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = int(n[i]);
+        const float v = k < 0x100 ? __builtin_inff() : k < 0x10000 && (k & 0xff) == 0 ? -__builtin_inff() : __builtin_nanf("");
+        acc[b][i] += k == 0 ? 0.0f : v;
+      }
+    }
+  }
+}
+
+// Stores 32 rows' results times f, rounded: lane l has row l % 32; the halves exchange pieces, so that each lane
+// stores 16 bytes at a time.
+template <int D>
+__device__ inline void store_columns(const f32x16 (&v)[D / 32], float f, uint16_t* row, bool real, int dim) {
+  const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      u32x4 out;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t lo = pack_bf16x2(v[b][8 * u + 2 * i] * f, v[b][8 * u + 2 * i + 1] * f);
+        const uint32_t hi = pack_bf16x2(v[b][8 * u + 4 + 2 * i] * f, v[b][8 * u + 4 + 2 * i + 1] * f);
+        const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(lo, hi, false, false));
+        out[i] = both[0];
+        out[2 + i] = both[1];
+      }
+      const int col = 32 * b + 16 * u + 8 * h;
+      if (real && col < dim) *reinterpret_cast<u32x4*>(row + col) = out;
+    }
+}
+
+// 8 columns of fragments of row `row` (null: zeros).
+template <int D>
+__device__ inline void load_rows(bf16x8 (&f)[D / 16], const uint16_t* row, int dim) {
+  const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (row != nullptr && 16 * s + 8 * h < dim) w = *reinterpret_cast<const u32x4*>(row + 16 * s + 8 * h);
+    f[s] = __builtin_bit_cast(bf16x8, w);
+  }
+}
+
+// Host side.
+inline Heads heads_of(const HeadsView& v) { return Heads{static_cast<uint16_t*>(v.p), v.row, v.head}; }
+inline Shape shape_of(const AttentionPlan& a) {
+  Shape s{};
+  s.q = Seqs{a.q_starts, a.q_rows, a.q_starts ? 0 : a.q_rows / a.batch};
+  s.k = Seqs{a.k_starts, a.k_rows, a.k_starts ? 0 : a.k_rows / a.batch};
+  s.k_lens = a.k_lens;
+  s.batch = int(a.batch);
+  s.heads = int(a.heads);
+  s.kv_heads = int(a.kv_heads);
+  s.group = int(a.heads / a.kv_heads);
+  s.dim = int(a.dim);
+  s.causal = a.causal;
+  s.fill = a.fill;
+  s.inv_group = s.group == 1 ? 0xffffffffu : uint32_t((uint64_t(1) << 32) / uint64_t(s.group));
+  s.scale = a.scale;
+  return s;
+}
+// The most tiles of `per` rows that a side has, a row counting `times` times.
+inline int64_t tiles_of(const Seqs& s, int64_t batch, bool fill, int64_t times, int64_t per) {
+  if (s.starts == nullptr) return (s.each * times + per - 1) / per * batch;
+  return s.rows * times / per + batch + (fill ? 1 : 0);
+}
+// Dynamic LDS beyond 64 KB has to be asked for, once per kernel and device.
+inline hipError_t allow_lds(const void* kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
+  const uint64_t bit = uint64_t(1) << dev;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+}  // namespace attn
+}  // namespace lmbp

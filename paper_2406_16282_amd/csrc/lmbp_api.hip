@@ -7,6 +7,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <limits>
 
 namespace {
@@ -581,6 +582,299 @@ lmbp_status linear_q8_bwd_impl(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64
                                              workspace, static_cast<hipStream_t>(stream)));
 }
 
+// ---- tensors of heads
+
+// Elements from a tensor's first to behind its last; 0 for none.
+uint64_t extent(const lmbp_heads& t, int64_t rows, int64_t heads, int64_t dim) {
+  if (rows == 0 || heads == 0) return 0;
+  return uint64_t(rows - 1) * uint64_t(t.row) + uint64_t(heads - 1) * uint64_t(t.head) + uint64_t(dim);
+}
+
+// One tensor of a call: its sizes beside its place.
+struct Part {
+  const lmbp_heads* t;
+  int64_t rows, heads, dim;
+  int eb;
+  Span span() const { return ::span(t->data, extent(*t, rows, heads, dim) * eb); }
+};
+
+bool bad_strides(const lmbp_heads& t, int64_t rows, int64_t heads) {
+  const int64_t lim = int64_t(1) << 40;
+  if (t.row < 0 || t.head < 0 || t.row > lim || t.head > lim) return true;
+  return double(rows) * double(t.row) + double(heads) * double(t.head) > double(int64_t(1) << 58);
+}
+
+// Written: no element twice.
+bool meets_itself(const Part& p) {
+  const bool by_row = p.heads == 1 || p.t->head >= p.dim, by_head = p.rows == 1 || p.t->row >= p.dim;
+  if (p.rows == 1) return !by_row;
+  if (p.heads == 1) return !by_head;
+  return !((by_row && p.t->row >= (p.heads - 1) * p.t->head + p.dim) || (by_head && p.t->head >= (p.rows - 1) * p.t->row + p.dim));
+}
+
+// Whether two tensors share memory: not if they lie in different parts of the same rows.
+bool share(const Part& a, const Part& b) {
+  if (!overlaps(a.span(), b.span())) return false;
+  if (a.eb != b.eb || a.t->row != b.t->row || a.t->row <= 0) return true;
+  const int64_t pitch = a.t->row * a.eb;
+  const int64_t wa = ((a.heads - 1) * a.t->head + a.dim) * a.eb, wb = ((b.heads - 1) * b.t->head + b.dim) * b.eb;
+  if (wa > pitch || wb > pitch) return true;
+  const int64_t pa = int64_t(reinterpret_cast<uintptr_t>(a.t->data) % uint64_t(pitch));
+  const int64_t pb = int64_t(reinterpret_cast<uintptr_t>(b.t->data) % uint64_t(pitch));
+  const int64_t off = (pb - pa + pitch) % pitch;
+  return !(off >= wa && off + wb <= pitch);
+}
+
+bool same_place(const lmbp_heads& a, const lmbp_heads& b) { return a.data == b.data && a.row == b.row && a.head == b.head; }
+
+lmbp::HeadsView view(const lmbp_heads* t) {
+  lmbp::HeadsView v;
+  if (t) v.p = t->data, v.row = t->row, v.head = t->head;
+  return v;
+}
+
+lmbp_status check_rope(const lmbp_rope* r) {
+  if (!r) return LMBP_EINVAL;
+  const int64_t lim = int64_t(1) << 31;
+  if (r->tokens < 0 || r->dim < 1 || r->dim > lmbp::kRopeDim || r->q_heads < 1 || r->k_heads < 0 || r->q_heads >= lim ||
+      r->k_heads >= lim || r->pairs < 0 || 2 * r->pairs > r->dim || r->n_axes < 1 || r->n_axes > 255)
+    return LMBP_EINVAL;
+  if (r->tokens >= int64_t(1) << 40 || r->q_heads * r->dim >= lim || r->k_heads * r->dim >= lim) return LMBP_EINVAL;
+  if (r->pairs > 0 && !r->freqs) return LMBP_EINVAL;
+  for (int64_t p = 0; p < r->pairs; ++p) {
+    if (!std::isfinite(r->freqs[p])) return LMBP_EINVAL;
+    if (r->axes && (r->axes[p] < 0 || r->axes[p] >= r->n_axes)) return LMBP_EINVAL;
+  }
+  return LMBP_OK;
+}
+
+lmbp::RopePlan rope_plan(const lmbp_rope& r) {
+  return lmbp::RopePlan{r.tokens, r.dim, r.pairs, {r.q_heads, r.k_heads}, r.positions, r.tokens, r.freqs, r.axes, r.wide != 0,
+                        r.interleaved != 0};
+}
+
+// The tensors of a call on queries and keys: in[i] read, out[i] written (it may be in[i]), kept[i] read or null.
+lmbp_status check_sides(lmbp_dtype dt, const lmbp_rope& r, const lmbp_heads* const (&in)[2], const lmbp_heads* const (&out)[2],
+                        const lmbp_heads* const (&kept)[2], bool with_kept) {
+  const int eb = elem_bytes(dt);
+  const int64_t heads[2] = {r.q_heads, r.k_heads};
+  const Span pos = span(r.positions, uint64_t(r.n_axes) * uint64_t(r.tokens) * (r.wide ? 8 : 4));
+  if (r.pairs > 0 && (!r.positions || !aligned(r.positions, r.wide ? 8 : 4))) return LMBP_EINVAL;
+  for (int i = 0; i < 2; ++i) {
+    if (heads[i] == 0) continue;
+    for (const lmbp_heads* t : {in[i], out[i], with_kept ? kept[i] : in[i]}) {
+      if (!t || !t->data || !aligned(t->data, eb) || bad_strides(*t, r.tokens, heads[i])) return LMBP_EINVAL;
+    }
+    if (meets_itself(Part{out[i], r.tokens, heads[i], r.dim, eb})) return LMBP_EINVAL;
+  }
+  for (int i = 0; i < 2; ++i) {
+    if (heads[i] == 0) continue;
+    const Part o{out[i], r.tokens, heads[i], r.dim, eb};
+    if (r.pairs > 0 && overlaps(o.span(), pos)) return LMBP_EOVERLAP;
+    for (int j = 0; j < 2; ++j) {
+      if (heads[j] == 0) continue;
+      if (!(i == j && same_place(*in[j], *out[i])) && share(o, Part{in[j], r.tokens, heads[j], r.dim, eb})) return LMBP_EOVERLAP;
+      if (j != i && share(o, Part{out[j], r.tokens, heads[j], r.dim, eb})) return LMBP_EOVERLAP;
+      if (with_kept && share(o, Part{kept[j], r.tokens, heads[j], r.dim, eb})) return LMBP_EOVERLAP;
+    }
+  }
+  return LMBP_OK;
+}
+
+// A flat buffer beside the tensors that are written (reads: those that are read too).
+lmbp_status check_flat(Span s, lmbp_dtype dt, const lmbp_rope& r, std::initializer_list<const lmbp_heads*> q,
+                       std::initializer_list<const lmbp_heads*> k) {
+  for (const lmbp_heads* t : q)
+    if (t && overlaps(s, Part{t, r.tokens, r.q_heads, r.dim, elem_bytes(dt)}.span())) return LMBP_EOVERLAP;
+  for (const lmbp_heads* t : k)
+    if (t && r.k_heads > 0 && overlaps(s, Part{t, r.tokens, r.k_heads, r.dim, elem_bytes(dt)}.span())) return LMBP_EOVERLAP;
+  return LMBP_OK;
+}
+
+lmbp_status rope_impl(bool back, lmbp_dtype dt, const lmbp_rope* r, const lmbp_heads* q, const lmbp_heads* k, const lmbp_heads* yq,
+                      const lmbp_heads* yk, void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  const lmbp_status st = check_rope(r);
+  if (st != LMBP_OK || r->tokens == 0) return st;
+  const lmbp_status bad = check_sides(dt, *r, {q, k}, {yq, yk}, {nullptr, nullptr}, false);
+  if (bad != LMBP_OK) return bad;
+  return from_hip(lmbp::launch_rope(dt == LMBP_BF16, rope_plan(*r), back, {view(q), view(k)}, {view(yq), view(yk)},
+                                    static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status check_gains(lmbp_dtype dt_gain, const lmbp_rope& r, const void* q_gain, const void* k_gain) {
+  if (!known_dtype(dt_gain)) return LMBP_EDTYPE;
+  if (r.k_heads > 0 ? (q_gain == nullptr) != (k_gain == nullptr) : k_gain != nullptr) return LMBP_EINVAL;
+  const int eb = elem_bytes(dt_gain);
+  return (q_gain && !aligned(q_gain, eb)) || (k_gain && !aligned(k_gain, eb)) ? LMBP_EINVAL : LMBP_OK;
+}
+
+lmbp_status msrms_rope_fwd_impl(lmbp_dtype dt, lmbp_dtype dt_gain, const lmbp_rope* r, float eps, const void* q_gain, const void* k_gain,
+                                const lmbp_heads* q, const lmbp_heads* k, const lmbp_heads* yq, const lmbp_heads* yk, float* rstd_q,
+                                float* rstd_k, void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  lmbp_status st = check_rope(r);
+  if (st != LMBP_OK) return st;
+  if (!(std::isfinite(eps) && eps > 0.0f)) return LMBP_EINVAL;
+  st = check_gains(dt_gain, *r, q_gain, k_gain);
+  if (st != LMBP_OK || r->tokens == 0) return st;
+  st = check_sides(dt, *r, {q, k}, {yq, yk}, {nullptr, nullptr}, false);
+  if (st != LMBP_OK) return st;
+  if (!rstd_q || !aligned(rstd_q, 4) || (r->k_heads > 0 && (!rstd_k || !aligned(rstd_k, 4)))) return LMBP_EINVAL;
+  const Span sq = span(rstd_q, uint64_t(r->tokens) * r->q_heads * 4);
+  const Span sk = span(rstd_k, r->k_heads > 0 ? uint64_t(r->tokens) * r->k_heads * 4 : 0);
+  const Span pos = span(r->positions, r->pairs > 0 ? uint64_t(r->n_axes) * uint64_t(r->tokens) * (r->wide ? 8 : 4) : 0);
+  if (overlaps(sq, sk) || overlaps(sq, pos) || overlaps(sk, pos)) return LMBP_EOVERLAP;
+  for (const Span& s : {sq, sk}) {
+    st = check_flat(s, dt, *r, {q, yq}, {k, yk});
+    if (st != LMBP_OK) return st;
+  }
+  const uint64_t gb = uint64_t(r->dim) * elem_bytes(dt_gain);
+  for (const void* g : {q_gain, k_gain}) {
+    if (!g) continue;
+    const Span s = span(g, gb);
+    if (overlaps(s, sq) || overlaps(s, sk) || check_flat(s, dt, *r, {yq}, {yk}) != LMBP_OK) return LMBP_EOVERLAP;
+  }
+  return from_hip(lmbp::launch_msrms_rope_fwd(dt == LMBP_BF16, rope_plan(*r), eps, dt_gain == LMBP_BF16, {q_gain, k_gain},
+                                              {view(q), view(k)}, {view(yq), view(yk)}, {rstd_q, rstd_k},
+                                              static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status msrms_rope_bwd_impl(lmbp_dtype dt, lmbp_dtype dt_gain, const lmbp_rope* r, const void* q_gain, const void* k_gain,
+                                const lmbp_heads* dq, const lmbp_heads* dk, const lmbp_heads* kept_q, const lmbp_heads* kept_k,
+                                const float* rstd_q, const float* rstd_k, const lmbp_heads* dxq, const lmbp_heads* dxk,
+                                void* dq_gain, void* dk_gain, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!known_dtype(dt)) return LMBP_EDTYPE;
+  lmbp_status st = check_rope(r);
+  if (st != LMBP_OK) return st;
+  st = check_gains(dt_gain, *r, q_gain, k_gain);
+  if (st != LMBP_OK) return st;
+  const bool gains = q_gain != nullptr;
+  if (gains ? !dq_gain || (r->k_heads > 0) != (dk_gain != nullptr) : dq_gain || dk_gain) return LMBP_EINVAL;
+  if (!gains && r->tokens == 0) return LMBP_OK;
+  const int gbytes = elem_bytes(dt_gain);
+  const uint64_t need = gains ? lmbp_msrms_rope_bwd_bytes(r->dim) : 0;
+  if (gains) {
+    if (!aligned(dq_gain, gbytes) || (dk_gain && !aligned(dk_gain, gbytes)) || !workspace || !aligned(workspace, 16) ||
+        workspace_bytes < 0 || uint64_t(workspace_bytes) < need)
+      return LMBP_EINVAL;
+  }
+  const lmbp_heads* none = nullptr;
+  const Span sw = span(workspace, need), gq = span(dq_gain, gains ? uint64_t(r->dim) * gbytes : 0);
+  const Span gk = span(dk_gain, dk_gain ? uint64_t(r->dim) * gbytes : 0);
+  Span ins[5] = {span(q_gain, q_gain ? uint64_t(r->dim) * gbytes : 0), span(k_gain, k_gain ? uint64_t(r->dim) * gbytes : 0), span(none, 0),
+                 span(none, 0), span(none, 0)};
+  if (r->tokens > 0) {
+    st = check_sides(dt, *r, {dq, dk}, {dxq, dxk}, {kept_q, kept_k}, true);
+    if (st != LMBP_OK) return st;
+    if (!rstd_q || !aligned(rstd_q, 4) || (r->k_heads > 0 && (!rstd_k || !aligned(rstd_k, 4)))) return LMBP_EINVAL;
+    ins[2] = span(rstd_q, uint64_t(r->tokens) * r->q_heads * 4);
+    ins[3] = span(rstd_k, r->k_heads > 0 ? uint64_t(r->tokens) * r->k_heads * 4 : 0);
+    ins[4] = span(r->positions, r->pairs > 0 ? uint64_t(r->n_axes) * uint64_t(r->tokens) * (r->wide ? 8 : 4) : 0);
+    for (const Span& s : ins)
+      if (check_flat(s, dt, *r, {dxq}, {dxk}) != LMBP_OK) return LMBP_EOVERLAP;
+    for (const Span& s : {sw, gq, gk})
+      if (check_flat(s, dt, *r, {dq, kept_q, dxq}, {dk, kept_k, dxk}) != LMBP_OK) return LMBP_EOVERLAP;
+  }
+  if (overlaps(gq, gk) || overlaps(sw, gq) || overlaps(sw, gk)) return LMBP_EOVERLAP;
+  for (const Span& in : ins)
+    if (overlaps(in, sw) || overlaps(in, gq) || overlaps(in, gk)) return LMBP_EOVERLAP;
+  return from_hip(lmbp::launch_msrms_rope_bwd(dt == LMBP_BF16, rope_plan(*r), dt_gain == LMBP_BF16, {q_gain, k_gain},
+                                              {view(dq), view(dk)}, {view(kept_q), view(kept_k)}, {rstd_q, rstd_k},
+                                              {view(dxq), view(dxk)}, {dq_gain, dk_gain}, workspace,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status check_attention(const lmbp_attention* a) {
+  if (!a) return LMBP_EINVAL;
+  const int64_t lim = (int64_t(1) << 31) - 1024;
+  if (a->batch < 1 || a->batch >= lim || a->heads < 1 || a->kv_heads < 1 || a->heads >= lim || a->heads % a->kv_heads != 0) return LMBP_EINVAL;
+  if (a->dim < 8 || a->dim > lmbp::kAttentionDim || a->dim % 8 != 0) return LMBP_EINVAL;
+  if (a->q_rows < 0 || a->k_rows < 0 || a->k_rows >= lim || a->q_rows >= lim || a->q_rows >= lim / (a->heads / a->kv_heads)) return LMBP_EINVAL;
+  if ((!a->q_starts && a->q_rows % a->batch != 0) || (!a->k_starts && a->k_rows % a->batch != 0)) return LMBP_EINVAL;
+  if (!aligned(a->q_starts, 4) || !aligned(a->k_starts, 4) || !aligned(a->k_lens, 4)) return LMBP_EINVAL;
+  return std::isfinite(a->scale) && a->scale > 0.0f ? LMBP_OK : LMBP_EINVAL;
+}
+
+lmbp::AttentionPlan attention_plan(const lmbp_attention& a) {
+  return lmbp::AttentionPlan{a.batch, a.heads, a.kv_heads, a.dim, a.q_rows, a.k_rows, a.q_starts, a.k_starts, a.k_lens, a.causal != 0,
+                             a.fill != 0, a.scale};
+}
+
+// Inputs first, then `written` outputs; flat: the other buffers that are read, and lse (written or not) and the workspace.
+lmbp_status check_heads(const Part* parts, int inputs, int count, const Span* read, int reads, const Span* flat, int flats) {
+  const int64_t lim = int64_t(1) << 30;
+  for (int i = 0; i < count; ++i) {
+    const Part& p = parts[i];
+    if (p.rows == 0) continue;
+    if (!p.t || !p.t->data || !aligned(p.t->data, 16) || bad_strides(*p.t, p.rows, p.heads) || p.t->row % 8 != 0 || p.t->head % 8 != 0)
+      return LMBP_EINVAL;
+    if (p.t->row >= lim / 128 || p.heads * p.t->head >= lim - 128 * p.t->row) return LMBP_EINVAL;
+    if (i >= inputs && meets_itself(p)) return LMBP_EINVAL;
+  }
+  for (int i = inputs; i < count; ++i) {
+    if (parts[i].rows == 0) continue;
+    for (int j = 0; j < count; ++j)
+      if (j != i && parts[j].rows > 0 && share(parts[i], parts[j])) return LMBP_EOVERLAP;
+    for (int j = 0; j < reads; ++j)
+      if (overlaps(parts[i].span(), read[j])) return LMBP_EOVERLAP;
+  }
+  for (int i = 0; i < flats; ++i) {
+    for (int j = 0; j < count; ++j)
+      if (parts[j].rows > 0 && overlaps(flat[i], parts[j].span())) return LMBP_EOVERLAP;
+    for (int j = 0; j < reads; ++j)
+      if (overlaps(flat[i], read[j])) return LMBP_EOVERLAP;
+    for (int j = 0; j < i; ++j)
+      if (overlaps(flat[i], flat[j])) return LMBP_EOVERLAP;
+  }
+  return LMBP_OK;
+}
+
+bool bad_workspace(const void* workspace, int64_t bytes, uint64_t need) {
+  return need > 0 && (!workspace || !aligned(workspace, 16) || bytes < 0 || uint64_t(bytes) < need);
+}
+
+Span starts_span(const int32_t* p, int64_t count) { return span(p, p ? uint64_t(count) * 4 : 0); }
+
+lmbp_status attention_fwd_impl(lmbp_dtype dt, const lmbp_attention* a, const lmbp_heads* q, const lmbp_heads* k, const lmbp_heads* v,
+                               const lmbp_heads* o, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!known_dtype(dt) || dt != LMBP_BF16) return LMBP_EDTYPE;
+  const lmbp_status st = check_attention(a);
+  if (st != LMBP_OK || a->q_rows == 0) return st;
+  if (!lse || !aligned(lse, 4)) return LMBP_EINVAL;
+  const uint64_t need = lmbp_attention_fwd_bytes(a);
+  if (bad_workspace(workspace, workspace_bytes, need)) return LMBP_EINVAL;
+  const Part parts[4] = {{q, a->q_rows, a->heads, a->dim, 2}, {k, a->k_rows, a->kv_heads, a->dim, 2}, {v, a->k_rows, a->kv_heads, a->dim, 2},
+                         {o, a->q_rows, a->heads, a->dim, 2}};
+  const Span read[3] = {starts_span(a->q_starts, a->batch + 1), starts_span(a->k_starts, a->batch + 1), starts_span(a->k_lens, a->batch)};
+  const Span flat[2] = {span(lse, uint64_t(a->q_rows) * a->heads * 4), span(workspace, need)};
+  const lmbp_status bad = check_heads(parts, 3, 4, read, 3, flat, 2);
+  if (bad != LMBP_OK) return bad;
+  return from_hip(lmbp::launch_attention_fwd(attention_plan(*a), view(q), view(k), view(v), view(o), lse, workspace,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+lmbp_status attention_bwd_impl(lmbp_dtype dt, const lmbp_attention* a, const lmbp_heads* d_o, const lmbp_heads* q, const lmbp_heads* k,
+                               const lmbp_heads* v, const lmbp_heads* o, const float* lse, const lmbp_heads* dq, const lmbp_heads* dk,
+                               const lmbp_heads* dv, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!known_dtype(dt) || dt != LMBP_BF16) return LMBP_EDTYPE;
+  const lmbp_status st = check_attention(a);
+  if (st != LMBP_OK || (a->q_rows == 0 && a->k_rows == 0)) return st;
+  if (a->q_rows > 0 && (!lse || !aligned(lse, 4))) return LMBP_EINVAL;
+  const uint64_t need = lmbp_attention_bwd_bytes(a);
+  if (bad_workspace(workspace, workspace_bytes, need)) return LMBP_EINVAL;
+  const Part parts[8] = {{d_o, a->q_rows, a->heads, a->dim, 2}, {q, a->q_rows, a->heads, a->dim, 2},    {k, a->k_rows, a->kv_heads, a->dim, 2},
+                         {v, a->k_rows, a->kv_heads, a->dim, 2}, {o, a->q_rows, a->heads, a->dim, 2},    {dq, a->q_rows, a->heads, a->dim, 2},
+                         {dk, a->k_rows, a->kv_heads, a->dim, 2}, {dv, a->k_rows, a->kv_heads, a->dim, 2}};
+  const Span read[4] = {starts_span(a->q_starts, a->batch + 1), starts_span(a->k_starts, a->batch + 1), starts_span(a->k_lens, a->batch),
+                        span(lse, a->q_rows > 0 ? uint64_t(a->q_rows) * a->heads * 4 : 0)};
+  const Span flat[1] = {span(workspace, need)};
+  const lmbp_status bad = check_heads(parts, 5, 8, read, 4, flat, 1);
+  if (bad != LMBP_OK) return bad;
+  return from_hip(lmbp::launch_attention_bwd(attention_plan(*a), view(d_o), view(q), view(k), view(v), view(o), lse, view(dq), view(dk),
+                                             view(dv), workspace, static_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -757,6 +1051,45 @@ lmbp_status linear_q8_bwd(lmbp_dtype dt, lmbp_dtype dt_dx, int64_t m, int64_t n,
                           const int8_t* w, const float* w_scale, const void* add, void* dx, void* workspace,
                           int64_t workspace_bytes, void* stream) {
   return linear_q8_bwd_impl(dt, dt_dx, m, n, k, dy, w, w_scale, add, dx, workspace, workspace_bytes, stream);
+}
+
+lmbp_status rope_fwd(lmbp_dtype dt, const lmbp_rope* r, const lmbp_heads* q, const lmbp_heads* k, const lmbp_heads* yq,
+                     const lmbp_heads* yk, void* stream) {
+  return rope_impl(false, dt, r, q, k, yq, yk, stream);
+}
+lmbp_status rope_bwd(lmbp_dtype dt, const lmbp_rope* r, const lmbp_heads* dq, const lmbp_heads* dk, const lmbp_heads* dxq,
+                     const lmbp_heads* dxk, void* stream) {
+  return rope_impl(true, dt, r, dq, dk, dxq, dxk, stream);
+}
+lmbp_status msrms_rope_fwd(lmbp_dtype dt, lmbp_dtype dt_gain, const lmbp_rope* r, float eps, const void* q_gain, const void* k_gain,
+                           const lmbp_heads* q, const lmbp_heads* k, const lmbp_heads* yq, const lmbp_heads* yk, float* rstd_q,
+                           float* rstd_k, void* stream) {
+  return msrms_rope_fwd_impl(dt, dt_gain, r, eps, q_gain, k_gain, q, k, yq, yk, rstd_q, rstd_k, stream);
+}
+lmbp_status msrms_rope_bwd(lmbp_dtype dt, lmbp_dtype dt_gain, const lmbp_rope* r, const void* q_gain, const void* k_gain,
+                           const lmbp_heads* dq, const lmbp_heads* dk, const lmbp_heads* kept_q, const lmbp_heads* kept_k,
+                           const float* rstd_q, const float* rstd_k, const lmbp_heads* dxq, const lmbp_heads* dxk, void* dq_gain,
+                           void* dk_gain, void* workspace, int64_t workspace_bytes, void* stream) {
+  return msrms_rope_bwd_impl(dt, dt_gain, r, q_gain, k_gain, dq, dk, kept_q, kept_k, rstd_q, rstd_k, dxq, dxk, dq_gain, dk_gain,
+                             workspace, workspace_bytes, stream);
+}
+size_t lmbp_msrms_rope_bwd_bytes(int64_t dim) {
+  return dim < 1 || dim > lmbp::kRopeDim ? 0 : lmbp::msrms_rope_bwd_workspace(dim);
+}
+lmbp_status attention_fwd(lmbp_dtype dt, const lmbp_attention* a, const lmbp_heads* q, const lmbp_heads* k, const lmbp_heads* v,
+                          const lmbp_heads* o, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  return attention_fwd_impl(dt, a, q, k, v, o, lse, workspace, workspace_bytes, stream);
+}
+lmbp_status attention_bwd(lmbp_dtype dt, const lmbp_attention* a, const lmbp_heads* d_o, const lmbp_heads* q, const lmbp_heads* k,
+                          const lmbp_heads* v, const lmbp_heads* o, const float* lse, const lmbp_heads* dq, const lmbp_heads* dk,
+                          const lmbp_heads* dv, void* workspace, int64_t workspace_bytes, void* stream) {
+  return attention_bwd_impl(dt, a, d_o, q, k, v, o, lse, dq, dk, dv, workspace, workspace_bytes, stream);
+}
+size_t lmbp_attention_fwd_bytes(const lmbp_attention* a) {
+  return check_attention(a) == LMBP_OK && a->q_rows > 0 ? lmbp::attention_fwd_workspace(attention_plan(*a)) : 0;
+}
+size_t lmbp_attention_bwd_bytes(const lmbp_attention* a) {
+  return check_attention(a) == LMBP_OK && (a->q_rows > 0 || a->k_rows > 0) ? lmbp::attention_bwd_workspace(attention_plan(*a)) : 0;
 }
 
 lmbp_status lmbp_copy(const void* src, void* dst, int64_t bytes, void* stream) {

@@ -165,6 +165,48 @@ size_t linear_bias_grad_workspace(int64_t m, int64_t n);
 hipError_t launch_linear_bias_grad(bool bf16, bool db_bf16, int64_t m, int64_t n, const void* dy, void* db, void* workspace,
                                    hipStream_t s);
 
+// A tensor of heads: elements from row to row and from head to head; a head's columns lie together.
+struct HeadsView {
+  void* p = nullptr;
+  int64_t row = 0, head = 0;
+};
+
+// Rotary positions (rope_kernels.hip): up to kRopePairs pairs of kRopeDim columns, freqs and axes in host memory.
+constexpr int kRopePairs = 256, kRopeDim = 512;
+struct RopePlan {
+  int64_t tokens, dim, pairs;
+  int64_t heads[2];        // of queries and keys, not both 0
+  const void* positions;   // [axes][tokens], 4 or (wide) 8 bytes each
+  int64_t axis_stride;
+  const double* freqs;     // [pairs], finite
+  const int32_t* axes;     // [pairs] or null
+  bool wide, interleaved;
+};
+hipError_t launch_rope(bool bf16, const RopePlan& r, bool back, const HeadsView (&x)[2], const HeadsView (&y)[2], hipStream_t s);
+hipError_t launch_msrms_rope_fwd(bool bf16, const RopePlan& r, float eps, bool gain_bf16, const void* const (&gain)[2],
+                                 const HeadsView (&x)[2], const HeadsView (&y)[2], float* const (&rstd)[2], hipStream_t s);
+// kept: y without gains, x with. dgain and the workspace (msrms_rope_bwd_workspace bytes) only with gains.
+size_t msrms_rope_bwd_workspace(int64_t dim);
+hipError_t launch_msrms_rope_bwd(bool bf16, const RopePlan& r, bool gain_bf16, const void* const (&gain)[2], const HeadsView (&dy)[2],
+                                 const HeadsView (&kept)[2], const float* const (&rstd)[2], const HeadsView (&dx)[2],
+                                 void* const (&dgain)[2], void* workspace, hipStream_t s);
+
+// Attention (bf16). rows of all sequences one behind the other; starts null: batch sequences of one length.
+struct AttentionPlan {
+  int64_t batch, heads, kv_heads, dim, q_rows, k_rows;
+  const int32_t *q_starts, *k_starts, *k_lens;
+  bool causal, fill;
+  float scale;
+};
+constexpr int kAttentionDim = 128;   // widest head
+size_t attention_fwd_workspace(const AttentionPlan& a);
+hipError_t launch_attention_fwd(const AttentionPlan& a, const HeadsView& q, const HeadsView& k, const HeadsView& v, const HeadsView& o,
+                                float* lse, void* workspace, hipStream_t s);
+size_t attention_bwd_workspace(const AttentionPlan& a);
+hipError_t launch_attention_bwd(const AttentionPlan& a, const HeadsView& d_o, const HeadsView& q, const HeadsView& k, const HeadsView& v,
+                                const HeadsView& o, const float* lse, const HeadsView& dq, const HeadsView& dk, const HeadsView& dv,
+                                void* workspace, hipStream_t s);
+
 hipError_t launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);
 
 }  // namespace lmbp

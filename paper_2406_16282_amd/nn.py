@@ -22,6 +22,14 @@
   two fp32 values per row for the norm's backward; the frozen layers keep nothing of it. The
   output z itself is not handed out: where something else reads it (an adapter beside a
   layer), ``MSRMSNorm`` and ``LinearQ8`` are the pair to use, and z stays in its own type.
+* ``Rope``: rotary positions of query and key heads (one or several axes); keeps nothing but the positions.
+* ``MSRMSNormRope``: RMSNorm of each query and key head and the rotation in one pass. Without gains it keeps its
+  outputs, which attention keeps anyway, and one fp32 rstd per head: the rotation keeps products, so the norm's
+  backward works from them as it is. With gains it keeps its inputs instead.
+* ``Attention``: softmax(scale q k^T) v of bf16 heads, causal or not, grouped heads, equal or packed sequences;
+  keeps q, k, v, its output and one fp32 value per row.
+* ``QKVAttention``: rotation (with the norm of the heads in front, if asked for) and attention on the one output of a
+  fused projection, as one node: the gradients are written into one tensor.
 * ``merge_norm_into_linears``: folds a norm's affine (alpha, beta) into the linear layers
   that consume its output, W~ = W diag(alpha), b~ = W beta + b (Sec. 5.2), and returns
   the parameter-free MS norm to use in its place.
@@ -416,6 +424,190 @@ class MSRMSNormLinearQ8(nn.Module):
 
     def extra_repr(self):
         return f"eps={self.eps}"
+
+
+class _Rope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, rotation):
+        ctx.rotation = rotation
+        ctx.save_for_backward(positions)
+        ctx.set_materialize_grads(False)
+        return binding.rope_fwd(_head_rows(q), _head_rows(k), positions, rotation)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk):
+        (positions,) = ctx.saved_tensors
+        if dq is None:
+            return None, None if dk is None else binding.rope_bwd(_head_rows(dk), None, positions, ctx.rotation)[0], None, None
+        return (*binding.rope_bwd(_head_rows(dq), _head_rows(dk), positions, ctx.rotation), None, None)
+
+
+def _head_rows(t):
+    """A tensor of heads as the operators take it: copied only if its rows do not lie one behind the other."""
+    if t is None:
+        return None
+    try:
+        binding._heads(t, "a tensor")
+    except ValueError:
+        return t.contiguous()
+    return t
+
+
+def _wide_rows(t):
+    """The same for attention, which reads 16 bytes at a time."""
+    t = _head_rows(t)
+    return t if t.data_ptr() % 16 == 0 and all(s % 8 == 0 for s in t.stride()[:-1]) else t.clone(memory_format=torch.contiguous_format)
+
+
+def _flat_positions(positions):
+    return positions if positions is None or positions.is_contiguous() else positions.contiguous()
+
+
+class Rope(nn.Module):
+    """Rotary positions: forward(q, k, positions) turns both, q [..., heads, dim], k the same with its own
+    heads (or None); positions one whole number per row, or [axes, rows]."""
+
+    def __init__(self, rotation):
+        super().__init__()
+        self.rotation = rotation
+
+    def forward(self, q, k, positions):
+        return _Rope.apply(q, k, _flat_positions(positions), self.rotation)
+
+    def extra_repr(self):
+        return repr(self.rotation)
+
+
+class _NormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, rotation, eps, q_gain, k_gain):
+        q, k = _head_rows(q), _head_rows(k)
+        yq, yk, rstd_q, rstd_k = binding.msrms_rope_fwd(q, k, eps, positions, rotation, q_gain, k_gain)
+        ctx.rotation = rotation
+        kept = (yq, yk) if q_gain is None else (q, k)
+        ctx.save_for_backward(*kept, rstd_q, rstd_k, positions, q_gain, k_gain)
+        return yq, yk
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk):
+        q, k, rstd_q, rstd_k, positions, q_gain, k_gain = ctx.saved_tensors
+        out = binding.msrms_rope_bwd(_head_rows(dq), _head_rows(dk), _head_rows(q), _head_rows(k), rstd_q, rstd_k, positions, ctx.rotation,
+                                     q_gain, k_gain)
+        return (*out[:2], None, None, None, *(out[2:] if q_gain is not None else (None, None)))
+
+
+class MSRMSNormRope(nn.Module):
+    """RMSNorm of each head (Alg. 3) and the rotation in one pass: forward(q, k, positions) as Rope. ``dim``: the heads'
+    width, for a gain per column of q and of k (parameters, fp32 unless ``dtype`` says otherwise); None: no gains."""
+
+    def __init__(self, rotation, eps=1e-5, dim=None, device=None, dtype=torch.float32):
+        super().__init__()
+        self.rotation, self.eps = rotation, float(eps)
+        self.q_gain = None if dim is None else nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
+        self.k_gain = None if dim is None else nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
+
+    def forward(self, q, k, positions):
+        return _NormRope.apply(q, k, _flat_positions(positions), self.rotation, self.eps, self.q_gain,
+                               None if k is None else self.k_gain)
+
+    def extra_repr(self):
+        return f"{self.rotation}, eps={self.eps}, gains={self.q_gain is not None}"
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, causal, scale, q_starts, k_starts, k_lens):
+        q, k, v = _wide_rows(q), _wide_rows(k), _wide_rows(v)
+        o, lse = binding.attention_fwd(q, k, v, causal, scale, q_starts, k_starts, k_lens)
+        ctx.how = causal, scale
+        ctx.save_for_backward(q, k, v, o, lse, q_starts, k_starts, k_lens)
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do):
+        q, k, v, o, lse, *where = ctx.saved_tensors
+        grads = binding.attention_bwd(_wide_rows(do), *(_wide_rows(t) for t in (q, k, v, o)), lse.contiguous(), *ctx.how, *where)
+        return (*grads, None, None, None, None, None)
+
+
+class Attention(nn.Module):
+    """softmax(scale q k^T) v (bf16): forward(q, k, v) with q [sequences, rows, heads, dim] and k, v the same with
+    their own rows and heads, or packed as [rows, heads, dim] with q_starts / k_starts (int32, sequences + 1);
+    k_lens: keys in use of each sequence. Causal: the last query sees the last key. scale: dim ** -0.5 unless given."""
+
+    def __init__(self, causal=False, scale=None):
+        super().__init__()
+        self.causal, self.scale = bool(causal), scale
+
+    def forward(self, q, k, v, q_starts=None, k_starts=None, k_lens=None):
+        return _Attention.apply(q, k, v, self.causal, self.scale, q_starts, k_starts, k_lens)
+
+    def extra_repr(self):
+        return f"causal={self.causal}, scale={self.scale}"
+
+
+class _QKVAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, positions, starts, rotation, heads, kv_heads, causal, scale, eps):
+        qkv = _wide_rows(qkv)
+        q, k, v = qkv.split((heads, kv_heads, kv_heads), -2)
+        rstd = (None, None)
+        if eps is not None:
+            q, k, *rstd = binding.msrms_rope_fwd(q, k, eps, positions, rotation)
+        elif rotation.freqs:
+            q, k = binding.rope_fwd(q, k, positions, rotation)
+        o, lse = binding.attention_fwd(q, k, v, causal, scale, starts, starts)
+        ctx.how = rotation, causal, scale, eps
+        ctx.save_for_backward(q, k, v, o, lse, positions, starts, *rstd)
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do):
+        q, k, v, o, lse, positions, starts, rstd_q, rstd_k = ctx.saved_tensors
+        rotation, causal, scale, eps = ctx.how
+        heads, kv_heads = q.shape[-2], k.shape[-2]
+        d = torch.empty((*q.shape[:-2], heads + 2 * kv_heads, q.shape[-1]), dtype=q.dtype, device=q.device)
+        if starts is not None:
+            d.zero_()   # rows of no sequence
+        dq, dk, dv = d.split((heads, kv_heads, kv_heads), -2)
+        q, k, v, o = (_wide_rows(t) for t in (q, k, v, o))
+        binding.attention_bwd(_wide_rows(do), q, k, v, o, lse.contiguous(), causal, scale, starts, starts, dq=dq, dk=dk, dv=dv)
+        if eps is not None:
+            binding.msrms_rope_bwd(dq, dk, q, k, rstd_q, rstd_k, positions, rotation, q_out=dq, k_out=dk)
+        elif rotation.freqs:
+            binding.rope_bwd(dq, dk, positions, rotation, q_out=dq, k_out=dk)
+        return d, None, None, None, None, None, None, None, None
+
+
+class QKVAttention(nn.Module):
+    """Rotation and attention on the output of a block's fused projection: forward(qkv, positions) with qkv
+    [sequences, rows, heads + 2 kv_heads, dim] (queries, keys, values) gives [sequences, rows, heads, dim]; packed as
+    [rows, ..] with ``starts`` (int32, sequences + 1). ``eps``: MS-RMSNorm of each query and key head in front of the
+    rotation (without gains). One node: keeps the turned queries and keys, the values as they lie in qkv,
+    the output and one fp32 value per row (two per head more with the norm); the gradient comes as one tensor."""
+
+    def __init__(self, heads, kv_heads, dim, rotation, causal=True, scale=None, eps=None):
+        super().__init__()
+        if heads % kv_heads:
+            raise ValueError("kv_heads must divide heads")
+        if 2 * len(rotation.freqs) > dim:
+            raise ValueError("the rotation has more columns than a head")
+        self.heads, self.kv_heads, self.dim, self.rotation = heads, kv_heads, dim, rotation
+        self.causal, self.scale, self.eps = bool(causal), scale, None if eps is None else float(eps)
+
+    def forward(self, qkv, positions, starts=None):
+        if qkv.shape[-2:] != (self.heads + 2 * self.kv_heads, self.dim):
+            raise ValueError(f"qkv must be [..., {self.heads + 2 * self.kv_heads}, {self.dim}]")
+        return _QKVAttention.apply(qkv, _flat_positions(positions), starts, self.rotation, self.heads, self.kv_heads, self.causal,
+                                   self.scale, self.eps)
+
+    def extra_repr(self):
+        return (f"heads={self.heads}, kv_heads={self.kv_heads}, dim={self.dim}, {self.rotation}, causal={self.causal}, "
+                f"eps={self.eps}")
 
 
 @torch.no_grad()
