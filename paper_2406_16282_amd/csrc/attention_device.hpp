@@ -40,8 +40,21 @@ __device__ inline f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c)
 }
 __device__ inline s16x4 read_tr(const uint16_t* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)); }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-// The value of the other lane of the same column.
-__device__ inline float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+// The lane, as a value of its own: what is derived from it takes no register before.
+__device__ inline int lane_again() {
+  int v = threadIdx.x & (kWave - 1);
+  asm volatile("" : "+v"(v));
+  return v;
+}
+// The largest, and the sum, of the values of a column's two lanes.
+__device__ inline float column_max(float v) {
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float column_sum(float v) {
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ inline int64_t uniform(int64_t v) {
   return int64_t(uint64_t(uint32_t(uniform(int(v)))) | uint64_t(uint32_t(uniform(int(v >> 32)))) << 32);
@@ -84,15 +97,18 @@ struct Shape {
 };
 
 // r / group and the rest, for r < 2^31.
-__device__ inline void split_row(const Shape& s, uint32_t r, uint32_t& token, uint32_t& member) {
-  uint32_t t = __umulhi(r, s.inv_group);
-  uint32_t m = r - t * s.group;
-  if (m >= uint32_t(s.group)) {
-    m -= s.group;
+__device__ inline void split_row(uint32_t group, uint32_t inv_group, uint32_t r, uint32_t& token, uint32_t& member) {
+  uint32_t t = __umulhi(r, inv_group);
+  uint32_t m = r - t * group;
+  if (m >= group) {
+    m -= group;
     ++t;
   }
   token = t;
   member = m;
+}
+__device__ inline void split_row(const Shape& s, uint32_t r, uint32_t& token, uint32_t& member) {
+  split_row(uint32_t(s.group), s.inv_group, r, token, member);
 }
 
 // Rows [first, first + len) of sequence b; b = batch: the rows behind the last one. Starts that do not
@@ -191,18 +207,19 @@ __device__ inline bool locate(const Shape& s, int64_t t, int per, int times, Par
   return true;
 }
 
-// A tile of rows in LDS: D columns of 2 bytes, in pieces of 16 bytes. Piece c of row r is stored at c ^ swizzle(r): the
-// 16 rows of a row-wise read fall on 16 (D = 64: 8 in each half of a line) different places, and so do the four
-// rows of a transposing one.
+// A tile of rows in LDS: D columns of 2 bytes, in pieces of 16 bytes. Piece c of row r is stored at c ^ swizzle(r): 16 rows
+// of a row-wise read (16 bytes to a lane, 4 cycles) fall on distinct banks, and so do the 64 bytes of each of four rows that
+// a transposing read takes at once (8 bytes to a lane, 2 cycles; with rows 1 apart 32 bytes apart, as smaller tiles
+// of 16 columns want them, it took 4).
 template <int D>
 struct Tile {
   static constexpr int kPieces = D / 8;
   static constexpr int kSteps = D / 16;    // of 16 columns
   static constexpr int kBlocks = D / 32;   // of 32 columns
   static constexpr int kRowsPerLoad = 64 / kPieces;
-  static __device__ inline int swizzle(int r) {
-    if constexpr (D == 128) return ((r & 3) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 3);
-    else return (((r >> 1) & 1) << 1) | (((r >> 2) & 1) << 2) | ((r >> 3) & 1);
+  static constexpr __device__ int swizzle(int r) {
+    if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   }
   // Element offset of piece c of row r.
   static __device__ inline int at(int r, int c) { return r * D + (c ^ swizzle(r)) * 8; }
@@ -259,22 +276,23 @@ struct Loader {
       load_lds16_asm(r, dst + at + j * WAVES * 1024, row < left && c * 8 < dim ? off : kOutOfRange);
     }
   }
-  // Packed rows row0 .. of `rows`: token t of row0 + i relative to row0's, t pitch + member * head bytes.
-  __device__ inline void load_packed(const Shape& s, uint64_t base, int64_t pitch, uint32_t head, uint32_t row0, uint32_t rows,
-                                     uint32_t dst) const {
+  // This lane's byte offsets of packed rows row0 .., from the token of row0 on.
+  __device__ inline void packed(const Shape& s, uint32_t pitch, uint32_t head, uint32_t row0, uint32_t (&off)[kLoads]) const {
     uint32_t t0, m0;
     split_row(s, row0, t0, m0);
-    t0 = uint32_t(uniform(int(t0)));
-    const u32x4 r = rsrc_words(base + uint64_t(t0) * uint64_t(pitch), kAllRecords);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const uint32_t row = row0 + first + j * kStep;
       const int c = piece ^ T::swizzle(j * kStep);
       uint32_t t, m;
-      split_row(s, row, t, m);
-      const uint32_t off = (t - t0) * uint32_t(pitch) + m * head + uint32_t(c) * 16;
-      load_lds16_asm(r, dst + at + j * WAVES * 1024, row < rows && c * 8 < dim ? off : kOutOfRange);
+      split_row(s, row0 + first + j * kStep, t, m);
+      off[j] = c * 8 < dim ? (t - t0) * pitch + m * head + uint32_t(c) * 16 : kOutOfRange;
     }
+  }
+  // Rows at those offsets from `base`, of which `left` exist.
+  __device__ inline void load_at(uint64_t base, const uint32_t (&off)[kLoads], int left, uint32_t dst) const {
+    const u32x4 r = rsrc_words(base, kAllRecords);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_lds16_asm(r, dst + at + j * WAVES * 1024, first + j * kStep < left ? off[j] : kOutOfRange);
   }
 };
 
@@ -298,33 +316,59 @@ __device__ inline bf16x8 seen_of(int n0, int lo, int hi) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// Whether a tile of ROWS rows in LDS holds an infinity or NaN: the same for the whole block of 4 waves, which meets here. Two
+// flags, cleared before; once one is set the caller asks no more.
+template <int D, int ROWS>
+__device__ inline bool tile_is_odd(const uint16_t* tile, int* flags, int which) {
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < ROWS * D / 2048; ++i) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(tile + (i * 256 + threadIdx.x) * 8);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[j] & 0x7fff7fffu));
+  }
+  if (most[0] >= 0x7f80 || most[1] >= 0x7f80) flags[which] = 1;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  asm volatile("s_barrier" ::: "memory");
+  return uniform(*const_cast<volatile int*>(flags + which)) != 0;
+}
+
 // acc += tile^T p for 16 rows of the tile of which a column sees those of `see`, and the others, where p is 0, may
-// hold anything: infinities and NaN are taken out of the product and go to the columns that see them, counted by a
-// product with ones. NANS: an infinity too makes NaN.
+// hold anything. Infinities and NaN are looked for first; where there are any they are taken out of the product and go to
+// the columns that see them, counted by a product with ones. NANS: an infinity too makes NaN.
 template <bool NANS, int D>
 __device__ inline void add_guarded(f32x16 (&acc)[D / 32], const uint16_t* tile, const Reader<D>& rd, int first, const bf16x8& p,
                                    const bf16x8& see) {
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) {
     __builtin_amdgcn_sched_barrier(0);   // one block of columns at a time: registers
-    u32x4 w = __builtin_bit_cast(u32x4, rd.across(tile, first, b));
-    u32x4 odd;   // +inf 1, -inf 2^8, NaN 2^16: sums of 16 say which there are
+    const u32x4 f = __builtin_bit_cast(u32x4, rd.across(tile, first, b));
+    u16x2 most = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t part[2], rest = w[i];
+    for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, f[i] & 0x7fff7fffu));
+    const bool bad = __any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
+    u32x4 w = f;
+    if (bad) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t v = (w[i] >> (16 * e)) & 0xffffu;
-        const uint32_t kind = NANS ? 0x4780u : v == 0x7f80u ? 0x3f80u : v == 0xff80u ? 0x4380u : 0x4780u;
-        const bool is = (v & 0x7f80u) == 0x7f80u;
-        part[e] = is ? kind : 0u;
-        rest &= is ? (e ? 0xffffu : 0xffff0000u) : 0xffffffffu;
-      }
-      w[i] = rest;
-      odd[i] = part[0] | (part[1] << 16);
+      for (int i = 0; i < 4; ++i)
+        w[i] &= ((f[i] & 0x7f80u) == 0x7f80u ? 0xffff0000u : ~0u) & ((f[i] & 0x7f800000u) == 0x7f800000u ? 0xffffu : ~0u);
     }
     acc[b] = mfma(__builtin_bit_cast(bf16x8, w), p, acc[b]);
-    if (__any((odd[0] | odd[1] | odd[2] | odd[3]) != 0u)) {
+    if (bad) {
+      u32x4 odd;   // +inf 1, -inf 2^8, NaN 2^16: sums of 16 say which there are
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t part[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t v = (f[i] >> (16 * e)) & 0xffffu;
+          const uint32_t kind = NANS ? 0x4780u : v == 0x7f80u ? 0x3f80u : v == 0xff80u ? 0x4380u : 0x4780u;
+          part[e] = (v & 0x7f80u) == 0x7f80u ? kind : 0u;
+        }
+        odd[i] = part[0] | (part[1] << 16);
+      }
       const f32x16 n = mfma(__builtin_bit_cast(bf16x8, odd), see, f32x16{});
 #pragma unroll
       for (int i = 0; i < 16; ++i) {

@@ -7,6 +7,7 @@
 #include "attention_device.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lmbp {
 namespace attn {
@@ -17,7 +18,7 @@ struct BwdArgs {
   const float* lse;   // [rows][heads]
   float* stats;       // [kv_heads][rows * group][2]: lse in log2, D
   float* part;        // shares > 1: [shares][2][rows of k][kv_heads][dim]: dk, dv
-  int shares;
+  int shares, share;  // the most shares of a key tile's rows; row tiles that one share should have
   int64_t first;      // block number of this launch's first block
 };
 
@@ -32,27 +33,71 @@ struct Queries {
   float lse, share;   // lse in log2; D
   int limit;
 
-  // 32 keys, the tile's from `first` on.
-  template <bool MASKED>
-  __device__ inline void step(const uint16_t* K, const uint16_t* V, Reader<D>& rd, int first, int key0, float c) {
-    f32x16 x = f32x16{}, y = f32x16{};
+  // P (D less) of value i from its scores.
+  __device__ inline void weight(f32x16& x, const f32x16& y, int i, float c) const {
+    x[i] = exp2_fast(__builtin_fmaf(x[i], c, -lse)) * (y[i] - share);
+  }
+  // q k^T and do v^T of 32 keys, the tile's from `first` on; operands are read two steps ahead.
+  __device__ inline void scores(f32x16& x, f32x16& y, const uint16_t* K, const uint16_t* V, Reader<D>& rd, int first) const {
+    constexpr int kS = T::kSteps, kAhead = 2;
+    bf16x8 a[kS], b[kS];
     rd.refresh();
-#pragma unroll
-    for (int s = 0; s < T::kSteps; ++s) {
-      x = mfma(rd.rows(K, first, s), q[s], x);
-      y = mfma(rd.rows(V, first, s), d_o[s], y);
-    }
+    auto read = [&](int s) {
+      a[s] = rd.rows(K, first, s);
+      b[s] = rd.rows(V, first, s);
+    };
     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) read(s);
+    x = y = f32x16{};
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      if (s + kAhead < kS) read(s + kAhead);
+      x = mfma(a[s], q[s], x);
+      y = mfma(b[s], d_o[s], y);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // 32 keys that the whole block sees. Half of the exponentials stand between the MFMAs of the other half's sums.
+  __device__ inline void whole(const uint16_t* K, const uint16_t* V, Reader<D>& rd, int first, float c) {
+    constexpr int kN = 2 * T::kBlocks, kAhead = 2;
+    f32x16 x, y;
+    bf16x8 k[kN];
+    scores(x, y, K, V, rd, first);
+    auto read = [&](int n) { k[n] = rd.across(K, first + 16 * (n / T::kBlocks), n % T::kBlocks); };
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) read(n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) weight(x, y, i, c);
+    bf16x8 ds = pack8(x, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      if (n == T::kBlocks) ds = pack8(x, 8);
+      dq[n % T::kBlocks] = mfma(k[n], ds, dq[n % T::kBlocks]);
+      if (n + kAhead < kN) read(n + kAhead);
+      if (n < T::kBlocks) {
+#pragma unroll
+        for (int i = 8 + n * 8 / T::kBlocks; i < 8 + (n + 1) * 8 / T::kBlocks; ++i) weight(x, y, i, c);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // 32 keys from key0 on, of which a row sees those below its limit. GUARD: K may hold infinities and NaN.
+  template <bool GUARD>
+  __device__ inline void masked(const uint16_t* K, const uint16_t* V, Reader<D>& rd, int first, int key0, float c) {
+    f32x16 x, y;
+    scores(x, y, K, V, rd, first);
     const int left = limit - key0 - 4 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      x[i] = exp2_fast(__builtin_fmaf(x[i], c, -lse)) * (y[i] - share);
-      if constexpr (MASKED) x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
+      weight(x, y, i, c);
+      x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const bf16x8 ds = pack8(x, 8 * t);
-      if constexpr (MASKED) {
+      if constexpr (GUARD) {
         add_guarded<true, D>(dq, K, rd, first + 16 * t, ds, seen_of(key0 + 16 * t, 0, limit));
       } else {
 #pragma unroll
@@ -68,6 +113,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdArgs a) {
   using T = Tile<D>;
   constexpr int kTile = kKeys * D;
   extern __shared__ __attribute__((aligned(16))) uint16_t lds[];   // two slots of K and V
+  __shared__ int flags[2];
+  if (threadIdx.x < 2) flags[threadIdx.x] = 0;   // a barrier follows in any case
   const Shape& s = a.s;
   const int64_t id = a.first + blockIdx.x;
   const int head = int(id % s.kv_heads);
@@ -117,7 +164,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdArgs a) {
   for (int i = 0; i < T::kSteps; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(float(w.d_o[i][e]), float(o[i][e]), sum);
-  w.share = sum + other_half(sum);
+  w.share = column_sum(sum);
   // A row that sees one key has P = 1 and dS = 0: there D is formed as do v^T is, so that their difference is 0 and not
   // what two orders of the sum leave.
   if (__any(w.limit == 1)) {
@@ -144,12 +191,22 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdArgs a) {
   for (; t < end && t < whole; ++t) {
     const uint16_t* K = next();
 #pragma unroll
-    for (int f = 0; f < kKeys; f += 32) w.template step<false>(K, K + kTile, rd, f, t * kKeys + f, c);
+    for (int f = 0; f < kKeys; f += 32) w.whole(K, K + kTile, rd, f, c);
+  }
+  const uint16_t* K = nullptr;
+  bool odd = false;
+  for (; t < end; ++t) {
+    K = next();
+    odd = tile_is_odd<D, kKeys>(K, flags, t & 1);
+    if (odd) break;
+#pragma unroll 1
+    for (int f = 0; f < kKeys && t * kKeys + f < wave_max; f += 32) w.template masked<false>(K, K + kTile, rd, f, t * kKeys + f, c);
   }
   for (; t < end; ++t) {
-    const uint16_t* K = next();
+    if (!odd) K = next();
+    odd = false;
 #pragma unroll 1
-    for (int f = 0; f < kKeys && t * kKeys + f < wave_max; f += 32) w.template step<true>(K, K + kTile, rd, f, t * kKeys + f, c);
+    for (int f = 0; f < kKeys && t * kKeys + f < wave_max; f += 32) w.template masked<true>(K, K + kTile, rd, f, t * kKeys + f, c);
   }
   wait_all();   // no load into LDS outlives the block
   const auto& e = late_args<BwdArgs>();
@@ -164,9 +221,78 @@ struct Keys {
   f32x16 dk[T::kBlocks], dv[T::kBlocks];
   int from;   // packed rows from it on see this lane's key
 
-  // 32 packed rows from row0 on, with their lse and D. V: the block's values, this wave's from row `mine` on.
-  template <bool MASKED>
-  __device__ inline void step(const uint16_t* Q, const uint16_t* O, const uint16_t* V, int mine, const float* stats, Reader<D>& rd, int row0, float c) {
+  // The lse and D of this lane's rows 2 i and 2 i + 1 (of its 16).
+  static __device__ inline f32x4 stats_of(const float* stats, int i) {
+    return *reinterpret_cast<const f32x4*>(stats + (8 * (i / 2) + 4 * ((threadIdx.x >> 5) & 1)) * 2 + 4 * (i % 2));
+  }
+  // From the scores of values 2 i and 2 i + 1 P and dS.
+  static __device__ inline void weights(f32x16& x, f32x16& y, const f32x4& st, int i, float c) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float p = exp2_fast(__builtin_fmaf(x[2 * i + e], c, -st[2 * e]));
+      y[2 * i + e] = p * (y[2 * i + e] - st[2 * e + 1]);
+      x[2 * i + e] = p;
+    }
+  }
+  // A tile of 32 packed rows that needs no mask. V: the block's values, this wave's from row `mine` on. The order is written out:
+  // operands are read a few MFMAs ahead (left to itself the compiler reads each just before its MFMA and waits for
+  // LDS every time), and half of the exponentials stand between the sums' MFMAs.
+  __device__ inline void whole(const uint16_t* Q, const uint16_t* O, const uint16_t* V, int mine, const float* stats, Reader<D>& rd, float c) {
+    constexpr int kS = T::kSteps, kB = T::kBlocks, kAhead = 2;
+    bf16x8 a[kS], b[kS], d[kS], fo[2 * kB], fq[2 * kB];
+    f32x4 st[8];
+    f32x16 x = f32x16{}, y = f32x16{};
+    rd.refresh();
+    auto scores = [&](int s) {
+      a[s] = rd.rows(Q, 0, s);
+      b[s] = rd.rows(O, 0, s);
+      d[s] = rd.rows(V, mine, s);
+    };
+    auto sums = [&](int i) {
+      fo[i] = rd.across(O, 16 * (i / kB), i % kB);
+      fq[i] = rd.across(Q, 16 * (i / kB), i % kB);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) scores(s);
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      if (s + kAhead < kS) scores(s + kAhead);
+      else st[s + kAhead - kS] = stats_of(stats, s + kAhead - kS);
+      x = mfma(a[s], k[s], x);
+      y = mfma(b[s], d[s], y);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i + 2 < 5) st[i + 2] = stats_of(stats, i + 2);
+      if (i >= 4 - kAhead) sums(i + kAhead - 4);
+      weights(x, y, st[i], i, c);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    bf16x8 p = pack8(x, 0), ds = pack8(y, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * kB; ++i) {
+      if (i == kB) {
+        p = pack8(x, 8);
+        ds = pack8(y, 8);
+      }
+      dv[i % kB] = mfma(fo[i], p, dv[i % kB]);
+      if (i + kAhead < 2 * kB) sums(i + kAhead);
+      if (i < kB) {
+#pragma unroll
+        for (int j = 4 + i * 4 / kB; j < 4 + (i + 1) * 4 / kB; ++j) {
+          if (j + 1 < 8) st[j + 1] = stats_of(stats, j + 1);
+          weights(x, y, st[j], j, c);
+        }
+      }
+      dk[i % kB] = mfma(fq[i], ds, dk[i % kB]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // A tile that needs a mask; GUARD: q and do may hold infinities and NaN.
+  template <bool GUARD>
+  __device__ inline void masked(const uint16_t* Q, const uint16_t* O, const uint16_t* V, int mine, const float* stats, Reader<D>& rd, int row0, float c) {
     f32x16 x = f32x16{}, y = f32x16{};
     rd.refresh();
 #pragma unroll
@@ -175,47 +301,51 @@ struct Keys {
       y = mfma(rd.rows(O, 0, s), rd.rows(V, mine, s), y);
     }
     __builtin_amdgcn_sched_barrier(0);
-    const int h = (threadIdx.x >> 5) & 1;
-    const int skip = from - row0 - 4 * h;
+    const int skip = from - row0 - 4 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4* st = reinterpret_cast<const f32x4*>(stats + (8 * g + 4 * h) * 2);
-      const f32x4 lo = st[0], hi = st[1];
+    for (int i = 0; i < 8; ++i) weights(x, y, stats_of(stats, i), i, c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 4 * g + e;
-        const float lse = e < 2 ? lo[2 * e] : hi[2 * e - 4], share = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
-        x[i] = exp2_fast(__builtin_fmaf(x[i], c, -lse));
-        y[i] = x[i] * (y[i] - share);
-        if constexpr (MASKED) {
-          const bool sees = 8 * g + e >= skip;
-          x[i] = sees ? x[i] : 0.0f;
-          y[i] = sees ? y[i] : 0.0f;
-        }
-      }
+    for (int i = 0; i < 16; ++i) {
+      const bool sees = 8 * (i / 4) + i % 4 >= skip;
+      x[i] = sees ? x[i] : 0.0f;
+      y[i] = sees ? y[i] : 0.0f;
     }
     const bf16x8 p[2] = {pack8(x, 0), pack8(x, 8)}, ds[2] = {pack8(y, 0), pack8(y, 8)};
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (MASKED) {
 #pragma unroll 1
-      for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 pt = t == 0 ? p[0] : p[1], dt = t == 0 ? ds[0] : ds[1];
+      if constexpr (GUARD) {
         const bf16x8 see = seen_of(row0 + 16 * t, from, 0x7fffffff);
-        add_guarded<false, D>(dv, O, rd, 16 * t, t == 0 ? p[0] : p[1], see);
-        add_guarded<true, D>(dk, Q, rd, 16 * t, t == 0 ? ds[0] : ds[1], see);
-      }
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
+        add_guarded<false, D>(dv, O, rd, 16 * t, pt, see);
+        add_guarded<true, D>(dk, Q, rd, 16 * t, dt, see);
+      } else {
 #pragma unroll
         for (int b = 0; b < T::kBlocks; ++b) {
-          dv[b] = mfma(rd.across(O, 16 * t, b), p[t], dv[b]);
-          dk[b] = mfma(rd.across(Q, 16 * t, b), ds[t], dk[b]);
+          dv[b] = mfma(rd.across(O, 16 * t, b), pt, dv[b]);
+          dk[b] = mfma(rd.across(Q, 16 * t, b), dt, dk[b]);
         }
+      }
     }
   }
 };
 
-// A block of 4 waves: 128 keys of one head, 32 to a wave, against all (or a share of) the packed rows that see them.
+// The tiles of packed rows that see keys from key0 on, and the shares that they are split into.
+struct RowTiles {
+  int lowest, all, shares;
+};
+__device__ inline RowTiles row_tiles(const BwdArgs& a, const Part& p, int key0) {
+  const int rows = p.q_len * a.s.group, off = p.k_len - p.q_len;
+  RowTiles r;
+  r.lowest = a.s.causal && key0 > off ? (key0 - off) * a.s.group / kRows : 0;
+  r.all = key0 < p.k_len && r.lowest * kRows < rows ? (rows + kRows - 1) / kRows - r.lowest : 0;
+  const int want = (r.all + a.share - 1) / a.share;
+  r.shares = want < 1 ? 1 : want < a.shares ? want : a.shares;
+  return r;
+}
+
+// A block of 4 waves: 128 keys of one head, 32 to a wave, against all (or a share of) the packed rows that see them, from the last
+// row on: so blocks that run at once read the same rows at the same time.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
   using T = Tile<D>;
@@ -231,22 +361,22 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
   Part p;
   if (!locate<false>(s, rest / a.shares, 128, 1, p)) return;
   const int wave = wave_in_block(), lane = threadIdx.x & (kWave - 1);
-  const int key_b = p.tile * 128, key_w = key_b + wave * 32, key = key_w + (lane & 31);
-  const bool used = key < p.k_len;
+  const int key_b = p.tile * 128, key_w = key_b + wave * 32;
   const int rows = p.q_len * s.group, off = p.k_len - p.q_len;
   auto first_row = [&](int j) { return s.causal && j > off ? (j - off) * s.group : 0; };   // that sees key j
   Keys<D> w;
 #pragma unroll
   for (int b = 0; b < T::kBlocks; ++b) w.dk[b] = w.dv[b] = f32x16{};
-  w.from = first_row(key);
-  load_rows<D>(w.k, used ? a.k.p + (p.k0 + key) * a.k.row + head * a.k.head : nullptr, s.dim);
+  {
+    const int key = key_w + (lane & 31);
+    load_rows<D>(w.k, key < p.k_len ? a.k.p + (p.k0 + key) * a.k.row + head * a.k.head : nullptr, s.dim);
+  }
+  const RowTiles rt = row_tiles(a, p, key_b);
+  if (part >= rt.shares) return;
+  const int each = (rt.all + rt.shares - 1) / rt.shares;
+  const int begin = uniform(rt.lowest + part * each);
+  const int end = uniform(rt.lowest + (part * each + each < rt.all ? part * each + each : rt.all));
   const int masked = uniform((first_row(key_b + 127) + kRows - 1) / kRows);   // tiles from it on need no mask
-
-  const int lowest = key_b < p.k_len ? first_row(key_b) / kRows : 0;
-  const int all = key_b < p.k_len && lowest * kRows < rows ? (rows + kRows - 1) / kRows - lowest : 0;   // tiles
-  const int each = (all + a.shares - 1) / a.shares;
-  const int begin = uniform(lowest + part * each);
-  const int end = uniform(lowest + (part * each + each < all ? part * each + each : all));
 
   const Loader<D, kRows, 4> ld(wave, s.dim);
   Reader<D> rd;
@@ -255,47 +385,70 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
   const uint64_t qb = reinterpret_cast<uint64_t>(a.q.p + p.q0 * a.q.row + q_head0 * a.q.head);
   const uint64_t ob = reinterpret_cast<uint64_t>(a.d_o.p + p.q0 * a.d_o.row + q_head0 * a.d_o.head);
   const uint64_t sb = reinterpret_cast<uint64_t>(a.stats + (int64_t(head) * s.q.rows + p.q0) * s.group * 2);
+  // Where a tile is whole tokens the offsets within it are those of every tile.
+  const bool whole_tokens = kRows % s.group == 0;
+  const uint32_t q_pitch = uint32_t(a.q.row * 2), q_step = uint32_t(a.q.head * 2), o_pitch = uint32_t(a.d_o.row * 2), o_step = uint32_t(a.d_o.head * 2);
+  uint32_t q_off[decltype(ld)::kLoads], o_off[decltype(ld)::kLoads];
+  ld.packed(s, q_pitch, q_step, 0, q_off);
+  ld.packed(s, o_pitch, o_step, 0, o_off);
   auto fetch = [&](int t, int slot) {
     const uint32_t row0 = uint32_t(t) * kRows;
-    ld.load_packed(s, qb, a.q.row * 2, uint32_t(a.q.head * 2), row0, uint32_t(rows), lds0 + slot * 4 * kTile);
-    ld.load_packed(s, ob, a.d_o.row * 2, uint32_t(a.d_o.head * 2), row0, uint32_t(rows), lds0 + slot * 4 * kTile + 2 * kTile);
+    if (!whole_tokens) {
+      ld.packed(s, q_pitch, q_step, row0, q_off);
+      ld.packed(s, o_pitch, o_step, row0, o_off);
+    }
+    const uint64_t token = uint64_t(row0 / uint32_t(s.group));
+    ld.load_at(qb + token * q_pitch, q_off, rows - int(row0), lds0 + slot * 4 * kTile);
+    ld.load_at(ob + token * o_pitch, o_off, rows - int(row0), lds0 + slot * 4 * kTile + 2 * kTile);
     if (wave == 0)
       load_lds4_asm(rsrc_words(sb + uint64_t(row0) * 8, kAllRecords), lds0 + 8 * kTile + 256 * D + slot * kRows * 8,
                     int(row0) + lane / 2 < rows ? uint32_t(lane) * 4 : kOutOfRange);
   };
   const float c = s.scale * kLog2e;
+  int t = end - 1;
   if (begin < end) {
     const Loader<D, 128, 4> lv(wave, s.dim);
     lv.load(reinterpret_cast<uint64_t>(a.v.p + (p.k0 + key_b) * a.v.row + head * a.v.head), uint32_t(a.v.row * 2), p.k_len - key_b,
             lds0 + 8 * kTile);
-    fetch(begin, 0);
+    fetch(t, t & 1);
   }
-  int t = begin;
-  auto next = [&]() {   // the tile in LDS
-    const int slot = (t - begin) & 1;
+  auto next = [&]() {   // tile t has landed
     wait_and_meet();
-    if (t + 1 < end) fetch(t + 1, slot ^ 1);
-    return slot;
+    if (t > begin) fetch(t - 1, (t - 1) & 1);
   };
-  for (; t < end && t < masked; ++t) {
-    const int slot = next();
-    const uint16_t* Q = lds + slot * 2 * kTile;
-    w.template step<true>(Q, Q + kTile, V, wave * 32, stats + slot * kRows * 2, rd, t * kRows, c);
+  auto q_of = [&]() { return lds + (t & 1) * 2 * kTile; };
+  auto st_of = [&]() { return stats + (t & 1) * kRows * 2; };
+  for (; t >= begin && t >= masked; --t) {
+    next();
+    w.whole(q_of(), q_of() + kTile, V, wave * 32, st_of(), rd, c);
   }
-  for (; t < end; ++t) {
-    const int slot = next();
-    const uint16_t* Q = lds + slot * 2 * kTile;
-    w.template step<false>(Q, Q + kTile, V, wave * 32, stats + slot * kRows * 2, rd, t * kRows, c);
+  // This lane's key: formed again behind the loop, which has no register for it.
+  const int key = key_w + (lane_again() & 31);
+  const bool used = key < p.k_len;
+  w.from = first_row(key);
+  // A row of q or do that holds an infinity or NaN has such an lse or D (so has one that sees no key): where no row
+  // of a tile has, unseen rows' zeros as factors are all that a mask takes.
+  bool odd = false;
+  for (; t >= begin; --t) {
+    next();
+    odd = __any((__float_as_uint(st_of()[lane_again()]) & 0x7f800000u) == 0x7f800000u);
+    if (odd) break;
+    w.template masked<false>(q_of(), q_of() + kTile, V, wave * 32, st_of(), rd, t * kRows, c);
+  }
+  for (; t >= begin; --t) {
+    if (!odd) next();
+    odd = false;
+    w.template masked<true>(q_of(), q_of() + kTile, V, wave * 32, st_of(), rd, t * kRows, c);
   }
   wait_all();   // no load into LDS outlives the block
   const auto& e = late_args<BwdArgs>();
   // keys that are not in use get zeros where the rows of no sequence do
   const bool real = key < (e.s.fill ? p.k_slot : p.k_len);
-  if (e.shares > 1) {
+  if (rt.shares > 1) {
     if (key >= p.k_len) return;   // the sum takes them as zeros
     const int64_t size = e.s.k.rows * e.s.kv_heads * e.s.dim;
     float* to = e.part + int64_t(part) * 2 * size + ((p.k0 + key) * e.s.kv_heads + head) * e.s.dim;
-    const int h = lane >> 5;
+    const int h = lane_again() >> 5;
 #pragma unroll
     for (int b = 0; b < T::kBlocks; ++b)
 #pragma unroll
@@ -318,6 +471,8 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(BwdArgs a) {
   const int head = int(id % s.kv_heads);
   Part p;
   if (!locate<false>(s, id / s.kv_heads, 128, 1, p)) return;
+  const int shares = row_tiles(a, p, p.tile * 128).shares;
+  if (shares == 1) return;
   const int64_t size = s.k.rows * s.kv_heads * s.dim;
   const int pieces = s.dim / 4;
   for (int i = threadIdx.x; i < 128 * pieces; i += 256) {
@@ -326,7 +481,7 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(BwdArgs a) {
     f32x4 dk = {0.0f, 0.0f, 0.0f, 0.0f}, dv = dk;
     if (key < p.k_len) {
       const float* from = a.part + ((p.k0 + key) * s.kv_heads + head) * s.dim + col;
-      for (int n = 0; n < a.shares; ++n) {
+      for (int n = 0; n < shares; ++n) {
         dk += *reinterpret_cast<const f32x4*>(from + 2 * n * size);
         dv += *reinterpret_cast<const f32x4*>(from + (2 * n + 1) * size);
       }
@@ -338,14 +493,20 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(BwdArgs a) {
   }
 }
 
-// Shares of the packed rows that a key's sums are split into: where the keys give fewer blocks than the device takes
-// at once, each at least 8 tiles, their sums at most 256 MiB.
-static int row_shares(const AttentionPlan& a, int cus) {
+// How the packed rows that see a key tile are shared out, where the key tiles give fewer than 4 blocks to each place on the
+// device: a share has the tiles that a place would have on average, if all sequences were of one length; at most 2
+// shares (4: no faster, and more to add up), their sums at most 256 MiB. A longer sequence among short ones is split by the kernel, which knows the lengths.
+static void row_shares(const AttentionPlan& a, int cus, int& shares, int& share) {
   const Shape s = shape_of(a);
-  const int64_t blocks = tiles_of(s.k, a.batch, false, 1, 128) * a.kv_heads;
-  const int64_t rows = a.q_rows / a.batch * s.group, bytes = a.k_rows * a.kv_heads * a.dim * 8;
-  if (blocks == 0 || bytes == 0) return 1;
-  return int(std::max<int64_t>(1, std::min<int64_t>({2 * cus / blocks, rows / (8 * kRows), (int64_t(256) << 20) / bytes})));
+  const int64_t places = 2 * cus, tiles = tiles_of(s.k, a.batch, false, 1, 128), blocks = tiles * a.kv_heads;
+  // row tiles that a key can have: a sequence's, or all where only the device knows the lengths
+  const int64_t rows = ((a.q_starts ? a.q_rows : a.q_rows / a.batch) * s.group + kRows - 1) / kRows;
+  const int64_t average = (a.q_rows / a.batch * s.group + kRows - 1) / kRows, bytes = a.k_rows * a.kv_heads * a.dim * 8;
+  shares = share = 1;
+  if (blocks == 0 || bytes == 0 || rows == 0) return;
+  share = int(std::max<int64_t>(8, tiles * average * a.kv_heads / (a.causal ? 2 : 1) / places));
+  if (blocks >= 4 * places) return;
+  shares = int(std::max<int64_t>(1, std::min<int64_t>({2, (rows + share - 1) / share, (int64_t(256) << 20) / bytes})));
 }
 
 template <int D>
@@ -382,7 +543,8 @@ size_t stats_bytes(const AttentionPlan& a) { return (size_t(a.q_rows) * size_t(a
 size_t attention_bwd_workspace(const AttentionPlan& a) {
   int dev = 0, cus = 256;
   if (current_device(dev, cus) != hipSuccess) cus = 256;
-  const int shares = attn::row_shares(a, cus);
+  int shares, share;
+  attn::row_shares(a, cus, shares, share);
   return stats_bytes(a) + (shares > 1 ? size_t(shares) * size_t(a.k_rows) * size_t(a.kv_heads) * size_t(a.dim) * 8 : 0);
 }
 
@@ -405,7 +567,7 @@ hipError_t launch_attention_bwd(const AttentionPlan& a, const HeadsView& d_o, co
   f.lse = lse;
   f.stats = static_cast<float*>(workspace);
   f.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + stats_bytes(a));
-  f.shares = attn::row_shares(a, cus);
+  attn::row_shares(a, cus, f.shares, f.share);
   return a.dim <= 64 ? attn::launch_bwd<64>(f, dev, st) : attn::launch_bwd<128>(f, dev, st);
 }
 

@@ -3,6 +3,7 @@
 #include "attention_device.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lmbp {
 namespace attn {
@@ -36,31 +37,38 @@ struct Rows {
     sum = 0.0f;
   }
 
-  // Keys key0 .. + 32 B - 1, the tile's from `first` on.
-  template <bool MASKED, int kB>
-  __device__ inline void step(const uint16_t* K, const uint16_t* V, const Reader<D>& rd, int first, int key0, float c) {
-    f32x16 x[kB];
+  // Scores of 32 kB keys, the tile's from `first` on: a lane has its row's, 16 of each 32 keys. Operands are read two steps
+  // ahead: left to itself the compiler reads each just before its MFMA and waits for LDS every time.
+  template <int kB>
+  __device__ inline void scores(f32x16 (&x)[kB], const uint16_t* K, const Reader<D>& rd, int first) const {
+    constexpr int kS = T::kSteps, kAhead = 2;
+    bf16x8 k[kS][kB];
+    auto read = [&](int s) {
+#pragma unroll
+      for (int b = 0; b < kB; ++b) k[s][b] = rd.rows(K, first + 32 * b, s);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) read(s);
 #pragma unroll
     for (int b = 0; b < kB; ++b) x[b] = f32x16{};
 #pragma unroll
-    for (int s = 0; s < T::kSteps; ++s)
+    for (int s = 0; s < kS; ++s) {
+      if (s + kAhead < kS) read(s + kAhead);
 #pragma unroll
-      for (int b = 0; b < kB; ++b) x[b] = mfma(rd.rows(K, first + 32 * b, s), q[s], x[b]);
-    const int h = (threadIdx.x >> 5) & 1;
-    if constexpr (MASKED) {
-      const int left = limit - key0 - 4 * h;
-#pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * b + 8 * (i / 4) + i % 4 >= left) x[b][i] = -__builtin_inff();
+      for (int b = 0; b < kB; ++b) x[b] = mfma(k[s][b], q[s], x[b]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  }
+  // The running maximum behind these scores.
+  template <int kB>
+  __device__ inline void follow(const f32x16 (&x)[kB], float c) {
     float most = x[0][0];
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
-    most = fmaxf(most, other_half(most)) * c;
+    most = column_max(most) * c;
     const bool behind = most > top + kSlack;   // each row by itself: its results do not depend on its neighbours'
     if (__any(behind)) {
       const float now = behind ? most : top, f = exp2_fast(top - now);
@@ -71,17 +79,58 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] *= f;
     }
+  }
+  __device__ inline void weight(f32x16& x, int i, float c) {
+    const float p = exp2_fast(__builtin_fmaf(x[i], c, -top));
+    sum += p;
+    x[i] = p;
+  }
+  // 32 kB keys that the whole block sees. Half of the exponentials stand between the MFMAs of the other half's sums.
+  template <int kB>
+  __device__ inline void whole(const uint16_t* K, const uint16_t* V, const Reader<D>& rd, float c) {
+    constexpr int kN = 2 * kB * T::kBlocks, kAhead = 3;   // MFMAs of the sums
+    constexpr int kFirst = 8 * kB;                          // exponentials in front of them
+    f32x16 x[kB];
+    bf16x8 v[kN];
+    scores<kB>(x, K, rd, 0);
+    follow<kB>(x, c);
+    auto read = [&](int n) { v[n] = rd.across(V, 16 * (n / T::kBlocks), n % T::kBlocks); };
 #pragma unroll
-    for (int b = 0; b < kB; ++b)
+    for (int n = 0; n < kAhead; ++n) read(n);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[b][i] = exp2_fast(__builtin_fmaf(x[b][i], c, -top));
-        sum += x[b][i];
+    for (int i = 0; i < kFirst; ++i) weight(x[i / 16], i % 16, c);
+    bf16x8 p = pack8(x[0], 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      const int t = n / T::kBlocks;
+      if (n % T::kBlocks == 0 && n > 0) p = pack8(x[t / 2], 8 * (t % 2));
+      o[n % T::kBlocks] = mfma(v[n], p, o[n % T::kBlocks]);
+      if (n + kAhead < kN) read(n + kAhead);
+      if (n < kN / 2) {
+#pragma unroll
+        for (int i = kFirst + n * kFirst * 2 / kN; i < kFirst + (n + 1) * kFirst * 2 / kN; ++i) weight(x[i / 16], i % 16, c);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // 32 keys from key0 on, the tile's from `first` on, of which a row sees those below its limit. GUARD: V may hold
+  // infinities and NaN.
+  template <bool GUARD>
+  __device__ inline void masked(const uint16_t* K, const uint16_t* V, const Reader<D>& rd, int first, int key0, float c) {
+    f32x16 x[1];
+    scores<1>(x, K, rd, first);
+    const int left = limit - key0 - 4 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
-    for (int t = 0; t < 2 * kB; ++t) {
-      const bf16x8 p = pack8(x[t / 2], 8 * (t % 2));
-      if constexpr (MASKED) {
+    for (int i = 0; i < 16; ++i)
+      if (8 * (i / 4) + i % 4 >= left) x[0][i] = -__builtin_inff();
+    follow<1>(x, c);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) weight(x[0], i, c);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 p = pack8(x[0], 8 * t);
+      if constexpr (GUARD) {
         add_guarded<false>(o, V, rd, first + 16 * t, p, seen_of(key0 + 16 * t, 0, limit));
       } else {
 #pragma unroll
@@ -97,6 +146,8 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
   using T = Tile<D>;
   constexpr int kTile = kKeys * D;   // elements
   extern __shared__ __attribute__((aligned(16))) uint16_t lds[];   // two slots of K and V
+  __shared__ int flags[2];
+  if (threadIdx.x < 2) flags[threadIdx.x] = 0;   // a barrier follows in any case
   const Shape& s = a.s;
   const int64_t id = a.first + blockIdx.x;
   const int head = int(id % s.kv_heads);
@@ -143,26 +194,37 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
     ld.load(vb + uint64_t(t) * kKeys * v_pitch, v_pitch, left, lds0 + slot * 4 * kTile + 2 * kTile);
   };
   const float c = s.scale * kLog2e;
-  if (begin < end) fetch(begin, 0);
+  if (begin < end) fetch(begin, begin & 1);
   int t = begin;
-  auto next = [&]() {   // the tile in LDS
-    const int slot = (t - begin) & 1;
+  auto next = [&]() {   // tile t has landed
     wait_and_meet();
-    if (t + 1 < end) fetch(t + 1, slot ^ 1);
-    return lds + slot * 2 * kTile;
+    if (t + 1 < end) fetch(t + 1, (t + 1) & 1);
   };
-  for (; t < end && t < whole; ++t) {
-    const uint16_t* K = next();
-    w.template step<false, kKeys / 32>(K, K + kTile, rd, 0, t * kKeys, c);
+  auto k_of = [&]() { return lds + (t & 1) * 2 * kTile; };
+  for (const int last = whole < end ? whole : end; t < last; ++t) {
+    next();
+    w.template whole<kKeys / 32>(k_of(), k_of() + kTile, rd, c);
+  }
+  auto masked = [&](auto guard) {
+#pragma unroll 1
+    for (int f = 0; f < kKeys && t * kKeys + f < wave_max; f += 32)
+      w.template masked<decltype(guard)::value>(k_of(), k_of() + kTile, rd, f, t * kKeys + f, c);
+  };
+  bool odd = false;
+  for (; t < end; ++t) {
+    next();
+    odd = tile_is_odd<D, kKeys>(k_of() + kTile, flags, t & 1);
+    if (odd) break;
+    masked(std::false_type{});
   }
   for (; t < end; ++t) {
-    const uint16_t* K = next();
-#pragma unroll 1
-    for (int f = 0; f < kKeys && t * kKeys + f < wave_max; f += 32) w.template step<true, 1>(K, K + kTile, rd, f, t * kKeys + f, c);
+    if (!odd) next();
+    odd = false;
+    masked(std::true_type{});
   }
   wait_all();   // no load into LDS outlives the block
   const auto& e = late_args<FwdArgs>();
-  const float sum = w.sum + other_half(w.sum);
+  const float sum = column_sum(w.sum);
   const int64_t o_head = int64_t(head) * e.s.group + member, out_row = (p.q0 + token) * e.s.heads + o_head;
   if (e.splits > 1 && p.b < e.s.batch) {
     if (!real) return;
@@ -190,56 +252,216 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
   if (real && lane < 32) e.lse[out_row] = w.limit > 0 ? (w.top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
 }
 
-// The shares' results of each row: a wave per row, its columns over the lanes.
-__global__ __launch_bounds__(256) void attention_join_kernel(FwdArgs a) {
+// Few rows, many keys: a block of kFewWaves waves has 32 packed rows and a share of their keys; each wave walks keys of its own
+// through two slots of its own, with no barrier, and the block's waves join at the end. Memory is what it waits
+// for: 16 KB to a wave are on their way while 16 KB are multiplied, 64 KB to a CU.
+constexpr int kFewWaves = 2;
+template <int D>
+constexpr int kFewKeys = 4096 / D;   // keys to a wave's tile: 8 KB of K, 8 of V
+template <int D>
+constexpr int kFewLds = kFewWaves * 32768;
+
+template <int D>
+__global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(FwdArgs a) {
+  constexpr int kT = kFewKeys<D>, kTile = kT * D;
+  constexpr int kPitch = D + 4;   // floats from row to row of a wave's sums: 16 rows on distinct banks
+  extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
+  __shared__ float tops[kFewWaves][32], sums[kFewWaves][32], norm[32];
   const Shape& s = a.s;
-  const int64_t row = a.first + int64_t(blockIdx.x) * 4 + wave_in_block();
-  const int64_t count = s.q.rows * s.heads;
-  if (row >= count) return;
-  const int64_t token = row / s.heads;
-  if (s.q.starts != nullptr && token >= s.q.starts[s.batch]) return;   // a row of no sequence
-  const int lane = threadIdx.x & (kWave - 1);
-  float top = kLowest;
-  for (int i = 0; i < a.splits; ++i) top = fmaxf(top, a.stats[(i * count + row) * 2]);
-  float sum = 0.0f, v[2] = {0.0f, 0.0f};
-  bool any = false;
-  for (int i = 0; i < a.splits; ++i) {
-    const float m = a.stats[(i * count + row) * 2], l = a.stats[(i * count + row) * 2 + 1];
-    if (l == 0.0f && m == kLowest) continue;   // no key in this share
-    any = true;
-    const float f = exp2_fast(m - top);
-    sum = __builtin_fmaf(l, f, sum);
-    const float* from = a.part + (i * count + row) * s.dim;
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (2 * lane + e < s.dim) v[e] = __builtin_fmaf(from[2 * lane + e], f, v[e]);
+  const int64_t id = a.first + blockIdx.x;
+  const int head = int(id % s.kv_heads);
+  const int64_t rest = id / s.kv_heads;
+  const int split = int(rest % a.splits);
+  Part p;
+  if (!locate<true>(s, rest / a.splits, 32, s.group, p)) return;
+  const int wave = wave_in_block(), lane = threadIdx.x & (kWave - 1), h = lane >> 5, in = lane & 31;
+  const uint32_t rows = uint32_t(p.q_len) * uint32_t(s.group), row0 = uint32_t(p.tile) * 32;
+  const bool real = row0 + in < rows;
+  uint32_t token, member;
+  split_row(s, real ? row0 + in : 0, token, member);
+  auto seen = [&](uint32_t r) {
+    if (!s.causal) return p.k_len;
+    const uint32_t last = r < rows ? r : rows - 1;
+    const int n = int(last / uint32_t(s.group)) + 1 + p.k_len - p.q_len;
+    return n < 0 ? 0 : n < p.k_len ? n : p.k_len;
+  };
+  Rows<D> w;
+  w.clear();
+  w.limit = real ? seen(row0 + in) : 0;
+  const int most = uniform(seen(row0 + 31));
+  const int all = (most + kT - 1) / kT, whole = uniform(seen(row0)) / kT;
+  const int share = (all + a.splits - 1) / a.splits;
+  const int begin = split * share, end = begin + share < all ? begin + share : all;
+  const Loader<D, kT, 1> ld(0, s.dim);
+  const Reader<D> rd;
+  uint16_t* mine = lds + wave * 16384;
+  const uint32_t at = lds_addr(mine), k_pitch = uint32_t(a.k.row * 2), v_pitch = uint32_t(a.v.row * 2);
+  const uint64_t kb = reinterpret_cast<uint64_t>(a.k.p + p.k0 * a.k.row + head * a.k.head);
+  const uint64_t vb = reinterpret_cast<uint64_t>(a.v.p + p.k0 * a.v.row + head * a.v.head);
+  auto fetch = [&](int t, int slot) {   // past the share: zeros, so that the count of loads on their way stays the same
+    const int left = t < end ? p.k_len - t * kT : 0;
+    const int64_t from = t < end ? int64_t(t) * kT : 0;
+    ld.load(kb + uint64_t(from) * k_pitch, k_pitch, left, at + slot * 16384);
+    ld.load(vb + uint64_t(from) * v_pitch, v_pitch, left, at + slot * 16384 + 8192);
+  };
+  const float c = s.scale * kLog2e;
+  const int64_t q_head = int64_t(head) * s.group + member;
+  if (begin < end) {
+    load_rows<D>(w.q, real ? a.q.p + (p.q0 + token) * a.q.row + q_head * a.q.head : nullptr, s.dim);
+    int t = begin + wave, slot = 0;
+    fetch(t, 0);
+    auto next = [&]() {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot to be filled has been read
+      fetch(t + kFewWaves, slot ^ 1);
+      asm volatile("s_waitcnt vmcnt(16)" ::: "memory");    // all but those loads have landed
+      const uint16_t* K = mine + slot * 8192;
+      slot ^= 1;
+      return K;
+    };
+    for (; t < end && t < whole; t += kFewWaves) {
+      const uint16_t* K = next();
+      w.template whole<kT / 32>(K, K + kTile, rd, c);
+    }
+    for (; t < end; t += kFewWaves) {
+      const uint16_t* K = next();
+#pragma unroll 1
+      for (int f = 0; f < kT && t * kT + f < most; f += 32) w.template masked<true>(K, K + kTile, rd, f, t * kT + f, c);
+    }
   }
-  const float f = any ? 1.0f / sum : 0.0f;
+  wait_all();
+  w.sum = column_sum(w.sum);
+  if (h == 0) {
+    tops[wave][in] = w.top;
+    sums[wave][in] = w.sum;
+  }
+  __syncthreads();
+  float top = kLowest, sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kFewWaves; ++i) top = fmaxf(top, tops[i][in]);
+#pragma unroll
+  for (int i = 0; i < kFewWaves; ++i) sum = __builtin_fmaf(sums[i][in], exp2_fast(tops[i][in] - top), sum);
+  const float f = exp2_fast(w.top - top);
+  float* part = reinterpret_cast<float*>(lds);
+  static_assert(kFewWaves * 32 * kPitch * 4 <= kFewLds<D>, "the sums fit");
+  float* own = part + (wave * 32 + in) * kPitch;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<f32x4*>(own + 32 * b + 8 * g + 4 * h) =
+          f32x4{w.o[b][4 * g] * f, w.o[b][4 * g + 1] * f, w.o[b][4 * g + 2] * f, w.o[b][4 * g + 3] * f};
+  const auto& e = late_args<FwdArgs>();
+  const int64_t o_head = int64_t(head) * e.s.group + member, out_row = (p.q0 + token) * e.s.heads + o_head;
+  const bool joined = e.splits > 1 && p.b < e.s.batch;   // by the next kernel
+  if (!joined && split > 0) return;
+  if (real && wave == 0 && h == 0) {
+    if (joined) {
+      float* st = e.stats + (int64_t(split) * e.s.q.rows * e.s.heads + out_row) * 2;
+      st[0] = top;
+      st[1] = sum;
+    } else {
+      e.lse[out_row] = w.limit > 0 ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+      norm[in] = w.limit > 0 ? 1.0f / sum : 0.0f;
+    }
+  }
+  __syncthreads();
+  if (joined && begin >= end) return;
+  for (int i = threadIdx.x; i < 32 * (D / 4); i += kFewWaves * 64) {
+    const int r = i / (D / 4), col = i % (D / 4) * 4;
+    if (row0 + r >= rows || col >= e.s.dim) continue;
+    f32x4 v = *reinterpret_cast<const f32x4*>(part + r * kPitch + col);
+#pragma unroll
+    for (int j = 1; j < kFewWaves; ++j) v += *reinterpret_cast<const f32x4*>(part + (j * 32 + r) * kPitch + col);
+    uint32_t tok, mem;
+    split_row(e.s.group, e.s.inv_group, row0 + r, tok, mem);
+    const int64_t hd = int64_t(head) * e.s.group + mem;
+    if (joined) {
+      *reinterpret_cast<f32x4*>(e.part + (int64_t(split) * e.s.q.rows * e.s.heads + (p.q0 + tok) * e.s.heads + hd) * e.s.dim + col) = v;
+    } else {
+      const float n = norm[r];
+      const u32x2 out = {pack_bf16x2(v[0] * n, v[1] * n), pack_bf16x2(v[2] * n, v[3] * n)};
+      *reinterpret_cast<u32x2*>(e.o.p + (p.q0 + tok) * e.o.row + hd * e.o.head + col) = out;
+    }
+  }
+}
+
+// The shares' results of each row: a block per row. Its waves take the shares in turn, lanes two columns each.
+__global__ __launch_bounds__(256) void attention_join_kernel(FwdArgs a) {
+  __shared__ float lds[3][2 * kWave];
+  const Shape& s = a.s;
+  const int64_t row = a.first + blockIdx.x, count = s.q.rows * s.heads, token = row / s.heads;
+  if (s.q.starts != nullptr && token >= s.q.starts[s.batch]) return;   // a row of no sequence
+  const int lane = threadIdx.x & (kWave - 1), wave = wave_in_block();
+  // lane i has share i's maximum and sum; a share without keys counts nothing
+  float m = kLowest, l = 0.0f;
+  if (lane < a.splits) {
+    m = a.stats[(lane * count + row) * 2];
+    l = a.stats[(lane * count + row) * 2 + 1];
+  }
+  const bool none = l == 0.0f && m == kLowest;
+  float top = m;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+  const float f = none ? 0.0f : exp2_fast(m - top), sum = wave_sum(none ? 0.0f : l * f);
+  const bool any = __any(!none);
+  const int col = 2 * lane < s.dim ? 2 * lane : 0;
+  float v[2] = {0.0f, 0.0f};
+  for (int i = wave; i < a.splits; i += 4) {
+    if (__shfl(int(none), i, kWave)) continue;
+    const float g = __shfl(f, i, kWave);
+    const f32x2 x = *reinterpret_cast<const f32x2*>(a.part + (i * count + row) * s.dim + col);
+    v[0] = __builtin_fmaf(x[0], g, v[0]);
+    v[1] = __builtin_fmaf(x[1], g, v[1]);
+  }
+  if (wave > 0) {
+    lds[wave - 1][lane] = v[0];
+    lds[wave - 1][kWave + lane] = v[1];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    v[0] += lds[i][lane];
+    v[1] += lds[i][kWave + lane];
+  }
+  const float n = any ? 1.0f / sum : 0.0f;
   uint16_t* o = a.o.p + token * a.o.row + (row - token * s.heads) * a.o.head;
-  if (2 * lane < s.dim) *reinterpret_cast<uint32_t*>(o + 2 * lane) = pack_bf16x2(v[0] * f, v[1] * f);
+  if (2 * lane < s.dim) *reinterpret_cast<uint32_t*>(o + 2 * lane) = pack_bf16x2(v[0] * n, v[1] * n);
   if (lane == 0) a.lse[row] = any ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
 }
 
-// Shares of the keys: where the rows give fewer blocks than the device takes at once, each at least 4 tiles.
-static int key_shares(const AttentionPlan& a, int cus) {
+// How a call is taken: blocks of 32 packed rows (few) or of 128, and the shares of the keys.
+struct FwdForm {
+  bool few;
+  int splits;
+};
+static FwdForm fwd_form(const AttentionPlan& a, int cus) {
   const Shape s = shape_of(a);
-  const int64_t blocks = tiles_of(s.q, a.batch, false, s.group, 128) * a.kv_heads;
   const int64_t keys = a.k_rows / a.batch;
-  if (blocks == 0) return 1;
-  return int(std::max<int64_t>(1, std::min<int64_t>({2 * cus / blocks, keys / (4 * kKeys), 64})));
+  FwdForm f;
+  f.few = a.q_rows * s.group <= 32 * a.batch;
+  const int64_t blocks = tiles_of(s.q, a.batch, false, s.group, f.few ? 32 : 128) * a.kv_heads;
+  // keys to a share: 4 tiles of each wave (few) or of the block
+  const int64_t least = f.few ? 4 * kFewWaves * (s.dim <= 64 ? kFewKeys<64> : kFewKeys<128>) : 4 * kKeys;
+  const int64_t want = blocks == 0 ? 1 : (f.few ? 16 : 2) * int64_t(cus) / blocks;
+  f.splits = int(std::max<int64_t>(1, std::min<int64_t>({want, keys / least, kWave})));
+  return f;
 }
 
 template <int D>
-hipError_t launch_fwd(FwdArgs f, int dev, hipStream_t st) {
-  static std::atomic<uint64_t> done{0};
+hipError_t launch_fwd(FwdArgs f, bool few, int dev, hipStream_t st) {
+  static std::atomic<uint64_t> done{0}, done_few{0};
   constexpr int kBytes = 4 * kKeys * D * 2;
-  const hipError_t e = allow_lds(reinterpret_cast<const void*>(attention_fwd_kernel<D>), kBytes, dev, done);
+  hipError_t e = few ? allow_lds(reinterpret_cast<const void*>(attention_few_kernel<D>), kFewLds<D>, dev, done_few)
+                     : allow_lds(reinterpret_cast<const void*>(attention_fwd_kernel<D>), kBytes, dev, done);
   if (e != hipSuccess) return e;
-  const int64_t blocks = tiles_of(f.s.q, f.s.batch, f.s.fill, f.s.group, 128) * f.s.kv_heads * f.splits;
-  return in_parts(blocks, most_blocks(256), [&](int64_t first, int64_t count) {
+  const int threads = few ? kFewWaves * 64 : 256;
+  const int64_t blocks = tiles_of(f.s.q, f.s.batch, f.s.fill, f.s.group, few ? 32 : 128) * f.s.kv_heads * f.splits;
+  return in_parts(blocks, most_blocks(threads), [&](int64_t first, int64_t count) {
     FwdArgs g = f;
     g.first = first;
-    attention_fwd_kernel<D><<<uint32_t(count), 256, kBytes, st>>>(g);
+    if (few) attention_few_kernel<D><<<uint32_t(count), threads, kFewLds<D>, st>>>(g);
+    else attention_fwd_kernel<D><<<uint32_t(count), threads, kBytes, st>>>(g);
   });
 }
 
@@ -254,7 +476,7 @@ int cus_or_default(int& dev) {
 
 size_t attention_fwd_workspace(const AttentionPlan& a) {
   int dev = 0;
-  const int splits = attn::key_shares(a, cus_or_default(dev));
+  const int splits = attn::fwd_form(a, cus_or_default(dev)).splits;
   return splits > 1 ? size_t(splits) * size_t(a.q_rows) * size_t(a.heads) * size_t(a.dim + 2) * 4 : 0;
 }
 
@@ -270,14 +492,15 @@ hipError_t launch_attention_fwd(const AttentionPlan& a, const HeadsView& q, cons
   f.v = attn::heads_of(v);
   f.o = attn::heads_of(o);
   f.lse = lse;
-  f.splits = attn::key_shares(a, cus);
+  const attn::FwdForm form = attn::fwd_form(a, cus);
+  f.splits = form.splits;
   f.part = static_cast<float*>(workspace);
   f.stats = f.part + int64_t(f.splits) * a.q_rows * a.heads * a.dim;
-  e = a.dim <= 64 ? attn::launch_fwd<64>(f, dev, st) : attn::launch_fwd<128>(f, dev, st);
+  e = a.dim <= 64 ? attn::launch_fwd<64>(f, form.few, dev, st) : attn::launch_fwd<128>(f, form.few, dev, st);
   if (e != hipSuccess || f.splits == 1) return e;
-  return in_parts((a.q_rows * a.heads + 3) / 4, most_blocks(256), [&](int64_t first, int64_t count) {
+  return in_parts(a.q_rows * a.heads, most_blocks(256), [&](int64_t first, int64_t count) {
     attn::FwdArgs g = f;
-    g.first = first * 4;
+    g.first = first;
     attn::attention_join_kernel<<<uint32_t(count), 256, 0, st>>>(g);
   });
 }
