@@ -8,6 +8,13 @@
 // Norm (per head, D columns): rstd = 1 / sqrt(D^-1 |x|^2 + eps), z = x rstd, y = turn(gain z). The turn keeps lengths and
 // products, so without a gain the backward needs no z: with y as it was kept, dx = turn_back(rstd (dy - y D^-1 (y . dy))). With a
 // gain g = turn_back(dy), dz = gain g, dx = rstd (dz - z D^-1 (z . dz)), dgain = sum of g z over the rows, from x.
+//
+// What bounds it: memory. A wave takes heads of one token, 4 (backward 2) of each lane's at a time whose loads run while the
+// angles are formed: each pair's by one lane, handed round through LDS (formed by every lane for its own columns they cost
+// 7 us on each pass over the token, 8 us more in all). Loads and stores are non-temporal (52 us without). 8192 tokens of 32 + 32
+// heads of 128, bf16: turned 43 to 46 us (5.9 to 6.2 TB/s), norm and turn 48, its backward 64 (6.3); 2, 4 and 8 waves to a token
+// instead of one 47 -> 45, 48 -> 48, 67 -> 64. Odd widths (a half that is no multiple of 16 bytes) go element by element: 1531
+// tokens of 12 heads of 72, fp32, with gains 12 us, backward 13 and 4 for the sum of the gains' gradients.
 #include "lmbp_device.hpp"
 #include "lmbp_launch.hpp"
 
@@ -17,7 +24,8 @@
 namespace lmbp {
 namespace rope {
 
-enum { kTurn = 0, kNorm = 1, kNormBack = 2, kNormBackGain = 3 };
+enum { kTurn = 0, kNorm = 1, kNormBack = 2, kNormGain = 3, kNormBackGain = 4 };
+enum { kSingle = 0, kHalves = 1, kPairs = 2 };   // element by element; 16-byte pieces of pairs half apart, side by side
 
 // Queries or keys: one tensor's heads.
 struct Side {
@@ -27,7 +35,7 @@ struct Side {
   float* rstd;        // [tokens][heads]; written by the forward
   const void* gain;   // [dim] or null
   int64_t x_row, x_head, y_row, y_head, kept_row, kept_head;
-  int heads, shares;  // shares: waves that take a token's heads in turn
+  int heads, steps;   // steps: of `rows` heads
 };
 
 struct Args {
@@ -37,6 +45,7 @@ struct Args {
   float* part;        // kNormBackGain: [2][blocks][dim]
   int64_t first;      // token of this launch's first block
   int dim, pairs, lanes, rows;   // lanes to a head (a power of two), heads to a wave at a time
+  int shares;         // waves that take a token's heads in turn
   float eps, sign;
   uint8_t wide, interleaved, gain_bf16;
   uint8_t axis[kRopePairs];
@@ -44,16 +53,18 @@ struct Args {
 };
 
 // This lane's place in a head: E pairs, two pieces of E columns or 2 E single columns.
-template <class IO, bool VEC>
+template <class IO, int FORM>
 struct Place {
   static constexpr int E = IO::kPerVec;
+  static constexpr bool VEC = FORM != kSingle;
   int pair, a, b;   // first pair; VEC: where the pieces start
   int dim, half;
-  bool inside, interleaved;
+  bool inside;
+  bool interleaved;   // known when compiled but for kSingle
   __device__ inline Place(const Args& f, int at) {
     dim = f.dim;
     half = f.pairs;
-    interleaved = f.interleaved;
+    interleaved = FORM == kSingle ? f.interleaved : FORM == kPairs;
     pair = at * E;
     inside = 2 * pair < dim;
     if (interleaved) {
@@ -88,16 +99,33 @@ struct Place {
     asm volatile("" : "+v"(m));
     return __int_as_float(__float_as_int(v) & m);
   }
-  __device__ inline void load(const void* row, float (&x)[E], float (&y)[E]) const {
+  // A head's values of this lane as they come from memory, so that several heads' loads run before the first is used.
+  struct Raw {
+    u32x4 u, v;             // VEC
+    float x[VEC ? 1 : E], y[VEC ? 1 : E];
+  };
+  __device__ inline void load(const void* row, Raw& r) const {
     if constexpr (VEC) {
-      u32x4 u = {0u, 0u, 0u, 0u}, v = u;
+      r.u = r.v = u32x4{0u, 0u, 0u, 0u};
       if (inside) {
-        u = *reinterpret_cast<const u32x4*>(static_cast<const char*>(row) + a * IO::kBytes);
-        v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(row) + b * IO::kBytes);
+        r.u = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const char*>(row) + a * IO::kBytes));
+        r.v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const char*>(row) + b * IO::kBytes));
       }
+    } else {
+      const Place p = again();
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = p.first(e), j = p.second(e);
+        r.x[e] = within(IO::load1(row, i < dim ? i : 0), i);
+        r.y[e] = within(IO::load1(row, j < dim ? j : 0), j);
+      }
+    }
+  }
+  __device__ inline void unpack(const Raw& r, float (&x)[E], float (&y)[E]) const {
+    if constexpr (VEC) {
       float s[E], t[E];
-      IO::unpack(u, s);
-      IO::unpack(v, t);
+      IO::unpack(r.u, s);
+      IO::unpack(r.v, t);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float left = e < E / 2 ? s[2 * e % E] : t[2 * e % E], right = e < E / 2 ? s[(2 * e + 1) % E] : t[(2 * e + 1) % E];
@@ -105,12 +133,10 @@ struct Place {
         y[e] = interleaved ? right : t[e];
       }
     } else {
-      const Place p = again();
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int i = p.first(e), j = p.second(e);
-        x[e] = within(IO::load1(row, i < dim ? i : 0), i);
-        y[e] = within(IO::load1(row, j < dim ? j : 0), j);
+        x[e] = r.x[e];
+        y[e] = r.y[e];
       }
     }
   }
@@ -123,8 +149,8 @@ struct Place {
         t[e] = interleaved ? (e % 2 ? y[(E + e) / 2] : x[(E + e) / 2]) : y[e];
       }
       if (inside) {
-        *reinterpret_cast<u32x4*>(static_cast<char*>(row) + a * IO::kBytes) = IO::pack(s);
-        *reinterpret_cast<u32x4*>(static_cast<char*>(row) + b * IO::kBytes) = IO::pack(t);
+        __builtin_nontemporal_store(IO::pack(s), reinterpret_cast<u32x4*>(static_cast<char*>(row) + a * IO::kBytes));
+        __builtin_nontemporal_store(IO::pack(t), reinterpret_cast<u32x4*>(static_cast<char*>(row) + b * IO::kBytes));
       }
     } else {
       const Place p = again();
@@ -164,19 +190,31 @@ __device__ inline void cos_sin(uint64_t turns, float& c, float& s) {
   s = quarter >= 2 ? -y : y;
 }
 
-template <class IO, bool VEC>
-__device__ inline void angles(const Args& f, const Place<IO, VEC>& at, int64_t token, float (&c)[IO::kPerVec], float (&s)[IO::kPerVec]) {
-#pragma unroll
-  for (int e = 0; e < IO::kPerVec; ++e) {
-    c[e] = 1.0f;
-    s[e] = 0.0f;
-    const int p = at.pair + e;
+// Cosines and sines of a token's pairs: each formed once, by one lane of the wave, and handed to the lanes that hold the pair's
+// columns through LDS of the wave's own (`table`: kRopePairs cosines, then sines; 1 and 0 behind the pairs).
+template <class IO, int FORM>
+__device__ inline void angles(const Args& f, const Place<IO, FORM>& at, int64_t token, float* table, float (&c)[IO::kPerVec],
+                              float (&s)[IO::kPerVec]) {
+  constexpr int E = IO::kPerVec;
+  const int held = f.lanes * E;   // pairs, those behind the row's end included
+  __builtin_amdgcn_wave_barrier();   // the last token's have been read (a wave's LDS operations run in order)
+  for (int p = threadIdx.x & (kWave - 1); p < held; p += kWave) {
+    float co = 1.0f, si = 0.0f;
     if (p < f.pairs) {
       const int64_t i = int64_t(f.axis[p]) * f.axis_stride + token;
       const int64_t pos = f.wide ? static_cast<const int64_t*>(f.positions)[i] : static_cast<const int32_t*>(f.positions)[i];
-      cos_sin(uint64_t(pos) * f.freq[p], c[e], s[e]);
-      s[e] *= f.sign;
+      cos_sin(uint64_t(pos) * f.freq[p], co, si);
     }
+    table[p] = co;
+    table[kRopePairs + p] = si * f.sign;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int e = 0; e < E; e += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(table + at.pair + e), y = *reinterpret_cast<const float4*>(table + kRopePairs + at.pair + e);
+    c[e] = x.x, c[e + 1] = x.y, c[e + 2] = x.z, c[e + 3] = x.w;
+    s[e] = y.x, s[e + 1] = y.y, s[e + 2] = y.z, s[e + 3] = y.w;
   }
 }
 
@@ -185,103 +223,135 @@ __device__ inline float sum_lanes(float v, int lanes) {
   return v;
 }
 
-// Blocks of 4 waves, queries (blockIdx.y 0) or keys; `shares` waves take a token's heads in turn, `rows` heads at a time.
-template <class IO, int MODE, bool VEC>
+// Blocks of 4 waves; `shares` waves take a token's heads in turn, `rows` of the queries' or of the keys' at a time, with the
+// token's angles formed once. With gains, which a wave holds over all its tokens (and sums
+// their gradients), blocks are the queries' or the keys'.
+template <class IO, int MODE, int FORM>
 __global__ __launch_bounds__(256) void rope_kernel(Args f) {
   constexpr int E = IO::kPerVec;
+  constexpr bool VEC = FORM != kSingle;
   const int lane = threadIdx.x & (kWave - 1);
-  const Side d = blockIdx.y == 0 ? f.side[0] : f.side[1];
-  const Place<IO, VEC> at(f, lane & (f.lanes - 1));
+  const Place<IO, FORM> at(f, lane & (f.lanes - 1));
   const int in_step = lane / f.lanes;
+  __shared__ __attribute__((aligned(16))) float tables[4][2 * kRopePairs];
+  constexpr bool kGain = MODE == kNormGain || MODE == kNormBackGain, kForward = MODE == kTurn || MODE == kNorm || MODE == kNormGain;
   float ga[E], gb[E], sum_a[E], sum_b[E];
-  bool gains = false;
-  if constexpr (MODE == kNorm || MODE == kNormBackGain) {
-    gains = d.gain != nullptr;
+  if constexpr (kGain) {
+    at.load_gain(f.side[blockIdx.y].gain, f.gain_bf16, ga, gb);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      ga[e] = gb[e] = 1.0f;
-      sum_a[e] = sum_b[e] = 0.0f;
-    }
-    if (gains) at.load_gain(d.gain, f.gain_bf16, ga, gb);
+    for (int e = 0; e < E; ++e) sum_a[e] = sum_b[e] = 0.0f;
   }
-  const int64_t units = (f.tokens - f.first) * d.shares;
+  const int64_t units = (f.tokens - f.first) * f.shares;
   for (int64_t u = int64_t(blockIdx.x) * 4 + wave_in_block(); u < units; u += int64_t(gridDim.x) * 4) {
-    const int64_t token = f.first + u / d.shares;
+    const int64_t token = f.first + u / f.shares;
+    int start = int(u % f.shares);   // this wave's first step of the side
     float c[E], s[E];
-    angles(f, at, token, c, s);
-    for (int head = int(u % d.shares) * f.rows + in_step; head - in_step < d.heads; head += d.shares * f.rows) {
-      const bool real = head < d.heads;
-      const int h = real ? head : 0;
-      const char* x = static_cast<const char*>(d.x) + (token * d.x_row + h * d.x_head) * IO::kBytes;
-      char* y = static_cast<char*>(d.y) + (token * d.y_row + h * d.y_head) * IO::kBytes;
-      float a[E], b[E];
-      at.load(x, a, b);
-      if constexpr (MODE == kTurn) {
+    bool ready = false;
+#pragma unroll 1
+    for (int side = kGain ? int(blockIdx.y) : 0; side < (kGain ? int(blockIdx.y) + 1 : 2); ++side) {
+      const Side d = side == 0 ? f.side[0] : f.side[1];
+      // kBatch heads of each lane at a time: their loads run while the angles are formed
+      constexpr int kBatch = !VEC ? 1 : kForward ? 4 : 2;
+      const int stride = f.shares * f.rows;
+      int group = start * f.rows;
+      for (; group < d.heads; group += kBatch * stride) {
+        typename Place<IO, FORM>::Raw rx[kBatch], rk[kBatch];
+        float rs[kBatch];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float p = a[e], q = b[e];
-          a[e] = __builtin_fmaf(p, c[e], -q * s[e]);
-          b[e] = __builtin_fmaf(p, s[e], q * c[e]);
-        }
-      } else if constexpr (MODE == kNorm) {
-        float sq = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) sq = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], sq));
-        float mean = sum_lanes(sq, f.lanes) / float(f.dim) + f.eps, unit_ = 1.0f;
-        // squares that fp32 does not hold are added up again as (x unit)^2
-        const bool large = !(mean < 3.0e38f), tiny = mean < 0x1p-90f;
-        if (__any(large || tiny)) {
-          unit_ = large ? 0x1p-96f : tiny ? 0x1p60f : 1.0f;
-          sq = 0.0f;
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            sq = __builtin_fmaf(a[e] * unit_, a[e] * unit_, __builtin_fmaf(b[e] * unit_, b[e] * unit_, sq));
-          mean = sum_lanes(sq, f.lanes) / float(f.dim) + f.eps * unit_ * unit_;
-        }
-        const float r = rsqrtf(mean);
-        if (real && (lane & (f.lanes - 1)) == 0) d.rstd[token * d.heads + head] = r * unit_;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float p = a[e] * unit_ * r * ga[e], q = b[e] * unit_ * r * gb[e];
-          a[e] = __builtin_fmaf(p, c[e], -q * s[e]);
-          b[e] = __builtin_fmaf(p, s[e], q * c[e]);
-        }
-      } else {
-        float p[E], q[E];
-        at.load(static_cast<const char*>(d.kept) + (token * d.kept_row + h * d.kept_head) * IO::kBytes, p, q);
-        const float r = d.rstd[token * d.heads + h];
-        float along = 0.0f;
-        if constexpr (MODE == kNormBack) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) along = __builtin_fmaf(a[e], p[e], __builtin_fmaf(b[e], q[e], along));
-          along = sum_lanes(along, f.lanes) / float(f.dim);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float v = r * __builtin_fmaf(-p[e], along, a[e]), w = r * __builtin_fmaf(-q[e], along, b[e]);
-            a[e] = __builtin_fmaf(v, c[e], -w * s[e]);
-            b[e] = __builtin_fmaf(v, s[e], w * c[e]);
+        for (int j = 0; j < kBatch; ++j) {
+          if (group + j * stride >= d.heads) break;
+          const int head = group + j * stride + in_step, h = head < d.heads ? head : 0;
+          at.load(static_cast<const char*>(d.x) + (token * d.x_row + h * d.x_head) * IO::kBytes, rx[j]);
+          if constexpr (!kForward) {
+            if constexpr (!VEC) __builtin_amdgcn_sched_barrier(0);   // masks of one load at a time
+            at.load(static_cast<const char*>(d.kept) + (token * d.kept_row + h * d.kept_head) * IO::kBytes, rk[j]);
+            rs[j] = d.rstd[token * d.heads + h];
           }
-        } else {
+        }
+        if (!ready) angles(f, at, token, tables[wave_in_block()], c, s);
+        ready = true;
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float v = __builtin_fmaf(a[e], c[e], -b[e] * s[e]), w = __builtin_fmaf(a[e], s[e], b[e] * c[e]);
-            p[e] *= r;
-            q[e] *= r;
-            sum_a[e] = __builtin_fmaf(real ? v : 0.0f, real ? p[e] : 0.0f, sum_a[e]);
-            sum_b[e] = __builtin_fmaf(real ? w : 0.0f, real ? q[e] : 0.0f, sum_b[e]);
-            a[e] = v * ga[e];
-            b[e] = w * gb[e];
-            along = __builtin_fmaf(a[e], p[e], __builtin_fmaf(b[e], q[e], along));
-          }
-          along = sum_lanes(along, f.lanes) / float(f.dim);
+        for (int j = 0; j < kBatch; ++j) {
+          if (group + j * stride >= d.heads) break;
+          const int head = group + j * stride + in_step;
+          const bool real = head < d.heads;
+          const int h = real ? head : 0;
+          char* y = static_cast<char*>(d.y) + (token * d.y_row + h * d.y_head) * IO::kBytes;
+          float a[E], b[E];
+          at.unpack(rx[j], a, b);
+          if constexpr (MODE == kTurn) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            a[e] = r * __builtin_fmaf(-p[e], along, a[e]);
-            b[e] = r * __builtin_fmaf(-q[e], along, b[e]);
+            for (int e = 0; e < E; ++e) {
+              const float p = a[e], q = b[e];
+              a[e] = __builtin_fmaf(p, c[e], -q * s[e]);
+              b[e] = __builtin_fmaf(p, s[e], q * c[e]);
+            }
+          } else if constexpr (kForward) {
+            float sq = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) sq = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], sq));
+            float mean = sum_lanes(sq, f.lanes) / float(f.dim) + f.eps, unit_ = 1.0f;
+            // squares that fp32 does not hold are added up again as (x unit)^2
+            const bool large = !(mean < 3.0e38f), tiny = mean < 0x1p-90f;
+            if (__any(large || tiny)) {
+              unit_ = large ? 0x1p-96f : tiny ? 0x1p60f : 1.0f;
+              sq = 0.0f;
+#pragma unroll
+              for (int e = 0; e < E; ++e)
+                sq = __builtin_fmaf(a[e] * unit_, a[e] * unit_, __builtin_fmaf(b[e] * unit_, b[e] * unit_, sq));
+              mean = sum_lanes(sq, f.lanes) / float(f.dim) + f.eps * unit_ * unit_;
+            }
+            const float r = rsqrtf(mean);
+            if (real && (lane & (f.lanes - 1)) == 0) d.rstd[token * d.heads + head] = r * unit_;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              float p = a[e] * unit_ * r, q = b[e] * unit_ * r;
+              if constexpr (kGain) {
+                p *= ga[e];
+                q *= gb[e];
+              }
+              a[e] = __builtin_fmaf(p, c[e], -q * s[e]);
+              b[e] = __builtin_fmaf(p, s[e], q * c[e]);
+            }
+          } else {
+            float p[E], q[E];
+            at.unpack(rk[j], p, q);
+            const float r = rs[j];
+            float along = 0.0f;
+            if constexpr (MODE == kNormBack) {
+#pragma unroll
+              for (int e = 0; e < E; ++e) along = __builtin_fmaf(a[e], p[e], __builtin_fmaf(b[e], q[e], along));
+              along = sum_lanes(along, f.lanes) / float(f.dim);
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                const float v = r * __builtin_fmaf(-p[e], along, a[e]), w = r * __builtin_fmaf(-q[e], along, b[e]);
+                a[e] = __builtin_fmaf(v, c[e], -w * s[e]);
+                b[e] = __builtin_fmaf(v, s[e], w * c[e]);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                const float v = __builtin_fmaf(a[e], c[e], -b[e] * s[e]), w = __builtin_fmaf(a[e], s[e], b[e] * c[e]);
+                p[e] *= r;
+                q[e] *= r;
+                sum_a[e] = __builtin_fmaf(real ? v : 0.0f, real ? p[e] : 0.0f, sum_a[e]);
+                sum_b[e] = __builtin_fmaf(real ? w : 0.0f, real ? q[e] : 0.0f, sum_b[e]);
+                a[e] = v * ga[e];
+                b[e] = w * gb[e];
+                along = __builtin_fmaf(a[e], p[e], __builtin_fmaf(b[e], q[e], along));
+              }
+              along = sum_lanes(along, f.lanes) / float(f.dim);
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                a[e] = r * __builtin_fmaf(-p[e], along, a[e]);
+                b[e] = r * __builtin_fmaf(-q[e], along, b[e]);
+              }
+            }
           }
+          if (real) at.store(y, a, b);
         }
       }
-      if (real) at.store(y, a, b);
+      start = (start + f.shares - d.steps % f.shares) % f.shares;
     }
   }
   if constexpr (MODE == kNormBackGain) {   // heads of a wave, waves of the block, in order
@@ -332,37 +402,39 @@ int lanes_of(int64_t dim, int per) {
 
 // How a launch is split: a token's heads over more waves while the device has room.
 template <class IO>
-void plan(rope::Args& f) {
+void plan(rope::Args& f, bool apart) {
   f.lanes = lanes_of(f.dim, IO::kPerVec);
   f.rows = kWave / f.lanes;
+  int steps = 0;   // that a token's waves share
   for (rope::Side& d : f.side) {
-    const int steps = (d.heads + f.rows - 1) / f.rows;
-    d.shares = 1;
-    while (d.shares < steps && f.tokens * d.shares < 4096) d.shares *= 2;
-    d.shares = std::max(1, std::min(d.shares, steps));
+    d.steps = (d.heads + f.rows - 1) / f.rows;
+    steps = apart ? std::max(steps, d.steps) : steps + d.steps;
   }
+  f.shares = 1;
+  while (f.shares < steps && f.tokens * f.shares < 32768) f.shares *= 2;
+  f.shares = std::min(f.shares, steps);
 }
-// Blocks for `tokens` tokens of the side that takes more of them.
-int64_t blocks_of(const rope::Args& f, int64_t tokens) { return (tokens * std::max(f.side[0].shares, f.side[1].shares) + 3) / 4; }
+int64_t blocks_of(const rope::Args& f, int64_t tokens) { return (tokens * f.shares + 3) / 4; }
 int gain_blocks(const rope::Args& f) { return int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, kGainBlocks)); }
 
 template <class IO, int MODE>
 hipError_t launch(const rope::Args& f, bool vec, hipStream_t s) {
-  if constexpr (MODE == rope::kNormBackGain) {
-    const dim3 grid(gain_blocks(f), 2);
-    if (vec) rope::rope_kernel<IO, MODE, true><<<grid, 256, 0, s>>>(f);
-    else rope::rope_kernel<IO, MODE, false><<<grid, 256, 0, s>>>(f);
+  auto go = [&](const rope::Args& g, dim3 grid) {
+    if (!vec) rope::rope_kernel<IO, MODE, rope::kSingle><<<grid, 256, 0, s>>>(g);
+    else if (g.interleaved) rope::rope_kernel<IO, MODE, rope::kPairs><<<grid, 256, 0, s>>>(g);
+    else rope::rope_kernel<IO, MODE, rope::kHalves><<<grid, 256, 0, s>>>(g);
+  };
+  if constexpr (MODE == rope::kNormBackGain || MODE == rope::kNormGain) {
+    const int blocks = MODE == rope::kNormGain ? int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, 4 * kGainBlocks)) : gain_blocks(f);
+    go(f, dim3(blocks, f.side[1].heads > 0 ? 2 : 1));
     return hipGetLastError();
   } else {
     // tokens to a launch; the kernel takes what lies from its first token on
-    const int64_t part = most_blocks(256) / std::max(f.side[0].shares, f.side[1].shares) * 4;
-    return in_parts(f.tokens, part, [&](int64_t first, int64_t count) {
+    return in_parts(f.tokens, most_blocks(256) / f.shares * 4, [&](int64_t first, int64_t count) {
       rope::Args g = f;
       g.first = first;
       g.tokens = first + count;
-      const dim3 grid(uint32_t(blocks_of(f, count)), f.side[1].heads > 0 ? 2 : 1);
-      if (vec) rope::rope_kernel<IO, MODE, true><<<grid, 256, 0, s>>>(g);
-      else rope::rope_kernel<IO, MODE, false><<<grid, 256, 0, s>>>(g);
+      go(g, dim3(uint32_t(blocks_of(f, count))));
     });
   }
 }
@@ -407,8 +479,9 @@ void side_of(rope::Side& d, const HeadsView& x, const HeadsView& y, const HeadsV
 
 template <int MODE>
 hipError_t launch_type(bool bf16, rope::Args& f, bool vec, hipStream_t s) {
-  if (bf16) plan<BF16>(f);
-  else plan<F32>(f);
+  constexpr bool kApart = MODE == rope::kNormBackGain || MODE == rope::kNormGain;   // queries and keys in blocks of their own
+  if (bf16) plan<BF16>(f, kApart);
+  else plan<F32>(f, kApart);
   return bf16 ? launch<BF16, MODE>(f, vec, s) : launch<F32, MODE>(f, vec, s);
 }
 
@@ -432,7 +505,7 @@ hipError_t launch_msrms_rope_fwd(bool bf16, const RopePlan& r, float eps, bool g
   f.eps = eps;
   f.gain_bf16 = gain_bf16;
   for (int i = 0; i < 2; ++i) side_of(f.side[i], x[i], y[i], HeadsView{}, rstd[i], gain[i], r.heads[i], bf16, vec);
-  return launch_type<rope::kNorm>(bf16, f, vec, s);
+  return gain[0] != nullptr ? launch_type<rope::kNormGain>(bf16, f, vec, s) : launch_type<rope::kNorm>(bf16, f, vec, s);
 }
 
 hipError_t launch_msrms_rope_bwd(bool bf16, const RopePlan& r, bool gain_bf16, const void* const (&gain)[2], const HeadsView (&dy)[2],
@@ -448,7 +521,7 @@ hipError_t launch_msrms_rope_bwd(bool bf16, const RopePlan& r, bool gain_bf16, c
   if (gain[0] == nullptr && gain[1] == nullptr) return launch_type<rope::kNormBack>(bf16, f, vec, s);
   const hipError_t e = launch_type<rope::kNormBackGain>(bf16, f, vec, s);
   if (e != hipSuccess) return e;
-  rope::rope_gain_kernel<<<dim3(uint32_t((r.dim + 3) / 4), 2), 256, 0, s>>>(f.part, gain_blocks(f), int(r.dim), gain_bf16, dgain[0], dgain[1]);
+  rope::rope_gain_kernel<<<dim3(uint32_t((r.dim + 3) / 4), r.heads[1] > 0 ? 2 : 1), 256, 0, s>>>(f.part, gain_blocks(f), int(r.dim), gain_bf16, dgain[0], dgain[1]);
   return hipGetLastError();
 }
 
