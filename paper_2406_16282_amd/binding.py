@@ -180,7 +180,8 @@ def _bind_fast(L):
                       "`python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning, stacklevel=3)
         return
     for name in (*ACT_OPS, *NORM_OPS, *GLU_OPS, "linear_act_fwd", "linear_swiglu_fwd", "msrms_linear_act_fwd",
-                 "msrms_linear_swiglu_fwd", *Q8_OPS, "lmbp_linear_q8_fwd_bytes", "lmbp_linear_q8_bwd_bytes"):
+                 "msrms_linear_swiglu_fwd", *Q8_OPS, "lmbp_linear_q8_fwd_bytes", "lmbp_linear_q8_bwd_bytes", *ROPE_OPS, *ATTENTION_OPS,
+                 "lmbp_msrms_rope_bwd_bytes", "lmbp_attention_fwd_bytes", "lmbp_attention_bwd_bytes"):
         _address[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
     _fast = module
 
@@ -1000,6 +1001,9 @@ class Rotation:
         self._axes = None if self.axes is None else (ctypes.c_int32 * len(self.axes))(*self.axes)
         self._freqs_at = ctypes.addressof(self._freqs)
         self._axes_at = None if self._axes is None else ctypes.addressof(self._axes)
+        # what a call of any sizes has of this rotation, for the native marshalling
+        self._plan = _Rope(0, 0, 0, 0, len(self.freqs), self._freqs_at, self._axes_at, None, self.n_axes, 1, self.interleaved)
+        self._plan_at = ctypes.addressof(self._plan)
 
     def __reduce__(self):   # copies and pickles are built anew, with arrays of their own
         return Rotation, (self.freqs, self.axes, self.interleaved)
@@ -1094,6 +1098,10 @@ def _rope_sides(q, k, positions, rotation):
 
 
 def _rope(op, q, k, positions, rotation, q_out, k_out, stream):
+    if _fast is not None and stream is None and type(rotation) is Rotation:
+        out = _fast.rope(_address[op], q, k, positions, rotation._plan_at, q_out, k_out)
+        if out is not None:
+            return _done(op, out)
     plan, lq, lk = _rope_sides(q, k, positions, rotation)
     dt = _dtype_code(q)
     yq = _heads_out(q_out, q, "q_out")
@@ -1133,6 +1141,10 @@ def _gains(q, k, q_gain, k_gain, dim):
 def msrms_rope_fwd(q, k, eps, positions, rotation, q_gain=None, k_gain=None, q_out=None, k_out=None, stream=None):
     """MS-RMSNorm of each head [..., heads, dim], times a gain per column (None: none), and the rotation in one
     pass: returns (q, k, rstd_q, rstd_k), None for a k of None."""
+    if _fast is not None and q_out is None and k_out is None and stream is None and type(rotation) is Rotation:
+        out = _fast.norm_rope_fwd(_address["msrms_rope_fwd"], q, k, eps, positions, rotation._plan_at, q_gain, k_gain)
+        if out is not None:
+            return _done("msrms_rope_fwd", out)
     plan, lq, lk = _rope_sides(q, k, positions, rotation)
     dt, dt_gain = _dtype_code(q), _gains(q, k, q_gain, k_gain, lq[2])
     yq = _heads_out(q_out, q, "q_out")
@@ -1152,6 +1164,11 @@ def msrms_rope_bwd(dq, dk, q, k, rstd_q, rstd_k, positions, rotation, q_gain=Non
                    stream=None):
     """Backward of msrms_rope_fwd. q and k: the forward's results without gains, its arguments with. Returns
     (dq, dk) or, with gains, (dq, dk, dq_gain, dk_gain); q_out and k_out may be given, dq and dk included."""
+    if _fast is not None and stream is None and type(rotation) is Rotation:
+        out = _fast.norm_rope_bwd(_address["msrms_rope_bwd"], _address["lmbp_msrms_rope_bwd_bytes"], dq, dk, q, k, rstd_q, rstd_k, positions,
+                                  rotation._plan_at, q_gain, k_gain, q_out, k_out)
+        if out is not None:
+            return _done("msrms_rope_bwd", out)
     plan, lq, lk = _rope_sides(dq, dk, positions, rotation)
     dt, dt_gain = _dtype_code(dq), _gains(dq, dk, q_gain, k_gain, lq[2])
     kept = []
@@ -1231,6 +1248,11 @@ def attention_fwd(q, k, v, causal=False, scale=None, q_starts=None, k_starts=Non
     only ``k_lens`` (int32) keys may be in use (a padded cache). Causal: the last query sees the last key. scale:
     dim ** -0.5 unless given.
     Rows of no sequence are zeros (lse -inf); in an o and lse given here they stay as they were."""
+    if _fast is not None and o is None and lse is None and stream is None:
+        out = _fast.attention_forward(_address["attention_fwd"], _address["lmbp_attention_fwd_bytes"], q, k, v, causal, scale, q_starts,
+                                      k_starts, k_lens)
+        if out is not None:
+            return _done("attention_fwd", out)
     fill = o is None and lse is None
     plan, lq, lk, lv = _attention(q, k, v, causal, scale, q_starts, k_starts, k_lens, fill)
     o = _heads_out(o, q, "o")
@@ -1251,6 +1273,11 @@ def attention_bwd(do, q, k, v, o, lse, causal=False, scale=None, q_starts=None, 
     """Backward of attention_fwd from its arguments and results: returns (dq, dk, dv). They may be given (parts of
     one tensor, too); rows of no sequence and keys not in use are zeros, and stay as they were where all
     three are given."""
+    if _fast is not None and stream is None:
+        out = _fast.attention_backward(_address["attention_bwd"], _address["lmbp_attention_bwd_bytes"], do, q, k, v, causal, scale, q_starts,
+                                       k_starts, k_lens, o, lse, dq, dk, dv)
+        if out is not None:
+            return _done("attention_bwd", out)
     fill = dq is None or dk is None or dv is None
     plan, lq, lk, lv = _attention(q, k, v, causal, scale, q_starts, k_starts, k_lens, fill)
     parts = []

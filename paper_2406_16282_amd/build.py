@@ -60,7 +60,7 @@ def fast_command(out):
     includes = [f for d in (*cpp_extension.include_paths(), sysconfig.get_paths()["include"]) for f in ("-isystem", d)]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     return [exe, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
-            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes,
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes, "-I", INCLUDE,
             os.path.join(CSRC, "fastcall.cpp"), "-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", out]
 
 

@@ -17,7 +17,10 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdint>
+
+#include "lmbp.h"
 
 namespace {
 
@@ -556,6 +559,286 @@ PyObject* linear_q8_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- tensors of heads
+
+// A tensor in GPU memory, of any strides.
+bool strided(PyObject* o, at::Tensor& t) {
+  if (!THPVariable_CheckExact(o)) return false;
+  t = THPVariable_Unpack(o);
+  return t.defined() && t.device().type() == c10::DeviceType::CUDA && t.layout() == c10::kStrided && t.has_storage();
+}
+// The same, or None: an undefined tensor.
+bool strided_or_none(PyObject* o, at::Tensor& t) { return o == Py_None || strided(o, t); }
+
+// [.., heads, dim] with leading dimensions one behind the other, not empty.
+struct Layout {
+  int64_t rows, heads, dim;
+  lmbp_heads view;
+};
+bool layout_of(const at::Tensor& t, Layout& l) {
+  const int64_t n = t.dim();
+  if (n < 3 || t.numel() == 0) return false;
+  l.heads = t.size(n - 2);
+  l.dim = t.size(n - 1);
+  if (l.dim > 1 && t.stride(n - 1) != 1) return false;
+  l.rows = 1;
+  int64_t row = t.stride(n - 3), size = 0;
+  for (int64_t i = n - 3; i >= 0; --i) {
+    l.rows *= t.size(i);
+    if (t.size(i) == 1) continue;
+    if (size == 0) {
+      row = t.stride(i);
+      size = t.size(i);
+    } else if (t.stride(i) != row * size) {
+      return false;
+    } else {
+      size *= t.size(i);
+    }
+  }
+  l.view.data = t.data_ptr();
+  l.view.row = l.rows > 1 ? row : l.heads * l.dim;
+  l.view.head = l.heads > 1 ? t.stride(n - 2) : l.dim;
+  return true;
+}
+at::Tensor dense_like(const at::Tensor& t) { return at::empty(t.sizes(), t.options()); }
+at::Tensor per_head(const at::Tensor& t) { return at::empty(t.sizes().slice(0, size_t(t.dim() - 1)), t.options().dtype(at::kFloat)); }
+at::Tensor bytes_on(size_t count, const at::Tensor& t) { return at::empty({int64_t(count)}, t.options().dtype(at::kByte)); }
+void* data_of(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// Queries and keys (k: or undefined) with positions and a rotation's address; false: anything but the common form.
+bool rope_plan(const at::Tensor& q, const at::Tensor& k, PyObject* positions, PyObject* rotation, lmbp_rope& r, Layout& lq, Layout& lk) {
+  if (dtype_of(q) < 0 || !on_current_device(q) || !layout_of(q, lq)) return false;
+  if (k.defined() && (!layout_of(k, lk) || k.scalar_type() != q.scalar_type() || k.device() != q.device() || lk.rows != lq.rows ||
+                      lk.dim != lq.dim))
+    return false;
+  r = *reinterpret_cast<const lmbp_rope*>(PyLong_AsVoidPtr(rotation));
+  r.tokens = lq.rows;
+  r.dim = lq.dim;
+  r.q_heads = lq.heads;
+  r.k_heads = k.defined() ? lk.heads : 0;
+  if (2 * r.pairs > r.dim) return false;
+  if (r.pairs > 0) {
+    at::Tensor p;
+    if (!plain(positions, p) || p.device() != q.device() || (p.scalar_type() != at::kLong && p.scalar_type() != at::kInt)) return false;
+    const int64_t axes = p.numel() == lq.rows && r.n_axes == 1 ? 1 : p.dim() > 1 ? p.size(0) : 1;
+    if (axes < r.n_axes || axes > 255 || p.numel() != axes * lq.rows) return false;
+    r.n_axes = int(axes);
+    r.wide = p.scalar_type() == at::kLong;
+    r.positions = p.data_ptr();
+  }
+  return true;
+}
+// An output like t: the one given (None: allocated).
+bool output(PyObject* o, const at::Tensor& like, at::Tensor& t, Layout& l) {
+  if (o == Py_None) {
+    t = dense_like(like);
+  } else if (!strided(o, t) || t.scalar_type() != like.scalar_type() || t.device() != like.device() || t.sizes() != like.sizes()) {
+    return false;
+  }
+  return layout_of(t, l);
+}
+
+// (function, q, k or None, positions, rotation, q_out or None, k_out or None) -> (q, k)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor q, k, yq, yk;
+  lmbp_rope r;
+  Layout lq, lk, oq, ok;
+  if (n != 7 || !strided(a[1], q) || !strided_or_none(a[2], k) || !rope_plan(q, k, a[3], a[4], r, lq, lk)) Py_RETURN_NONE;
+  if (!output(a[5], q, yq, oq) || (k.defined() && !output(a[6], k, yk, ok))) Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(q, s)) return nullptr;
+  const auto f = address<decltype(&rope_fwd)>(a[0]);
+  int status;
+  {
+    NoGil released;
+    const bool two = k.defined();
+    status = f(lmbp_dtype(dtype_of(q)), &r, &lq.view, two ? &lk.view : nullptr, &oq.view, two ? &ok.view : nullptr, s);
+  }
+  return result(status, yq, yk);
+  END_HANDLE_TH_ERRORS
+}
+
+// Gains: both undefined, or one for each tensor, of one type.
+bool gains_of(PyObject* oq, PyObject* ok, const at::Tensor& q, const at::Tensor& k, int64_t dim, at::Tensor& gq, at::Tensor& gk) {
+  if ((oq != Py_None && !plain(oq, gq)) || (ok != Py_None && !plain(ok, gk))) return false;
+  if (!gq.defined()) return !gk.defined();
+  if (gk.defined() != k.defined() || dtype_of(gq) < 0 || gq.numel() != dim || gq.device() != q.device()) return false;
+  return !gk.defined() || same(gk, gq);
+}
+
+// (function, q, k or None, eps, positions, rotation, q_gain, k_gain or None) -> (q, k, rstd_q, rstd_k)
+PyObject* norm_rope_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor q, k, gq, gk, yq, yk, rq, rk;
+  lmbp_rope r;
+  Layout lq, lk, oq, ok;
+  if (n != 8 || !strided(a[1], q) || !strided_or_none(a[2], k) || !PyFloat_CheckExact(a[3]) || !rope_plan(q, k, a[4], a[5], r, lq, lk) ||
+      !gains_of(a[6], a[7], q, k, lq.dim, gq, gk))
+    Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(q, s)) return nullptr;
+  const auto f = address<decltype(&msrms_rope_fwd)>(a[0]);
+  const bool two = k.defined();
+  int status;
+  {
+    NoGil released;
+    yq = dense_like(q);
+    rq = per_head(q);
+    layout_of(yq, oq);
+    if (two) {
+      yk = dense_like(k);
+      rk = per_head(k);
+      layout_of(yk, ok);
+    }
+    status = f(lmbp_dtype(dtype_of(q)), lmbp_dtype(gq.defined() ? dtype_of(gq) : kBf16), &r, float(PyFloat_AS_DOUBLE(a[3])), data_of(gq),
+               data_of(gk), &lq.view, two ? &lk.view : nullptr, &oq.view, two ? &ok.view : nullptr, rq.data_ptr<float>(),
+               static_cast<float*>(data_of(rk)), s);
+  }
+  return result(status, yq, yk, rq, rk);
+  END_HANDLE_TH_ERRORS
+}
+
+// (function, bytes, dq, dk or None, q, k, rstd_q, rstd_k, positions, rotation, q_gain, k_gain, q_out, k_out or None) ->
+// (dq, dk) or (dq, dk, dq_gain, dk_gain)
+PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor dq, dk, q, k, rq, rk, gq, gk, xq, xk, dgq, dgk, work;
+  lmbp_rope r;
+  Layout lq, lk, kq, kk, oq, ok;
+  if (n != 14 || !strided(a[2], dq) || !strided_or_none(a[3], dk) || !strided(a[4], q) || !strided_or_none(a[5], k) || !plain(a[6], rq) ||
+      !rope_plan(dq, dk, a[8], a[9], r, lq, lk) || !gains_of(a[10], a[11], dq, dk, lq.dim, gq, gk))
+    Py_RETURN_NONE;
+  const bool two = dk.defined();
+  if (k.defined() != two || q.scalar_type() != dq.scalar_type() || q.device() != dq.device() || q.sizes() != dq.sizes() || !layout_of(q, kq) ||
+      rq.device() != dq.device() || rq.scalar_type() != at::kFloat || rq.numel() != lq.rows * lq.heads)
+    Py_RETURN_NONE;
+  if (two && (k.scalar_type() != dq.scalar_type() || k.device() != dq.device() || k.sizes() != dk.sizes() || !layout_of(k, kk) ||
+              !plain(a[7], rk) || rk.device() != dq.device() || rk.scalar_type() != at::kFloat || rk.numel() != lk.rows * lk.heads))
+    Py_RETURN_NONE;
+  if (!output(a[12], dq, xq, oq) || (two && !output(a[13], dk, xk, ok))) Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(dq, s)) return nullptr;
+  const auto f = address<decltype(&msrms_rope_bwd)>(a[0]);
+  const auto bytes = address<decltype(&lmbp_msrms_rope_bwd_bytes)>(a[1]);
+  int status;
+  {
+    NoGil released;
+    size_t need = 0;
+    if (gq.defined()) {
+      need = bytes(lq.dim);
+      work = bytes_on(need, dq);
+      dgq = at::empty_like(gq);
+      if (two) dgk = at::empty_like(gk);
+    }
+    status = f(lmbp_dtype(dtype_of(dq)), lmbp_dtype(gq.defined() ? dtype_of(gq) : kBf16), &r, data_of(gq), data_of(gk), &lq.view,
+               two ? &lk.view : nullptr, &kq.view, two ? &kk.view : nullptr, rq.data_ptr<float>(), static_cast<const float*>(data_of(rk)),
+               &oq.view, two ? &ok.view : nullptr, data_of(dgq), data_of(dgk), data_of(work), int64_t(need), s);
+  }
+  return gq.defined() ? result(status, xq, xk, dgq, dgk) : result(status, xq, xk);
+  END_HANDLE_TH_ERRORS
+}
+
+// int32 numbers on q's device, or None.
+bool numbers(PyObject* o, const at::Tensor& q, int64_t count, const int32_t*& p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  at::Tensor t;
+  if (!plain(o, t) || t.scalar_type() != at::kInt || t.device() != q.device() || t.numel() != count) return false;
+  p = t.data_ptr<int32_t>();
+  return true;
+}
+// Sequences of q or k; 0: not the common form.
+int64_t sequences(const at::Tensor& t, PyObject* starts) {
+  if (starts != Py_None) {
+    at::Tensor s;
+    return plain(starts, s) ? s.numel() - 1 : 0;
+  }
+  return t.dim() == 4 ? t.size(0) : t.dim() == 3 ? 1 : 0;
+}
+// a: q, k, v, causal, scale or None, q_starts, k_starts, k_lens.
+bool attention_plan(PyObject* const* a, lmbp_attention& p, at::Tensor& q, at::Tensor& k, at::Tensor& v, Layout& lq, Layout& lk, Layout& lv) {
+  if (!strided(a[0], q) || !strided(a[1], k) || !strided(a[2], v)) return false;
+  for (const at::Tensor* t : {&q, &k, &v})
+    if (t->scalar_type() != at::kBFloat16 || t->device() != q.device()) return false;
+  if (!on_current_device(q) || !layout_of(q, lq) || !layout_of(k, lk) || !layout_of(v, lv) || k.sizes() != v.sizes() || lk.dim != lq.dim ||
+      lq.heads % lk.heads != 0)
+    return false;
+  PyObject* k_starts = a[6];
+  if (a[5] != Py_None && k_starts == Py_None && a[7] == Py_None && k.sizes().slice(0, size_t(k.dim() - 2)) == q.sizes().slice(0, size_t(q.dim() - 2)))
+    k_starts = a[5];
+  p.batch = sequences(q, a[5]);
+  if (p.batch < 1 || sequences(k, k_starts) != p.batch) return false;
+  if (!numbers(a[5], q, p.batch + 1, p.q_starts) || !numbers(k_starts, q, p.batch + 1, p.k_starts) || !numbers(a[7], q, p.batch, p.k_lens))
+    return false;
+  p.heads = lq.heads;
+  p.kv_heads = lk.heads;
+  p.dim = lq.dim;
+  p.q_rows = lq.rows;
+  p.k_rows = lk.rows;
+  p.causal = a[3] == Py_True;
+  if (a[3] != Py_True && a[3] != Py_False) return false;
+  if (a[4] == Py_None) p.scale = float(1.0 / std::sqrt(double(lq.dim)));
+  else if (PyFloat_CheckExact(a[4])) p.scale = float(PyFloat_AS_DOUBLE(a[4]));
+  else return false;
+  return true;
+}
+
+// (function, bytes, q, k, v, causal, scale, q_starts, k_starts, k_lens) -> (o, lse)
+PyObject* attention_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor q, k, v, o, lse, work;
+  lmbp_attention p;
+  Layout lq, lk, lv, lo;
+  if (n != 10 || !attention_plan(a + 2, p, q, k, v, lq, lk, lv)) Py_RETURN_NONE;
+  p.fill = 1;
+  void* s;
+  if (!stream_of(q, s)) return nullptr;
+  const auto f = address<decltype(&attention_fwd)>(a[0]);
+  const auto bytes = address<decltype(&lmbp_attention_fwd_bytes)>(a[1]);
+  int status;
+  {
+    NoGil released;
+    o = dense_like(q);
+    lse = per_head(q);
+    layout_of(o, lo);
+    const size_t need = bytes(&p);
+    if (need > 0) work = bytes_on(need, q);
+    status = f(LMBP_BF16, &p, &lq.view, &lk.view, &lv.view, &lo.view, lse.data_ptr<float>(), data_of(work), int64_t(need), s);
+  }
+  return result(status, o, lse);
+  END_HANDLE_TH_ERRORS
+}
+
+// (function, bytes, do, q, k, v, causal, scale, q_starts, k_starts, k_lens, o, lse, dq, dk, dv or None) -> (dq, dk, dv)
+PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  at::Tensor d, q, k, v, o, lse, dq, dk, dv, work;
+  lmbp_attention p;
+  Layout ld, lq, lk, lv, lo, oq, ok, ov;
+  if (n != 16 || !strided(a[2], d) || !attention_plan(a + 3, p, q, k, v, lq, lk, lv) || !strided(a[11], o) || !plain(a[12], lse)) Py_RETURN_NONE;
+  for (const at::Tensor* t : {&d, &o})
+    if (t->scalar_type() != at::kBFloat16 || t->device() != q.device() || t->sizes() != q.sizes()) Py_RETURN_NONE;
+  if (!layout_of(d, ld) || !layout_of(o, lo) || lse.scalar_type() != at::kFloat || lse.device() != q.device() || lse.numel() != lq.rows * lq.heads)
+    Py_RETURN_NONE;
+  p.fill = a[13] == Py_None || a[14] == Py_None || a[15] == Py_None;
+  if (!output(a[13], q, dq, oq) || !output(a[14], k, dk, ok) || !output(a[15], v, dv, ov)) Py_RETURN_NONE;
+  void* s;
+  if (!stream_of(q, s)) return nullptr;
+  const auto f = address<decltype(&attention_bwd)>(a[0]);
+  const auto bytes = address<decltype(&lmbp_attention_bwd_bytes)>(a[1]);
+  int status;
+  {
+    NoGil released;
+    const size_t need = bytes(&p);
+    if (need > 0) work = bytes_on(need, q);
+    status = f(LMBP_BF16, &p, &ld.view, &lq.view, &lk.view, &lv.view, &lo.view, lse.data_ptr<float>(), &oq.view, &ok.view, &ov.view,
+               data_of(work), int64_t(need), s);
+  }
+  return result(status, dq, dk, dv);
+  END_HANDLE_TH_ERRORS
+}
+
 // (torch's raw-stream accessor)
 PyObject* bind(PyObject*, PyObject* accessor) {
   Py_INCREF(accessor);
@@ -569,7 +852,8 @@ PyMethodDef kMethods[] = {LMBP_FAST(act_fwd), LMBP_FAST(act_bwd), LMBP_FAST(glu_
                           LMBP_FAST(linear_swiglu_fwd), LMBP_FAST(norm_linear_act_fwd),
                           LMBP_FAST(norm_linear_swiglu_fwd), LMBP_FAST(q8_rows), LMBP_FAST(q8_values),
                           LMBP_FAST(msrms_q8_fwd), LMBP_FAST(msrms_q8_bwd), LMBP_FAST(linear_q8_fwd),
-                          LMBP_FAST(linear_q8_bwd), {"bind", bind, METH_O, nullptr},
+                          LMBP_FAST(linear_q8_bwd), LMBP_FAST(rope), LMBP_FAST(norm_rope_fwd), LMBP_FAST(norm_rope_bwd),
+                          LMBP_FAST(attention_forward), LMBP_FAST(attention_backward), {"bind", bind, METH_O, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
