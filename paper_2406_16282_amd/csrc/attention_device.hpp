@@ -144,6 +144,42 @@ struct Part {
   int k_slot;         // keys up to the next sequence
 };
 
+// The t-th tile of causal sequences of different lengths, those that see (or are seen by) most first: by their distance from
+// their sequence's lightest tile. 10 sequences of 1 to 2048 tokens, 8 key heads of 4 query heads, dim 128: the gradients of keys and
+// values 276 us, in the sequences' order 337, the forward pass 155 and 166. A wave's lanes hold a sequence each.
+template <bool QUERIES>
+__device__ inline bool heaviest_first(const Shape& s, int64_t t, int per, int times, int& b, Part& p) {
+  const Seqs& side = QUERIES ? s.q : s.k;
+  const int lane = threadIdx.x & (kWave - 1), all = s.batch + (s.fill ? 1 : 0);
+  int64_t first, len = 0;
+  if (lane < all) rows_of(side, s.batch, lane, first, len);
+  const int n = int((len * times + per - 1) / per);
+  // How many tiles are at a distance of at least `from`; the largest distance with more than t of them.
+  auto tiles_from = [&](int from) {
+    int count = 0;
+    for (int i = 0; i < all; ++i) {
+      const int over = __builtin_amdgcn_readlane(n, i) - from;
+      count += over > 0 ? over : 0;
+    }
+    return count;
+  };
+  const int64_t most = (side.rows * times + per - 1) / per;
+  int step = 1, low = 0, count = 0, at = 0;
+  while (int64_t(step) * kWave <= most) step *= kWave;
+  for (; step > 0; step /= kWave) {   // each lane tries a distance
+    count = tiles_from(low + lane * step);
+    at = __popcll(__ballot(count > t)) - 1;
+    if (at < 0) return false;
+    low += at * step;
+  }
+  const uint64_t there = __ballot(n > low);   // the sequences that have a tile at this distance, in order
+  const int rank = int(t) - uniform(__shfl(count, at, kWave)) + __popcll(there);
+  b = __builtin_ctzll(__ballot(n > low && __popcll(there & ((uint64_t(1) << lane) - 1)) == rank));
+  p.tiles = uniform(__shfl(n, b, kWave));
+  p.tile = p.tiles - 1 - low;
+  return true;
+}
+
 // The t-th tile of `per` rows, a row of the side counting `times` times. false: there is none.
 template <bool QUERIES>
 __device__ inline bool locate(const Shape& s, int64_t t, int per, int times, Part& p) {
@@ -155,6 +191,8 @@ __device__ inline bool locate(const Shape& s, int64_t t, int per, int times, Par
     b = int(t / tiles);
     p.tile = int(t - b * tiles);
     p.tiles = int(tiles);
+  } else if (s.causal && s.batch + (s.fill ? 1 : 0) <= kWave) {
+    if (!heaviest_first<QUERIES>(s, t, per, times, b, p)) return false;
   } else {
     const int lane = threadIdx.x & (kWave - 1);
     const int all = s.batch + (s.fill ? 1 : 0);

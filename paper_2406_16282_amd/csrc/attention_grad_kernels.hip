@@ -464,30 +464,39 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
   store_columns<D>(w.dv, used ? 1.0f : 0.0f, e.dv.p + (p.k0 + key) * e.dv.row + head * e.dv.head, real, e.s.dim);
 }
 
-// The shares' sums of dk and dv, in order: a block per tile of 128 keys and head.
+// The shares' sums of dk and dv, in order: a block per tile of 128 keys, head and quarter of its values, which it reads all at once.
+constexpr int kJoinParts = 4;
 __global__ __launch_bounds__(256) void attention_dkv_join_kernel(BwdArgs a) {
   const Shape& s = a.s;
-  const int64_t id = a.first + blockIdx.x;
-  const int head = int(id % s.kv_heads);
+  const int64_t id = a.first + blockIdx.x, rest = id / kJoinParts;
+  const int quarter = int(id % kJoinParts), head = int(rest % s.kv_heads);
   Part p;
-  if (!locate<false>(s, id / s.kv_heads, 128, 1, p)) return;
+  if (!locate<false>(s, rest / s.kv_heads, 128, 1, p)) return;
   const int shares = row_tiles(a, p, p.tile * 128).shares;
   if (shares == 1) return;
   const int64_t size = s.k.rows * s.kv_heads * s.dim;
-  const int pieces = s.dim / 4;
-  for (int i = threadIdx.x; i < 128 * pieces; i += 256) {
+  const int pieces = s.dim / 4, last = s.fill ? p.k_slot : p.k_len;
+  constexpr int kEach = 128 * (kAttentionDim / 4) / kJoinParts / 256;
+  f32x4 dk[kEach], dv[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = (quarter * kEach + j) * 256 + int(threadIdx.x);
     const int key = p.tile * 128 + i / pieces, col = i % pieces * 4;
-    if (key >= (s.fill ? p.k_slot : p.k_len)) break;
-    f32x4 dk = {0.0f, 0.0f, 0.0f, 0.0f}, dv = dk;
-    if (key < p.k_len) {
-      const float* from = a.part + ((p.k0 + key) * s.kv_heads + head) * s.dim + col;
-      for (int n = 0; n < shares; ++n) {
-        dk += *reinterpret_cast<const f32x4*>(from + 2 * n * size);
-        dv += *reinterpret_cast<const f32x4*>(from + (2 * n + 1) * size);
-      }
+    dk[j] = dv[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (i >= 128 * pieces || key >= p.k_len) continue;
+    const float* from = a.part + ((p.k0 + key) * s.kv_heads + head) * s.dim + col;
+    for (int n = 0; n < shares; ++n) {
+      dk[j] += *reinterpret_cast<const f32x4*>(from + 2 * n * size);
+      dv[j] += *reinterpret_cast<const f32x4*>(from + (2 * n + 1) * size);
     }
-    const u32x2 wk = {pack_bf16x2(dk[0] * s.scale, dk[1] * s.scale), pack_bf16x2(dk[2] * s.scale, dk[3] * s.scale)};
-    const u32x2 wv = {pack_bf16x2(dv[0], dv[1]), pack_bf16x2(dv[2], dv[3])};
+  }
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = (quarter * kEach + j) * 256 + int(threadIdx.x);
+    const int key = p.tile * 128 + i / pieces, col = i % pieces * 4;
+    if (i >= 128 * pieces || key >= last) continue;
+    const u32x2 wk = {pack_bf16x2(dk[j][0] * s.scale, dk[j][1] * s.scale), pack_bf16x2(dk[j][2] * s.scale, dk[j][3] * s.scale)};
+    const u32x2 wv = {pack_bf16x2(dv[j][0], dv[j][1]), pack_bf16x2(dv[j][2], dv[j][3])};
     *reinterpret_cast<u32x2*>(a.dk.p + (p.k0 + key) * a.dk.row + head * a.dk.head + col) = wk;
     *reinterpret_cast<u32x2*>(a.dv.p + (p.k0 + key) * a.dv.row + head * a.dv.head + col) = wv;
   }
@@ -528,7 +537,7 @@ hipError_t launch_bwd(const BwdArgs& f, int dev, hipStream_t st) {
     attention_dkv_kernel<D><<<uint32_t(count), 256, kBytesKv, st>>>(g);
   });
   if (e != hipSuccess || f.shares == 1) return e;
-  return in_parts(tiles, most_blocks(256), [&](int64_t first, int64_t count) {
+  return in_parts(tiles * kJoinParts, most_blocks(256), [&](int64_t first, int64_t count) {
     g.first = first;
     attention_dkv_join_kernel<<<uint32_t(count), 256, 0, st>>>(g);
   });
