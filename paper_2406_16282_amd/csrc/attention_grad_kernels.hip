@@ -238,7 +238,7 @@ struct Keys {
   // operands are read a few MFMAs ahead (left to itself the compiler reads each just before its MFMA and waits for
   // LDS every time), and half of the exponentials stand between the sums' MFMAs.
   __device__ inline void whole(const uint16_t* Q, const uint16_t* O, const uint16_t* V, int mine, const float* stats, Reader<D>& rd, float c) {
-    constexpr int kS = T::kSteps, kB = T::kBlocks, kAhead = 2;
+    constexpr int kS = T::kSteps, kB = T::kBlocks, kAhead = D <= 64 ? 1 : 2;
     bf16x8 a[kS], b[kS], d[kS], fo[2 * kB], fq[2 * kB];
     f32x4 st[8];
     f32x16 x = f32x16{}, y = f32x16{};
@@ -258,7 +258,7 @@ struct Keys {
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       if (s + kAhead < kS) scores(s + kAhead);
-      else st[s + kAhead - kS] = stats_of(stats, s + kAhead - kS);
+      if (s + 2 >= kS) st[s + 2 - kS] = stats_of(stats, s + 2 - kS);
       x = mfma(a[s], k[s], x);
       y = mfma(b[s], d[s], y);
       __builtin_amdgcn_sched_barrier(0);
@@ -347,12 +347,13 @@ __device__ inline RowTiles row_tiles(const BwdArgs& a, const Part& p, int key0) 
 // A block of 4 waves: 128 keys of one head, 32 to a wave, against all (or a share of) the packed rows that see them, from the last
 // row on: so blocks that run at once read the same rows at the same time.
 template <int D>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
+__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(BwdArgs a) {
   using T = Tile<D>;
   constexpr int kTile = kRows * D;
   extern __shared__ __attribute__((aligned(16))) uint16_t lds[];   // two slots of Q and dO, V, two slots of the rows' values
-  const uint16_t* V = lds + 4 * kTile;
-  float* stats = reinterpret_cast<float*>(lds + 4 * kTile + 128 * D);
+  constexpr int kV = 4 * kTile;   // elements in front of V
+  const uint16_t* V = lds + kV;
+  float* stats = reinterpret_cast<float*>(lds + kV + 128 * D);
   const Shape& s = a.s;
   const int64_t id = a.first + blockIdx.x;
   const int head = int(id % s.kv_heads);
@@ -401,7 +402,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
     ld.load_at(qb + token * q_pitch, q_off, rows - int(row0), lds0 + slot * 4 * kTile);
     ld.load_at(ob + token * o_pitch, o_off, rows - int(row0), lds0 + slot * 4 * kTile + 2 * kTile);
     if (wave == 0)
-      load_lds4_asm(rsrc_words(sb + uint64_t(row0) * 8, kAllRecords), lds0 + 8 * kTile + 256 * D + slot * kRows * 8,
+      load_lds4_asm(rsrc_words(sb + uint64_t(row0) * 8, kAllRecords), lds0 + 2 * kV + 256 * D + slot * kRows * 8,
                     int(row0) + lane / 2 < rows ? uint32_t(lane) * 4 : kOutOfRange);
   };
   const float c = s.scale * kLog2e;
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdArgs a) {
   if (begin < end) {
     const Loader<D, 128, 4> lv(wave, s.dim);
     lv.load(reinterpret_cast<uint64_t>(a.v.p + (p.k0 + key_b) * a.v.row + head * a.v.head), uint32_t(a.v.row * 2), p.k_len - key_b,
-            lds0 + 8 * kTile);
+            lds0 + 2 * kV);
     fetch(t, t & 1);
   }
   auto next = [&]() {   // tile t has landed

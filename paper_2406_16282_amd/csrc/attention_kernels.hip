@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
 // Few rows, many keys: a block of kFewWaves waves has 32 packed rows and a share of their keys; each wave walks keys of its own
 // through two slots of its own, with no barrier, and the block's waves join at the end. Memory is what it waits
 // for: 16 KB to a wave are on their way while 16 KB are multiplied, 64 KB to a CU.
-constexpr int kFewWaves = 2;
+constexpr int kFewWaves = 2, kFewTiles = 4;   // at least so many tiles of keys to a wave, where rows' keys are shared out
 template <int D>
 constexpr int kFewKeys = 4096 / D;   // keys to a wave's tile: 8 KB of K, 8 of V
 template <int D>
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(FwdArgs a
   w.limit = real ? seen(row0 + in) : 0;
   const int most = uniform(seen(row0 + 31));
   const int all = (most + kT - 1) / kT, whole = uniform(seen(row0)) / kT;
-  const int share = (all + a.splits - 1) / a.splits;
+  const int even = (all + a.splits - 1) / a.splits, share = even > kFewTiles * kFewWaves ? even : kFewTiles * kFewWaves;
   const int begin = split * share, end = begin + share < all ? begin + share : all;
   const Loader<D, kT, 1> ld(0, s.dim);
   const Reader<D> rd;
@@ -402,16 +402,24 @@ __global__ __launch_bounds__(256) void attention_join_kernel(FwdArgs a) {
   float top = m;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-  const float f = none ? 0.0f : exp2_fast(m - top), sum = wave_sum(none ? 0.0f : l * f);
+  const float f = none ? -1.0f : exp2_fast(m - top), sum = wave_sum(none ? 0.0f : l * f);
   const bool any = __any(!none);
   const int col = 2 * lane < s.dim ? 2 * lane : 0;
   float v[2] = {0.0f, 0.0f};
-  for (int i = wave; i < a.splits; i += 4) {
-    if (__shfl(int(none), i, kWave)) continue;
-    const float g = __shfl(f, i, kWave);
-    const f32x2 x = *reinterpret_cast<const f32x2*>(a.part + (i * count + row) * s.dim + col);
-    v[0] = __builtin_fmaf(x[0], g, v[0]);
-    v[1] = __builtin_fmaf(x[1], g, v[1]);
+  constexpr int kAtOnce = 4;
+  for (int base = wave; base < a.splits; base += 4 * kAtOnce) {
+    f32x2 x[kAtOnce];
+    float g[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {   // a share without keys has written no sums: they are read, and not used
+      const int i = base + 4 * j < a.splits ? base + 4 * j : base;
+      x[j] = *reinterpret_cast<const f32x2*>(a.part + (i * count + row) * s.dim + col);
+      g[j] = base + 4 * j < a.splits ? __shfl(f, i, kWave) : -1.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[e] = g[j] < 0.0f ? v[e] : __builtin_fmaf(x[j][e], g[j], v[e]);
   }
   if (wave > 0) {
     lds[wave - 1][lane] = v[0];
@@ -442,7 +450,7 @@ static FwdForm fwd_form(const AttentionPlan& a, int cus) {
   f.few = a.q_rows * s.group <= 32 * a.batch;
   const int64_t blocks = tiles_of(s.q, a.batch, false, s.group, f.few ? 32 : 128) * a.kv_heads;
   // keys to a share: 4 tiles of each wave (few) or of the block
-  const int64_t least = f.few ? 4 * kFewWaves * (s.dim <= 64 ? kFewKeys<64> : kFewKeys<128>) : 4 * kKeys;
+  const int64_t least = f.few ? kFewTiles * kFewWaves * (s.dim <= 64 ? kFewKeys<64> : kFewKeys<128>) : 4 * kKeys;
   const int64_t want = blocks == 0 ? 1 : (f.few ? 16 : 2) * int64_t(cus) / blocks;
   f.splits = int(std::max<int64_t>(1, std::min<int64_t>({want, keys / least, kWave})));
   return f;
