@@ -144,6 +144,12 @@ struct Part {
   int k_slot;         // keys up to the next sequence
 };
 
+// A block's number where each XCD gets a run of per_xcd blocks (0: no such runs).
+__device__ inline int64_t block_number(int64_t first, uint32_t per_xcd) {
+  const uint32_t b = blockIdx.x;
+  return first + (b < per_xcd * kXcds ? (b % kXcds) * per_xcd + b / kXcds : b);
+}
+
 // The t-th tile of causal sequences of different lengths, those that see (or are seen by) most first: by their distance from
 // their sequence's lightest tile. 10 sequences of 1 to 2048 tokens, 8 key heads of 4 query heads, dim 128: the gradients of keys and
 // values 276 us, in the sequences' order 337, the forward pass 155 and 166. A wave's lanes hold a sequence each.
@@ -470,6 +476,13 @@ inline Shape shape_of(const AttentionPlan& a) {
   s.inv_group = s.group == 1 ? 0xffffffffu : uint32_t((uint64_t(1) << 32) / uint64_t(s.group));
   s.scale = a.scale;
   return s;
+}
+// Consecutive blocks go to the XCDs in turn: with a multiple of 8 key heads all tiles of a head come to one XCD, whose L2 keeps what
+// they share. With others each XCD gets a run of blocks, where these have about the same work: 64 images of 197 tokens, 12 heads of
+// 64, take 28 us forward and 35 and 35 backward so, 31, 37 and 38 with blocks in turn.
+inline uint32_t blocks_per_xcd(const Shape& s, int64_t blocks) {
+  const bool alike = s.q.starts == nullptr && s.k.starts == nullptr && (!s.causal || s.batch % kXcds == 0);
+  return alike && s.kv_heads % kXcds != 0 ? uint32_t(blocks / kXcds) : 0;
 }
 // The most tiles of `per` rows that a side has, a row counting `times` times.
 inline int64_t tiles_of(const Seqs& s, int64_t batch, bool fill, int64_t times, int64_t per) {

@@ -20,6 +20,7 @@ struct BwdArgs {
   float* part;        // shares > 1: [shares][2][rows of k][kv_heads][dim]: dk, dv
   int shares, share;  // the most shares of a key tile's rows; row tiles that one share should have
   int64_t first;      // block number of this launch's first block
+  uint32_t per_xcd;
 };
 
 constexpr int kKeys = 64;   // keys to a tile of the dq kernel
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdArgs a) {
   __shared__ int flags[2];
   if (threadIdx.x < 2) flags[threadIdx.x] = 0;   // a barrier follows in any case
   const Shape& s = a.s;
-  const int64_t id = a.first + blockIdx.x;
+  const int64_t id = block_number(a.first, a.per_xcd);
   const int head = int(id % s.kv_heads);
   Part p;
   if (!locate<true>(s, id / s.kv_heads, 128, s.group, p)) return;
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(Bwd
   const uint16_t* V = lds + kV;
   float* stats = reinterpret_cast<float*>(lds + kV + 128 * D);
   const Shape& s = a.s;
-  const int64_t id = a.first + blockIdx.x;
+  const int64_t id = block_number(a.first, a.per_xcd);
   const int head = int(id % s.kv_heads);
   const int64_t rest = id / s.kv_heads;
   const int part = int(rest % a.shares);
@@ -529,12 +530,14 @@ hipError_t launch_bwd(const BwdArgs& f, int dev, hipStream_t st) {
   BwdArgs g = f;
   e = in_parts(tiles_of(f.s.q, f.s.batch, f.s.fill, f.s.group, 128) * f.s.kv_heads, most_blocks(256), [&](int64_t first, int64_t count) {
     g.first = first;
+    g.per_xcd = blocks_per_xcd(g.s, count);
     attention_dq_kernel<D><<<uint32_t(count), 256, kBytesQ, st>>>(g);
   });
   if (e != hipSuccess) return e;
   const int64_t tiles = tiles_of(f.s.k, f.s.batch, f.s.fill, 1, 128) * f.s.kv_heads;
   e = in_parts(tiles * f.shares, most_blocks(256), [&](int64_t first, int64_t count) {
     g.first = first;
+    g.per_xcd = blocks_per_xcd(g.s, count);
     attention_dkv_kernel<D><<<uint32_t(count), 256, kBytesKv, st>>>(g);
   });
   if (e != hipSuccess || f.shares == 1) return e;

@@ -16,6 +16,7 @@ struct FwdArgs {
   float* stats;      // splits > 1: [splits][rows * heads][2]: running maximum (log2), sum
   int splits;
   int64_t first;     // block number of this launch's first block
+  uint32_t per_xcd;
 };
 
 constexpr int kKeys = 64;      // keys to a tile
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
   __shared__ int flags[2];
   if (threadIdx.x < 2) flags[threadIdx.x] = 0;   // a barrier follows in any case
   const Shape& s = a.s;
-  const int64_t id = a.first + blockIdx.x;
+  const int64_t id = block_number(a.first, a.per_xcd);
   const int head = int(id % s.kv_heads);
   const int64_t rest = id / s.kv_heads;
   const int split = int(rest % a.splits);
@@ -468,6 +469,7 @@ hipError_t launch_fwd(FwdArgs f, bool few, int dev, hipStream_t st) {
   return in_parts(blocks, most_blocks(threads), [&](int64_t first, int64_t count) {
     FwdArgs g = f;
     g.first = first;
+    g.per_xcd = blocks_per_xcd(g.s, count);
     if (few) attention_few_kernel<D><<<uint32_t(count), threads, kFewLds<D>, st>>>(g);
     else attention_fwd_kernel<D><<<uint32_t(count), threads, kBytes, st>>>(g);
   });
