@@ -588,7 +588,9 @@ class QKVAttention(nn.Module):
     [sequences, rows, heads + 2 kv_heads, dim] (queries, keys, values) gives [sequences, rows, heads, dim]; packed as
     [rows, ..] with ``starts`` (int32, sequences + 1). ``eps``: MS-RMSNorm of each query and key head in front of the
     rotation (without gains). One node: keeps the turned queries and keys, the values as they lie in qkv,
-    the output and one fp32 value per row (two per head more with the norm); the gradient comes as one tensor."""
+    the output and one fp32 value per row and head (with the norm one more per query and key head); the gradient comes as one
+    tensor. To capture forward and backward of this or the modules above in a graph, let go of the eager graphs of the
+    same leaves first."""
 
     def __init__(self, heads, kv_heads, dim, rotation, causal=True, scale=None, eps=None):
         super().__init__()

@@ -1,0 +1,146 @@
+"""Rotary positions, norms of heads and attention where offsets pass 32 bits, with many sequences, from several threads
+and behind a growing cache."""
+
+import threading
+
+import pytest
+import torch
+
+import paper_2406_16282_amd as lmbp
+import plain_heads as P
+from test_gpu_attention import normal, run, starts_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def apart(parts, rows, pitch):
+    """Copies of ``parts`` [rows, heads, dim] side by side in rows of ``pitch`` elements, and empty places like them."""
+    room = torch.empty(rows * pitch, device=DEV, dtype=parts[0].dtype).view(rows, pitch)
+    at, out = 0, []
+    for t in (*parts, *parts):
+        n = t.shape[1] * t.shape[2]
+        out.append(room[:, at:at + n].unflatten(1, t.shape[1:]))
+        at += n
+    assert at <= pitch and room.data_ptr() % 16 == 0
+    for t, place in zip(parts, out):
+        place.copy_(t)
+    return out[:len(parts)], out[len(parts):]
+
+
+@pytest.mark.parametrize("starts", [None, [70, 1, 229]])
+def test_rows_gibibytes_apart(starts):
+    """Layouts do not change results: rows 16 MiB apart, the last beyond 2^32 bytes and 2^31 elements."""
+    rows, pitch = 300, (1 << 23) - 8
+    q, k, v, do = (normal((rows, h, 128), i) for i, h in enumerate((4, 2, 2, 4)))
+    kw = dict(causal=True) if starts is None else dict(causal=True, q_starts=starts_of(starts))
+    o, lse = lmbp.attention_fwd(q, k, v, **kw)
+    grads = lmbp.attention_bwd(do, q, k, v, o, lse, **kw)
+    (fq, fk, fv, fdo, fo), (dq, dk, dv, o2, _) = apart((q, k, v, do, o), rows, pitch)
+    assert (fq[-1].data_ptr() - fq[0].data_ptr()) > 1 << 32
+    lse2 = torch.empty_like(lse)
+    lmbp.attention_fwd(fq, fk, fv, o=o2, lse=lse2, **kw)
+    assert torch.equal(o2, o) and torch.equal(lse2, lse)
+    lmbp.attention_bwd(fdo, fq, fk, fv, fo, lse, dq=dq, dk=dk, dv=dv, **kw)
+    for got, want in zip((dq, dk, dv), grads):
+        assert torch.equal(got, want)
+    few = lmbp.attention_fwd(q[-1:], k, v)
+    got = lmbp.attention_fwd(fq[-1:], fk, fv)
+    assert torch.equal(got[0], few[0]) and torch.equal(got[1], few[1])
+
+
+@pytest.mark.parametrize("dim", [64, 33])
+def test_rotation_of_rows_gibibytes_apart(dim):
+    rows, pitch = 300, (1 << 23) - 8
+    q, k = normal((rows, 3, dim), 1), normal((rows, 1, dim), 2)
+    at, turn, gain = torch.arange(rows, device=DEV), lmbp.Rotation.of_base(dim // 2 * 2), normal((dim,), 3)
+    (fq, fk), (oq, ok) = apart((q, k), rows, pitch)
+    for back in (lmbp.rope_fwd, lmbp.rope_bwd):
+        back(fq, fk, at, turn, oq, ok)
+        assert all(torch.equal(a, b) for a, b in zip((oq, ok), back(q, k, at, turn)))
+    for g in ((), (gain, gain)):
+        want = lmbp.msrms_rope_fwd(q, k, 1e-6, at, turn, *g)
+        got = lmbp.msrms_rope_fwd(fq, fk, 1e-6, at, turn, *(g or (None, None)), oq, ok)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_cache_of_more_than_32_bits():
+    """One token behind 540001 keys of 32 heads: 4.4 GB of each. The first and the last head against 64 bits."""
+    keys, heads = 540001, 32
+    k, v = (torch.empty(1, keys, heads, 128, device=DEV, dtype=torch.bfloat16).normal_(generator=torch.Generator(DEV).manual_seed(i)) for i in (1, 2))
+    q = normal((1, 1, heads, 128), 3)
+    used = torch.tensor([keys - 2], device=DEV, dtype=torch.int32)
+    o, lse = lmbp.attention_fwd(q, k, v, causal=True, k_lens=used)
+    for h in (0, heads - 1):
+        P.check_forward(o[0, :, h], lse[0, :, h], q[0, :, h], k[0, :keys - 2, h], v[0, :keys - 2, h], True, 128 ** -0.5, f"head {h}")
+
+
+@pytest.mark.parametrize("count", [63, 64, 65, 130])
+def test_many_sequences(count):
+    lengths = [(11 * i * i + 3 * i) % 47 for i in range(count)]
+    lengths[5], lengths[count - 2] = 300, 260
+    run(2, 1, 64, lengths, lengths, True)
+
+
+def test_many_sequences_of_other_keys():
+    lengths = [(7 * i) % 13 for i in range(62)]
+    run(4, 2, 64, lengths, [n + (5 * i) % 90 for i, n in enumerate(lengths)], True)
+
+
+def test_two_threads():
+    work = [[normal((50 + 30 * i, h, 64), 10 * i + h) for h in (8, 2, 2)] for i in range(2)]
+    at, turn = torch.arange(80, device=DEV), lmbp.Rotation.of_base(64)
+
+    def step(q, k, v):
+        q, k = lmbp.rope_fwd(q, k, at[:q.shape[0]], turn)
+        o, lse = lmbp.attention_fwd(q, k, v, True)
+        return [q, k, o, lse, *lmbp.attention_bwd(o, q, k, v, o, lse, True), *lmbp.attention_fwd(q[-1:], k, v)]
+
+    want = [step(*w) for w in work]
+    torch.cuda.synchronize()
+    wrong, errors = [], []
+
+    def body(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(30):
+                    got = step(*work[i])
+                    wrong.extend(n for n, (a, b) in enumerate(zip(got, want[i])) if not torch.equal(a, b))
+        except Exception as e:   # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=body, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    assert not wrong and not errors
+
+
+def test_a_captured_token_behind_a_growing_cache():
+    """One graph takes the tokens one after the other: the position, the number of keys in use and the cache change in place."""
+    heads, kv, room, dim = 8, 2, 4000, 128
+    cache = normal((2, 2, room, kv, dim), 1)
+    new = normal((2, 1, heads + 2 * kv, dim), 2)
+    used, at = torch.zeros(2, device=DEV, dtype=torch.int32), torch.zeros(2, device=DEV, dtype=torch.int64)
+    turn = lmbp.Rotation.of_base(dim)
+
+    def token():
+        q, _, _, _ = lmbp.msrms_rope_fwd(new[:, :, :heads], None, 1e-6, at, turn)
+        return lmbp.attention_fwd(q, cache[0], cache[1], True, k_lens=used)
+
+    token()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = token()
+    for n in ([1, 3], [700, 65], [4000, 2], [0, 4000]):
+        used.copy_(torch.tensor(n)), at.copy_(torch.tensor(n) + 5), new.copy_(normal(new.shape, n[0]))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = token()
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1]), n
+        for i in range(2):
+            q = lmbp.msrms_rope_fwd(new[i:i + 1, :, :heads], None, 1e-6, at[i:i + 1], turn)[0][0]
+            for h in (0, heads - 1):
+                g = h // (heads // kv)
+                P.check_forward(o[i, :, h], lse[i, :, h], q[:, h], cache[0, i, :n[i], g], cache[1, i, :n[i], g], True, dim ** -0.5, f"{n} {i} {h}")
