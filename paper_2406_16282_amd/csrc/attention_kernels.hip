@@ -439,7 +439,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(FwdArgs a) {
   if (lane == 0) a.lse[row] = any ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
 }
 
-// How a call is taken: blocks of 32 packed rows (few) or of 128, and the shares of the keys.
+// How a call is taken: blocks of 32 packed rows (few) or of 128, and the shares of the keys. One token of 16 sequences of 1 to
+// 4096 keys, 32 heads: few 102 us, 128 rows to a block 144; 64 sequences of 1000 keys 190 and 201; 4 rows of 8 key heads each of 8
+// sequences of 500 keys 14 and 14; 8 queries of 16 sequences of 200 keys 11.8 and 9.3, so short sequences do not take it.
 struct FwdForm {
   bool few;
   int splits;
@@ -448,12 +450,16 @@ static FwdForm fwd_form(const AttentionPlan& a, int cus) {
   const Shape s = shape_of(a);
   const int64_t keys = a.k_rows / a.batch;
   FwdForm f;
-  f.few = a.q_rows * s.group <= 32 * a.batch;
+  f.few = a.q_rows * s.group <= 32 * a.batch && keys >= 512;
   const int64_t blocks = tiles_of(s.q, a.batch, false, s.group, f.few ? 32 : 128) * a.kv_heads;
-  // keys to a share: 4 tiles of each wave (few) or of the block
+  // Keys to a share: 4 tiles of each wave (few) or of the block, where blocks are to fill the device; 4 times as many where shares of few
+  // queries' keys only even out sequences of different lengths (the device alone knows them). 256 queries and 16384 keys of 8 heads 37 us
+  // (one share 378); 16 sequences of 2000 keys, 32 heads, one token in one share 98 (7 shares 119), 32 tokens 101 (161), and the sequences
+  // of 1 to 4096 keys in 4 shares 102 (2: 110).
   const int64_t least = f.few ? kFewTiles * kFewWaves * (s.dim <= 64 ? kFewKeys<64> : kFewKeys<128>) : 4 * kKeys;
-  const int64_t want = blocks == 0 ? 1 : (f.few ? 16 : 2) * int64_t(cus) / blocks;
-  f.splits = int(std::max<int64_t>(1, std::min<int64_t>({want, keys / least, kWave})));
+  const int64_t filling = std::min(blocks == 0 ? 1 : 2 * int64_t(cus) / blocks, keys / least);
+  const int64_t evening = f.few && blocks > 0 ? std::min(8 * int64_t(cus) / blocks, keys / (4 * least)) : 1;
+  f.splits = int(std::max<int64_t>(1, std::min<int64_t>(std::max(filling, evening), kWave)));
   return f;
 }
 
