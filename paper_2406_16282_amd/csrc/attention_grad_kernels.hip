@@ -4,6 +4,13 @@
 //
 // Two kernels, each forming the scores again: dq per rows (which also writes each row's lse and D for the other),
 // dk and dv per keys. One kernel for all three would have to add dq up with atomics, whose order changes results.
+//
+// The matrix units bound both: three and four products of the forward's size. P and dS are formed in fp32 and rounded to bf16 once, as
+// operands. 16384 tokens of 32 heads on 8, dim 128, causal: dq 2.83 ms (1167 TFLOP/s, matrix units 62% of the cycles), dk and dv 3.93
+// (1120, 56%), at the power limit's 1.8 to 1.9 GHz; 4 sequences of 2048, 32 heads: 232 and 304 us. The order of LDS reads, MFMAs and
+// exponentials is written out (left to the compiler dk and dv took 4.75 ms). Two waves to a SIMD with 256 registers: one with 512,
+// which reads LDS less often, took 4.44 to 5.18, since a lone wave issues too seldom. Narrow heads' dk and dv fit three waves (64
+// images of 197, 12 heads of 64: 37.4 us, two 42.6).
 #include "attention_device.hpp"
 
 #include <algorithm>

@@ -144,3 +144,26 @@ def test_a_captured_token_behind_a_growing_cache():
             for h in (0, heads - 1):
                 g = h // (heads // kv)
                 P.check_forward(o[i, :, h], lse[i, :, h], q[:, h], cache[0, i, :n[i], g], cache[1, i, :n[i], g], True, dim ** -0.5, f"{n} {i} {h}")
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,n", [(1, 1, 128, 1), (8, 1, 128, 4), (6, 2, 64, 10), (32, 1, 72, 1), (5, 1, 40, 6), (2, 2, 128, 32)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_queries_of_caches_of_all_lengths(heads, kv_heads, dim, n, causal):
+    """Blocks of few rows whose keys end at, before and behind a tile's edge, some with none, in rooms of 1100."""
+    used = [0, 1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 600, 1099, 1100]
+    room = 1100
+    q, k, v = normal((len(used), n, heads, dim), 1), normal((len(used), room, kv_heads, dim), 2), normal((len(used), room, kv_heads, dim), 3)
+    for i, m in enumerate(used):   # keys that are not in use may hold anything
+        k[i, m:], v[i, m:] = float("nan"), float("inf")
+    o, lse = lmbp.attention_fwd(q, k, v, causal, k_lens=torch.tensor(used, device=DEV, dtype=torch.int32))
+    group = heads // kv_heads
+    for i, m in enumerate(used):
+        for h in range(heads):
+            P.check_forward(o[i, :, h], lse[i, :, h], q[i, :, h], k[i, :m, h // group], v[i, :m, h // group], causal, dim ** -0.5, f"{m} keys, head {h}")
+
+
+@pytest.mark.parametrize("tokens,heads,kv_heads,dim", [(1024, 8, 1, 128), (700, 4, 2, 64), (2500, 2, 1, 40)])
+def test_many_shares_of_rows(tokens, heads, kv_heads, dim):
+    """Few key tiles, whose rows go to as many blocks as fill the device."""
+    run(heads, kv_heads, dim, [tokens], [tokens], True)
+    run(heads, kv_heads, dim, [tokens - 300, 0, 299, 1], [tokens - 300, 40, 150, 2], False)
