@@ -1,6 +1,7 @@
 """Rotary positions, norms of heads and attention where offsets pass 32 bits, with many sequences, from several threads
 and behind a growing cache."""
 
+import math
 import threading
 
 import pytest
@@ -167,3 +168,18 @@ def test_many_shares_of_rows(tokens, heads, kv_heads, dim):
     """Few key tiles, whose rows go to as many blocks as fill the device."""
     run(heads, kv_heads, dim, [tokens], [tokens], True)
     run(heads, kv_heads, dim, [tokens - 300, 0, 299, 1], [tokens - 300, 40, 150, 2], False)
+
+
+def test_frequencies_of_any_size():
+    """From denormal numbers to ones whose every position is many turns, of either sign, and those that are whole turns almost."""
+    freqs = [5e-324, 1e-300, 2.0 ** -140, 2.0 ** -64, 2.0 ** -63, 1e-12, 1e-4, 0.5, 1.0, -1.0, 3.0, -3.2, 2 * math.pi, -2 * math.pi, 6.5, 1e3, -1e5, 2.0 ** 30, 3e12, -2.0 ** 45, 0.0]
+    turn = lmbp.Rotation(freqs)
+    x, at = torch.randn(6, 2, 42, device=DEV, generator=torch.Generator(DEV).manual_seed(1)), torch.tensor([1, -1, 2, 7, 0, 1000], device=DEV)
+    y, _ = lmbp.rope_fwd(x, None, at, turn)
+    t = P.angles(at, turn.freqs, turn.axes, 6)
+    want, size = P.turn(x.double(), t, False), P.pair_size(x.double(), 21, False)
+    own = torch.cat([t, t], -1).abs() * 2.0 ** -52   # what 64-bit angles themselves are off
+    P.inside(y, want, (6 * P.U + own) * size + P.half(torch.float32) * want.abs(), "turned")
+    huge = lmbp.Rotation([1e300, -1e18, 2.0 ** 53])   # no angle is meant by these: lengths are kept
+    y, _ = lmbp.rope_fwd(x, None, at, huge)
+    assert (y.square().sum(-1) - x.square().sum(-1)).abs().max() < 1e-4
