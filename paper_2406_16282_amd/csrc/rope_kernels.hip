@@ -20,12 +20,15 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace lmbp {
 namespace rope {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 enum { kTurn = 0, kNorm = 1, kNormBack = 2, kNormGain = 3, kNormBackGain = 4 };
-enum { kSingle = 0, kHalves = 1, kPairs = 2 };   // element by element; 16-byte pieces of pairs half apart, side by side
+enum { kSingle = 0, kHalves = 1, kPairs = 2 };   // element by element; 16- or 8-byte pieces of pairs half apart, side by side
 
 // Queries or keys: one tensor's heads.
 struct Side {
@@ -52,11 +55,33 @@ struct Args {
   uint64_t freq[kRopePairs];
 };
 
+// Pieces of 8 bytes, for heads whose halves are no multiple of 16.
+struct BF16Narrow : BF16 {
+  static constexpr int kPerVec = 4;
+  static __device__ inline void unpack(const u32x2& v, float (&f)[4]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      f[2 * k] = __uint_as_float(v[k] << 16);
+      f[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
+    }
+  }
+  static __device__ inline u32x2 pack(const float (&f)[4]) { return u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])}; }
+};
+struct F32Narrow : F32 {
+  static constexpr int kPerVec = 2;
+  static __device__ inline void unpack(const u32x2& v, float (&f)[2]) {
+    f[0] = __uint_as_float(v[0]);
+    f[1] = __uint_as_float(v[1]);
+  }
+  static __device__ inline u32x2 pack(const float (&f)[2]) { return u32x2{__float_as_uint(f[0]), __float_as_uint(f[1])}; }
+};
+
 // This lane's place in a head: E pairs, two pieces of E columns or 2 E single columns.
 template <class IO, int FORM>
 struct Place {
   static constexpr int E = IO::kPerVec;
   static constexpr bool VEC = FORM != kSingle;
+  using Vec = std::conditional_t<E * IO::kBytes == 16, u32x4, u32x2>;
   int pair, a, b;   // first pair; VEC: where the pieces start
   int dim, half;
   bool inside;
@@ -101,15 +126,15 @@ struct Place {
   }
   // A head's values of this lane as they come from memory, so that several heads' loads run before the first is used.
   struct Raw {
-    u32x4 u, v;             // VEC
+    Vec u, v;               // VEC
     float x[VEC ? 1 : E], y[VEC ? 1 : E];
   };
   __device__ inline void load(const void* row, Raw& r) const {
     if constexpr (VEC) {
-      r.u = r.v = u32x4{0u, 0u, 0u, 0u};
+      r.u = r.v = Vec{};
       if (inside) {
-        r.u = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const char*>(row) + a * IO::kBytes));
-        r.v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const char*>(row) + b * IO::kBytes));
+        r.u = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(static_cast<const char*>(row) + a * IO::kBytes));
+        r.v = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(static_cast<const char*>(row) + b * IO::kBytes));
       }
     } else {
       const Place p = again();
@@ -149,8 +174,8 @@ struct Place {
         t[e] = interleaved ? (e % 2 ? y[(E + e) / 2] : x[(E + e) / 2]) : y[e];
       }
       if (inside) {
-        __builtin_nontemporal_store(IO::pack(s), reinterpret_cast<u32x4*>(static_cast<char*>(row) + a * IO::kBytes));
-        __builtin_nontemporal_store(IO::pack(t), reinterpret_cast<u32x4*>(static_cast<char*>(row) + b * IO::kBytes));
+        __builtin_nontemporal_store(IO::pack(s), reinterpret_cast<Vec*>(static_cast<char*>(row) + a * IO::kBytes));
+        __builtin_nontemporal_store(IO::pack(t), reinterpret_cast<Vec*>(static_cast<char*>(row) + b * IO::kBytes));
       }
     } else {
       const Place p = again();
@@ -210,8 +235,14 @@ __device__ inline void angles(const Args& f, const Place<IO, FORM>& at, int64_t 
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
+  if constexpr (E == 2) {
+    const float2 x = *reinterpret_cast<const float2*>(table + at.pair), y = *reinterpret_cast<const float2*>(table + kRopePairs + at.pair);
+    c[0] = x.x, c[1] = x.y;
+    s[0] = y.x, s[1] = y.y;
+    return;
+  }
 #pragma unroll
-  for (int e = 0; e < E; e += 4) {
+  for (int e = 0; e + 4 <= E; e += 4) {
     const float4 x = *reinterpret_cast<const float4*>(table + at.pair + e), y = *reinterpret_cast<const float4*>(table + kRopePairs + at.pair + e);
     c[e] = x.x, c[e + 1] = x.y, c[e + 2] = x.z, c[e + 3] = x.w;
     s[e] = y.x, s[e + 1] = y.y, s[e + 2] = y.z, s[e + 3] = y.w;
@@ -420,9 +451,12 @@ int gain_blocks(const rope::Args& f) { return int(std::clamp<int64_t>(blocks_of(
 template <class IO, int MODE>
 hipError_t launch(const rope::Args& f, bool vec, hipStream_t s) {
   auto go = [&](const rope::Args& g, dim3 grid) {
-    if (!vec) rope::rope_kernel<IO, MODE, rope::kSingle><<<grid, 256, 0, s>>>(g);
-    else if (g.interleaved) rope::rope_kernel<IO, MODE, rope::kPairs><<<grid, 256, 0, s>>>(g);
-    else rope::rope_kernel<IO, MODE, rope::kHalves><<<grid, 256, 0, s>>>(g);
+    if (!vec) {
+      if constexpr (IO::kPerVec * IO::kBytes == 16) rope::rope_kernel<IO, MODE, rope::kSingle><<<grid, 256, 0, s>>>(g);
+    } else if (g.interleaved) rope::rope_kernel<IO, MODE, rope::kPairs><<<grid, 256, 0, s>>>(g);
+    else {
+      rope::rope_kernel<IO, MODE, rope::kHalves><<<grid, 256, 0, s>>>(g);
+    }
   };
   if constexpr (MODE == rope::kNormBackGain || MODE == rope::kNormGain) {
     const int blocks = MODE == rope::kNormGain ? int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, 4 * kGainBlocks)) : gain_blocks(f);
@@ -457,7 +491,7 @@ uint64_t turns_of(double f) {
   return f < 0 ? -uint64_t(part) : uint64_t(part);
 }
 
-rope::Args args_of(const RopePlan& r, bool bf16, bool& vec) {
+rope::Args args_of(const RopePlan& r) {
   rope::Args f{};
   f.positions = r.positions;
   f.axis_stride = r.axis_stride;
@@ -470,13 +504,10 @@ rope::Args args_of(const RopePlan& r, bool bf16, bool& vec) {
     f.axis[p] = uint8_t(r.axes ? r.axes[p] : 0);
     f.freq[p] = turns_of(r.freqs[p]);
   }
-  const int per = bf16 ? 8 : 4;
-  vec = r.dim % (2 * per) == 0 && (r.interleaved || r.pairs % per == 0);
   return f;
 }
 
-void side_of(rope::Side& d, const HeadsView& x, const HeadsView& y, const HeadsView& kept, float* rstd, const void* gain, int64_t heads,
-             bool bf16, bool& vec) {
+void side_of(rope::Side& d, const HeadsView& x, const HeadsView& y, const HeadsView& kept, float* rstd, const void* gain, int64_t heads) {
   d.x = x.p;
   d.y = y.p;
   d.kept = kept.p;
@@ -486,18 +517,36 @@ void side_of(rope::Side& d, const HeadsView& x, const HeadsView& y, const HeadsV
   d.y_row = y.row, d.y_head = y.head;
   d.kept_row = kept.row, d.kept_head = kept.head;
   d.heads = int(heads);
-  const int per = bf16 ? 8 : 4;
-  for (const HeadsView* v : {&x, &y, &kept})
-    if (heads > 0 && v->p != nullptr)
-      vec = vec && reinterpret_cast<uintptr_t>(v->p) % 16 == 0 && v->row % per == 0 && v->head % per == 0;
+}
+
+// Whether heads can be taken in pieces of `per` elements.
+bool in_pieces(const rope::Args& f, int per, int bytes) {
+  if (f.dim % (2 * per) != 0 || f.dim > 2 * per * kWave || (!f.interleaved && f.pairs % per != 0)) return false;
+  for (const rope::Side& d : f.side) {
+    if (d.heads == 0) continue;
+    for (const void* p : {d.x, static_cast<const void*>(d.y), d.kept})
+      if (reinterpret_cast<uintptr_t>(p) % uintptr_t(per * bytes) != 0) return false;
+    for (int64_t stride : {d.x_row, d.x_head, d.y_row, d.y_head, d.kept_row, d.kept_head})
+      if (stride % per != 0) return false;
+  }
+  return true;
+}
+
+template <class IO, class NARROW, int MODE>
+hipError_t launch_pieces(rope::Args& f, bool apart, hipStream_t s) {
+  const bool wide = in_pieces(f, IO::kPerVec, IO::kBytes);
+  if (!wide && in_pieces(f, NARROW::kPerVec, IO::kBytes)) {
+    plan<NARROW>(f, apart);
+    return launch<NARROW, MODE>(f, true, s);
+  }
+  plan<IO>(f, apart);
+  return launch<IO, MODE>(f, wide, s);
 }
 
 template <int MODE>
-hipError_t launch_type(bool bf16, rope::Args& f, bool vec, hipStream_t s) {
+hipError_t launch_type(bool bf16, rope::Args& f, hipStream_t s) {
   constexpr bool kApart = MODE == rope::kNormBackGain || MODE == rope::kNormGain;   // queries and keys in blocks of their own
-  if (bf16) plan<BF16>(f, kApart);
-  else plan<F32>(f, kApart);
-  return bf16 ? launch<BF16, MODE>(f, vec, s) : launch<F32, MODE>(f, vec, s);
+  return bf16 ? launch_pieces<BF16, rope::BF16Narrow, MODE>(f, kApart, s) : launch_pieces<F32, rope::F32Narrow, MODE>(f, kApart, s);
 }
 
 }  // namespace
@@ -505,36 +554,33 @@ hipError_t launch_type(bool bf16, rope::Args& f, bool vec, hipStream_t s) {
 size_t msrms_rope_bwd_workspace(int64_t dim) { return size_t(kGainBlocks) * 2 * size_t(dim) * 4; }
 
 hipError_t launch_rope(bool bf16, const RopePlan& r, bool back, const HeadsView (&x)[2], const HeadsView (&y)[2], hipStream_t s) {
-  bool vec;
-  rope::Args f = args_of(r, bf16, vec);
+  rope::Args f = args_of(r);
   f.sign = back ? -1.0f : 1.0f;
-  for (int i = 0; i < 2; ++i) side_of(f.side[i], x[i], y[i], HeadsView{}, nullptr, nullptr, r.heads[i], bf16, vec);
-  return launch_type<rope::kTurn>(bf16, f, vec, s);
+  for (int i = 0; i < 2; ++i) side_of(f.side[i], x[i], y[i], HeadsView{}, nullptr, nullptr, r.heads[i]);
+  return launch_type<rope::kTurn>(bf16, f, s);
 }
 
 hipError_t launch_msrms_rope_fwd(bool bf16, const RopePlan& r, float eps, bool gain_bf16, const void* const (&gain)[2],
                                  const HeadsView (&x)[2], const HeadsView (&y)[2], float* const (&rstd)[2], hipStream_t s) {
-  bool vec;
-  rope::Args f = args_of(r, bf16, vec);
+  rope::Args f = args_of(r);
   f.sign = 1.0f;
   f.eps = eps;
   f.gain_bf16 = gain_bf16;
-  for (int i = 0; i < 2; ++i) side_of(f.side[i], x[i], y[i], HeadsView{}, rstd[i], gain[i], r.heads[i], bf16, vec);
-  return gain[0] != nullptr ? launch_type<rope::kNormGain>(bf16, f, vec, s) : launch_type<rope::kNorm>(bf16, f, vec, s);
+  for (int i = 0; i < 2; ++i) side_of(f.side[i], x[i], y[i], HeadsView{}, rstd[i], gain[i], r.heads[i]);
+  return gain[0] != nullptr ? launch_type<rope::kNormGain>(bf16, f, s) : launch_type<rope::kNorm>(bf16, f, s);
 }
 
 hipError_t launch_msrms_rope_bwd(bool bf16, const RopePlan& r, bool gain_bf16, const void* const (&gain)[2], const HeadsView (&dy)[2],
                                  const HeadsView (&kept)[2], const float* const (&rstd)[2], const HeadsView (&dx)[2],
                                  void* const (&dgain)[2], void* workspace, hipStream_t s) {
-  bool vec;
-  rope::Args f = args_of(r, bf16, vec);
+  rope::Args f = args_of(r);
   f.sign = -1.0f;
   f.gain_bf16 = gain_bf16;
   f.part = static_cast<float*>(workspace);
   for (int i = 0; i < 2; ++i)
-    side_of(f.side[i], dy[i], dx[i], kept[i], const_cast<float*>(rstd[i]), gain[i], r.heads[i], bf16, vec);
-  if (gain[0] == nullptr && gain[1] == nullptr) return launch_type<rope::kNormBack>(bf16, f, vec, s);
-  const hipError_t e = launch_type<rope::kNormBackGain>(bf16, f, vec, s);
+    side_of(f.side[i], dy[i], dx[i], kept[i], const_cast<float*>(rstd[i]), gain[i], r.heads[i]);
+  if (gain[0] == nullptr && gain[1] == nullptr) return launch_type<rope::kNormBack>(bf16, f, s);
+  const hipError_t e = launch_type<rope::kNormBackGain>(bf16, f, s);
   if (e != hipSuccess) return e;
   rope::rope_gain_kernel<<<dim3(uint32_t((r.dim + 3) / 4), r.heads[1] > 0 ? 2 : 1), 256, 0, s>>>(f.part, gain_blocks(f), int(r.dim), gain_bf16, dgain[0], dgain[1]);
   return hipGetLastError();

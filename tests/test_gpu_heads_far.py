@@ -9,6 +9,7 @@ import torch
 
 import paper_2406_16282_amd as lmbp
 import plain_heads as P
+import test_gpu_rope as rope
 from test_gpu_attention import normal, run, starts_of
 
 pytestmark = pytest.mark.gpu
@@ -183,3 +184,35 @@ def test_frequencies_of_any_size():
     huge = lmbp.Rotation([1e300, -1e18, 2.0 ** 53])   # no angle is meant by these: lengths are kept
     y, _ = lmbp.rope_fwd(x, None, at, huge)
     assert (y.square().sum(-1) - x.square().sum(-1)).abs().max() < 1e-4
+
+
+# dim, pairs, interleaved: halves that are multiples of 8 bytes and not of 16, for one type or the other, widest ones included
+PIECES = [(72, 36, False), (72, 18, False), (24, 12, True), (40, 4, False), (8, 4, False), (4, 2, True), (256, 126, False), (248, 124, False),
+          (260, 130, False), (508, 254, False), (504, 252, True), (510, 255, False), (504, 12, False), (12, 0, False), (6, 2, False)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim,pairs,interleaved", PIECES)
+def test_heads_in_pieces_of_8_bytes(dim, pairs, interleaved, dtype):
+    for tokens, heads, kv_heads in ((70, 5, 2), (9, 17, 1)):
+        size = (tokens, heads, kv_heads, dim, pairs, 1, interleaved)
+        rope.test_rope(size, dtype)
+        for gain in (None, "fp32", "bf16"):
+            rope.test_norm_rope(size, gain, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shift", [0, 8, 4, 2])
+def test_addresses_of_all_alignments(dtype, shift):
+    """The same turn and norm, off by roundings, of heads that lie at multiples of 16, 8, 4 and 2 (4) bytes."""
+    step = max(1, shift // dtype.itemsize)
+    q = normal((33, 3, 64), 1).to(dtype)
+    at, turn = torch.arange(33, device=DEV), lmbp.Rotation.of_base(64)
+    room = torch.zeros(33 * 3 * 80 + 64, device=DEV, dtype=dtype)
+    here = room[step if shift else 0:][:33 * 3 * 80].view(33, 3, 80)[..., :64]
+    here.copy_(q)
+    want = lmbp.rope_fwd(q, None, at, turn)[0]
+    assert torch.equal(lmbp.rope_fwd(here, None, at, turn)[0], want)
+    lmbp.rope_fwd(here, None, at, turn, here)
+    assert torch.equal(here, want) and not room.view(-1)[:step if shift else 0].any()
+    assert not room[(step if shift else 0):][:33 * 3 * 80].view(33, 3, 80)[..., 64:].any()
