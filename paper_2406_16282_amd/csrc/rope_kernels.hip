@@ -13,8 +13,9 @@
 // angles are formed: each pair's by one lane, handed round through LDS (formed by every lane for its own columns they cost
 // 7 us on each pass over the token, 8 us more in all). Loads and stores are non-temporal (52 us without). 8192 tokens of 32 + 32
 // heads of 128, bf16: turned 43 to 46 us (5.9 to 6.2 TB/s), norm and turn 48, its backward 64 (6.3); 2, 4 and 8 waves to a token
-// instead of one 47 -> 45, 48 -> 48, 67 -> 64. Odd widths (a half that is no multiple of 16 bytes) go element by element: 1531
-// tokens of 12 heads of 72, fp32, with gains 12 us, backward 13 and 4 for the sum of the gains' gradients.
+// instead of one 47 -> 45, 48 -> 48, 67 -> 64. A half that is no multiple of 16 bytes goes in pieces of 8 where that does, else element by element: 1531
+// tokens of 12 heads of 72, 18 pairs, fp32, with gains 9.2 us, backward 10.7 and 3.8 for the sum of the gains' gradients (element by
+// element 11.5 and 12.1); 8192 of 32 of 72, bf16, 30 and 33 without gains (45 and 59).
 #include "lmbp_device.hpp"
 #include "lmbp_launch.hpp"
 
@@ -49,6 +50,7 @@ struct Args {
   int64_t first;      // token of this launch's first block
   int dim, pairs, lanes, rows;   // lanes to a head (a power of two), heads to a wave at a time
   int shares;         // waves that take a token's heads in turn
+  int blocks;         // kNormBackGain: of each side
   float eps, sign;
   uint8_t wide, interleaved, gain_bf16;
   uint8_t axis[kRopePairs];
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(256) void rope_gain_kernel(const float* part, int b
 
 namespace {
 
-constexpr int kGainBlocks = 512;   // of the backward with gains: one sum of each to the workspace
+constexpr int kGainBlocks = 1024;   // at most, of the backward with gains: one sum of each to the workspace
 
 int lanes_of(int64_t dim, int per) {
   int lanes = 1;
@@ -446,10 +448,16 @@ void plan(rope::Args& f, bool apart) {
   f.shares = std::min(f.shares, steps);
 }
 int64_t blocks_of(const rope::Args& f, int64_t tokens) { return (tokens * f.shares + 3) / 4; }
-int gain_blocks(const rope::Args& f) { return int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, kGainBlocks)); }
+// Blocks of the backward with gains, of each side: about as many as are resident at once, which walk over the tokens. Pieces of 8 bf16 (156
+// registers) leave room for 3 to a CU, 384 to a side: 8192 tokens of 32 + 32 heads of 128 83 us (512: 108, 256: 98), of 32 + 8 67 (91, 75).
+// The others 4: 4000 tokens of 12 + 12 fp32 heads of 64 22 us (twice as many 25, half 24).
+int gain_blocks(const rope::Args& f, bool wide) {
+  const int64_t most = (wide ? kGainBlocks / 4 * 3 : kGainBlocks) / (f.side[1].heads > 0 ? 2 : 1);
+  return int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, most));
+}
 
 template <class IO, int MODE>
-hipError_t launch(const rope::Args& f, bool vec, hipStream_t s) {
+hipError_t launch(rope::Args& f, bool vec, hipStream_t s) {
   auto go = [&](const rope::Args& g, dim3 grid) {
     if (!vec) {
       if constexpr (IO::kPerVec * IO::kBytes == 16) rope::rope_kernel<IO, MODE, rope::kSingle><<<grid, 256, 0, s>>>(g);
@@ -459,7 +467,8 @@ hipError_t launch(const rope::Args& f, bool vec, hipStream_t s) {
     }
   };
   if constexpr (MODE == rope::kNormBackGain || MODE == rope::kNormGain) {
-    const int blocks = MODE == rope::kNormGain ? int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, 4 * kGainBlocks)) : gain_blocks(f);
+    const int blocks = MODE == rope::kNormGain ? int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, 2 * kGainBlocks)) : gain_blocks(f, IO::kPerVec == 8);
+    f.blocks = blocks;
     go(f, dim3(blocks, f.side[1].heads > 0 ? 2 : 1));
     return hipGetLastError();
   } else {
@@ -551,7 +560,7 @@ hipError_t launch_type(bool bf16, rope::Args& f, hipStream_t s) {
 
 }  // namespace
 
-size_t msrms_rope_bwd_workspace(int64_t dim) { return size_t(kGainBlocks) * 2 * size_t(dim) * 4; }
+size_t msrms_rope_bwd_workspace(int64_t dim) { return size_t(kGainBlocks) * size_t(dim) * 4; }
 
 hipError_t launch_rope(bool bf16, const RopePlan& r, bool back, const HeadsView (&x)[2], const HeadsView (&y)[2], hipStream_t s) {
   rope::Args f = args_of(r);
@@ -582,7 +591,7 @@ hipError_t launch_msrms_rope_bwd(bool bf16, const RopePlan& r, bool gain_bf16, c
   if (gain[0] == nullptr && gain[1] == nullptr) return launch_type<rope::kNormBack>(bf16, f, s);
   const hipError_t e = launch_type<rope::kNormBackGain>(bf16, f, s);
   if (e != hipSuccess) return e;
-  rope::rope_gain_kernel<<<dim3(uint32_t((r.dim + 3) / 4), r.heads[1] > 0 ? 2 : 1), 256, 0, s>>>(f.part, gain_blocks(f), int(r.dim), gain_bf16, dgain[0], dgain[1]);
+  rope::rope_gain_kernel<<<dim3(uint32_t((r.dim + 3) / 4), r.heads[1] > 0 ? 2 : 1), 256, 0, s>>>(f.part, f.blocks, int(r.dim), gain_bf16, dgain[0], dgain[1]);
   return hipGetLastError();
 }
 
