@@ -216,3 +216,41 @@ def test_addresses_of_all_alignments(dtype, shift):
     lmbp.rope_fwd(here, None, at, turn, here)
     assert torch.equal(here, want) and not room.view(-1)[:step if shift else 0].any()
     assert not room[(step if shift else 0):][:33 * 3 * 80].view(33, 3, 80)[..., 64:].any()
+
+
+def test_keys_are_turned_into_a_cache():
+    """k_out may be a row of each sequence's cache; the next call reads it there."""
+    room, heads, kv, dim, n = 600, 8, 2, 64, 3
+    cache = normal((2, n, room, kv, dim), 1)
+    before, turn = cache.clone(), lmbp.Rotation.of_base(dim)
+    new = normal((n, 1, heads + 2 * kv, dim), 2)
+    q, k, v = new.split((heads, kv, kv), -2)
+    at = torch.full((n, 1), 7, device=DEV)
+    want = lmbp.rope_fwd(q, k, at, turn)
+    yq, yk = lmbp.rope_fwd(q, k, at, turn, k_out=cache[0, :, 7:8])
+    cache[1, :, 7:8].copy_(v)
+    assert torch.equal(yq, want[0]) and torch.equal(cache[0, :, 7:8], want[1]) and yk.data_ptr() == cache[0, :, 7:8].data_ptr()
+    assert torch.equal(cache[0, :, :7], before[0, :, :7]) and torch.equal(cache[0, :, 8:], before[0, :, 8:])
+    used = torch.full((n,), 8, device=DEV, dtype=torch.int32)
+    o, lse = lmbp.attention_fwd(yq, cache[0], cache[1], True, k_lens=used)
+    ref = lmbp.attention_fwd(yq, cache[0, :, :8].contiguous(), cache[1, :, :8].contiguous(), True)
+    for i in range(n):
+        for h in range(heads):
+            P.check_forward(o[i, :, h], lse[i, :, h], yq[i, :, h], cache[0, i, :8, h // 4], cache[1, i, :8, h // 4], True, dim ** -0.5, f"{i} {h}")
+            P.check_forward(ref[0][i, :, h], ref[1][i, :, h], yq[i, :, h], cache[0, i, :8, h // 4], cache[1, i, :8, h // 4], True, dim ** -0.5, f"{i} {h}")
+
+
+def test_gradients_inside_guards():
+    """Given outputs between rows of a value of their own: nothing else is written, rows of no sequence stay."""
+    rows, heads, kv, dim, lengths = 333, 4, 2, 64, [100, 0, 190, 3]
+    used = sum(lengths)
+    q, k, v, do = (normal((rows, h, dim), i) for i, h in enumerate((heads, kv, kv, heads)))
+    kw = dict(causal=True, q_starts=starts_of(lengths))
+    o, lse = lmbp.attention_fwd(q, k, v, **kw)
+    want = lmbp.attention_bwd(do, q, k, v, o, lse, **kw)
+    room = torch.full((rows + 2, heads + 2 * kv + 1, dim), 7.0, device=DEV, dtype=torch.bfloat16)
+    parts = room[1:rows + 1, :heads + 2 * kv].split((heads, kv, kv), 1)
+    lmbp.attention_bwd(do, q, k, v, o, lse, dq=parts[0], dk=parts[1], dv=parts[2], **kw)
+    for got, ref in zip(parts, want):
+        assert torch.equal(got[:used], ref[:used]) and (got[used:] == 7).all() and not ref[used:].any()
+    assert (room[0] == 7).all() and (room[-1] == 7).all() and (room[:, -1] == 7).all()
