@@ -515,7 +515,7 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(BwdArgs a) {
 // fewer than 2 to a place for sequences of different lengths, 5 to 4 places where causal tiles of one length even each other out,
 // fewer than places else. A share has half the tiles that a place would have on average, if all sequences were of one length; at
 // most as many shares as fill the places, but 2 where the tiles nearly do, their sums at most 256 MiB. A longer sequence among
-// short ones is split by the kernel, which knows the lengths. Backward, us, causal unless said: 4096 tokens of 8 heads on 1 230 (one share
+// short ones is split by the kernel, which knows the lengths, but where the average is a quarter of a share or less. Backward, us, causal unless said: 4096 tokens of 8 heads on 1 230 (one share
 // 1276, 2 707, 32 248); 16384 tokens of the same 2150 (64 shares 1948); 1024 tokens of 32 on 8 86 (16 shares 106); 8192 tokens of 8 on 8 (512
 // blocks) 560 (one share 597), not causal 866 in one (907 in 2), 12288 tokens (768) 1041 in one (1094); 16384 of 32 on 8 (1024): dk and dv 3926 in
 // one (4757: shares read different rows). Packed sequences of 1 to 2048, 32 on 8 (552): 473 (one share 528, 4 560), of 1 to 4048 (800) 1110 (1220).
@@ -529,7 +529,7 @@ static void row_shares(const AttentionPlan& a, int cus, int& shares, int& share)
   if (blocks == 0 || bytes == 0 || rows == 0) return;
   share = int(std::max<int64_t>(8, tiles * average * a.kv_heads / (a.causal ? 4 : 2) / places));
   const int64_t enough = a.q_starts || a.k_starts ? 2 * places : a.causal ? places * 5 / 4 : places;
-  if (blocks >= enough) return;
+  if (blocks >= enough || (a.q_starts && 4 * average <= share)) return;
   const int64_t most = std::max<int64_t>(2, places / blocks);
   shares = int(std::max<int64_t>(1, std::min<int64_t>({most, (rows + share - 1) / share, (int64_t(256) << 20) / bytes})));
 }

@@ -254,3 +254,29 @@ def test_gradients_inside_guards():
     for got, ref in zip(parts, want):
         assert torch.equal(got[:used], ref[:used]) and (got[used:] == 7).all() and not ref[used:].any()
     assert (room[0] == 7).all() and (room[-1] == 7).all() and (room[:, -1] == 7).all()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("spare", [0, 5])
+def test_more_than_512_sequences(causal, spare):
+    """The same as one call per sequence's tokens side by side: lengths of 0 to 3, one of 150, rows of no sequence behind them."""
+    lengths = [(5 * i * i + i) % 4 for i in range(1100)]
+    lengths[700] = 150
+    total = sum(lengths)
+    q, k, v, do = (normal((total + spare, h, 64), i) for i, h in enumerate((2, 1, 1, 2)))
+    kw = dict(causal=causal, q_starts=starts_of(lengths))
+    o, lse = lmbp.attention_fwd(q, k, v, **kw)
+    dq, dk, dv = lmbp.attention_bwd(do, q, k, v, o, lse, **kw)
+    assert not any(t[total:].any() for t in (o, dq, dk, dv)) and (lse[total:] == -math.inf).all()
+    row = 0
+    for i, n in enumerate(lengths):
+        if n > 0 and (i % 50 < 3 or n > 3 or i > 1080):
+            at = slice(row, row + n)
+            for h in range(2):
+                P.check_forward(o[at, h], lse[at, h], q[at, h], k[at, 0], v[at, 0], causal, 64 ** -0.5, f"sequence {i}")
+                parts = P.back_with_room(*(t.double() for t in (do[at, h], q[at, h], k[at, 0], v[at, 0], o[at, h], lse[at, h])), causal, 64 ** -0.5)
+                P.inside(dq[at, h], parts[0], parts[3][0] + P.half(torch.bfloat16) * parts[0].abs(), f"sequence {i}: dq")
+        row += n
+    picked = slice(sum(lengths[:700]), sum(lengths[:701]))   # the long one by itself
+    alone = lmbp.attention_fwd(q[picked], k[picked], v[picked], causal)
+    assert torch.equal(alone[0], o[picked]) and torch.equal(alone[1], lse[picked])
