@@ -1247,13 +1247,13 @@ def attention_fwd(q, k, v, causal=False, scale=None, q_starts=None, k_starts=Non
     sequences + 1, from 0 on; k_starts that are not given are q_starts where k has q's rows), and of each
     only ``k_lens`` (int32) keys may be in use (a padded cache). Causal: the last query sees the last key. scale:
     dim ** -0.5 unless given.
-    Rows of no sequence are zeros (lse -inf); in an o and lse given here they stay as they were."""
+    Rows of no sequence are zeros (lse -inf); where o and lse are both given they stay as they were."""
     if _fast is not None and o is None and lse is None and stream is None:
         out = _fast.attention_forward(_address["attention_fwd"], _address["lmbp_attention_fwd_bytes"], q, k, v, causal, scale, q_starts,
                                       k_starts, k_lens)
         if out is not None:
             return _done("attention_fwd", out)
-    fill = o is None and lse is None
+    fill = o is None or lse is None
     plan, lq, lk, lv = _attention(q, k, v, causal, scale, q_starts, k_starts, k_lens, fill)
     o = _heads_out(o, q, "o")
     lo = _heads(o, "o", q)

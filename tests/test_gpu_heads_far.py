@@ -280,3 +280,20 @@ def test_more_than_512_sequences(causal, spare):
     picked = slice(sum(lengths[:700]), sum(lengths[:701]))   # the long one by itself
     alone = lmbp.attention_fwd(q[picked], k[picked], v[picked], causal)
     assert torch.equal(alone[0], o[picked]) and torch.equal(alone[1], lse[picked])
+
+
+def test_one_result_given():
+    """Where one of o and lse is allocated by the call, rows of no sequence are zeros and -inf in both; with both given they stay."""
+    q, k, v = normal((50, 2, 64), 1), normal((50, 2, 64), 2), normal((50, 2, 64), 3)
+    kw = dict(q_starts=starts_of([20, 17]))
+    want = lmbp.attention_fwd(q, k, v, **kw)
+    full = lambda: (torch.full_like(q, 7.0), torch.full((50, 2), 7.0, device=DEV))
+    trash = [torch.full((50, 2), 9.0, device=DEV) for _ in range(20)]   # what a new lse may find
+    del trash
+    for given in ({"o": full()[0]}, {"lse": full()[1]}):
+        got = lmbp.attention_fwd(q, k, v, **given, **kw)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert not got[0][37:].any() and (got[1][37:] == -math.inf).all()
+    o, lse = full()
+    lmbp.attention_fwd(q, k, v, o=o, lse=lse, **kw)
+    assert torch.equal(o[:37], want[0][:37]) and (o[37:] == 7).all() and torch.equal(lse[:37], want[1][:37]) and (lse[37:] == 7).all()
