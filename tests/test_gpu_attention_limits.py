@@ -1,0 +1,47 @@
+"""Attention where keys are not in use, where scores or factors are infinite, and where a group is very large: what the
+definition gives, in whichever form the sizes take."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2406_16282_amd as lmbp
+import plain_heads as P
+from test_gpu_attention import check_all, normal, starts_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+INF, NAN = math.inf, math.nan
+
+
+# (heads, kv_heads, rows, cache rows, keys in use): a key tile's rows in one share, in several, and a tile that no key in use is in
+UNUSED = [(64, 64, 40, 100, 70), (16, 1, 600, 130, 33), (2, 2, 33, 300, 1), (12, 4, 197, 197, 196)]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("what", ["low scores", "infinite do", "NaN q"])
+@pytest.mark.parametrize("heads,kv_heads,rows,room,used", UNUSED)
+def test_gradients_of_keys_not_in_use_are_zeros(heads, kv_heads, rows, room, used, what, dim, causal):
+    """Whatever the queries hold: logarithms of sums far below 0 (a key of zeros would weigh 2^130 and more), rows that are not finite."""
+    q, do = normal((2, rows, heads, dim), 1), normal((2, rows, heads, dim), 2)
+    k, v = normal((2, room, kv_heads, dim), 3), normal((2, room, kv_heads, dim), 4)
+    if what == "low scores":   # every score at most -200 sqrt(dim)
+        q, k = q.abs() + 2, -(k.abs() + 100)
+    elif what == "infinite do":
+        do[:, rows // 2, :, 1] = INF
+    else:
+        q[:, rows // 3] = NAN
+    lens = torch.tensor([used, room], device=DEV, dtype=torch.int32)
+    kw = dict(causal=causal, k_lens=lens)
+    o, lse = lmbp.attention_fwd(q, k, v, **kw)
+    _, dk, dv = lmbp.attention_bwd(do, q, k, v, o, lse, **kw)
+    assert (dk[0, used:] == 0).all() and (dv[0, used:] == 0).all()
+    if what == "low scores":
+        assert lse.max() < -100 and dk.isfinite().all() and dv.isfinite().all()
+    # a call that leaves them alone has the same gradients of the keys in use
+    mine = [torch.full_like(t, 7.0) for t in (q, k, v)]
+    lmbp.attention_bwd(do, q, k, v, o, lse, **kw, dq=mine[0], dk=mine[1], dv=mine[2])
+    for got, want in zip(mine[1:], (dk, dv)):
+        assert torch.equal(got[0, :used].view(torch.int16), want[0, :used].view(torch.int16)) and (got[0, used:] == 7).all()
