@@ -455,9 +455,9 @@ __device__ inline void add_guarded(f32x16 (&acc)[D / 32], const uint16_t* tile, 
 }
 
 // Stores 32 rows' results times f, rounded: lane l has row l % 32; the halves exchange pieces, so that each lane
-// stores 16 bytes at a time.
+// stores 16 bytes at a time. keep: the bits of a row's values that are stored, all or none.
 template <int D>
-__device__ inline void store_columns(const f32x16 (&v)[D / 32], float f, uint16_t* row, bool real, int dim) {
+__device__ inline void store_columns(const f32x16 (&v)[D / 32], float f, uint16_t* row, bool real, int dim, uint32_t keep = ~0u) {
   const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
@@ -473,7 +473,7 @@ __device__ inline void store_columns(const f32x16 (&v)[D / 32], float f, uint16_
         out[2 + i] = both[1];
       }
       const int col = 32 * b + 16 * u + 8 * h;
-      if (real && col < dim) *reinterpret_cast<u32x4*>(row + col) = out;
+      if (real && col < dim) *reinterpret_cast<u32x4*>(row + col) = out & keep;
     }
 }
 

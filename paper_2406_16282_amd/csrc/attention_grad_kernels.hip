@@ -469,17 +469,10 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(Bwd
       }
     return;
   }
-  if (__any(!used)) {   // zeros, not a factor of 0: a key of zeros weighs exp(-lse), which may be infinite or NaN
-#pragma unroll
-    for (int b = 0; b < T::kBlocks; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        w.dk[b][i] = used ? w.dk[b][i] : 0.0f;
-        w.dv[b][i] = used ? w.dv[b][i] : 0.0f;
-      }
-  }
-  store_columns<D>(w.dk, e.s.scale, e.dk.p + (p.k0 + key) * e.dk.row + head * e.dk.head, real, e.s.dim);
-  store_columns<D>(w.dv, 1.0f, e.dv.p + (p.k0 + key) * e.dv.row + head * e.dv.head, real, e.s.dim);
+  // zeros, not a factor of 0: a key of zeros weighs exp(-lse), which may be infinite or NaN
+  const uint32_t keep = used ? ~0u : 0u;
+  store_columns<D>(w.dk, e.s.scale, e.dk.p + (p.k0 + key) * e.dk.row + head * e.dk.head, real, e.s.dim, keep);
+  store_columns<D>(w.dv, 1.0f, e.dv.p + (p.k0 + key) * e.dv.row + head * e.dv.head, real, e.s.dim, keep);
 }
 
 // The shares' sums of dk and dv, in order: a block per tile of 128 keys, head and quarter of its values, which it reads all at once.
