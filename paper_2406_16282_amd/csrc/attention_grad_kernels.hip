@@ -345,8 +345,9 @@ struct RowTiles {
 __device__ inline RowTiles row_tiles(const BwdArgs& a, const Part& p, int key0) {
   const int rows = p.q_len * a.s.group, off = p.k_len - p.q_len;
   RowTiles r;
-  r.lowest = a.s.causal && key0 > off ? (key0 - off) * a.s.group / kRows : 0;
-  r.all = key0 < p.k_len && r.lowest * kRows < rows ? (rows + kRows - 1) / kRows - r.lowest : 0;
+  const bool any = key0 < p.k_len;   // keys in use
+  r.lowest = a.s.causal && any && key0 > off ? (key0 - off) * a.s.group / kRows : 0;
+  r.all = any && r.lowest * kRows < rows ? (rows + kRows - 1) / kRows - r.lowest : 0;
   const int want = (r.all + a.share - 1) / a.share;
   r.shares = want < 1 ? 1 : want < a.shares ? want : a.shares;
   return r;
@@ -372,7 +373,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(Bwd
   const int wave = wave_in_block(), lane = threadIdx.x & (kWave - 1);
   const int key_b = p.tile * 128, key_w = key_b + wave * 32;
   const int rows = p.q_len * s.group, off = p.k_len - p.q_len;
-  auto first_row = [&](int j) { return s.causal && j > off ? (j - off) * s.group : 0; };   // that sees key j
+  // that sees key j; rows of a tile behind the last key stand at it, since times the group's heads they may pass 32 bits
+  auto first_row = [&](int j) {
+    const int n = (j < p.k_len ? j : p.k_len - 1) - off;
+    return s.causal && n > 0 ? n * s.group : 0;
+  };
   Keys<D> w;
 #pragma unroll
   for (int b = 0; b < T::kBlocks; ++b) w.dk[b] = w.dv[b] = f32x16{};

@@ -45,3 +45,22 @@ def test_gradients_of_keys_not_in_use_are_zeros(heads, kv_heads, rows, room, use
     lmbp.attention_bwd(do, q, k, v, o, lse, **kw, dq=mine[0], dk=mine[1], dv=mine[2])
     for got, want in zip(mine[1:], (dk, dv)):
         assert torch.equal(got[0, :used].view(torch.int16), want[0, :used].view(torch.int16)) and (got[0, used:] == 7).all()
+
+
+def test_a_group_of_many_millions_of_heads():
+    """Rows of a key tile behind the last key, times the heads of a group, pass 32 bits: the mask of the keys in use holds. Two queries of 17
+    million heads on one key head: the first query's gradient comes to the first key alone."""
+    heads = 17_000_000
+    room = lambda fill: torch.full((heads, 2, 8), fill, device=DEV, dtype=torch.bfloat16).transpose(0, 1)
+    q, o, dq, do = room(0.0), room(7.0), room(7.0), room(0.0)
+    do[0] = 1.0
+    k = torch.ones(2, 1, 8, device=DEV, dtype=torch.bfloat16)
+    v = torch.tensor([1.0, 3.0], device=DEV, dtype=torch.bfloat16)[:, None, None].repeat(1, 1, 8)
+    lse = torch.empty(2, heads, device=DEV)
+    lmbp.attention_fwd(q, k, v, causal=True, o=o, lse=lse)
+    assert (o[0] == 1).all() and (o[1] == 2).all()
+    dk, dv = torch.empty_like(k), torch.empty_like(k)
+    lmbp.attention_bwd(do, q, k, v, o, lse, causal=True, dq=dq, dk=dk, dv=dv)
+    assert (dq == 0).all() and (dk == 0).all() and (dv[1] == 0).all()
+    # P is within 4 u of 1; sums of ones are whole numbers: at most 2^24 of them exact, beyond that u each of 512 shares
+    assert ((dv[0].double() - heads).abs() <= heads * (P.half(torch.bfloat16) + 520 * P.U)).all()
