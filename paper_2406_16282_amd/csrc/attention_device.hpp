@@ -409,6 +409,19 @@ __device__ inline bool tile_is_odd(const uint16_t* tile, int* flags, int which) 
   return uniform(*const_cast<volatile int*>(flags + which)) != 0;
 }
 
+// Whether a wave's fragments hold an infinity or NaN.
+template <int N>
+__device__ inline bool any_odd(const bf16x8 (&f)[N]) {
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int s = 0; s < N; ++s) {
+    const u32x4 w = __builtin_bit_cast(u32x4, f[s]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[j] & 0x7fff7fffu));
+  }
+  return __any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
+}
+
 // acc += tile^T p for 16 rows of the tile of which a column sees those of `see`, and the others, where p is 0, may
 // hold anything. Infinities and NaN are looked for first; where there are any they are taken out of the product and go to
 // the columns that see them, counted by a product with ones. NANS: an infinity too makes NaN.

@@ -227,7 +227,7 @@ struct Keys {
   using T = Tile<D>;
   bf16x8 k[T::kSteps];
   f32x16 dk[T::kBlocks], dv[T::kBlocks];
-  int from;   // packed rows from it on see this lane's key
+  int from, rows;   // packed rows from the first on see this lane's key; all of them
 
   // The lse and D of this lane's rows 2 i and 2 i + 1 (of its 16).
   static __device__ inline f32x4 stats_of(const float* stats, int i) {
@@ -309,12 +309,14 @@ struct Keys {
       y = mfma(rd.rows(O, 0, s), rd.rows(V, mine, s), y);
     }
     __builtin_amdgcn_sched_barrier(0);
+    // rows behind the last one are zeros, of which a key with an infinity would make NaN
     const int skip = from - row0 - 4 * ((threadIdx.x >> 5) & 1);
+    const uint32_t count = uint32_t(rows - from);
 #pragma unroll
     for (int i = 0; i < 8; ++i) weights(x, y, stats_of(stats, i), i, c);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const bool sees = 8 * (i / 4) + i % 4 >= skip;
+      const bool sees = uint32_t(8 * (i / 4) + i % 4 - skip) < count;
       x[i] = sees ? x[i] : 0.0f;
       y[i] = sees ? y[i] : 0.0f;
     }
@@ -324,7 +326,7 @@ struct Keys {
     for (int t = 0; t < 2; ++t) {
       const bf16x8 pt = t == 0 ? p[0] : p[1], dt = t == 0 ? ds[0] : ds[1];
       if constexpr (GUARD) {
-        const bf16x8 see = seen_of(row0 + 16 * t, from, 0x7fffffff);
+        const bf16x8 see = seen_of(row0 + 16 * t, from, rows);
         add_guarded<false, D>(dv, O, rd, 16 * t, pt, see);
         add_guarded<true, D>(dk, Q, rd, 16 * t, dt, see);
       } else {
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(Bwd
   const int each = (rt.all + rt.shares - 1) / rt.shares;
   const int begin = uniform(rt.lowest + part * each);
   const int end = uniform(rt.lowest + (part * each + each < rt.all ? part * each + each : rt.all));
-  const int masked = uniform((first_row(key_b + 127) + kRows - 1) / kRows);   // tiles from it on need no mask
+  int masked = uniform((first_row(key_b + 127) + kRows - 1) / kRows);   // tiles from it on need no mask
 
   const Loader<D, kRows, 4> ld(wave, s.dim);
   Reader<D> rd;
@@ -432,6 +434,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(Bwd
   };
   auto q_of = [&]() { return lds + (t & 1) * 2 * kTile; };
   auto st_of = [&]() { return stats + (t & 1) * kRows * 2; };
+  // Nor do rows behind the last one, zeros that weigh exp(0) and add 0: but where one of the wave's keys holds an infinity they
+  // would weigh NaN.
+  if (rows % kRows != 0 && any_odd(w.k)) masked = 0x7fffffff;
   for (; t >= begin && t >= masked; --t) {
     next();
     w.whole(q_of(), q_of() + kTile, V, wave * 32, st_of(), rd, c);
@@ -440,6 +445,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attention_dkv_kernel(Bwd
   const int key = key_w + (lane_again() & 31);
   const bool used = key < p.k_len;
   w.from = first_row(key);
+  w.rows = rows;
   // A row of q or do that holds an infinity or NaN has such an lse or D (so has one that sees no key): where no row
   // of a tile has, unseen rows' zeros as factors are all that a mask takes.
   bool odd = false;

@@ -64,3 +64,27 @@ def test_a_group_of_many_millions_of_heads():
     assert (dq == 0).all() and (dk == 0).all() and (dv[1] == 0).all()
     # P is within 4 u of 1; sums of ones are whole numbers: at most 2^24 of them exact, beyond that u each of 512 shares
     assert ((dv[0].double() - heads).abs() <= heads * (P.half(torch.bfloat16) + 520 * P.U)).all()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim,n", [(2, 2, 64, 150), (2, 2, 128, 160), (4, 1, 128, 33), (3, 1, 64, 65), (1, 1, 128, 5), (6, 2, 40, 300)])
+def test_a_key_that_weighs_nothing(heads, kv_heads, dim, n, causal):
+    """A key that holds an infinity and whose scores are all -inf: no weight and gradients of 0, as one far below the others, also where
+    the rows end inside a tile (what is behind them is no row). dq has its infinity times 0 in one column."""
+    at, col = 2, 5
+    q, do = normal((n, heads, dim), 1), normal((n, heads, dim), 2)
+    k, v = normal((n, kv_heads, dim), 3), normal((n, kv_heads, dim), 4)
+    q[:, :, col] = 1.0
+    kw = dict(causal=causal, q_starts=starts_of([n]))
+    k[at, :, col] = -1e4   # weighs 0 in fp32 beside any other key of these
+    clean = lmbp.attention_fwd(q, k, v, **kw)
+    want = lmbp.attention_bwd(do, q, k, v, *clean, **kw)
+    assert (want[2][at] == 0).all()
+    k[at, :, col] = -INF
+    o, lse = lmbp.attention_fwd(q, k, v, **kw)
+    assert torch.equal(o, clean[0]) and torch.equal(lse, clean[1])
+    dq, dk, dv = lmbp.attention_bwd(do, q, k, v, o, lse, **kw)
+    assert torch.equal(dk, want[1]) and torch.equal(dv, want[2])
+    rest = [c for c in range(dim) if c != col]
+    sees = at if causal else 0   # the first query that sees the key
+    assert torch.equal(dq[..., rest], want[0][..., rest]) and dq[sees:, :, col].isnan().all() and dq[:sees].isfinite().all()
