@@ -20,7 +20,7 @@ struct FwdArgs {
   Heads q, k, v, o;
   float* lse;        // [rows][heads]
   float* part;       // splits > 1: [splits][rows * heads][dim], unnormalised
-  float* stats;      // splits > 1: [splits][rows * heads][2]: running maximum (log2), sum
+  float* stats;      // splits > 1: [splits][rows * heads][2]: running maximum (log2), sum; kNoKeys where the row sees none of the share
   int splits;
   int64_t first;     // block number of this launch's first block
   uint32_t per_xcd;
@@ -30,6 +30,8 @@ constexpr int kKeys = 64;      // keys to a tile
 // A row's running maximum may stay this much (log2) behind its largest score, so that sums are seldom rescaled: exponentials up to 2^8
 // lose nothing in fp32 or bf16. 16384 tokens 2064 us, without 2156.
 constexpr float kSlack = 8.0f;
+
+constexpr float kNoKeys = -1.0f;   // no sum: one of 0 has keys whose scores are all -inf
 
 // One wave's 32 rows over keys in LDS.
 template <int D>
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
     if (h == 0) {
       float* st = e.stats + (int64_t(split) * e.s.q.rows * e.s.heads + out_row) * 2;
       st[0] = w.top;
-      st[1] = sum;
+      st[1] = begin < end && begin * kKeys < w.limit ? sum : kNoKeys;
     }
     return;
   }
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(FwdArgs a
     if (joined) {
       float* st = e.stats + (int64_t(split) * e.s.q.rows * e.s.heads + out_row) * 2;
       st[0] = top;
-      st[1] = sum;
+      st[1] = begin < end && begin * kT < w.limit ? sum : kNoKeys;
     } else {
       e.lse[out_row] = w.limit > 0 ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
       norm[in] = w.limit > 0 ? 1.0f / sum : 0.0f;
@@ -403,13 +405,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(FwdArgs a) {
   const int64_t row = a.first + blockIdx.x, count = s.q.rows * s.heads, token = row / s.heads;
   if (s.q.starts != nullptr && token >= s.q.starts[s.batch]) return;   // a row of no sequence
   const int lane = threadIdx.x & (kWave - 1), wave = wave_in_block();
-  // lane i has share i's maximum and sum; a share without keys counts nothing
-  float m = kLowest, l = 0.0f;
+  // lane i has share i's maximum and sum; a share without keys counts nothing, one whose scores are all -inf weighs 0
+  float m = kLowest, l = kNoKeys;
   if (lane < a.splits) {
     m = a.stats[(lane * count + row) * 2];
     l = a.stats[(lane * count + row) * 2 + 1];
   }
-  const bool none = l == 0.0f && m == kLowest;
+  const bool none = l == kNoKeys;
   float top = m;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));

@@ -88,3 +88,31 @@ def test_a_key_that_weighs_nothing(heads, kv_heads, dim, n, causal):
     rest = [c for c in range(dim) if c != col]
     sees = at if causal else 0   # the first query that sees the key
     assert torch.equal(dq[..., rest], want[0][..., rest]) and dq[sees:, :, col].isnan().all() and dq[:sees].isfinite().all()
+
+
+# (heads, kv_heads, rows, keys): few queries in one share and in several, 128 rows to a block in one share and in several
+FORMS = [(8, 2, 1, 300), (8, 2, 1, 600), (8, 2, 3, 20000), (1, 1, 256, 16384), (2, 2, 200, 200)]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,kv_heads,rows,keys", FORMS)
+def test_rows_all_of_whose_scores_are_minus_infinity(heads, kv_heads, rows, keys, dim):
+    """Scores that overflow: the definition has no weights (NaN) and a logarithm of -inf, in any form; no other row changes."""
+    q, k, v = normal((rows, heads, dim), 1), normal((keys, kv_heads, dim), 2), normal((keys, kv_heads, dim), 3)
+    k[:, :, 0] = -1024.0
+    q[:, :, 0] = 0.0
+    clean = lmbp.attention_fwd(q, k, v)
+    head = heads - 1
+    q[rows // 2, head] = 0.0
+    q[rows // 2, head, 0] = 2.0 ** 127
+    o, lse = lmbp.attention_fwd(q, k, v)
+    assert o[rows // 2, head].isnan().all() and lse[rows // 2, head] == -INF
+    keep = torch.ones(rows, heads, dtype=torch.bool, device=DEV)
+    keep[rows // 2, head] = False
+    assert torch.equal(o[keep], clean[0][keep]) and torch.equal(lse[keep], clean[1][keep])
+    # one key with a score among the others has all of the weight, and no key at all gives 0
+    k[keys // 3, :, 0] = 0.0
+    o, lse = lmbp.attention_fwd(q, k, v)
+    assert torch.equal(o[rows // 2, head], v[keys // 3, kv_heads - 1]) and lse[rows // 2, head] == 0
+    o, lse = lmbp.attention_fwd(q, k, v, k_lens=torch.zeros(1, device=DEV, dtype=torch.int32))
+    assert (o == 0).all() and (lse == -INF).all()
