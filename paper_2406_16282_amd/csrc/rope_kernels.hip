@@ -196,6 +196,27 @@ struct Place {
       y[e] = bf16 ? BF16::load1(g, j) : F32::load1(g, j);
     }
   }
+  // Pair e turned. Columns behind the pairs are left as they are: not by an angle of 0, since 0 times an infinite neighbour is NaN.
+  __device__ inline void turn(int e, float p, float q, float c, float s, float& x, float& y) const {
+    const bool turns = pair + e < half;
+    x = turns ? __builtin_fmaf(p, c, -q * s) : p;
+    y = turns ? __builtin_fmaf(p, s, q * c) : q;
+  }
+  // This lane's pairs turned. VEC: whether all do is asked once (a select for every pair: 43.1 us for 40.4 at 8192 tokens of 32 + 32
+  // heads of 72, norm and turn; element by element it is the other way round, 122 and 129).
+  __device__ inline void turn(float (&x)[E], float (&y)[E], const float (&c)[E], const float (&s)[E]) const {
+    if (VEC && pair + E <= half) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float p = x[e], q = y[e];
+        x[e] = __builtin_fmaf(p, c[e], -q * s[e]);
+        y[e] = __builtin_fmaf(p, s[e], q * c[e]);
+      }
+    } else if constexpr (FORM != kHalves) {   // halves turn in whole pieces
+#pragma unroll
+      for (int e = 0; e < E; ++e) turn(e, x[e], y[e], c[e], s[e], x[e], y[e]);
+    }
+  }
   // The columns of pair e.
   __device__ inline int column_a(int e) const { return VEC ? (interleaved ? a + 2 * e : a + e) : first(e); }
   __device__ inline int column_b(int e) const { return VEC ? (interleaved ? a + 2 * e + 1 : b + e) : second(e); }
@@ -218,7 +239,7 @@ __device__ inline void cos_sin(uint64_t turns, float& c, float& s) {
 }
 
 // Cosines and sines of a token's pairs: each formed once, by one lane of the wave, and handed to the lanes that hold the pair's
-// columns through LDS of the wave's own (`table`: kRopePairs cosines, then sines; 1 and 0 behind the pairs).
+// columns through LDS of the wave's own (`table`: kRopePairs cosines, then sines; behind the pairs there are numbers that nothing uses).
 template <class IO, int FORM>
 __device__ inline void angles(const Args& f, const Place<IO, FORM>& at, int64_t token, float* table, float (&c)[IO::kPerVec],
                               float (&s)[IO::kPerVec]) {
@@ -313,12 +334,7 @@ __global__ __launch_bounds__(256) void rope_kernel(Args f) {
           float a[E], b[E];
           at.unpack(rx[j], a, b);
           if constexpr (MODE == kTurn) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float p = a[e], q = b[e];
-              a[e] = __builtin_fmaf(p, c[e], -q * s[e]);
-              b[e] = __builtin_fmaf(p, s[e], q * c[e]);
-            }
+            at.turn(a, b, c, s);
           } else if constexpr (kForward) {
             float sq = 0.0f;
 #pragma unroll
@@ -338,14 +354,14 @@ __global__ __launch_bounds__(256) void rope_kernel(Args f) {
             if (real && (lane & (f.lanes - 1)) == 0) d.rstd[token * d.heads + head] = r * unit_;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-              float p = a[e] * unit_ * r, q = b[e] * unit_ * r;
+              a[e] = a[e] * unit_ * r;
+              b[e] = b[e] * unit_ * r;
               if constexpr (kGain) {
-                p *= ga[e];
-                q *= gb[e];
+                a[e] *= ga[e];
+                b[e] *= gb[e];
               }
-              a[e] = __builtin_fmaf(p, c[e], -q * s[e]);
-              b[e] = __builtin_fmaf(p, s[e], q * c[e]);
             }
+            at.turn(a, b, c, s);
           } else {
             float p[E], q[E];
             at.unpack(rk[j], p, q);
@@ -357,14 +373,15 @@ __global__ __launch_bounds__(256) void rope_kernel(Args f) {
               along = sum_lanes(along, f.lanes) / float(f.dim);
 #pragma unroll
               for (int e = 0; e < E; ++e) {
-                const float v = r * __builtin_fmaf(-p[e], along, a[e]), w = r * __builtin_fmaf(-q[e], along, b[e]);
-                a[e] = __builtin_fmaf(v, c[e], -w * s[e]);
-                b[e] = __builtin_fmaf(v, s[e], w * c[e]);
+                a[e] = r * __builtin_fmaf(-p[e], along, a[e]);
+                b[e] = r * __builtin_fmaf(-q[e], along, b[e]);
               }
+              at.turn(a, b, c, s);
             } else {
 #pragma unroll
-              for (int e = 0; e < E; ++e) {
-                const float v = __builtin_fmaf(a[e], c[e], -b[e] * s[e]), w = __builtin_fmaf(a[e], s[e], b[e] * c[e]);
+              for (int e = 0; e < E; ++e) {   // pair by pair: the branch of a whole lane costs this kernel registers that it has not
+                float v, w;
+                at.turn(e, a[e], b[e], c[e], s[e], v, w);
                 p[e] *= r;
                 q[e] *= r;
                 sum_a[e] = __builtin_fmaf(real ? v : 0.0f, real ? p[e] : 0.0f, sum_a[e]);

@@ -1,0 +1,69 @@
+"""Rotation of part of a head's columns beside columns that are not finite, positions of any size, rows of no sequence and
+heads that lie inside each other's rows."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2406_16282_amd as lmbp
+import plain_heads as P
+from paper_2406_16282_amd import binding as B
+from paper_2406_16282_amd import nn as lnn
+from test_gpu_attention import normal, starts_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 1e-5
+INF, NAN = math.inf, math.nan
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+
+# (dim, pairs, interleaved): pieces of 16 and of 8 bytes, element by element, a lane whose pairs turn in part, no pair at all
+PART = [(128, 32, False), (64, 16, True), (72, 18, False), (80, 4, True), (96, 21, True), (7, 3, False), (7, 2, True), (40, 5, False), (64, 0, False)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim,pairs,interleaved", PART)
+def test_columns_that_do_not_turn_are_left_as_they_are(dim, pairs, interleaved, dtype):
+    """To the bit: infinities, NaN beside numbers, zeros of either sign."""
+    r = B.Rotation([0.7 ** p for p in range(pairs)], None, interleaved)
+    x = normal((9, 5, dim), 1).to(dtype)
+    clean = x.clone()
+    still = range(2 * pairs, dim)
+    for i, c in enumerate(still):
+        if i % 2 == 0:
+            x[i % 9, :, c] = (INF, -INF, NAN)[i // 2 % 3]
+        x[(i + 4) % 9, :, c] = -0.0
+    pos = torch.arange(9, device=DEV) * 37
+    for op in (lmbp.rope_fwd, lmbp.rope_bwd):
+        y = op(x, x[:, :2], pos, r)
+        want = op(clean, None, pos, r)[0]
+        assert torch.equal(bits(y[0][..., 2 * pairs:]), bits(x[..., 2 * pairs:])) and torch.equal(y[0][..., :2 * pairs], want[..., :2 * pairs])
+        assert torch.equal(bits(y[1]), bits(y[0][:, :2]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim,pairs,interleaved", PART)
+def test_norm_beside_columns_that_do_not_turn(dim, pairs, interleaved, dtype):
+    """An infinite mean square has rstd 0, which leaves 0 of every finite column and NaN of the infinite one alone; an infinite gradient of a
+    column that does not turn reaches the gain of that column alone."""
+    if 2 * pairs == dim:
+        pytest.skip("every column turns")
+    r = B.Rotation([0.7 ** p for p in range(pairs)], None, interleaved)
+    x, dy = normal((9, 5, dim), 1).to(dtype), normal((9, 5, dim), 2).to(dtype)
+    col = dim - 1
+    pos = torch.arange(9, device=DEV) * 37
+    one = torch.ones(dim, device=DEV)
+    spoilt = x.clone()
+    spoilt[4, 2, col] = INF
+    for gain in (None, one):
+        y, _, rstd, _ = lmbp.msrms_rope_fwd(spoilt, None, EPS, pos, r, gain)
+        assert y[4, 2, col].isnan() and (y[4, 2, :col] == 0).all() and rstd[4, 2] == 0
+    dy[4, 2, col] = INF
+    rstd = lmbp.msrms_rope_fwd(x, None, EPS, pos, r, one)[2]
+    dgain = lmbp.msrms_rope_bwd(dy, None, x, None, rstd, None, pos, r, one)[2]
+    assert dgain[:col].isfinite().all() and dgain[col].isinf()
