@@ -450,7 +450,8 @@ lmbp_status rope_bwd(lmbp_dtype dt, const lmbp_rope *r, const lmbp_heads *dq, co
  *           dx = turned back (rstd (dy - y D^-1 (y . dy))).
  *           With gain from x: g = dy turned back, dz = gain g, dx = rstd (dz - z D^-1 (z . dz)),
  *           dgain = sum of g z over tokens and heads, in fp32 in an order fixed by the sizes.
- *           The products y . dy (z . dz) have to be among fp32's numbers.
+ *           The products y . dy (z . dz) have to be among fp32's numbers. A head that is not finite (rstd 0 or NaN) and whose dy
+ *           is zeros gets zeros and adds nothing to dgain: rows of no sequence may hold anything.
  *
  *   eps     : finite, > 0. rstd_q, rstd_k: fp32 [tokens][heads].
  *   q_gain, k_gain : dim values of dt_gain (fp32 or bf16), both NULL or (k_gain only with k_heads) both given;

@@ -1163,7 +1163,8 @@ def msrms_rope_fwd(q, k, eps, positions, rotation, q_gain=None, k_gain=None, q_o
 def msrms_rope_bwd(dq, dk, q, k, rstd_q, rstd_k, positions, rotation, q_gain=None, k_gain=None, q_out=None, k_out=None,
                    stream=None):
     """Backward of msrms_rope_fwd. q and k: the forward's results without gains, its arguments with. Returns
-    (dq, dk) or, with gains, (dq, dk, dq_gain, dk_gain); q_out and k_out may be given, dq and dk included."""
+    (dq, dk) or, with gains, (dq, dk, dq_gain, dk_gain); q_out and k_out may be given, dq and dk included. A head that
+    is not finite and whose gradient is zeros gets zeros (rows of no sequence)."""
     if _fast is not None and stream is None and type(rotation) is Rotation:
         out = _fast.norm_rope_bwd(_address["msrms_rope_bwd"], _address["lmbp_msrms_rope_bwd_bytes"], dq, dk, q, k, rstd_q, rstd_k, positions,
                                   rotation._plan_at, q_gain, k_gain, q_out, k_out)

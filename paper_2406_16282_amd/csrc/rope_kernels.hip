@@ -198,7 +198,9 @@ struct Place {
   }
   // Pair e turned. Columns behind the pairs are left as they are: not by an angle of 0, since 0 times an infinite neighbour is NaN.
   __device__ inline void turn(int e, float p, float q, float c, float s, float& x, float& y) const {
-    const bool turns = pair + e < half;
+    int p0 = FORM == kHalves ? pair : pair + e;        // halves turn in whole pieces
+    if constexpr (FORM == kPairs) asm volatile("" : "+v"(p0));   // asked each time: held over the loop the answers take scalar registers
+    const bool turns = p0 < half;
     x = turns ? __builtin_fmaf(p, c, -q * s) : p;
     y = turns ? __builtin_fmaf(p, s, q * c) : q;
   }
@@ -212,7 +214,7 @@ struct Place {
         x[e] = __builtin_fmaf(p, c[e], -q * s[e]);
         y[e] = __builtin_fmaf(p, s[e], q * c[e]);
       }
-    } else if constexpr (FORM != kHalves) {   // halves turn in whole pieces
+    } else if constexpr (FORM != kHalves) {
 #pragma unroll
       for (int e = 0; e < E; ++e) turn(e, x[e], y[e], c[e], s[e], x[e], y[e]);
     }
@@ -365,8 +367,22 @@ __global__ __launch_bounds__(256) void rope_kernel(Args f) {
           } else {
             float p[E], q[E];
             at.unpack(rk[j], p, q);
-            const float r = rs[j];
-            float along = 0.0f;
+            float r = rs[j], along = 0.0f;
+            // a head that is not finite (its rstd is 0 or NaN) and gets no gradient gives none, whatever it holds
+            if (__any(!(r > 0.0f))) {
+              uint32_t any = 0u;
+#pragma unroll
+              for (int e = 0; e < E; ++e) any |= (__float_as_uint(a[e]) | __float_as_uint(b[e])) & 0x7fffffffu;
+              for (int off = f.lanes >> 1; off > 0; off >>= 1) any |= uint32_t(__shfl_xor(int(any), off, kWave));
+              uint32_t keep = r > 0.0f || any != 0u ? ~0u : 0u;   // a mask in a vector register: there is no scalar one left
+              asm volatile("" : "+v"(keep));
+              r = __uint_as_float(__float_as_uint(r) & keep);
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                p[e] = __uint_as_float(__float_as_uint(p[e]) & keep);
+                q[e] = __uint_as_float(__float_as_uint(q[e]) & keep);
+              }
+            }
             if constexpr (MODE == kNormBack) {
 #pragma unroll
               for (int e = 0; e < E; ++e) along = __builtin_fmaf(a[e], p[e], __builtin_fmaf(b[e], q[e], along));

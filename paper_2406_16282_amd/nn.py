@@ -586,7 +586,8 @@ class _QKVAttention(torch.autograd.Function):
 class QKVAttention(nn.Module):
     """Rotation and attention on the output of a block's fused projection: forward(qkv, positions) with qkv
     [sequences, rows, heads + 2 kv_heads, dim] (queries, keys, values) gives [sequences, rows, heads, dim]; packed as
-    [rows, ..] with ``starts`` (int32, sequences + 1). ``eps``: MS-RMSNorm of each query and key head in front of the
+    [rows, ..] with ``starts`` (int32, sequences + 1; rows behind the last one may hold anything, their output and gradient are zeros).
+    ``eps``: MS-RMSNorm of each query and key head in front of the
     rotation (without gains). One node: keeps the turned queries and keys, the values as they lie in qkv,
     the output and one fp32 value per row and head (with the norm one more per query and key head); the gradient comes as one
     tensor. To capture forward and backward of this or the modules above in a graph, let go of the eager graphs of the

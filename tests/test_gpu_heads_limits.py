@@ -67,3 +67,49 @@ def test_norm_beside_columns_that_do_not_turn(dim, pairs, interleaved, dtype):
     rstd = lmbp.msrms_rope_fwd(x, None, EPS, pos, r, one)[2]
     dgain = lmbp.msrms_rope_bwd(dy, None, x, None, rstd, None, pos, r, one)[2]
     assert dgain[:col].isfinite().all() and dgain[col].isinf()
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+def test_rows_of_no_sequence_may_hold_anything(bad):
+    """Padding behind the last start: zeros of output and gradient, the sequences' as without it."""
+    heads, kv_heads, dim, lengths = 6, 2, 64, [20, 100, 1, 29]
+    n, rows = sum(lengths), sum(lengths) + 11
+    r, pos = B.Rotation.of_base(dim), torch.arange(rows, device=DEV)
+    qkv, do = normal((rows, heads + 2 * kv_heads, dim), 1), normal((rows, heads, dim), 2)
+    qkv[n:], do[n:] = bad, bad
+    for eps in (None, EPS):
+        m = lnn.QKVAttention(heads, kv_heads, dim, r, eps=eps)
+        got = []
+        for x in (qkv, qkv[:n].contiguous()):
+            x = x.detach().requires_grad_()
+            o = m(x, pos[:len(x)], starts_of(lengths))
+            got.append((o, *torch.autograd.grad(o, x, do[:len(x)])))
+        for a, b in zip(*got):
+            assert torch.equal(a[:n], b) and (a[n:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gain", [False, True])
+@pytest.mark.parametrize("dim", [128, 72, 7])
+def test_heads_that_get_no_gradient_give_none(dim, gain, dtype):
+    """A head that is not finite, whose gradient is 0: zeros, and nothing to the gain's gradient. One that gets a gradient gives NaN."""
+    r = B.Rotation([0.7 ** p for p in range(dim // 4)])
+    x, dy = normal((9, 5, dim), 1).to(dtype), normal((9, 5, dim), 2).to(dtype)
+    pos = torch.arange(9, device=DEV)
+    w = (torch.ones(dim, device=DEV),) if gain else ()
+    dy[4, 2] = 0.0
+    dy[5, 1] = -0.0
+
+    def back(x):
+        y, _, rstd, _ = lmbp.msrms_rope_fwd(x, None, EPS, pos, r, *w)
+        return lmbp.msrms_rope_bwd(dy, None, x if gain else y, None, rstd, None, pos, r, *w)
+
+    want = back(x)
+    x[4, 2, 1], x[5, 1] = INF, NAN
+    got = back(x)
+    assert torch.equal(got[0], want[0]) and (got[0][4, 2] == 0).all()
+    if gain:
+        assert torch.equal(got[2], want[2])
+    x[6, 3, 0] = NAN
+    got = back(x)
+    assert got[0][6, 3].isnan().all() and (not gain or got[2].isnan().all())
