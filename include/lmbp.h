@@ -405,7 +405,7 @@ size_t lmbp_linear_bias_grad_bytes(int64_t m, int64_t n);
  * are the elements from one row, one head to the next (>= 0; 0 for inputs only). So queries, keys and values
  * may lie in the one output of a fused projection. Written tensors must not meet themselves: row at least
  * (heads - 1) head + dim, or head at least (rows - 1) row + dim. Two tensors of a call that are interleaved
- * without sharing an element (parts of the same rows) do not overlap.
+ * without sharing an element (parts of the same rows, or of the heads of rows: [rows][heads][3][dim]) do not overlap.
  * ------------------------------------------------------------------------ */
 typedef struct {
   void *data;

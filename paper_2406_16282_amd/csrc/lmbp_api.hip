@@ -9,6 +9,7 @@
 #include <cstdint>
 #include <initializer_list>
 #include <limits>
+#include <numeric>
 
 namespace {
 
@@ -612,17 +613,29 @@ bool meets_itself(const Part& p) {
   return !((by_row && p.t->row >= (p.heads - 1) * p.t->head + p.dim) || (by_head && p.t->head >= (p.rows - 1) * p.t->row + p.dim));
 }
 
-// Whether two tensors share memory: not if they lie in different parts of the same rows.
-bool share(const Part& a, const Part& b) {
-  if (!overlaps(a.span(), b.span())) return false;
-  if (a.eb != b.eb || a.t->row != b.t->row || a.t->row <= 0) return true;
-  const int64_t pitch = a.t->row * a.eb;
-  const int64_t wa = ((a.heads - 1) * a.t->head + a.dim) * a.eb, wb = ((b.heads - 1) * b.t->head + b.dim) * b.eb;
-  if (wa > pitch || wb > pitch) return true;
+// Whether two tensors share memory: not if they lie in different parts of the same rows, or of the heads of one row after the other
+// (queries, keys and values of each head side by side): then their elements' places differ modulo a step that all strides are
+// multiples of.
+bool apart(const Part& a, const Part& b, int64_t pitch, int64_t a_width, int64_t b_width) {
+  pitch *= a.eb;
+  a_width *= a.eb;
+  b_width *= a.eb;
+  if (pitch <= 0 || a_width > pitch || b_width > pitch) return false;
   const int64_t pa = int64_t(reinterpret_cast<uintptr_t>(a.t->data) % uint64_t(pitch));
   const int64_t pb = int64_t(reinterpret_cast<uintptr_t>(b.t->data) % uint64_t(pitch));
   const int64_t off = (pb - pa + pitch) % pitch;
-  return !(off >= wa && off + wb <= pitch);
+  return off >= a_width && off + b_width <= pitch;
+}
+bool share(const Part& a, const Part& b) {
+  if (!overlaps(a.span(), b.span())) return false;
+  if (a.eb != b.eb) return true;
+  if (a.t->row == b.t->row && apart(a, b, a.t->row, (a.heads - 1) * a.t->head + a.dim, (b.heads - 1) * b.t->head + b.dim)) return false;
+  int64_t step = 0;
+  for (const Part* p : {&a, &b}) {
+    if (p->rows > 1) step = std::gcd(step, p->t->row);
+    if (p->heads > 1) step = std::gcd(step, p->t->head);
+  }
+  return !apart(a, b, step, a.dim, b.dim);
 }
 
 bool same_place(const lmbp_heads& a, const lmbp_heads& b) { return a.data == b.data && a.row == b.row && a.head == b.head; }

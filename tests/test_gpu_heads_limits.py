@@ -113,3 +113,24 @@ def test_heads_that_get_no_gradient_give_none(dim, gain, dtype):
     x[6, 3, 0] = NAN
     got = back(x)
     assert got[0][6, 3].isnan().all() and (not gain or got[2].isnan().all())
+
+
+def test_heads_side_by_side_with_their_keys_and_values():
+    """Queries, keys and values of each head side by side ([rows, heads, 3, dim]): turned in place, gradients into one tensor."""
+    rows, heads, dim = 70, 4, 64
+    r, pos = B.Rotation.of_base(dim), torch.arange(rows, device=DEV)
+    qkv, do = normal((rows, heads, 3, dim), 1), normal((rows, heads, dim), 2)
+    q, k, v = (t.contiguous() for t in qkv.unbind(2))
+    yq, yk = lmbp.rope_fwd(q, k, pos, r)
+    x = qkv.clone()
+    lmbp.rope_fwd(x[:, :, 0], x[:, :, 1], pos, r, q_out=x[:, :, 0], k_out=x[:, :, 1])
+    assert torch.equal(x[:, :, 0], yq) and torch.equal(x[:, :, 1], yk) and torch.equal(x[:, :, 2], v)
+    o, lse = lmbp.attention_fwd(yq, yk, v, causal=True)
+    want = lmbp.attention_bwd(do, yq, yk, v, o, lse, causal=True)
+    for at in (slice(None), slice(0, 1)):   # one row, too
+        if at.stop == 1:
+            yq, yk, v, o, lse, do, x = yq[:1], yk[:1], v[:1], o[:1], lse[:1], do[:1], x[:1]
+            want = lmbp.attention_bwd(do, yq, yk, v, o, lse, causal=True)
+        d = torch.full_like(x, 7.0)
+        lmbp.attention_bwd(do, x[:, :, 0], x[:, :, 1], x[:, :, 2], o, lse, causal=True, dq=d[:, :, 0], dk=d[:, :, 1], dv=d[:, :, 2])
+        assert all(torch.equal(a, b) for a, b in zip(d.unbind(2), want))
