@@ -494,7 +494,7 @@ size_t lmbp_msrms_rope_bwd_bytes(int64_t dim);
  *   dt          : LMBP_BF16 (LMBP_EDTYPE otherwise).
  *   heads, kv_heads : kv_heads divides heads. dim: a multiple of 8, 8 .. 128.
  *   q_rows heads / kv_heads and k_rows : below 2^31 - 1024. batch >= 1.
- *   scale       : finite, > 0.
+ *   scale       : > 0; scale log2(e) finite.
  *   fill        : 0 leaves o and lse, dq, dk, dv of rows of no sequence (and dk, dv of keys not in use) as they
  *                 were; otherwise they get zeros (lse -inf).
  *   q, k, v, o, d_o, dq, dk, dv : 16-byte aligned, strides multiples of 8; 128 row + heads head of each below 2^30.

@@ -806,7 +806,7 @@ lmbp_status check_attention(const lmbp_attention* a) {
   if (a->q_rows < 0 || a->k_rows < 0 || a->k_rows >= lim || a->q_rows >= lim || a->q_rows >= lim / (a->heads / a->kv_heads)) return LMBP_EINVAL;
   if ((!a->q_starts && a->q_rows % a->batch != 0) || (!a->k_starts && a->k_rows % a->batch != 0)) return LMBP_EINVAL;
   if (!aligned(a->q_starts, 4) || !aligned(a->k_starts, 4) || !aligned(a->k_lens, 4)) return LMBP_EINVAL;
-  return std::isfinite(a->scale) && a->scale > 0.0f ? LMBP_OK : LMBP_EINVAL;
+  return a->scale > 0.0f && std::isfinite(a->scale * 1.44269504f) ? LMBP_OK : LMBP_EINVAL;   // a factor of the kernels
 }
 
 lmbp::AttentionPlan attention_plan(const lmbp_attention& a) {

@@ -41,3 +41,14 @@ def test_parts_of_the_heads_of_one_tensor_do_not_overlap(L, rows):
         return L.rope_fwd(B.BF16, ref(r), ref(part(q_at)), ref(part(k_at)), ref(part(q_at)), ref(part(k_at)), None)
     assert turned() == turned(q_at=129) == PASSES   # 129 .. 192 of each head's 192 and 64 .. 127
     assert turned(k_at=63) == turned(q_at=65) == turned(k_at=129, q_at=128) == B.EOVERLAP
+
+
+def test_the_largest_scale(L):
+    """A scale whose product with log2(e) fp32 does not hold makes every score NaN: refused, with no workspace."""
+    large = dict(batch=1, q_rows=1, k_rows=65536)
+    for scale in (2.4e38, 3.4e38):
+        a = attention(scale=scale, **large)
+        assert L.attention_fwd(B.BF16, ref(a), ref(heads(0)), ref(heads(1)), ref(heads(2)), ref(heads(3)), at(4), at(5), 1 << 30, None) == B.EINVAL
+        assert L.lmbp_attention_fwd_bytes(ref(a)) == L.lmbp_attention_bwd_bytes(ref(a)) == 0
+    for scale in (2.3e38, 1e-44):
+        assert L.lmbp_attention_fwd_bytes(ref(attention(scale=scale, **large))) > 0

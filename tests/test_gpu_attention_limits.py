@@ -116,3 +116,14 @@ def test_rows_all_of_whose_scores_are_minus_infinity(heads, kv_heads, rows, keys
     assert torch.equal(o[rows // 2, head], v[keys // 3, kv_heads - 1]) and lse[rows // 2, head] == 0
     o, lse = lmbp.attention_fwd(q, k, v, k_lens=torch.zeros(1, device=DEV, dtype=torch.int32))
     assert (o == 0).all() and (lse == -INF).all()
+
+
+@pytest.mark.parametrize("scale", [2.3e38, 1e-44])
+def test_the_largest_and_smallest_scale(scale):
+    """Scores of 0 stay 0 and equal weights equal."""
+    q, k, v = torch.zeros(40, 2, 64, device=DEV, dtype=torch.bfloat16), normal((70, 2, 64), 1), normal((70, 2, 64), 2)
+    v[:] = v[:1]
+    o, lse = lmbp.attention_fwd(q, k, v, scale=scale)
+    # 70 equal values: P = 1, a sum of 70 in fp32, its reciprocal, the result's rounding
+    P.inside(o, v[:1].double().expand(40, 2, 64), (80 * P.U + P.half(torch.bfloat16)) * v[:1].double().abs(), "o")
+    P.inside(lse, torch.full((40, 2), math.log(70), dtype=torch.float64, device=DEV), 20 * P.U, "lse")
