@@ -416,8 +416,9 @@ typedef struct {
  * Rotary positions. Columns are taken in pairs; pair p of a token's head turns by the angle
  * t = freqs[p] * positions[axes[p]][token]:  (a, b) -> (a cos t - b sin t, a sin t + b cos t).
  *
- *   rope_fwd : y = x turned;  rope_bwd: dx = dy turned back. fp32 arithmetic, one rounding; the angle is
- *              right for any position (formed modulo a turn in 64-bit whole numbers).
+ *   rope_fwd : y = x turned;  rope_bwd: dx = dy turned back. fp32 arithmetic, one rounding. A frequency (of less
+ *              than 2^52 radians) is cut to a whole number of 2^-64 turns, within 1.5 of them, and nothing else is lost before
+ *              sine and cosine: the angle is off by less than 1.5 |position| 2^-64 turns, 6e-7 radians at 2^40, 5e-3 at 2^53.
  *
  *   tokens, dim : tokens >= 0; 1 <= dim <= 512.
  *   q_heads, k_heads : heads of the two tensors; k_heads = 0: there is no second one (k, yk NULL).
@@ -489,6 +490,7 @@ size_t lmbp_msrms_rope_bwd_bytes(int64_t dim);
  * Of sequence lengths nq and nk (keys in use), query i sees keys j < nk and, if causal, j <= i + nk - nq: the
  * last query sees all. A query that sees none has o = 0 and lse = -inf, and gives and gets no gradient.
  * Keys that a query does not see may hold anything, infinities and NaN included.
+ * An infinity in v of a key that is seen makes o infinite there, or NaN where the key's weight rounds to 0 on the way.
  * Starts or k_lens that break the rules above give wrong results, but no access outside the tensors.
  *
  *   dt          : LMBP_BF16 (LMBP_EDTYPE otherwise).

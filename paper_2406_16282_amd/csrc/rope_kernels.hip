@@ -516,8 +516,8 @@ hipError_t launch(rope::Args& f, bool vec, hipStream_t s) {
   }
 }
 
-// A frequency of |f| < 2^53 radians in revolutions modulo 1, as a whole number of 2^-64 (cut off, so within one of them): its 53 bits times
-// 1 / (2 pi) to 128 bits. In long double this took 4 us of a call with 64 pairs (10.0 us in all, 6.2 so).
+// A frequency of |f| < 2^52 radians in revolutions modulo 1, as a whole number of 2^-64 (cut off twice, so within 1.5 of them): its 53 bits
+// times 1 / (2 pi) to 128 bits. In long double this took 4 us of a call with 64 pairs (10.0 us in all, 6.2 so).
 uint64_t turns_of(double f) {
   constexpr uint64_t kInverse[2] = {0x28be60db9391054aull, 0x7f09d5f47d4d3770ull};
   int e = 0;

@@ -134,3 +134,34 @@ def test_heads_side_by_side_with_their_keys_and_values():
         d = torch.full_like(x, 7.0)
         lmbp.attention_bwd(do, x[:, :, 0], x[:, :, 1], x[:, :, 2], o, lse, causal=True, dq=d[:, :, 0], dk=d[:, :, 1], dv=d[:, :, 2])
         assert all(torch.equal(a, b) for a, b in zip(d.unbind(2), want))
+
+
+TWO_PI = 6283185307179586476925286766559005768394338798750211641949889184615632812572417997256069650684234135964296173026564613294187689219101164463450718816256   # 2 pi 10^150
+
+
+def exact_angle(pos, freq):
+    """pos freq modulo a turn in whole numbers, in radians from -pi to pi."""
+    n, d = freq.as_integer_ratio()
+    turn = TWO_PI * d
+    rest = pos * n * 10 ** 150 % turn
+    return (rest - turn if 2 * rest > turn else rest) / turn * 2 * math.pi
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_of_positions_of_any_size(dtype, interleaved):
+    """Against angles in whole numbers: a frequency is cut to within 1.5 of 2^-64 turns, which a position multiplies, and nothing else is lost."""
+    freqs = [1.0, -1.0, 0.3, 1e-4, 10000.0 ** (-5 / 64), 3.0, 1e3, 2.0 ** 40 + 1.0, 2.0 ** 51 + 0.5, 1e-12, 1.0 / 3.0, -2.0 ** -30, 0.0]
+    r = B.Rotation(freqs, None, interleaved)
+    pos = [0, 1, -1, 12345, 2 ** 24 + 1, -(2 ** 30) - 1, 2 ** 31 - 1, -2 ** 31]
+    if dtype == torch.int64:
+        pos += [2 ** 40 - 1, 2 ** 50 + 3, -2 ** 53 - 1]
+    x = torch.randn(len(pos), 3, 2 * len(freqs), device=DEV)
+    t = torch.tensor([[exact_angle(p, f) for f in freqs] for p in pos], dtype=torch.float64, device=DEV)[:, None]
+    slack = torch.tensor([abs(p) * 1.5 * 2.0 ** -64 * 2 * math.pi for p in pos], dtype=torch.float64, device=DEV)[:, None, None]
+    for op, sign in ((lmbp.rope_fwd, 1), (lmbp.rope_bwd, -1)):
+        y, _ = op(x, None, torch.tensor(pos, device=DEV, dtype=dtype), r)
+        want = P.turn(x.double(), sign * t, interleaved)
+        # 6 u of a pair's size as in any turn; the cut; the 64-bit angle, cosine and sine of the reference (below 2^-48)
+        room = (6 * P.U + slack + 2.0 ** -48) * P.pair_size(x.double(), len(freqs), interleaved)
+        P.inside(y, want, room + P.U * want.abs(), op.__name__)
