@@ -127,3 +127,27 @@ def test_the_largest_and_smallest_scale(scale):
     # 70 equal values: P = 1, a sum of 70 in fp32, its reciprocal, the result's rounding
     P.inside(o, v[:1].double().expand(40, 2, 64), (80 * P.U + P.half(torch.bfloat16)) * v[:1].double().abs(), "o")
     P.inside(lse, torch.full((40, 2), math.log(70), dtype=torch.float64, device=DEV), 20 * P.U, "lse")
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("heads,kv_heads,dim,n,m", [(2, 2, 64, 100, 60), (6, 2, 128, 150, 33), (8, 1, 128, 20, 3)])
+def test_queries_that_see_no_key_or_some_reach_only_those(heads, kv_heads, dim, n, m, bad):
+    """More queries than keys: those in front see none, whatever they hold, and the first that sees one reaches that key's
+    gradients and no later one's."""
+    q, do = normal((n, heads, dim), 1), normal((n, heads, dim), 2)
+    k, v = normal((m, kv_heads, dim), 3), normal((m, kv_heads, dim), 4)
+    o, lse = lmbp.attention_fwd(q, k, v, causal=True)
+    want = lmbp.attention_bwd(do, q, k, v, o, lse, causal=True)
+    first = n - m   # sees key 0
+    for t in (q, do):
+        t[:first] = bad
+    o2, lse2 = lmbp.attention_fwd(q, k, v, causal=True)
+    assert torch.equal(o2, o) and torch.equal(lse2, lse)
+    got = lmbp.attention_bwd(do, q, k, v, o2, lse2, causal=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and (got[0][:first] == 0).all()
+    q[first, :, 1], do[first, :, 1] = bad, bad
+    o2, lse2 = lmbp.attention_fwd(q, k, v, causal=True)
+    got = lmbp.attention_bwd(do, q, k, v, o2, lse2, causal=True)
+    assert torch.equal(got[0][first + 1:], want[0][first + 1:])
+    for a, b in zip(got[1:], want[1:]):
+        assert torch.equal(a[1:], b[1:]) and not a[0].isfinite().all()
