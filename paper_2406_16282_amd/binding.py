@@ -1246,8 +1246,8 @@ def attention_fwd(q, k, v, causal=False, scale=None, q_starts=None, k_starts=Non
     returns (o, lse), lse the fp32 logarithm of each query's sum. Sequences lie side by side in [sequences, rows,
     heads, dim], one behind the other in [rows, heads, dim] with ``q_starts`` / ``k_starts`` (int32,
     sequences + 1, from 0 on; k_starts that are not given are q_starts where k has q's rows), and of each
-    only ``k_lens`` (int32) keys may be in use (a padded cache). Causal: the last query sees the last key. scale:
-    dim ** -0.5 unless given.
+    only ``k_lens`` (int32) keys may be in use (a padded cache, [sequences, room, kv_heads, dim], given whole).
+    Causal: the last query sees the last key. scale: dim ** -0.5 unless given.
     Rows of no sequence are zeros (lse -inf); where o and lse are both given they stay as they were."""
     if _fast is not None and o is None and lse is None and stream is None:
         out = _fast.attention_forward(_address["attention_fwd"], _address["lmbp_attention_fwd_bytes"], q, k, v, causal, scale, q_starts,

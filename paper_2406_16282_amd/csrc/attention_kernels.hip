@@ -266,8 +266,8 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(FwdArgs a) {
 
 // Few rows, many keys: a block of kFewWaves waves has 32 packed rows and a share of their keys; each wave walks keys of its own
 // through two slots of its own, with no barrier, and the block's waves join at the end. Memory is what it waits
-// for: 16 KB to a wave are on their way while 16 KB are multiplied, 64 KB to a CU. 16 sequences of 1 to 4096 keys, 32 heads: 90 us (5.1
-// TB/s); one of 65537 keys, 8 key heads: 50 (5.4), with one wave to a block 62, with four 54.
+// for: 16 KB to a wave are on their way while 16 KB are multiplied, 64 KB to a CU. The kernel alone: 16 sequences of 1 to 4096 keys, 32 heads:
+// 90 us (5.1 TB/s); one of 65537 keys, 8 key heads: 50 (5.4), with one wave to a block 62, with four 54.
 constexpr int kFewWaves = 2, kFewTiles = 4;   // at least so many tiles of keys to a wave, where rows' keys are shared out
 template <int D>
 constexpr int kFewKeys = 4096 / D;   // keys to a wave's tile: 8 KB of K, 8 of V
@@ -451,9 +451,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(FwdArgs a) {
   if (lane == 0) a.lse[row] = any ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
 }
 
-// How a call is taken: blocks of 32 packed rows (few) or of 128, and the shares of the keys. One token of 16 sequences of 1 to
-// 4096 keys, 32 heads: few 102 us, 128 rows to a block 144; 64 sequences of 1000 keys 190 and 201; 4 rows of 8 key heads each of 8
-// sequences of 500 keys 14 and 14; 8 queries of 16 sequences of 200 keys 11.8 and 9.3, so short sequences do not take it.
+// How a call is taken: blocks of 32 packed rows (few) or of 128, and the shares of the keys. Both kernels of a call, in a graph: one token of
+// 16 sequences of 1 to 4096 keys, 32 heads: few 96 us (one share 104), 128 rows to a block 103 to 137; 64 sequences of 1000 keys 183 and 198; 4
+// rows of 8 key heads each of 8 sequences of 500 keys 14 and 14; 8 queries of 16 sequences of 200 keys, 32 heads on 8, 11.3 and 8.7, so short
+// sequences do not take it.
 struct FwdForm {
   bool few;
   int splits;
@@ -466,8 +467,8 @@ static FwdForm fwd_form(const AttentionPlan& a, int cus) {
   const int64_t blocks = tiles_of(s.q, a.batch, false, s.group, f.few ? 32 : 128) * a.kv_heads;
   // Keys to a share: 4 tiles of each wave (few) or of the block, where blocks are to fill the device; 4 times as many where shares of few
   // queries' keys only even out sequences of different lengths (the device alone knows them). 256 queries and 16384 keys of 8 heads 37 us
-  // (one share 378); 16 sequences of 2000 keys, 32 heads, one token in one share 98 (7 shares 119), 32 tokens 101 (161), and the sequences
-  // of 1 to 4096 keys in 4 shares 102 (2: 110).
+  // (one share 364); 16 sequences of 2000 keys, 32 heads, one token in one share 95 (7 shares 112), 32 tokens 98 (158), and the sequences
+  // of 1 to 4096 keys in 4 shares 96 (2: 106, 5: 92, 8: 95).
   const int64_t least = f.few ? kFewTiles * kFewWaves * (s.dim <= 64 ? kFewKeys<64> : kFewKeys<128>) : 4 * kKeys;
   const int64_t filling = std::min(blocks == 0 ? 1 : 2 * int64_t(cus) / blocks, keys / least);
   const int64_t evening = f.few && blocks > 0 ? std::min(8 * int64_t(cus) / blocks, keys / (4 * least)) : 1;

@@ -15,7 +15,7 @@
 // heads of 128, bf16: turned 43 to 46 us (5.9 to 6.2 TB/s), norm and turn 48, its backward 64 (6.3); 2, 4 and 8 waves to a token
 // instead of one 47 -> 45, 48 -> 48, 67 -> 64. A half that is no multiple of 16 bytes goes in pieces of 8 where that does, else element by element: 1531
 // tokens of 12 heads of 72, 18 pairs, fp32, with gains 9.2 us, backward 10.7 and 3.8 for the sum of the gains' gradients (element by
-// element 11.5 and 12.1); 8192 of 32 of 72, bf16, 30 and 33 without gains (45 and 59).
+// element 11.5 and 12.1); 8192 of 16 + 16 of 72, bf16, 31 and 32 without gains (45 and 59).
 #include "lmbp_device.hpp"
 #include "lmbp_launch.hpp"
 
@@ -482,7 +482,7 @@ void plan(rope::Args& f, bool apart) {
 }
 int64_t blocks_of(const rope::Args& f, int64_t tokens) { return (tokens * f.shares + 3) / 4; }
 // Blocks of the backward with gains, of each side: about as many as are resident at once, which walk over the tokens. Pieces of 8 bf16 (156
-// registers) leave room for 3 to a CU, 384 to a side: 8192 tokens of 32 + 32 heads of 128 83 us (512: 108, 256: 98), of 32 + 8 67 (91, 75).
+// registers) leave room for 3 to a CU, 384 to a side: 8192 tokens of 32 + 32 heads of 128 85 us (512: 108, 256: 98), of 32 + 8 68 (91, 75).
 // The others 4: 4000 tokens of 12 + 12 fp32 heads of 64 22 us (twice as many 25, half 24).
 int gain_blocks(const rope::Args& f, bool wide) {
   const int64_t most = (wide ? kGainBlocks / 4 * 3 : kGainBlocks) / (f.side[1].heads > 0 ? 2 : 1);
@@ -500,7 +500,8 @@ hipError_t launch(rope::Args& f, bool vec, hipStream_t s) {
     }
   };
   if constexpr (MODE == rope::kNormBackGain || MODE == rope::kNormGain) {
-    // Forward: 8192 tokens of 32 + 32 heads of 128, bf16, 58 us; 1280 to a side 61, 640 69, one wave to each unit 82 (gains read as often).
+    // Forward: 8192 tokens of 32 + 32 heads of 128, bf16, 59 us; 1280 to a side 62, 640 71, one wave to each unit 83: it reads its gains by
+    // single elements, which so far is what many tokens to a wave make up for.
     const int blocks = MODE == rope::kNormGain ? int(std::clamp<int64_t>(blocks_of(f, f.tokens), 1, 2 * kGainBlocks)) : gain_blocks(f, IO::kPerVec == 8);
     f.blocks = blocks;
     go(f, dim3(blocks, f.side[1].heads > 0 ? 2 : 1));

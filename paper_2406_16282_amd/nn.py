@@ -536,7 +536,9 @@ class _Attention(torch.autograd.Function):
 class Attention(nn.Module):
     """softmax(scale q k^T) v (bf16): forward(q, k, v) with q [sequences, rows, heads, dim] and k, v the same with
     their own rows and heads, or packed as [rows, heads, dim] with q_starts / k_starts (int32, sequences + 1);
-    k_lens: keys in use of each sequence. Causal: the last query sees the last key. scale: dim ** -0.5 unless given."""
+    k_lens: keys in use of each sequence. Causal: the last query sees the last key. scale: dim ** -0.5 unless given.
+    Tensors whose rows do not lie one behind the other ([sequences, heads, rows, dim], the first rows of each of a cache's
+    sequences) are copied by every call: a cache lies as [sequences, room, heads, dim] and is given whole, with k_lens."""
 
     def __init__(self, causal=False, scale=None):
         super().__init__()
@@ -575,6 +577,8 @@ class _QKVAttention(torch.autograd.Function):
             d.zero_()   # rows of no sequence
         dq, dk, dv = d.split((heads, kv_heads, kv_heads), -2)
         q, k, v, o = (_wide_rows(t) for t in (q, k, v, o))
+        # dq and dk are rounded to the type here, and again where they are turned back in place: between the two kernels
+        # fp32 would take its own tensors, written and read once
         binding.attention_bwd(_wide_rows(do), q, k, v, o, lse.contiguous(), causal, scale, starts, starts, dq=dq, dk=dk, dv=dv)
         if eps is not None:
             binding.msrms_rope_bwd(dq, dk, q, k, rstd_q, rstd_k, positions, rotation, q_out=dq, k_out=dk)
