@@ -197,15 +197,18 @@ struct Place {
     }
   }
   // Pair e turned. Columns behind the pairs are left as they are: not by an angle of 0, since 0 times an infinite neighbour is NaN.
+  // AGAIN: asked each time, where held over the loop the answers would take more scalar registers than there are.
+  template <bool AGAIN>
   __device__ inline void turn(int e, float p, float q, float c, float s, float& x, float& y) const {
-    int p0 = FORM == kHalves ? pair : pair + e;        // halves turn in whole pieces
-    if constexpr (FORM == kPairs) asm volatile("" : "+v"(p0));   // asked each time: held over the loop the answers take scalar registers
+    int p0 = FORM == kHalves ? pair : pair + e;   // halves turn in whole pieces
+    if constexpr (AGAIN) asm volatile("" : "+v"(p0));
     const bool turns = p0 < half;
     x = turns ? __builtin_fmaf(p, c, -q * s) : p;
     y = turns ? __builtin_fmaf(p, s, q * c) : q;
   }
-  // This lane's pairs turned. VEC: whether all do is asked once (a select for every pair: 43.1 us for 40.4 at 8192 tokens of 32 + 32
-  // heads of 72, norm and turn; element by element it is the other way round, 122 and 129).
+  // This lane's pairs turned. VEC: whether all do is asked once. 8192 tokens of 32 + 32 heads of 72, halves, norm and turn 40.4 us, with
+  // a select for every pair 43.1; element by element it is the other way round (129 and 122 at 100 columns), and so is the norm's forward
+  // with pairs side by side (42.9 and 38.4), which turns them one by one.
   __device__ inline void turn(float (&x)[E], float (&y)[E], const float (&c)[E], const float (&s)[E]) const {
     if (VEC && pair + E <= half) {
 #pragma unroll
@@ -216,7 +219,7 @@ struct Place {
       }
     } else if constexpr (FORM != kHalves) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) turn(e, x[e], y[e], c[e], s[e], x[e], y[e]);
+      for (int e = 0; e < E; ++e) turn<false>(e, x[e], y[e], c[e], s[e], x[e], y[e]);
     }
   }
   // The columns of pair e.
@@ -362,8 +365,9 @@ __global__ __launch_bounds__(256) void rope_kernel(Args f) {
                 a[e] *= ga[e];
                 b[e] *= gb[e];
               }
+              if constexpr (FORM == kPairs) at.template turn<false>(e, a[e], b[e], c[e], s[e], a[e], b[e]);
             }
-            at.turn(a, b, c, s);
+            if constexpr (FORM != kPairs) at.turn(a, b, c, s);
           } else {
             float p[E], q[E];
             at.unpack(rk[j], p, q);
@@ -395,9 +399,9 @@ __global__ __launch_bounds__(256) void rope_kernel(Args f) {
               at.turn(a, b, c, s);
             } else {
 #pragma unroll
-              for (int e = 0; e < E; ++e) {   // pair by pair: the branch of a whole lane costs this kernel registers that it has not
+              for (int e = 0; e < E; ++e) {   // one by one: the branch of a whole lane takes registers that this kernel has not
                 float v, w;
-                at.turn(e, a[e], b[e], c[e], s[e], v, w);
+                at.template turn<FORM == kPairs && E < 8>(e, a[e], b[e], c[e], s[e], v, w);
                 p[e] *= r;
                 q[e] *= r;
                 sum_a[e] = __builtin_fmaf(real ? v : 0.0f, real ? p[e] : 0.0f, sum_a[e]);
